@@ -385,6 +385,69 @@ int metis_quantize_mx(void* stream, const metis_mat* A, metis_mxfp4* out);
  */
 int metis_mxfp4_gemm_nt(void* stream, const metis_mxfp4* A, const metis_mxfp4* B, metis_mat* C);
 
+/* ---- mixture of experts: routing --------------------------------------------------------------- */
+
+/*
+ * Routing of T tokens to experts.  x = logits [T, experts] (bf16 or fp32), evaluated in fp32:
+ *   score    softmax over the row's experts, or sigmoid(x) = 1 / (1 + exp(-x)) of each expert
+ *   key      what the selection compares: x + bias (softmax: the order of p * exp(bias)), score + bias (sigmoid).  bias (device fp32
+ *            [experts], optional) balances the load; it enters the selection alone, not the weights.  An expert whose logit is
+ *            -inf or NaN, or whose key is -inf, is not available; a token with valid[t] == 0 (device uint8 [T], optional) has no
+ *            expert at all.
+ *   groups   the experts form `groups` equal runs.  A group's score is its highest key (softmax) or the sum of its two highest
+ *            (sigmoid; of its highest alone where only one expert is available).  The top_groups best stay in the selection.
+ *   top-k    the k highest keys in descending order -> idx [T, k] (int32).  Ties go to the lowest index, among groups as well.  Where
+ *            fewer than k experts are available the rest of the row is idx -1, weight 0.
+ *   weights  fp32 [T, k]: scale * score, or with renorm scale * score / (sum of the chosen scores), for softmax evaluated as
+ *            a softmax over the chosen logits (0 where that sum is 0).
+ * Limits: 1 <= experts <= 512, 1 <= k <= 16, groups divides experts, 1 <= top_groups <= groups, k <= top_groups * experts / groups.
+ * Errors: METIS_INVALID_ARG (null pointer, dtype, unknown scores, parameters outside these rules), METIS_BAD_SHAPE (logits->cols !=
+ * experts, ld < cols, more than 2^31 - 1 choices), METIS_UNSUPPORTED (experts > 512, k > 16).  T = 0 is no work and no error.
+ */
+enum { METIS_SCORES_SOFTMAX = 0, METIS_SCORES_SIGMOID = 1 };
+typedef struct {
+    int   experts, k;
+    int   scores;               /* METIS_SCORES_SOFTMAX or METIS_SCORES_SIGMOID */
+    int   groups, top_groups;   /* 1, 1: no groups */
+    int   renorm;
+    float scale;
+} metis_router;
+int metis_route(void* stream, const metis_mat* logits, const metis_router* router, const float* bias, const uint8_t* valid,
+                int32_t* idx, float* weights);
+
+/*
+ * dlogits [T, experts] (bf16 or fp32) from dweights [T, k] (fp32) for the choices idx [T, k] that metis_route made.  The selection has
+ * no gradient.  With p the scores, v_j = scale * dweights_j (0 where idx_j is -1, or outside the experts):
+ *   softmax             dx_e = p_e (sum of v_j over idx_j = e  -  sum_j v_j p_j)          dense: every available expert has one
+ *   softmax, renorm     dx_j = q_j (v_j - sum_l v_l q_l), q the softmax over the chosen logits, 0 elsewhere
+ *   sigmoid             dx_j = v_j p_j (1 - p_j), 0 elsewhere
+ *   sigmoid, renorm     dx_j = (v_j - sum_l v_l p_l / Z) / Z * p_j (1 - p_j), Z = sum of the chosen p; 0 where Z is 0, and elsewhere
+ * router->groups, top_groups are not looked at.  Errors as for metis_route.
+ */
+int metis_route_grads(void* stream, const metis_mat* logits, const metis_router* router, const int32_t* idx, const float* dweights,
+                      metis_mat* dlogits);
+
+/*
+ * The plan of a batch: its S = tokens * k choices sorted into slots, expert by expert and within an expert in the order of the choices
+ * (a stable counting sort; no atomics, the same bits every time).  Expert e has the slots offsets[e] .. offsets[e + 1) - 1.
+ *   offsets  device int32 [experts + 1]
+ *   token    device int32 [S]: the token that a slot serves; -1 for the slots at and behind offsets[experts], which serve none
+ *   slot     device int32 [tokens, k]: the slot of a choice, -1 where idx is -1 (or outside the experts)
+ * Everything stays on the device: no call waits to learn how many tokens an expert has.
+ * workspace: metis_dispatch_workspace_bytes bytes, 16-byte aligned (may be null where that is 0).
+ * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE (more than 2^31 - 1 choices), METIS_UNSUPPORTED (experts > 512, k > 16),
+ * METIS_WORKSPACE_TOO_SMALL.
+ */
+typedef struct {
+    int32_t* offsets;
+    int32_t* token;
+    int32_t* slot;
+    int64_t  tokens;
+    int      experts, k;
+} metis_expert_plan;
+size_t metis_dispatch_workspace_bytes(int64_t tokens, int experts, int k);
+int metis_dispatch(void* stream, const int32_t* idx, metis_expert_plan* plan, void* workspace, size_t workspace_bytes);
+
 /* ---- measurement aid ---------------------------------------------------------------------- */
 
 /*

@@ -16,6 +16,8 @@ Modules
   hadamard   16-point random Hadamard rotation in front of the stochastic quantizer (the
              comparison recipe of Sec. 4.3).
   mx         MXFP4 quantizer of the microscaling family (Sec. 2.3 names it beside NVFP4).
+  experts    mixture of experts: routing and the plan of slots, the experts' MXFP4 products, the combination of their
+             rows, 8-bit checkpoints and the gated activation.
   linear     fprop / dgrad / wgrad on split-quantized operands (Eq. 2, Eq. 3
              and the W_R gradient listed after it).
 

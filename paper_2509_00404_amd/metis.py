@@ -34,6 +34,16 @@ class MxFp4(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64)]
 
 
+class Router(C.Structure):
+    _fields_ = [("experts", C.c_int), ("k", C.c_int), ("scores", C.c_int), ("groups", C.c_int), ("top_groups", C.c_int),
+                ("renorm", C.c_int), ("scale", C.c_float)]
+
+
+class Plan(C.Structure):
+    _fields_ = [("offsets", C.c_void_p), ("token", C.c_void_p), ("slot", C.c_void_p), ("tokens", C.c_int64), ("experts", C.c_int),
+                ("k", C.c_int)]
+
+
 class DecomposeJob(C.Structure):
     _fields_ = [("A", C.POINTER(Mat)), ("k", C.c_int), ("oversample", C.c_int), ("sample_rate", C.c_double),
                 ("seed", C.c_uint64), ("U", C.c_void_p), ("S", C.c_void_p), ("V", C.c_void_p), ("amax_out", C.c_void_p),
@@ -96,6 +106,10 @@ _SIGNATURES = {
                                         C.c_void_p, C.c_size_t]),
     "metis_quantize_mx": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(MxFp4)]),
     "metis_mxfp4_gemm_nt": (C.c_int, [C.c_void_p, C.POINTER(MxFp4), C.POINTER(MxFp4), C.POINTER(Mat)]),
+    "metis_route": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Router), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "metis_route_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Router), C.c_void_p, C.c_void_p, C.POINTER(Mat)]),
+    "metis_dispatch_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int, C.c_int]),
+    "metis_dispatch": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(Plan), C.c_void_p, C.c_size_t]),
     "metis_factor_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int]),
     "metis_fp4_factor_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Split), C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_size_t]),
@@ -158,12 +172,16 @@ assert _SPLIT.size == C.sizeof(Split)
 
 
 class MxTensor:
-    """Device MXFP4 matrix: codes [rows, cols/2] u8, scales [rows, cols/32] u8 (E8M0)."""
+    """Device MXFP4 matrix: codes [rows, cols/2] u8, scales [rows, cols/32] u8 (E8M0).  buffers: those two, where they exist already."""
 
-    def __init__(self, rows, cols, device="cuda"):
+    def __init__(self, rows, cols, device="cuda", buffers=None):
         self.rows, self.cols = rows, cols
-        self.codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=device)
-        self.scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=device)
+        if buffers is None:
+            buffers = (torch.empty((rows, cols // 2), dtype=torch.uint8, device=device),
+                       torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
+        self.codes, self.scales = buffers
+        assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
+        assert self.codes.numel() == rows * (cols // 2) and self.scales.numel() == rows * (cols // 32)
 
     def c(self):
         return MxFp4(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
@@ -427,6 +445,72 @@ def fp4_factor_grads(dW, W, dU, dS, dV, workspace=None):
     _check(lib().metis_fp4_factor_grads(_stream(), C.byref(m), C.byref(w), dU.data_ptr(), dS.data_ptr(),
                                         dV.data_ptr(), workspace.data_ptr(), workspace.numel()))
     return dU, dS, dV
+
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+class ExpertPlan:
+    """The slots of a batch's choices (see metis_expert_plan in include/metis.h): offsets [experts + 1], token [tokens * k], slot
+    [tokens, k], int32.  buffers: those three tensors, where they exist already."""
+
+    def __init__(self, tokens, experts, k, buffers=None, device="cuda"):
+        self.tokens, self.experts, self.k = tokens, experts, k
+        if buffers is None:
+            i32 = dict(dtype=torch.int32, device=device)
+            buffers = torch.empty((experts + 1,), **i32), torch.empty((tokens * k,), **i32), torch.empty((tokens, k), **i32)
+        self.offsets, self.token, self.slot = buffers
+        assert all(t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 for t in buffers)
+        assert self.offsets.numel() == experts + 1 and self.token.numel() == tokens * k == self.slot.numel()
+
+    def c(self):
+        return Plan(self.offsets.data_ptr(), self.token.data_ptr(), self.slot.data_ptr(), self.tokens, self.experts, self.k)
+
+
+def _ptr(t, dtype, shape):
+    """Address of a contiguous device tensor of that type and shape (None stays None)."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and tuple(t.shape) == shape
+    return t.data_ptr()
+
+
+def route(logits, k, bias=None, valid=None, scores="softmax", groups=1, top_groups=1, renorm=True, scale=1.0):
+    """Chosen experts idx [T, k] int32 and weights [T, k] fp32 of logits [T, experts] (see metis_route)."""
+    T, E = logits.shape
+    idx = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+    weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    m, r = _mat(logits), Router(E, k, SCORES[scores], groups, top_groups, renorm, scale)
+    _check(lib().metis_route(_stream(), C.byref(m), C.byref(r), _ptr(bias, torch.float32, (E,)), _ptr(valid, torch.uint8, (T,)),
+                             idx.data_ptr(), weights.data_ptr()))
+    return idx, weights
+
+
+def route_grads(logits, idx, dweights, scores="softmax", renorm=True, scale=1.0, out=None):
+    """Gradient of the logits from that of route's weights; `out` bf16 or fp32, by default of the logits' type."""
+    T, E = logits.shape
+    k = idx.shape[1]
+    if out is None:
+        out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    m, o, r = _mat(logits), _mat(out), Router(E, k, SCORES[scores], 1, 1, renorm, scale)
+    _check(lib().metis_route_grads(_stream(), C.byref(m), C.byref(r), _ptr(idx, torch.int32, (T, k)),
+                                   _ptr(dweights, torch.float32, (T, k)), C.byref(o)))
+    return out
+
+
+def dispatch(idx, experts, plan=None, workspace=None):
+    """Sorts the choices idx [T, k] into slots: the ExpertPlan of the batch."""
+    T, k = idx.shape
+    if plan is None:
+        plan = ExpertPlan(T, experts, k, device=idx.device)
+    if workspace is None:
+        nbytes = int(lib().metis_dispatch_workspace_bytes(T, experts, k))
+        workspace = torch.empty((nbytes,), dtype=torch.uint8, device=idx.device) if nbytes else None
+    p = plan.c()
+    _check(lib().metis_dispatch(_stream(), _ptr(idx, torch.int32, (plan.tokens, plan.k)), C.byref(p),
+                                workspace.data_ptr() if workspace is not None else None,
+                                workspace.numel() if workspace is not None else 0))
+    return plan
 
 
 def ceiling_copy(src, dst):
