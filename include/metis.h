@@ -448,6 +448,61 @@ typedef struct {
 size_t metis_dispatch_workspace_bytes(int64_t tokens, int experts, int k);
 int metis_dispatch(void* stream, const int32_t* idx, metis_expert_plan* plan, void* workspace, size_t workspace_bytes);
 
+/* ---- mixture of experts: rows back to tokens ----------------------------------------------------- */
+
+/*
+ * y [tokens, D] = sum over j of weights[t, j] * rows[slot[t, j], :], in fp32, the choices in their order, rounded once.  Choices without a
+ * slot add nothing.  weights: device fp32 [tokens, k], or null for ones (the input gradient of gathered rows).  rows [tokens * k, D]
+ * and y: bf16 or fp32 each; any D and row strides (whole 16-byte units where both allow them).  plan->slot is read alone.
+ * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (k > 16, or more than 2^25 columns or units).
+ */
+int metis_combine(void* stream, const metis_mat* rows, const metis_expert_plan* plan, const float* weights, metis_mat* y);
+
+/*
+ * Gradients of metis_combine from dy [tokens, D]: drows[slot[t, j], :] = weights[t, j] * dy[t, :], zeros in the slots that serve no
+ * choice; dweights [tokens, k] (fp32) = <dy[t, :], rows[slot[t, j], :]>, 0 without a slot; the sums in fp32, in an order that depends on D
+ * alone.  rows and drows share a type, dy has its own.  drows must not overlap rows.  Errors as above.
+ */
+int metis_combine_grads(void* stream, const metis_mat* dy, const metis_mat* rows, const metis_expert_plan* plan, const float* weights,
+                        metis_mat* drows, float* dweights);
+
+/* ---- 8-bit checkpoints and the gated activation --------------------------------------------------- */
+
+/*
+ * A device matrix held in 8 bits for the backward pass (1.03 bytes an element):
+ *   codes  [rows, cols]     one FP8-E4M3 bit pattern each
+ *   scales [rows, cols/32]  one E8M0 byte per block of 32 consecutive columns, value 2^(byte - 127)
+ * A block's scale is the smallest power of two 2^t, t >= -127, that keeps its largest magnitude within 448 * 2^t, so that nothing
+ * saturates; elements are the nearest E4M3 value of e / 2^t, ties to the even code (relative error at most 2^-4 down to 2^-6 * 2^t).  A block
+ * of zeros has scale byte 0 and keeps its signs; a block with an infinity or a NaN is NaN throughout (byte 255, codes 0x7F).
+ */
+typedef struct {
+    uint8_t* codes;
+    uint8_t* scales;
+    int64_t  rows, cols;
+} metis_mx8;
+
+/*
+ * Save A [rows, cols] (bf16 or fp32) into out; restore A into out.  cols % 32 == 0; the dense matrix's rows 16-byte aligned, codes 8-byte
+ * aligned.  No rows is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (rows of more than 2^28 columns).
+ */
+int metis_quantize_mx8(void* stream, const metis_mat* A, metis_mx8* out);
+int metis_dequantize_mx8(void* stream, const metis_mx8* A, metis_mat* out);
+
+/*
+ * Gated activation of a product whose output holds gate and up side by side: gate_up [S, 2 F] = (g | u), act [S, F] = g * sigmoid(g) * u in
+ * fp32, rounded once.  saved (optional, [S, 2 F]): the 8-bit checkpoint of gate_up, made on the way; with it the backward pass keeps 2.06
+ * bytes per gate-up pair where the bf16 gate, up and activation take 6.
+ *
+ * metis_swiglu_grads reads that checkpoint alone: with g, u its values and p = sigmoid(g),
+ *   dgate_up [S, 2 F] = (dact u p (1 + g (1 - p)) | dact g p),     act (optional, [S, F]) = g p u, recomputed for the gradient of the
+ * weight behind it.
+ * F % 32 == 0; gate_up, act, dact, dgate_up share a type (bf16 or fp32) and have 16-byte aligned rows; codes 8-byte aligned.
+ * No rows is no work.  Errors: as for metis_quantize_mx8.
+ */
+int metis_swiglu(void* stream, const metis_mat* gate_up, metis_mat* act, metis_mx8* saved);
+int metis_swiglu_grads(void* stream, const metis_mx8* saved, const metis_mat* dact, metis_mat* dgate_up, metis_mat* act);
+
 /* ---- measurement aid ---------------------------------------------------------------------- */
 
 /*

@@ -1,0 +1,153 @@
+// The experts' rows back to their tokens, and the gradients of that.
+#include <type_traits>
+#include "elementwise.h"
+
+#define COMBINE_MAX_K 16
+
+namespace {
+
+// a lane per W columns of a token
+template <typename T, typename O, int W>
+__global__ void __launch_bounds__(256)
+k_combine(const T* __restrict__ rows, int64_t ldr, int64_t S, const int32_t* __restrict__ slot, const float* __restrict__ weights, int k,
+          O* __restrict__ y, int64_t ldy, uint64_t total, FastDiv units) {
+    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= total) return;
+    const uint64_t t = div_by(units, n), c = (n - t * units.d) * W;
+    float acc[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) acc[i] = 0.0f;
+#pragma unroll 4
+    for (int j = 0; j < k; ++j) {
+        const int32_t s = slot[t * k + j];
+        if ((uint32_t)s >= (uint64_t)S) continue;
+        const float w = weights ? weights[t * k + j] : 1.0f;
+        float v[W];
+        load_row<W>(rows + s * ldr + c, v);
+#pragma unroll
+        for (int i = 0; i < W; ++i) acc[i] = fmaf(w, v[i], acc[i]);
+    }
+    store_row<W>(y + t * ldy + c, acc);
+}
+
+// A workgroup per token: its gradient row is read once for all its choices.  The products with the rows are added up per lane, then over
+// the wave, then over the waves, always in the same order.
+template <typename T, typename D, int W, int K>
+__global__ void __launch_bounds__(256)
+k_combine_grads(const D* __restrict__ dy, int64_t ldy, const T* __restrict__ rows, int64_t ldr, int64_t S, int64_t cols,
+                const int32_t* __restrict__ offsets, int E, const int32_t* __restrict__ slot, const float* __restrict__ weights, int k,
+                T* __restrict__ drows, int64_t ldd, float* __restrict__ dweights) {
+    __shared__ float s_part[4][K];
+    const int64_t t = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int32_t s[K];
+    float w[K], dot[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        s[j] = j < k ? slot[t * k + j] : -1;
+        if ((uint32_t)s[j] >= (uint64_t)S) s[j] = -1;
+        w[j] = s[j] >= 0 ? weights[t * k + j] : 0.0f;
+        dot[j] = 0.0f;
+    }
+    for (int64_t c = (int64_t)threadIdx.x * W; c < cols; c += (int64_t)blockDim.x * W) {
+        float d[W];
+        load_row<W>(dy + t * ldy + c, d);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (s[j] < 0) continue;
+            float v[W];
+            load_row<W>(rows + s[j] * ldr + c, v);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                dot[j] = fmaf(d[i], v[i], dot[j]);
+                v[i] = w[j] * d[i];
+            }
+            store_row<W>(drows + s[j] * ldd + c, v);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) dot[j] += __shfl_xor(dot[j], m);
+        if (lane == 0) s_part[wave][j] = dot[j];
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < k) {
+        float sum = 0.0f;
+        for (int v = 0; v < (int)blockDim.x / 64; ++v) sum += s_part[v][threadIdx.x];
+        dweights[t * k + threadIdx.x] = sum;
+    }
+    // the slots that serve no choice
+    const float zero[W] = {};
+    const int64_t used = offsets[E] > 0 ? offsets[E] : 0;
+    for (int64_t r = used + t; r < S; r += gridDim.x)
+        for (int64_t c = (int64_t)threadIdx.x * W; c < cols; c += (int64_t)blockDim.x * W) store_row<W>(drows + r * ldd + c, zero);
+}
+
+int plan_rows_status(const metis_mat* rows, const metis_expert_plan* p) {
+    if (!mat_ok(rows) || !p || !p->offsets || !p->slot || p->tokens < 1 || p->k < 1 || p->experts < 1) return METIS_INVALID_ARG;
+    if (p->k > COMBINE_MAX_K) return METIS_UNSUPPORTED;
+    if (p->tokens > 0x7FFFFFFFll / p->k || rows->rows != p->tokens * p->k || rows->cols < 1 || rows->cols > 0x7FFFFFFF || rows->ld < rows->cols)
+        return METIS_BAD_SHAPE;
+    return METIS_OK;
+}
+
+template <typename T, typename O>
+int launch_combine(hipStream_t s, const metis_mat* rows, const metis_expert_plan* p, const float* weights, metis_mat* y) {
+    const bool vec = rows->cols % 8 == 0 && mat_aligned16(rows) && mat_aligned16(y);
+    const int64_t units = vec ? rows->cols / 8 : rows->cols, total = p->tokens * units;
+    const int st = units_status(p->tokens, units);
+    if (st != METIS_OK) return st;
+    auto kern = vec ? k_combine<T, O, 8> : k_combine<T, O, 1>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div64(total, 256)), dim3(256), 0, s, (const T*)rows->ptr, rows->ld, rows->rows, p->slot,
+                       weights, p->k, (O*)y->ptr, y->ld, (uint64_t)total, fast_div((uint32_t)units));
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+
+template <typename T, typename D, int K>
+int launch_combine_grads(hipStream_t s, const metis_mat* dy, const metis_mat* rows, const metis_expert_plan* p, const float* weights,
+                         metis_mat* drows, float* dweights) {
+    const bool vec = rows->cols % 8 == 0 && mat_aligned16(rows) && mat_aligned16(drows) && mat_aligned16(dy);
+    const int64_t units = vec ? rows->cols / 8 : rows->cols;
+    auto kern = vec ? k_combine_grads<T, D, 8, K> : k_combine_grads<T, D, 1, K>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)p->tokens), dim3(units <= 64 ? 64 : units <= 128 ? 128 : 256), 0, s, (const D*)dy->ptr, dy->ld,
+                       (const T*)rows->ptr, rows->ld, rows->rows, rows->cols, p->offsets, p->experts, p->slot, weights, p->k, (T*)drows->ptr,
+                       drows->ld, dweights);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+
+}  // namespace
+
+extern "C" int metis_combine(void* stream, const metis_mat* rows, const metis_expert_plan* plan, const float* weights, metis_mat* y) {
+    if (plan && plan->tokens == 0) return METIS_OK;
+    const int st = plan_rows_status(rows, plan);
+    if (st != METIS_OK) return st;
+    if (!mat_ok(y)) return METIS_INVALID_ARG;
+    if (y->rows != plan->tokens || y->cols != rows->cols || y->ld < y->cols) return METIS_BAD_SHAPE;
+    hipStream_t s = (hipStream_t)stream;
+    if (rows->dtype == METIS_BF16)
+        return y->dtype == METIS_BF16 ? launch_combine<bf16_t, bf16_t>(s, rows, plan, weights, y) : launch_combine<bf16_t, float>(s, rows, plan, weights, y);
+    return y->dtype == METIS_BF16 ? launch_combine<float, bf16_t>(s, rows, plan, weights, y) : launch_combine<float, float>(s, rows, plan, weights, y);
+}
+
+extern "C" int metis_combine_grads(void* stream, const metis_mat* dy, const metis_mat* rows, const metis_expert_plan* plan, const float* weights,
+                                   metis_mat* drows, float* dweights) {
+    if (plan && plan->tokens == 0) return METIS_OK;
+    const int st = plan_rows_status(rows, plan);
+    if (st != METIS_OK) return st;
+    if (!mat_ok(dy) || !mat_ok(drows) || !weights || !dweights || drows->dtype != rows->dtype) return METIS_INVALID_ARG;
+    if (dy->rows != plan->tokens || dy->cols != rows->cols || dy->ld < dy->cols) return METIS_BAD_SHAPE;
+    if (drows->rows != rows->rows || drows->cols != rows->cols || drows->ld < drows->cols) return METIS_BAD_SHAPE;
+    hipStream_t s = (hipStream_t)stream;
+    auto by_k = [&](auto t, auto d) -> int {
+        typedef decltype(t) T;
+        typedef decltype(d) D;
+        if (plan->k <= 4) return launch_combine_grads<T, D, 4>(s, dy, rows, plan, weights, drows, dweights);
+        if (plan->k <= 8) return launch_combine_grads<T, D, 8>(s, dy, rows, plan, weights, drows, dweights);
+        return launch_combine_grads<T, D, 16>(s, dy, rows, plan, weights, drows, dweights);
+    };
+    if (rows->dtype == METIS_BF16) return dy->dtype == METIS_BF16 ? by_k(bf16_t(), bf16_t()) : by_k(bf16_t(), float());
+    return dy->dtype == METIS_BF16 ? by_k(float(), bf16_t()) : by_k(float(), float());
+}

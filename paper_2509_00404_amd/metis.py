@@ -44,6 +44,10 @@ class Plan(C.Structure):
                 ("k", C.c_int)]
 
 
+class Mx8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
 class DecomposeJob(C.Structure):
     _fields_ = [("A", C.POINTER(Mat)), ("k", C.c_int), ("oversample", C.c_int), ("sample_rate", C.c_double),
                 ("seed", C.c_uint64), ("U", C.c_void_p), ("S", C.c_void_p), ("V", C.c_void_p), ("amax_out", C.c_void_p),
@@ -110,6 +114,12 @@ _SIGNATURES = {
     "metis_route_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Router), C.c_void_p, C.c_void_p, C.POINTER(Mat)]),
     "metis_dispatch_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int, C.c_int]),
     "metis_dispatch": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(Plan), C.c_void_p, C.c_size_t]),
+    "metis_combine": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Plan), C.c_void_p, C.POINTER(Mat)]),
+    "metis_combine_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Plan), C.c_void_p, C.POINTER(Mat), C.c_void_p]),
+    "metis_quantize_mx8": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mx8)]),
+    "metis_dequantize_mx8": (C.c_int, [C.c_void_p, C.POINTER(Mx8), C.POINTER(Mat)]),
+    "metis_swiglu": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Mx8)]),
+    "metis_swiglu_grads": (C.c_int, [C.c_void_p, C.POINTER(Mx8), C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Mat)]),
     "metis_factor_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int]),
     "metis_fp4_factor_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Split), C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_size_t]),
@@ -185,6 +195,23 @@ class MxTensor:
 
     def c(self):
         return MxFp4(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
+
+
+class Mx8Tensor:
+    """Device matrix held in 8 bits: codes [rows, cols] u8 (E4M3 bits), scales [rows, cols/32] u8 (E8M0).  buffers: those two, where they
+    exist already."""
+
+    def __init__(self, rows, cols, device="cuda", buffers=None):
+        self.rows, self.cols = rows, cols
+        if buffers is None:
+            buffers = (torch.empty((rows, cols), dtype=torch.uint8, device=device),
+                       torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
+        self.codes, self.scales = buffers
+        assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
+        assert self.codes.numel() == rows * cols and self.scales.numel() == rows * (cols // 32)
+
+    def c(self):
+        return Mx8(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
 
 
 class SplitTensor:
@@ -511,6 +538,51 @@ def dispatch(idx, experts, plan=None, workspace=None):
                                 workspace.data_ptr() if workspace is not None else None,
                                 workspace.numel() if workspace is not None else 0))
     return plan
+
+
+def combine(rows, plan, y, weights=None):
+    """y [T, D] = sum of the tokens' rows, weighted by weights [T, k] (None: ones)."""
+    r, p, o = _mat(rows), plan.c(), _mat(y)
+    _check(lib().metis_combine(_stream(), C.byref(r), C.byref(p), _ptr(weights, torch.float32, (plan.tokens, plan.k)), C.byref(o)))
+    return y
+
+
+def combine_grads(dy, rows, plan, weights, drows=None, dweights=None):
+    """Gradients (drows like rows, dweights [T, k] fp32) of combine."""
+    if drows is None:
+        drows = torch.empty(rows.shape, dtype=rows.dtype, device=rows.device)
+    if dweights is None:
+        dweights = torch.empty((plan.tokens, plan.k), dtype=torch.float32, device=rows.device)
+    d, r, p, o, shape = _mat(dy), _mat(rows), plan.c(), _mat(drows), (plan.tokens, plan.k)
+    _check(lib().metis_combine_grads(_stream(), C.byref(d), C.byref(r), C.byref(p), _ptr(weights, torch.float32, shape), C.byref(o),
+                                     _ptr(dweights, torch.float32, shape)))
+    return drows, dweights
+
+
+def quantize_mx8(A, out):
+    a, o = _mat(A), out.c()
+    _check(lib().metis_quantize_mx8(_stream(), C.byref(a), C.byref(o)))
+    return out
+
+
+def dequantize_mx8(A, out):
+    a, o = A.c(), _mat(out)
+    _check(lib().metis_dequantize_mx8(_stream(), C.byref(a), C.byref(o)))
+    return out
+
+
+def swiglu(gate_up, act, saved=None):
+    """act [S, F] of gate_up [S, 2 F]; saved (Mx8Tensor [S, 2 F]): the checkpoint for the backward pass."""
+    g, a, q = _mat(gate_up), _mat(act), saved.c() if saved is not None else None
+    _check(lib().metis_swiglu(_stream(), C.byref(g), C.byref(a), C.byref(q) if q is not None else None))
+    return act
+
+
+def swiglu_grads(saved, dact, dgate_up, act=None):
+    """dgate_up [S, 2 F] from dact [S, F] and the checkpoint; act: recomputed from it where given."""
+    q, d, o, a = saved.c(), _mat(dact), _mat(dgate_up), _mat(act) if act is not None else None
+    _check(lib().metis_swiglu_grads(_stream(), C.byref(q), C.byref(d), C.byref(o), C.byref(a) if a is not None else None))
+    return dgate_up
 
 
 def ceiling_copy(src, dst):

@@ -63,3 +63,60 @@ def test_dispatch(metis):
     assert call(tokens=100000, size=need - 1) == WORKSPACE and call(tokens=100000, ws=None) == WORKSPACE
     assert call(tokens=100000, ws=FAKE + 4) == INVALID
     assert L.metis_dispatch(None, FAKE, None, None, 0) == INVALID
+
+
+def test_checkpoints(metis):
+    L = metis.lib()
+
+    def call(rows=4, cols=64, ld=64, dtype=0, ptr=FAKE, codes=FAKE, scales=FAKE, qrows=4, qcols=64, restore=False):
+        m, q = metis.Mat(ptr, rows, cols, ld, dtype), metis.Mx8(codes, scales, qrows, qcols)
+        return (L.metis_dequantize_mx8(None, C.byref(q), C.byref(m)) if restore else L.metis_quantize_mx8(None, C.byref(m), C.byref(q)))
+
+    for restore in (False, True):
+        assert call(ptr=None, restore=restore) == INVALID and call(codes=None, restore=restore) == INVALID
+        assert call(scales=None, restore=restore) == INVALID and call(dtype=3, restore=restore) == INVALID
+        assert call(qcols=48, restore=restore) == INVALID and call(qrows=5, restore=restore) == SHAPE and call(cols=32, restore=restore) == SHAPE
+        assert call(ld=60, restore=restore) == SHAPE and call(ld=68, restore=restore) == SHAPE and call(ptr=FAKE + 8, restore=restore) == SHAPE
+        assert call(codes=FAKE + 4, restore=restore) == SHAPE
+        assert call(cols=1 << 29, qcols=1 << 29, ld=1 << 29, restore=restore) == UNSUPPORTED
+        assert call(rows=0, qrows=0, ptr=None, restore=restore) == 0
+    assert L.metis_quantize_mx8(None, None, None) == INVALID and L.metis_dequantize_mx8(None, None, None) == INVALID
+
+
+def test_swiglu(metis):
+    L = metis.lib()
+
+    def call(S=4, F=32, gu=(4, 64, 64, 0), act=(4, 32, 32, 0), q=(4, 64), gp=FAKE, ap=FAKE, grads=False):
+        g, a, s = metis.Mat(gp, *gu), metis.Mat(ap, *act), metis.Mx8(FAKE, FAKE, *q)
+        if grads:
+            return L.metis_swiglu_grads(None, C.byref(s), C.byref(a), C.byref(g), None)
+        return L.metis_swiglu(None, C.byref(g), C.byref(a), C.byref(s))
+
+    for grads in (False, True):
+        assert call(gp=None, grads=grads) == INVALID and call(ap=None, grads=grads) == INVALID
+        assert call(act=(4, 32, 32, 1), grads=grads) == SHAPE and call(act=(4, 48, 48, 0), gu=(4, 96, 96, 0), q=(4, 96), grads=grads) == SHAPE
+        assert call(act=(3, 32, 32, 0), grads=grads) == SHAPE and call(act=(4, 32, 36, 0), grads=grads) == SHAPE
+        assert call(q=(4, 128), grads=grads) == SHAPE and call(gu=(4, 64, 66, 0), grads=grads) == SHAPE
+    assert L.metis_swiglu(None, None, None, None) == INVALID and L.metis_swiglu_grads(None, None, None, None, None) == INVALID
+
+
+def test_combine(metis):
+    L = metis.lib()
+
+    def call(rows=(8, 64, 64, 0), y=(4, 64, 64, 0), tokens=4, k=2, experts=8, rp=FAKE, yp=FAKE, slot=FAKE, w=FAKE, dw=FAKE, drows=None, grads=False):
+        r, o, p = metis.Mat(rp, *rows), metis.Mat(yp, *y), metis.Plan(FAKE, FAKE, slot, tokens, experts, k)
+        if grads:
+            d = metis.Mat(FAKE, *(drows or rows))
+            return L.metis_combine_grads(None, C.byref(o), C.byref(r), C.byref(p), w, C.byref(d), dw)
+        return L.metis_combine(None, C.byref(r), C.byref(p), w, C.byref(o))
+
+    for grads in (False, True):
+        assert call(rp=None, grads=grads) == INVALID and call(yp=None, grads=grads) == INVALID and call(slot=None, grads=grads) == INVALID
+        assert call(rows=(8, 64, 64, 2), grads=grads) == INVALID and call(tokens=-1, grads=grads) == INVALID
+        assert call(rows=(9, 64, 64, 0), grads=grads) == SHAPE and call(y=(5, 64, 64, 0), grads=grads) == SHAPE
+        assert call(y=(4, 32, 64, 0), grads=grads) == SHAPE and call(rows=(8, 64, 63, 0), grads=grads) == SHAPE
+        assert call(rows=(68, 64, 64, 0), k=17, grads=grads) == UNSUPPORTED
+        assert call(tokens=0, grads=grads) == 0
+    assert call(rows=(8, 1 << 29, 1 << 29, 0), y=(4, 1 << 29, 1 << 29, 0)) == UNSUPPORTED
+    assert call(w=None, grads=True) == INVALID and call(dw=None, grads=True) == INVALID
+    assert call(drows=(8, 64, 64, 1), grads=True) == INVALID and call(drows=(8, 64, 63, 0), grads=True) == SHAPE
