@@ -448,6 +448,40 @@ typedef struct {
 size_t metis_dispatch_workspace_bytes(int64_t tokens, int experts, int k);
 int metis_dispatch(void* stream, const int32_t* idx, metis_expert_plan* plan, void* workspace, size_t workspace_bytes);
 
+/* ---- mixture of experts: products in MXFP4 ------------------------------------------------------ */
+
+/*
+ * C [S, N] = the slots' rows times their experts' weights: C[s, :] = Q(A[r, :]) W_e^T, S = tokens * k, e the expert of slot s, r = token[s]
+ * with gather (A [tokens, K]), r = s without (A [S, K]).  W: the experts' weights [N, K] quantized by metis_quantize_mx, one below the
+ * other (rows = experts * N, cols = K).  A (bf16 or fp32) is quantized to MXFP4 on the way, as metis_quantize_mx does; the products are exact
+ * and accumulate in fp32.  C: bf16 or fp32; its rows of slots that serve no choice become 0.  With W of metis_quantize_mx_t this is the input gradient.
+ * The plan is read on the device: its offsets, and token with gather.
+ *   K % 32 == 0; A's rows 16-byte aligned; W's codes 16-byte, scales 8-byte aligned; workspace 256-byte aligned, metis_experts_workspace_bytes(A->rows, K).
+ * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (experts > 512, k > 16, a
+ * grid or an offset beyond the hardware's: 2^20 slots, 2^32 bytes of codes in A or in one expert's weights).
+ */
+size_t metis_experts_workspace_bytes(int64_t rows, int64_t K);
+int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W, const metis_expert_plan* plan, int gather, metis_mat* C,
+                          void* workspace, size_t workspace_bytes);
+
+/*
+ * MXFP4 with blocks along the rows: A [groups * M, cols] (bf16 or fp32) is `groups` matrices [M, cols], each of which is transposed and
+ * quantized along its M.  out [groups * cols, M].  For the input gradient the experts' stacked weights [experts * N, K] become [experts * K, N].
+ * M % 32 == 0, cols % 8 == 0, A's rows and out's codes 16-byte aligned.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED.
+ */
+int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups, metis_mxfp4* out);
+
+/*
+ * The experts' weight gradients dW [experts * N, K] (bf16 or fp32): dW_e = Q(G_e^T) Q(X_e^T)^T over the slots of expert e, G [S, N] by slot,
+ * X by slot ([S, K]) or, with gather, by token ([tokens, K]).  Both (bf16 or fp32) are quantized to MXFP4 in blocks of 32 consecutive
+ * slots of one expert, from its first; what its last block lacks is zeros.  An expert without slots gets 0.
+ *   N, K multiples of 8; G's and X's rows 16-byte aligned; workspace 256-byte aligned, metis_experts_wgrad_workspace_bytes(S, ...) bytes.
+ * Errors: as for metis_experts_product.
+ */
+size_t metis_experts_wgrad_workspace_bytes(int64_t slots, int experts, int64_t N, int64_t K);
+int metis_experts_wgrad(void* stream, const metis_mat* G, const metis_mat* X, const metis_expert_plan* plan, int gather, metis_mat* dW,
+                        void* workspace, size_t workspace_bytes);
+
 /* ---- mixture of experts: rows back to tokens ----------------------------------------------------- */
 
 /*

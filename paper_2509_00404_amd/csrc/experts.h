@@ -1,0 +1,86 @@
+// The experts' slots on the device, and MXFP4 blocks: what the kernels of the experts' products share.
+#pragma once
+#include "elementwise.h"
+
+#define EXPERTS_MAX 512
+#define SLOT_ALIGN 64                     // segments of a matrix quantized along the slots are padded to this many
+
+namespace {
+
+// Where unit u lies when every expert's slots are cut into units of `size` (the last of an expert may be short, an expert without slots has
+// none): the expert, its slots, and the unit's number among its own.  expert = -1 behind the last unit; `total` = units in all.  Every
+// wave looks for itself, its lanes holding neighbouring experts; offsets are held to 0 <= o <= S, whatever the memory says.
+struct SlotUnit {
+    int expert, local, total;
+    int64_t begin, end;                   // the expert's slots
+    int64_t padded;                       // slots of the experts before it, each padded to whole units
+};
+__device__ __forceinline__ int64_t held(int32_t o, int64_t S) { return o < 0 ? 0 : o > S ? S : o; }
+__device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offsets, int E, int64_t S, int size, int64_t u) {
+    const int lane = (int)threadIdx.x & 63, q = (E + 63) >> 6;
+    int mine = 0;
+    for (int i = 0; i < q; ++i) {
+        const int e = lane * q + i;
+        if (e < E) {
+            const int64_t n = held(offsets[e + 1], S) - held(offsets[e], S);
+            if (n > 0) mine += (int)((n + size - 1) / size);
+        }
+    }
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    SlotUnit r;
+    r.total = __builtin_amdgcn_readlane(upto, 63);
+    r.expert = -1;
+    r.local = 0;
+    r.begin = r.end = r.padded = 0;
+    if (u >= r.total) return r;
+    const uint64_t behind = __ballot(upto > u);
+    const int at = __ffsll((unsigned long long)behind) - 1;
+    int64_t before = __builtin_amdgcn_readlane(upto - mine, at);
+    for (int i = 0; i < q; ++i) {
+        const int e = at * q + i;
+        if (e >= E) break;
+        const int64_t b = held(offsets[e], S), n = held(offsets[e + 1], S) - b;
+        if (n <= 0) continue;
+        const int64_t units = (n + size - 1) / size;
+        if (u < before + units) {
+            r.expert = e;
+            r.local = (int)(u - before);
+            r.begin = b;
+            r.end = b + n;
+            r.padded = before * size;
+            return r;
+        }
+        before += units;
+    }
+    return r;
+}
+// units of `size` that S slots can fall into
+inline int64_t most_units(int64_t S, int E, int size) { return S / size + (E < S ? E : S); }
+
+// One MXFP4 block: X = 2^(floor(log2 amax) - 2), codes nearest, ties to the even one, saturated at 6
+__device__ __forceinline__ ew_u4 mx_block(const float (&v)[32], uint32_t& byte) {
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(v[i]));
+    const int field = (int)(__float_as_uint(amax) >> 23);
+    byte = field > 2 ? (field < 255 ? field - 2 : 254) : 0;
+    const float inv = __uint_as_float(byte < 254 ? (254u - byte) << 23 : 0x400000u);          // exact: a power of two
+    ew_u4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t c = 0u;
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i] * inv, v[8 * i + 1] * inv, 1.0f, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i + 2] * inv, v[8 * i + 3] * inv, 1.0f, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i + 4] * inv, v[8 * i + 5] * inv, 1.0f, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i + 6] * inv, v[8 * i + 7] * inv, 1.0f, 3);
+        w[i] = c;
+    }
+    return w;
+}
+
+}  // namespace

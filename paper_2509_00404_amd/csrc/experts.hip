@@ -1,0 +1,259 @@
+// The experts' products in MXFP4: the slots' rows with their experts' weights, and the weights' gradients.
+#include <type_traits>
+#include "experts.h"
+
+typedef int ex_i8 __attribute__((ext_vector_type(8)));
+typedef float ex_f4 __attribute__((ext_vector_type(4)));
+
+namespace {
+
+// ---- blocks along the rows: A^T quantized, segment by segment ----
+// A segment's result is a matrix of its own, [cols, its rows], behind those of the segments before it.  A lane holds 32 rows of two
+// neighbouring columns, a wave 128 columns, a workgroup 64 rows x 256 columns.  With a plan the segments are the experts' slots, padded
+// to 64 with zeros, and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows` rows.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols, const int32_t* __restrict__ offsets, int E, int64_t S,
+                const int32_t* __restrict__ token, int64_t rows, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t unit = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
+    int64_t begin, end, stride, base, first;              // the segment's rows, its padded length, its place, the unit's first row in it
+    if (offsets) {
+        const SlotUnit u = find_unit(offsets, E, S, SLOT_ALIGN, unit);
+        if (u.expert < 0) return;
+        begin = u.begin;
+        end = u.end;
+        stride = (end - begin + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
+        base = u.padded * cols;
+        first = (int64_t)u.local * SLOT_ALIGN;
+    } else {
+        const int64_t per = (rows + SLOT_ALIGN - 1) / SLOT_ALIGN, g = unit / per;
+        begin = g * rows;
+        end = begin + rows;
+        stride = rows;
+        base = begin * cols;
+        first = (unit - g * per) * SLOT_ALIGN;
+    }
+    first += 32 * (wave & 1);
+    const int64_t col = ((int64_t)blockIdx.x * 2 + (wave >> 1)) * 128 + 2 * lane;
+    if (first >= stride || col >= cols) return;
+    const int64_t left = end - begin - first;
+    float v[2][32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        v[0][i] = v[1][i] = 0.0f;
+        if (i < left) {
+            int64_t r = begin + first + i;
+            if (token) {
+                r = token[r];
+                if ((uint64_t)r >= (uint64_t)arows) continue;
+            }
+            const T* p = A + r * ld + col;
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+                v[0][i] = bf16lo_to_f32(w);
+                v[1][i] = bf16hi_to_f32(w);
+            } else {
+                const float2 w = *reinterpret_cast<const float2*>(p);
+                v[0][i] = w.x;
+                v[1][i] = w.y;
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        uint32_t byte;
+        const ew_u4 w = mx_block(v[c], byte);
+        const int64_t at = base + (col + c) * stride + first;
+        *reinterpret_cast<ew_u4*>(codes + at / 2) = w;
+        scales[at / 32] = (uint8_t)byte;
+    }
+}
+
+// ---- products straight from memory ----
+// A wave makes 16 x 16 outputs by v_mfma_scale_f32_16x16x128_f8f6f4: a lane's operand is the 32 codes (16 bytes) of row lane % 16,
+// contraction block lane / 16, and that block's scale.  X's rows (the first operand) are the outputs' fast axis: a lane ends with four
+// neighbouring ones.
+struct MxRows {
+    const uint8_t* codes;
+    const uint8_t* scales;
+};
+// this lane's row of either operand, blocks of 32 (nblk >= 0 in all)
+__device__ __forceinline__ ex_f4 mx_product16(MxRows x, MxRows y, int64_t nblk) {
+    const int kb = ((int)threadIdx.x & 63) >> 4;
+    ex_f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t b = kb; b - kb < nblk; b += 4) {
+        ew_u4 p = {0u, 0u, 0u, 0u}, q = {0u, 0u, 0u, 0u};
+        int ps = 0x7F, qs = 0x7F;
+        if (b < nblk) {
+            p = *reinterpret_cast<const ew_u4*>(x.codes + 16 * b);
+            q = *reinterpret_cast<const ew_u4*>(y.codes + 16 * b);
+            ps = x.scales[b];
+            qs = y.scales[b];
+        }
+        const ex_i8 pa = {(int)p[0], (int)p[1], (int)p[2], (int)p[3], 0, 0, 0, 0}, qa = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0};
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(pa, qa, acc, 4, 4, 0, ps, 0, qs);
+    }
+    return acc;
+}
+template <typename OUT>
+__device__ __forceinline__ void put4(OUT* p, ex_f4 v, int64_t left) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) {
+            const float one[1] = {v[i]};
+            store_row<1>(p + i, one);
+        }
+}
+
+// C[s, n] of up to 16 slots of one expert and 64 of its N outputs; behind the last unit of slots the workgroups clear the unused ones
+template <typename OUT>
+__global__ void __launch_bounds__(256)
+k_experts_few(MxRows A, int64_t arows, MxRows W, const int32_t* __restrict__ offsets, const int32_t* __restrict__ token, int E, int64_t S,
+              int64_t N, int64_t nblk, OUT* __restrict__ C, int64_t ldc) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15;
+    const SlotUnit u = find_unit(offsets, E, S, 16, blockIdx.y);
+    const int64_t n0 = ((int64_t)blockIdx.x * 4 + wave) * 16, nq = n0 + 4 * (lane >> 4);
+    if (u.expert < 0) {
+        const int64_t used = held(offsets[E], S), step = (int64_t)(gridDim.y - u.total) * 16;
+        for (int64_t s = used + ((int64_t)blockIdx.y - u.total) * 16 + li; s < S; s += step)
+            put4(C + s * ldc + nq, ex_f4{0.0f, 0.0f, 0.0f, 0.0f}, N - nq);
+        return;
+    }
+    if (n0 >= N) return;
+    const int64_t s = u.begin + 16 * (int64_t)u.local + li, sr = s < u.end ? s : u.end - 1;
+    uint64_t row = token ? (uint64_t)(uint32_t)token[sr] : (uint64_t)sr;
+    if (row >= (uint64_t)arows) row = arows - 1;
+    const uint64_t n = (uint64_t)u.expert * N + (n0 + li < N ? n0 + li : N - 1);
+    const ex_f4 acc = mx_product16({W.codes + n * nblk * 16, W.scales + n * nblk}, {A.codes + row * nblk * 16, A.scales + row * nblk}, nblk);
+    if (s < u.end) put4(C + s * ldc + nq, acc, N - nq);
+}
+
+// dW_e[n, k], 16 x 64 of it, over the expert's padded slots
+template <typename OUT>
+__global__ void __launch_bounds__(256)
+k_experts_wgrad(MxRows Gt, MxRows Xt, const int32_t* __restrict__ offsets, int E, int64_t S, int64_t N, int64_t K, OUT* __restrict__ dW,
+                int64_t ldw) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, e = blockIdx.z;
+    const int64_t n0 = (int64_t)blockIdx.y * 16, k0 = ((int64_t)blockIdx.x * 4 + wave) * 16, kq = k0 + 4 * (lane >> 4);
+    int64_t before = 0;
+    for (int i = 0; i < e; ++i) {
+        const int64_t n = held(offsets[i + 1], S) - held(offsets[i], S);
+        if (n > 0) before += (n + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
+    }
+    int64_t len = held(offsets[e + 1], S) - held(offsets[e], S);
+    len = len > 0 ? (len + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN : 0;
+    if (k0 >= K) return;
+    const int64_t g = before * N + (n0 + li < N ? n0 + li : N - 1) * len, x = before * K + (k0 + li < K ? k0 + li : K - 1) * len;
+    const ex_f4 acc = mx_product16({Xt.codes + x / 2, Xt.scales + x / 32}, {Gt.codes + g / 2, Gt.scales + g / 32}, len / 32);
+    if (n0 + li < N) put4(dW + ((int64_t)e * N + n0 + li) * ldw + kq, acc, K - kq);
+}
+
+int experts_plan_status(const metis_expert_plan* p) {
+    if (!p || !p->offsets || p->tokens < 0 || p->k < 1 || p->experts < 1) return METIS_INVALID_ARG;
+    if (p->experts > EXPERTS_MAX || p->k > 16) return METIS_UNSUPPORTED;
+    if (p->tokens > 0x7FFFFFFFll / p->k) return METIS_BAD_SHAPE;
+    return METIS_OK;
+}
+// quantize A^T by segments of a plan (token may be null) or of `rows` rows
+int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_plan* p, bool gather, int64_t rows, uint8_t* codes,
+                         uint8_t* scales) {
+    const int64_t S = p ? p->tokens * p->k : 0;
+    const int64_t units = p ? most_units(S, p->experts, SLOT_ALIGN) : A->rows / rows * ceil_div64(rows, SLOT_ALIGN);
+    const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
+    const dim3 grid((unsigned)ceil_div64(A->cols, 256), (unsigned)gy, (unsigned)gz);
+    if (gz > 65535) return METIS_UNSUPPORTED;
+    auto launch = [&](auto kern, auto zero) {
+        hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->rows, A->cols, p ? p->offsets : nullptr,
+                           p ? p->experts : 0, S, gather ? p->token : nullptr, rows, codes, scales);
+    };
+    if (A->dtype == METIS_BF16) launch(k_quantize_mx_t<bf16_t>, bf16_t());
+    else launch(k_quantize_mx_t<float>, float());
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+int64_t padded_slots(int64_t S, int E) { return most_units(S, E, SLOT_ALIGN) * SLOT_ALIGN; }
+size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * cols / 2, 256) + align_up((size_t)rows * cols / 32, 256); }
+
+}  // namespace
+
+extern "C" int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups, metis_mxfp4* out) {
+    if (!mat_ok(A) || !out || !out->codes || !out->scales || groups < 1 || A->rows < 1 || A->cols < 1) return METIS_INVALID_ARG;
+    if (A->rows % groups || A->rows / groups % 32 || A->cols % 8 || A->ld < A->cols || !mat_aligned16(A) || (uintptr_t)out->codes % 16 ||
+        out->rows != groups * A->cols || out->cols != A->rows / groups)
+        return METIS_BAD_SHAPE;
+    return launch_quantize_mx_t((hipStream_t)stream, A, nullptr, false, A->rows / groups, out->codes, out->scales);
+}
+
+extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int64_t K) { return rows > 0 && K > 0 && K % 32 == 0 ? mx_bytes(rows, K) : 0; }
+
+extern "C" int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W, const metis_expert_plan* plan, int gather,
+                                     metis_mat* C, void* workspace, size_t workspace_bytes) {
+    const int st = experts_plan_status(plan);
+    if (st != METIS_OK) return st;
+    if (plan->tokens == 0) return METIS_OK;
+    if (!mat_ok(A) || !W || !W->codes || !W->scales || !mat_ok(C) || (gather && !plan->token)) return METIS_INVALID_ARG;
+    const int64_t S = plan->tokens * plan->k, K = W->cols, N = W->rows / plan->experts;
+    if (K < 32 || K % 32 || W->rows < 1 || W->rows % plan->experts || A->cols != K || A->ld < K || A->rows != (gather ? plan->tokens : S) ||
+        C->rows != S || C->cols != N || C->ld < N || !mat_aligned16(A) || (uintptr_t)W->codes % 16)
+        return METIS_BAD_SHAPE;
+    if (!workspace || workspace_bytes < metis_experts_workspace_bytes(A->rows, K)) return METIS_WORKSPACE_TOO_SMALL;
+    if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
+    uint8_t* codes = (uint8_t*)workspace;
+    metis_mxfp4 q = {codes, codes + align_up((size_t)A->rows * K / 2, 256), A->rows, K};
+    const int qs = metis_quantize_mx(stream, A, &q);
+    if (qs != METIS_OK) return qs;
+    const int64_t units = most_units(S, plan->experts, 16) + 1, nb = ceil_div64(N, 64);
+    if (units > 65535 || nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    auto launch = [&](auto kern, auto zero) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)nb, (unsigned)units), dim3(256), 0, (hipStream_t)stream, MxRows{q.codes, q.scales}, A->rows,
+                           MxRows{W->codes, W->scales}, plan->offsets, gather ? plan->token : nullptr, plan->experts, S, N, K / 32,
+                           (decltype(zero)*)C->ptr, C->ld);
+    };
+    if (C->dtype == METIS_BF16) launch(k_experts_few<bf16_t>, bf16_t());
+    else launch(k_experts_few<float>, float());
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+
+extern "C" size_t metis_experts_wgrad_workspace_bytes(int64_t slots, int experts, int64_t N, int64_t K) {
+    if (slots < 1 || experts < 1 || experts > EXPERTS_MAX || N < 1 || K < 1) return 0;
+    const int64_t P = padded_slots(slots, experts);
+    return mx_bytes(N, P) + mx_bytes(K, P);
+}
+
+extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis_mat* X, const metis_expert_plan* plan, int gather,
+                                   metis_mat* dW, void* workspace, size_t workspace_bytes) {
+    const int st = experts_plan_status(plan);
+    if (st != METIS_OK) return st;
+    const int64_t S = plan->tokens * plan->k, E = plan->experts;
+    if (!G || !X || !mat_ok(dW) || (S > 0 && (!mat_ok(G) || !mat_ok(X) || (gather && !plan->token)))) return METIS_INVALID_ARG;
+    const int64_t N = G->cols, K = X->cols;
+    if (N < 1 || K < 1 || N % 8 || K % 8 || G->rows != S || X->rows != (gather ? plan->tokens : S) || dW->rows != E * N || dW->cols != K ||
+        dW->ld < K)
+        return METIS_BAD_SHAPE;
+    if (S > 0 && (G->ld < N || X->ld < K || !mat_aligned16(G) || !mat_aligned16(X))) return METIS_BAD_SHAPE;
+    if (ceil_div64(N, 16) > 65535) return METIS_UNSUPPORTED;
+    const size_t need = metis_experts_wgrad_workspace_bytes(S, (int)E, N, K);
+    if (workspace_bytes < need || (need && !workspace)) return METIS_WORKSPACE_TOO_SMALL;
+    if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
+    const int64_t P = S > 0 ? padded_slots(S, (int)E) : 0;
+    uint8_t* w = (uint8_t*)workspace;
+    const MxRows g = {w, w + align_up((size_t)N * P / 2, 256)};
+    w += mx_bytes(N, P);
+    const MxRows x = {w, w + align_up((size_t)K * P / 2, 256)};
+    hipStream_t s = (hipStream_t)stream;
+    if (S > 0) {
+        int r = launch_quantize_mx_t(s, G, plan, false, 0, (uint8_t*)g.codes, (uint8_t*)g.scales);
+        if (r == METIS_OK) r = launch_quantize_mx_t(s, X, plan, gather != 0, 0, (uint8_t*)x.codes, (uint8_t*)x.scales);
+        if (r != METIS_OK) return r;
+    }
+    auto launch = [&](auto kern, auto zero) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div64(K, 64), (unsigned)ceil_div64(N, 16), (unsigned)E), dim3(256), 0, s, g, x,
+                           plan->offsets, (int)E, S, N, K, (decltype(zero)*)dW->ptr, dW->ld);
+    };
+    if (dW->dtype == METIS_BF16) launch(k_experts_wgrad<bf16_t>, bf16_t());
+    else launch(k_experts_wgrad<float>, float());
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}

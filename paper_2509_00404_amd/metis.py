@@ -114,6 +114,13 @@ _SIGNATURES = {
     "metis_route_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Router), C.c_void_p, C.c_void_p, C.POINTER(Mat)]),
     "metis_dispatch_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int, C.c_int]),
     "metis_dispatch": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(Plan), C.c_void_p, C.c_size_t]),
+    "metis_experts_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "metis_experts_product": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(MxFp4), C.POINTER(Plan), C.c_int, C.POINTER(Mat), C.c_void_p,
+                                        C.c_size_t]),
+    "metis_quantize_mx_t": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.c_int, C.POINTER(MxFp4)]),
+    "metis_experts_wgrad_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int, C.c_int64, C.c_int64]),
+    "metis_experts_wgrad": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Plan), C.c_int, C.POINTER(Mat), C.c_void_p,
+                                      C.c_size_t]),
     "metis_combine": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Plan), C.c_void_p, C.POINTER(Mat)]),
     "metis_combine_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Plan), C.c_void_p, C.POINTER(Mat), C.c_void_p]),
     "metis_quantize_mx8": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mx8)]),
@@ -538,6 +545,42 @@ def dispatch(idx, experts, plan=None, workspace=None):
                                 workspace.data_ptr() if workspace is not None else None,
                                 workspace.numel() if workspace is not None else 0))
     return plan
+
+
+def experts_workspace_bytes(rows, K):
+    return int(lib().metis_experts_workspace_bytes(rows, K))
+
+
+def experts_product(A, W, plan, Cmat, gather=False, workspace=None):
+    """Cmat [S, N] = rows of A (by slot, or with gather by token) times their experts' weights W (MxTensor [experts * N, K])."""
+    a, w, p, c = _mat(A), W.c(), plan.c(), _mat(Cmat)
+    if workspace is None:
+        workspace = torch.empty((experts_workspace_bytes(A.shape[0], A.shape[1]),), dtype=torch.uint8, device=A.device)
+    _check(lib().metis_experts_product(_stream(), C.byref(a), C.byref(w), C.byref(p), gather, C.byref(c), workspace.data_ptr(),
+                                       workspace.numel()))
+    return Cmat
+
+
+def quantize_mx_t(A, out, groups=1):
+    """The `groups` matrices stacked in A [groups * M, cols], each transposed and quantized along M -> out (MxTensor [groups * cols, M])."""
+    a, o = _mat(A), out.c()
+    _check(lib().metis_quantize_mx_t(_stream(), C.byref(a), groups, C.byref(o)))
+    return out
+
+
+def experts_wgrad_workspace_bytes(slots, experts, N, K):
+    return int(lib().metis_experts_wgrad_workspace_bytes(slots, experts, N, K))
+
+
+def experts_wgrad(G, X, plan, dW, gather=False, workspace=None):
+    """dW [experts * N, K] of G [S, N] and X (by slot, or with gather by token), quantized along the slots of each expert."""
+    g, x, p, d = _mat(G), _mat(X), plan.c(), _mat(dW)
+    if workspace is None:
+        workspace = torch.empty((experts_wgrad_workspace_bytes(G.shape[0], plan.experts, G.shape[1], X.shape[1]),), dtype=torch.uint8,
+                                device=dW.device)
+    _check(lib().metis_experts_wgrad(_stream(), C.byref(g), C.byref(x), C.byref(p), gather, C.byref(d), workspace.data_ptr(),
+                                     workspace.numel()))
+    return dW
 
 
 def combine(rows, plan, y, weights=None):

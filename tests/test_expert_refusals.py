@@ -120,3 +120,43 @@ def test_combine(metis):
     assert call(rows=(8, 1 << 29, 1 << 29, 0), y=(4, 1 << 29, 1 << 29, 0)) == UNSUPPORTED
     assert call(w=None, grads=True) == INVALID and call(dw=None, grads=True) == INVALID
     assert call(drows=(8, 64, 64, 1), grads=True) == INVALID and call(drows=(8, 64, 63, 0), grads=True) == SHAPE
+
+
+def test_products(metis):
+    L = metis.lib()
+
+    def product(A=(8, 64, 64, 0), W=(128, 64), C_=(8, 16, 16, 0), tokens=8, k=1, experts=8, gather=0, ap=FAKE, wp=FAKE, ws=FAKE, size=1 << 40, token=FAKE):
+        a, w, c = metis.Mat(ap, *A), metis.MxFp4(wp, FAKE, *W), metis.Mat(FAKE, *C_)
+        p = metis.Plan(FAKE, token, FAKE, tokens, experts, k)
+        return L.metis_experts_product(None, C.byref(a), C.byref(w), C.byref(p), gather, C.byref(c), ws, size)
+
+    assert product(tokens=0) == 0
+    assert product(ap=None) == INVALID and product(wp=None) == INVALID and product(tokens=-1) == INVALID and product(A=(8, 64, 64, 5)) == INVALID
+    assert product(gather=1, token=None) == INVALID and product(ws=FAKE + 16) == INVALID
+    assert product(experts=513) == UNSUPPORTED and product(k=17) == UNSUPPORTED and product(tokens=1 << 31) == SHAPE
+    assert product(A=(8, 48, 48, 0), W=(128, 48)) == SHAPE and product(W=(129, 64)) == SHAPE and product(A=(7, 64, 64, 0)) == SHAPE
+    assert product(C_=(7, 16, 16, 0)) == SHAPE and product(C_=(8, 16, 15, 0)) == SHAPE and product(A=(8, 64, 60, 0)) == SHAPE
+    assert product(A=(8, 64, 68, 0)) == SHAPE and product(wp=FAKE + 8) == SHAPE and product(ap=FAKE + 2) == SHAPE
+    need = L.metis_experts_workspace_bytes(8, 64)
+    assert need >= 8 * 64 // 2 + 8 * 2 and product(size=need - 1) == WORKSPACE and product(ws=None) == WORKSPACE
+    assert L.metis_experts_workspace_bytes(8, 48) == 0
+
+    def wgrad(G=(8, 16, 16, 0), X=(8, 64, 64, 0), dW=(128, 64, 64, 0), tokens=8, k=1, experts=8, gather=0, gp=FAKE, dp=FAKE, ws=FAKE, size=1 << 40):
+        g, x, d = metis.Mat(gp, *G), metis.Mat(FAKE, *X), metis.Mat(dp, *dW)
+        p = metis.Plan(FAKE, FAKE, FAKE, tokens, experts, k)
+        return L.metis_experts_wgrad(None, C.byref(g), C.byref(x), C.byref(p), gather, C.byref(d), ws, size)
+
+    assert wgrad(gp=None) == INVALID and wgrad(dp=None) == INVALID and wgrad(ws=FAKE + 16) == INVALID
+    assert wgrad(G=(8, 12, 16, 0), dW=(96, 64, 64, 0)) == SHAPE and wgrad(G=(7, 16, 16, 0)) == SHAPE and wgrad(X=(4, 64, 64, 0)) == SHAPE
+    assert wgrad(dW=(127, 64, 64, 0)) == SHAPE and wgrad(dW=(128, 64, 63, 0)) == SHAPE and wgrad(G=(8, 16, 20, 0)) == SHAPE
+    need = L.metis_experts_wgrad_workspace_bytes(8, 8, 16, 64)
+    assert need > 0 and wgrad(size=need - 1) == WORKSPACE and wgrad(ws=None) == WORKSPACE
+
+    def quantize_t(A=(64, 16, 16, 0), out=(32, 32), groups=2, ap=FAKE, codes=FAKE):
+        a, o = metis.Mat(ap, *A), metis.MxFp4(codes, FAKE, *out)
+        return L.metis_quantize_mx_t(None, C.byref(a), groups, C.byref(o))
+
+    assert quantize_t(ap=None) == INVALID and quantize_t(codes=None) == INVALID and quantize_t(groups=0) == INVALID
+    assert quantize_t(groups=3) == SHAPE and quantize_t(groups=4) == SHAPE and quantize_t(out=(16, 32)) == SHAPE
+    assert quantize_t(A=(64, 12, 16, 0), out=(24, 32)) == SHAPE and quantize_t(codes=FAKE + 8) == SHAPE and quantize_t(A=(64, 16, 20, 0)) == SHAPE
+    assert L.metis_quantize_mx_t(None, None, 1, None) == INVALID and L.metis_experts_product(None, None, None, None, 0, None, None, 0) == INVALID
