@@ -3,7 +3,7 @@
 #include "elementwise.h"
 
 #define EXPERTS_MAX 512
-#define SLOT_ALIGN 64                     // segments of a matrix quantized along the slots are padded to this many
+#define SLOT_ALIGN 128                    // segments of a matrix quantized along the slots are padded to this many: rows of whole dwords of scales
 
 namespace {
 
@@ -62,24 +62,31 @@ __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offset
 // units of `size` that S slots can fall into
 inline int64_t most_units(int64_t S, int E, int size) { return S / size + (E < S ? E : S); }
 
-// One MXFP4 block: X = 2^(floor(log2 amax) - 2), codes nearest, ties to the even one, saturated at 6
+// MXFP4: X = 2^(floor(log2 amax) - 2) as its E8M0 byte, 1 / X, and eight codes: nearest, ties to the even one, saturated at 6
+__device__ __forceinline__ uint32_t mx_scale(float amax) {
+    const int field = (int)(__float_as_uint(amax) >> 23);
+    return field > 2 ? (field < 255 ? field - 2 : 254) : 0;
+}
+__device__ __forceinline__ float mx_inverse(uint32_t byte) { return __uint_as_float(byte < 254u ? (254u - byte) << 23 : 0x400000u); }
+__device__ __forceinline__ uint32_t mx_pack8(float a, float b, float c, float d, float e, float f, float g, float h) {
+    uint32_t w = 0u;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, c, d, 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e, f, 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, g, h, 1.0f, 3);
+}
+// one block of a lane's own
 __device__ __forceinline__ ew_u4 mx_block(const float (&v)[32], uint32_t& byte) {
     float amax = 0.0f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(v[i]));
-    const int field = (int)(__float_as_uint(amax) >> 23);
-    byte = field > 2 ? (field < 255 ? field - 2 : 254) : 0;
-    const float inv = __uint_as_float(byte < 254 ? (254u - byte) << 23 : 0x400000u);          // exact: a power of two
-    ew_u4 w = {0u, 0u, 0u, 0u};
+    byte = mx_scale(amax);
+    const float inv = mx_inverse(byte);
+    ew_u4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t c = 0u;
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i] * inv, v[8 * i + 1] * inv, 1.0f, 0);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i + 2] * inv, v[8 * i + 3] * inv, 1.0f, 1);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i + 4] * inv, v[8 * i + 5] * inv, 1.0f, 2);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * i + 6] * inv, v[8 * i + 7] * inv, 1.0f, 3);
-        w[i] = c;
-    }
+    for (int i = 0; i < 4; ++i)
+        w[i] = mx_pack8(v[8 * i] * inv, v[8 * i + 1] * inv, v[8 * i + 2] * inv, v[8 * i + 3] * inv, v[8 * i + 4] * inv, v[8 * i + 5] * inv,
+                        v[8 * i + 6] * inv, v[8 * i + 7] * inv);
     return w;
 }
 

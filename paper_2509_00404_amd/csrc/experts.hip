@@ -1,5 +1,6 @@
 // The experts' products in MXFP4: the slots' rows with their experts' weights, and the weights' gradients.
 #include <type_traits>
+#include "mx_tile.h"
 #include "experts.h"
 
 typedef int ex_i8 __attribute__((ext_vector_type(8)));
@@ -9,34 +10,36 @@ namespace {
 
 // ---- blocks along the rows: A^T quantized, segment by segment ----
 // A segment's result is a matrix of its own, [cols, its rows], behind those of the segments before it.  A lane holds 32 rows of two
-// neighbouring columns, a wave 128 columns, a workgroup 64 rows x 256 columns.  With a plan the segments are the experts' slots, padded
-// to 64 with zeros, and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows` rows.
+// neighbouring columns, a wave 128 columns, a workgroup's waves 128 rows of them.  With a plan the segments are the experts' slots, padded
+// to 64 with zeros (in rows of whole 128), and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows`
+// rows.
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols, const int32_t* __restrict__ offsets, int E, int64_t S,
                 const int32_t* __restrict__ token, int64_t rows, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t unit = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
-    int64_t begin, end, stride, base, first;              // the segment's rows, its padded length, its place, the unit's first row in it
+    int64_t begin, end, stride, written, base, first;     // the segment's rows, its padded length and what is written of it, its place, the unit's first row
     if (offsets) {
         const SlotUnit u = find_unit(offsets, E, S, SLOT_ALIGN, unit);
         if (u.expert < 0) return;
         begin = u.begin;
         end = u.end;
         stride = (end - begin + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
+        written = (end - begin + 63) / 64 * 64;
         base = u.padded * cols;
         first = (int64_t)u.local * SLOT_ALIGN;
     } else {
         const int64_t per = (rows + SLOT_ALIGN - 1) / SLOT_ALIGN, g = unit / per;
         begin = g * rows;
         end = begin + rows;
-        stride = rows;
+        stride = written = rows;
         base = begin * cols;
         first = (unit - g * per) * SLOT_ALIGN;
     }
-    first += 32 * (wave & 1);
-    const int64_t col = ((int64_t)blockIdx.x * 2 + (wave >> 1)) * 128 + 2 * lane;
-    if (first >= stride || col >= cols) return;
+    first += 32 * wave;
+    const int64_t col = (int64_t)blockIdx.x * 128 + 2 * lane;
+    if (first >= written || col >= cols) return;
     const int64_t left = end - begin - first;
     float v[2][32];
 #pragma unroll
@@ -129,24 +132,41 @@ k_experts_few(MxRows A, int64_t arows, MxRows W, const int32_t* __restrict__ off
     if (s < u.end) put4(C + s * ldc + nq, acc, N - nq);
 }
 
-// dW_e[n, k], 16 x 64 of it, over the expert's padded slots
-template <typename OUT>
+#include "experts_stream.h"
+
+// ---- rows quantized for the products: [rows, K] -> codes in rows of `units` * 4 bytes, K filled up with zeros to a multiple of 256 ----
+// A lane per 8 elements, four lanes per block of 32.
+template <typename T>
 __global__ void __launch_bounds__(256)
-k_experts_wgrad(MxRows Gt, MxRows Xt, const int32_t* __restrict__ offsets, int E, int64_t S, int64_t N, int64_t K, OUT* __restrict__ dW,
-                int64_t ldw) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, e = blockIdx.z;
-    const int64_t n0 = (int64_t)blockIdx.y * 16, k0 = ((int64_t)blockIdx.x * 4 + wave) * 16, kq = k0 + 4 * (lane >> 4);
-    int64_t before = 0;
-    for (int i = 0; i < e; ++i) {
-        const int64_t n = held(offsets[i + 1], S) - held(offsets[i], S);
-        if (n > 0) before += (n + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
-    }
-    int64_t len = held(offsets[e + 1], S) - held(offsets[e], S);
-    len = len > 0 ? (len + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN : 0;
-    if (k0 >= K) return;
-    const int64_t g = before * N + (n0 + li < N ? n0 + li : N - 1) * len, x = before * K + (k0 + li < K ? k0 + li : K - 1) * len;
-    const ex_f4 acc = mx_product16({Xt.codes + x / 2, Xt.scales + x / 32}, {Gt.codes + g / 2, Gt.scales + g / 32}, len / 32);
-    if (n0 + li < N) put4(dW + ((int64_t)e * N + n0 + li) * ldw + kq, acc, K - kq);
+k_quantize_rows(const T* __restrict__ A, int64_t ld, int64_t K, uint64_t total, FastDiv units, uint8_t* __restrict__ codes,
+                uint8_t* __restrict__ scales) {
+    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= total) return;                                               // total is a multiple of 4: whole blocks leave
+    const uint64_t row = div_by(units, n);
+    const int64_t c = 8 * (int64_t)(n - row * units.d);
+    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < K) load_row<8>(A + row * ld + c, v);
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[i]));
+    amax = fmaxf(amax, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(amax), 0xB1, 0xF, 0xF, true)));
+    amax = fmaxf(amax, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(amax), 0x4E, 0xF, 0xF, true)));
+    const uint32_t byte = mx_scale(amax);
+    const float inv = mx_inverse(byte);
+    *reinterpret_cast<uint32_t*>(codes + 4 * n) = mx_pack8(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+    if ((threadIdx.x & 3) == 0) scales[n >> 2] = (uint8_t)byte;
+}
+
+// the weights' scales in rows of whole units of 8
+__global__ void __launch_bounds__(256)
+k_pad_scales(const uint8_t* __restrict__ from, uint64_t rows, uint32_t have, uint8_t* __restrict__ to, FastDiv words) {
+    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = div_by(words, n);
+    if (row >= rows) return;
+    const uint32_t c = 4u * (uint32_t)(n - row * words.d);
+    uint32_t w = 0u;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) w |= (c + i < have ? (uint32_t)from[row * have + c + i] : 127u) << (8 * i);
+    *reinterpret_cast<uint32_t*>(to + 4 * n) = w;
 }
 
 int experts_plan_status(const metis_expert_plan* p) {
@@ -161,7 +181,7 @@ int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_p
     const int64_t S = p ? p->tokens * p->k : 0;
     const int64_t units = p ? most_units(S, p->experts, SLOT_ALIGN) : A->rows / rows * ceil_div64(rows, SLOT_ALIGN);
     const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
-    const dim3 grid((unsigned)ceil_div64(A->cols, 256), (unsigned)gy, (unsigned)gz);
+    const dim3 grid((unsigned)ceil_div64(A->cols, 128), (unsigned)gy, (unsigned)gz);
     if (gz > 65535) return METIS_UNSUPPORTED;
     auto launch = [&](auto kern, auto zero) {
         hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->rows, A->cols, p ? p->offsets : nullptr,
@@ -173,7 +193,53 @@ int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_p
     return METIS_OK;
 }
 int64_t padded_slots(int64_t S, int E) { return most_units(S, E, SLOT_ALIGN) * SLOT_ALIGN; }
-size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * cols / 2, 256) + align_up((size_t)rows * cols / 32, 256); }
+// (a last unit of the stream reaches up to 128 bytes behind a row)
+size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * cols / 2, 256) + align_up((size_t)rows * cols / 32 + 128, 256); }
+
+// The stream takes products of tiles that it can fill; the rest goes straight from memory.
+bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
+    const int64_t Kp = (K + 255) / 256 * 256;
+    if (arows * (Kp / 2) > 0xFFFFFFFFll || K > (1 << 24) || most_units(S, E, 256) * ceil_div64(N, 256) > 0x3FFFFFFF) return false;
+    return S >= 16 * (int64_t)E;
+}
+struct ProductPlace {
+    int64_t Kp;                                   // K as the quantized rows have it
+    size_t scales, wscales, bytes;                // of the rows, of the weights in whole units (0: as they are), in all
+};
+ProductPlace product_place(bool stream, int64_t rows, int E, int64_t N, int64_t K) {
+    const int64_t Kp = stream ? (K + 255) / 256 * 256 : K;
+    ProductPlace p = {Kp, align_up((size_t)rows * Kp / 2, 256), 0, 0};
+    p.bytes = p.scales + align_up((size_t)rows * Kp / 32, 256);
+    if (Kp != K) {
+        p.wscales = p.bytes;
+        p.bytes += align_up((size_t)E * N * Kp / 32, 256);
+    }
+    return p;
+}
+int launch_quantize_rows(hipStream_t s, const metis_mat* A, int64_t Kp, uint8_t* codes, uint8_t* scales) {
+    const int st = units_status(A->rows, Kp / 8);
+    if (st != METIS_OK) return st;
+    const int64_t total = A->rows * (Kp / 8);
+    const FastDiv units = fast_div((uint32_t)(Kp / 8));
+    const dim3 grid((unsigned)ceil_div64(total, 256));
+    if (A->dtype == METIS_BF16)
+        hipLaunchKernelGGL(k_quantize_rows<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)A->ptr, A->ld, A->cols, (uint64_t)total, units, codes, scales);
+    else
+        hipLaunchKernelGGL(k_quantize_rows<float>, grid, dim3(256), 0, s, (const float*)A->ptr, A->ld, A->cols, (uint64_t)total, units, codes, scales);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+template <typename OUT, int MODE>
+int launch_stream(hipStream_t s, const ExStream& a, int64_t tiles, metis_mat* C) {
+    const int cus = device_cu_count();
+    static LdsLimitCache lds_set;
+    auto kern = k_experts_stream<OUT, MODE>;
+    if (cus < 1 || !ensure_dyn_lds((const void*)kern, EX_LDS, lds_set)) return METIS_HIP_ERROR;
+    const bool vec = mat_aligned16(C);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles < cus ? tiles : cus)), dim3(512), EX_LDS, s, a, (OUT*)C->ptr, C->ld, vec);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
 
 }  // namespace
 
@@ -185,7 +251,11 @@ extern "C" int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups,
     return launch_quantize_mx_t((hipStream_t)stream, A, nullptr, false, A->rows / groups, out->codes, out->scales);
 }
 
-extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int64_t K) { return rows > 0 && K > 0 && K % 32 == 0 ? mx_bytes(rows, K) : 0; }
+extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int experts, int64_t N, int64_t K) {
+    if (rows < 1 || experts < 1 || experts > EXPERTS_MAX || N < 1 || K < 32 || K % 32) return 0;
+    const size_t a = product_place(false, rows, experts, N, K).bytes, b = product_place(true, rows, experts, N, K).bytes;
+    return a > b ? a : b;
+}
 
 extern "C" int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W, const metis_expert_plan* plan, int gather,
                                      metis_mat* C, void* workspace, size_t workspace_bytes) {
@@ -194,20 +264,38 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     if (plan->tokens == 0) return METIS_OK;
     if (!mat_ok(A) || !W || !W->codes || !W->scales || !mat_ok(C) || (gather && !plan->token)) return METIS_INVALID_ARG;
     const int64_t S = plan->tokens * plan->k, K = W->cols, N = W->rows / plan->experts;
-    if (K < 32 || K % 32 || W->rows < 1 || W->rows % plan->experts || A->cols != K || A->ld < K || A->rows != (gather ? plan->tokens : S) ||
-        C->rows != S || C->cols != N || C->ld < N || !mat_aligned16(A) || (uintptr_t)W->codes % 16)
+    const int E = plan->experts;
+    if (K < 32 || K % 32 || W->rows < 1 || W->rows % E || A->cols != K || A->ld < K || A->rows != (gather ? plan->tokens : S) ||
+        C->rows != S || C->cols != N || C->ld < N || !mat_aligned16(A) || (uintptr_t)W->codes % 16 || (uintptr_t)W->scales % 8)
         return METIS_BAD_SHAPE;
-    if (!workspace || workspace_bytes < metis_experts_workspace_bytes(A->rows, K)) return METIS_WORKSPACE_TOO_SMALL;
+    if (!workspace || workspace_bytes < metis_experts_workspace_bytes(A->rows, E, N, K)) return METIS_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
-    uint8_t* codes = (uint8_t*)workspace;
-    metis_mxfp4 q = {codes, codes + align_up((size_t)A->rows * K / 2, 256), A->rows, K};
-    const int qs = metis_quantize_mx(stream, A, &q);
+    const bool streams = product_streams(S, E, N, A->rows, K);
+    const ProductPlace place = product_place(streams, A->rows, E, N, K);
+    uint8_t* ws = (uint8_t*)workspace;
+    hipStream_t s = (hipStream_t)stream;
+    const int qs = launch_quantize_rows(s, A, place.Kp, ws, ws + place.scales);
     if (qs != METIS_OK) return qs;
-    const int64_t units = most_units(S, plan->experts, 16) + 1, nb = ceil_div64(N, 64);
+    if (streams) {
+        const uint8_t* wscales = W->scales;
+        if (place.wscales) {
+            const FastDiv words = fast_div((uint32_t)(place.Kp / 128));
+            hipLaunchKernelGGL(k_pad_scales, dim3((unsigned)ceil_div64(W->rows * (place.Kp / 128), 256)), dim3(256), 0, s, W->scales,
+                               (uint64_t)W->rows, (uint32_t)(K / 32), ws + place.wscales, words);
+            METIS_LAUNCH_CHECK();
+            wscales = ws + place.wscales;
+        }
+        const int tn = (int)ceil_div64(N, 256);
+        const ExStream a = {{ws, ws + place.scales}, {W->codes, wscales}, plan->offsets, gather ? plan->token : nullptr, S, A->rows, N, K,
+                            (uint32_t)(place.Kp / 2), (uint32_t)(place.Kp / 32), E, 0, tn};
+        const int64_t tiles = most_units(S, E, 256) * tn;
+        return C->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_PRODUCT>(s, a, tiles, C) : launch_stream<float, EX_PRODUCT>(s, a, tiles, C);
+    }
+    const int64_t units = most_units(S, E, 16) + 1, nb = ceil_div64(N, 64);
     if (units > 65535 || nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
     auto launch = [&](auto kern, auto zero) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)nb, (unsigned)units), dim3(256), 0, (hipStream_t)stream, MxRows{q.codes, q.scales}, A->rows,
-                           MxRows{W->codes, W->scales}, plan->offsets, gather ? plan->token : nullptr, plan->experts, S, N, K / 32,
+        hipLaunchKernelGGL(kern, dim3((unsigned)nb, (unsigned)units), dim3(256), 0, s, MxRows{ws, ws + place.scales}, A->rows,
+                           MxRows{W->codes, W->scales}, plan->offsets, gather ? plan->token : nullptr, E, S, N, K / 32,
                            (decltype(zero)*)C->ptr, C->ld);
     };
     if (C->dtype == METIS_BF16) launch(k_experts_few<bf16_t>, bf16_t());
@@ -233,7 +321,8 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
         dW->ld < K)
         return METIS_BAD_SHAPE;
     if (S > 0 && (G->ld < N || X->ld < K || !mat_aligned16(G) || !mat_aligned16(X))) return METIS_BAD_SHAPE;
-    if (ceil_div64(N, 16) > 65535) return METIS_UNSUPPORTED;
+    const int64_t tm = ceil_div64(N, 256), tn = ceil_div64(K, 256), tiles = E * tm * tn;
+    if (S > (1 << 25) || N > (1 << 30) || K > (1 << 30) || tiles > 0x3FFFFFFF) return METIS_UNSUPPORTED;
     const size_t need = metis_experts_wgrad_workspace_bytes(S, (int)E, N, K);
     if (workspace_bytes < need || (need && !workspace)) return METIS_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
@@ -248,12 +337,6 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
         if (r == METIS_OK) r = launch_quantize_mx_t(s, X, plan, gather != 0, 0, (uint8_t*)x.codes, (uint8_t*)x.scales);
         if (r != METIS_OK) return r;
     }
-    auto launch = [&](auto kern, auto zero) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div64(K, 64), (unsigned)ceil_div64(N, 16), (unsigned)E), dim3(256), 0, s, g, x,
-                           plan->offsets, (int)E, S, N, K, (decltype(zero)*)dW->ptr, dW->ld);
-    };
-    if (dW->dtype == METIS_BF16) launch(k_experts_wgrad<bf16_t>, bf16_t());
-    else launch(k_experts_wgrad<float>, float());
-    METIS_LAUNCH_CHECK();
-    return METIS_OK;
+    const ExStream a = {g, x, plan->offsets, nullptr, S, 0, N, K, 0, 0, (int)E, (int)tm, (int)tn};
+    return dW->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_WGRAD>(s, a, tiles, dW) : launch_stream<float, EX_WGRAD>(s, a, tiles, dW);
 }

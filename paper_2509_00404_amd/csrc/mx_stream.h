@@ -1,29 +1,6 @@
 // The MXFP4 GEMM for large outputs (included by mxfp4.hip, inside its namespace).
 #pragma once
 
-// acc (+)= X Y^T, 32 x 32 over 64 columns, block scales in byte 0 (HI: 2) of xs and ys; the accumulator in the accumulation registers.
-// In asm for its place and its registers.  What the compiler then does not see: an accumulator read by a vector
-// instruction soon after (mxs_settle); operands come from LDS, scales are shifted a step ahead.
-template <bool FIRST, bool HI>
-__device__ __forceinline__ void mxs_mfma(float16_t& acc, const uvec4_t& x, const uvec4_t& y, uint32_t xs, uint32_t ys) {
-    if constexpr (FIRST)
-        asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, 0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4"
-                     : "=a"(acc) : "v"(x), "v"(y), "v"(xs), "v"(ys));
-    else if constexpr (HI)
-        asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[1,1,0] cbsz:4 blgp:4"
-                     : "+a"(acc) : "v"(x), "v"(y), "v"(xs), "v"(ys));
-    else
-        asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4"
-                     : "+a"(acc) : "v"(x), "v"(y), "v"(xs), "v"(ys));
-}
-__device__ __forceinline__ void mxs_settle(float16_t (&a)[2]) {
-    asm volatile("s_nop 15\n\ts_nop 15" : "+a"(a[0]), "+a"(a[1]));
-}
-// between a vector instruction's result and the matrix instruction that reads it
-__device__ __forceinline__ void mxs_settle_scales(uint32_t (&x)[6]) {
-    asm volatile("s_nop 1" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]));
-}
-
 // 256 x 256 tiles, 8 waves of 128 x 64, two per SIMD; a unit is 256 contraction elements, 128 bytes of every row = whole cache lines.
 // What it changed against the kernel above, which it took these products from: codes and scales go straight into LDS (no registers, no
 // LDS stores, and the waits leave the loop), the accumulators stay in the accumulation registers, the next tile's first unit travels
@@ -36,14 +13,7 @@ __device__ __forceinline__ void mxs_settle_scales(uint32_t (&x)[6]) {
 // read a third less from LDS but leave the pipe idle whenever a transfer is issued (45 cycles each), 287; a unit's fragments read
 // two steps ahead and its buffer given back a step earlier, the transfers' offsets then formed where they are issued, 277; starts of the
 // workgroups staggered by 0.5 to 2 us, stores past the caches: no difference.
-// LDS: two buffers of a unit: A's and B's codes row by row, 128 bytes a row, its 16-byte segments permuted by their number xor row / 2 %
-// 8 (a transfer's lanes land side by side, and this is what spreads sixteen rows' reads of one segment over the banks), then 8 scale
-// bytes of every row of both.
-#define MXS_CODES 32768
-#define MXS_SCALES 2048
-#define MXS_UNIT (2 * MXS_CODES + 2 * MXS_SCALES)
-#define MXS_LDS (2 * MXS_UNIT)
-#define MXS_DMA 10                                       // transfers a wave makes for a unit
+// LDS: two buffers of a unit (mx_tile.h).
 template <typename OUT>
 __global__ void __launch_bounds__(512, 2)
 k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C, int64_t ldc, bool vec, MxOrder order, int total) {

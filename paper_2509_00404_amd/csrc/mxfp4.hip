@@ -4,14 +4,10 @@
 // LDS straight into v_mfma_scale_f32_32x32x64_f8f6f4 with no expansion in the vector ALUs: this is
 // the chip's FP4 rate, against which the NVFP4 path (E4M3 scales per 16, expanded to fp16) can be read.
 #include <type_traits>
-#include "common.h"
-#include "gemm_tile.h"
-#include "stream_dev.h"
+#include "mx_tile.h"
 #include "../../include/metis.h"
 
 typedef int int8v_t __attribute__((ext_vector_type(8)));
-typedef uint32_t uvec4_t __attribute__((ext_vector_type(4)));   // a native vector: copies stay in registers
-typedef uint32_t uvec2_t __attribute__((ext_vector_type(2)));
 
 namespace {
 
@@ -92,7 +88,6 @@ k_quantize_mx(const T* __restrict__ A, int64_t ld, int64_t M, int64_t nblk /* co
 //    us instead of 188, 6144 x 6144 x 1024 47 for 45, 4352 x 4352 x 512 23.8 for 22.5 (128 x 128 tiles, where it makes no difference,
 //    use the one path).
 // The stage body is branch-free (stage indices are clamped; the last stage loads and stores data nobody uses).
-#define MX_KI 256
 #define MX_CROW (MX_KI / 2 + 16)      // padded code row in LDS: 144 bytes, 16-byte reads of 8 consecutive rows hit 8 bank groups
 #define MX_SROW 8                     // the row's eight scale bytes of a stage
 #define MX_BAND 4                     // tiles side by side in a band: an XCD has 4 of B's panels and 8 of A's in work
@@ -107,82 +102,6 @@ struct MxOperand {
     const uint8_t* scales;            // [rows, K/32]
     int64_t rows;
 };
-
-// four neighbouring outputs of a row
-__device__ __forceinline__ void mx_put4(bf16_t* p, float x, float y, float z, float w) {
-    typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
-    typedef float f2_t __attribute__((ext_vector_type(2)));
-    const f2_t lo = {x, y}, hi = {z, w};
-    *reinterpret_cast<uvec2_t*>(p) = uvec2_t{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf2_t)),
-                                             __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf2_t))};
-}
-__device__ __forceinline__ void mx_put4(float* p, float x, float y, float z, float w) {
-    *reinterpret_cast<float4*>(p) = make_float4(x, y, z, w);
-}
-
-// A wave's TM x TN accumulator tiles to memory.  LINES: 32 rows of its columns at a time are staged at sm (mx_wave_rows bytes), else
-// straight from the registers.  whole: the workgroup's tile is stored without looking at each element (mx_whole).
-template <typename OUT, int TN>
-constexpr int mx_wave_rows() { return 32 * (32 * TN * (int)sizeof(OUT) + 16); }
-// A tile inside the matrix; by way of LDS C has to allow 16-byte stores too, as vec says.  (Straight from the registers it has not: asked
-// for it all the same, fp32 rows off 16 bytes took 151 us for 8192 x 14336 x 512 and 353 for x 4096, 131 and 332 without.)
-template <bool LINES>
-__device__ __forceinline__ bool mx_whole(bool inside, bool vec) { return inside && (!LINES || vec); }
-template <typename OUT, bool LINES, int TM, int TN>
-__device__ __forceinline__ void mx_store_wave(const float16_t (&acc)[TM][TN], uint8_t* sm, OUT* __restrict__ C, int64_t ldc, int64_t m0,
-                                              int64_t n0, int64_t M, int64_t N, bool vec, bool whole, int lane) {
-    const int li = lane & 31, half = lane >> 5;
-    if constexpr (!LINES) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int64_t c = n0 + 32 * j + li;
-                const int64_t rbase = m0 + 32 * i + 4 * half;
-                if (whole) {
-                    store_tile16<OUT>(C + rbase * ldc + c, ldc, acc[i][j], 1.0f);
-                } else {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int64_t r = rbase + 8 * (v >> 2) + (v & 3);
-                        if (r < M && c < N) store_out<OUT>(C + r * ldc + c, acc[i][j][v]);
-                    }
-                }
-            }
-    } else {
-        constexpr int E = 16 / (int)sizeof(OUT), LROW = 32 * TN * (int)sizeof(OUT) + 16, UNITS = 32 * TN / E, ROWS = 64 / UNITS;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; v += 4)
-                    mx_put4(reinterpret_cast<OUT*>(sm + li * LROW) + 32 * j + 2 * v + 4 * half, acc[i][j][v], acc[i][j][v + 1],
-                            acc[i][j][v + 2], acc[i][j][v + 3]);
-            gs_wave_order();
-#pragma unroll
-            for (int t = 0; t < 32 / ROWS; ++t) {
-                const int row = ROWS * t + lane / UNITS, unit = lane % UNITS;
-                const uint8_t* q = sm + row * LROW + 16 * unit;
-                const uvec4_t w = *reinterpret_cast<const uvec4_t*>(q);
-                const int64_t r = m0 + 32 * i + row, c = n0 + E * unit;
-                OUT* p = C + r * ldc + c;
-                if (whole) {
-                    *reinterpret_cast<uvec4_t*>(p) = w;
-                } else if (r < M) {
-                    const int64_t left = N - c;
-                    if (vec && left >= E) {
-                        *reinterpret_cast<uvec4_t*>(p) = w;
-                    } else {
-#pragma unroll 1
-                        for (int e = 0; e < E && e < left; ++e) p[e] = reinterpret_cast<const OUT*>(q)[e];
-                    }
-                }
-            }
-            gs_wave_order();
-        }
-    }
-}
 
 // MODE: MX_WHOLE for K a multiple of the 256-deep stage.  Else the last stage exists only in part, and its missing blocks of 32 enter as
 // zero codes under a unit scale.  MX_TAIL: what is missing is put in on the way to LDS, where the data has arrived, so that
