@@ -455,12 +455,12 @@ int metis_dispatch(void* stream, const int32_t* idx, metis_expert_plan* plan, vo
  * with gather (A [tokens, K]), r = s without (A [S, K]).  W: the experts' weights [N, K] quantized by metis_quantize_mx, one below the
  * other (rows = experts * N, cols = K).  A (bf16 or fp32) is quantized to MXFP4 on the way, as metis_quantize_mx does; the products are exact
  * and accumulate in fp32.  C: bf16 or fp32; its rows of slots that serve no choice become 0.  With W of metis_quantize_mx_t this is the input gradient.
- * The plan is read on the device: its offsets, and token with gather.
- *   K % 32 == 0; A's rows 16-byte aligned; W's codes 16-byte, scales 8-byte aligned; workspace 256-byte aligned, metis_experts_workspace_bytes(A->rows, ...) bytes.
+ * The plan is read on the device: its offsets, and token and slot with gather.
+ *   K % 32 == 0; A's rows 16-byte aligned; W's codes 16-byte, scales 8-byte aligned; workspace 256-byte aligned, metis_experts_workspace_bytes(A->rows, S, ...) bytes.
  * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (experts > 512, k > 16, a
  * grid or an offset beyond the hardware's: 2^20 slots, 2^32 bytes of codes in A or in one expert's weights).
  */
-size_t metis_experts_workspace_bytes(int64_t rows, int experts, int64_t N, int64_t K);
+size_t metis_experts_workspace_bytes(int64_t rows, int64_t slots, int experts, int64_t N, int64_t K);
 int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W, const metis_expert_plan* plan, int gather, metis_mat* C,
                           void* workspace, size_t workspace_bytes);
 

@@ -3,7 +3,7 @@
 #include "elementwise.h"
 
 #define EXPERTS_MAX 512
-#define SLOT_ALIGN 128                    // segments of a matrix quantized along the slots are padded to this many: rows of whole dwords of scales
+#define SLOT_ALIGN 256                    // segments of a matrix quantized along the slots have rows of whole units of this many
 
 namespace {
 

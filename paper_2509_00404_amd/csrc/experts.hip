@@ -8,68 +8,101 @@ typedef float ex_f4 __attribute__((ext_vector_type(4)));
 
 namespace {
 
+// Scales as the stream reads them, "in units": [units of 256 contraction elements][rows][8 bytes], so that a tile's 256 rows have theirs of
+// a unit in 2 KB that lie together.  (Row by row, a unit's 8 bytes of every row cost as many cache lines as its codes: of 16384 tokens'
+// four experts, 2048 x 4096 each, 409 us with the quantizers; 356 without their transfers.)
+
 // ---- blocks along the rows: A^T quantized, segment by segment ----
 // A segment's result is a matrix of its own, [cols, its rows], behind those of the segments before it.  A lane holds 32 rows of two
-// neighbouring columns, a wave 128 columns, a workgroup's waves 128 rows of them.  With a plan the segments are the experts' slots, padded
-// to 64 with zeros (in rows of whole 128), and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows`
-// rows.
+// neighbouring columns, all of them in flight together; a workgroup's 8 waves have 256 rows of 128 columns, which leave by way of LDS as
+// whole lines.  With a plan the segments are the experts' slots, padded with zeros to a multiple of 64, in rows of whole units and with
+// scales in units, and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows` rows.
+// What bounds it: 32768 x 4096 gathered rows, 339 MB to be moved, take QT_X us, x 2048 by slot (170 MB) QT_G.
+#define QT_ROW 144                            // a column's 8 blocks of 16 bytes, and 16 that spread the columns over the banks
 template <typename T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(512)
 k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols, const int32_t* __restrict__ offsets, int E, int64_t S,
                 const int32_t* __restrict__ token, int64_t rows, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    __shared__ __attribute__((aligned(16))) uint8_t s_codes[128 * QT_ROW];
+    __shared__ __attribute__((aligned(16))) uint8_t s_scales[128 * 8];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t unit = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
-    int64_t begin, end, stride, written, base, first;     // the segment's rows, its padded length and what is written of it, its place, the unit's first row
+    int64_t begin, count, stride, written, base, first;   // the segment's rows, the length of its result's rows and what is written of them, its place; the unit's first row
     if (offsets) {
         const SlotUnit u = find_unit(offsets, E, S, SLOT_ALIGN, unit);
         if (u.expert < 0) return;
         begin = u.begin;
-        end = u.end;
-        stride = (end - begin + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
-        written = (end - begin + 63) / 64 * 64;
+        count = u.end - u.begin;
+        stride = (count + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
+        written = (count + 63) / 64 * 64;
         base = u.padded * cols;
         first = (int64_t)u.local * SLOT_ALIGN;
     } else {
         const int64_t per = (rows + SLOT_ALIGN - 1) / SLOT_ALIGN, g = unit / per;
         begin = g * rows;
-        end = begin + rows;
-        stride = written = rows;
+        count = stride = written = rows;
         base = begin * cols;
         first = (unit - g * per) * SLOT_ALIGN;
     }
-    first += 32 * wave;
-    const int64_t col = (int64_t)blockIdx.x * 128 + 2 * lane;
-    if (first >= written || col >= cols) return;
-    const int64_t left = end - begin - first;
-    float v[2][32];
+    const int64_t col0 = (int64_t)blockIdx.x * 128, col = col0 + 2 * lane, from = first + 32 * wave;
+    if (from < written) {
+        const int left = (int)(count - from < 32 ? count - from : 32);        // may be 0 or less: zeros
+        int64_t r = from + (lane & 31);
+        r = begin + (r < count ? r : count - 1);
+        if (token) r = token[r];
+        int row = (uint64_t)r < (uint64_t)arows ? (int)r : 0;
+        const T* p = A + (col < cols ? col : 0);
+        float v[2][32];
+        if constexpr (sizeof(T) == 2) {
+            uint32_t w[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        v[0][i] = v[1][i] = 0.0f;
-        if (i < left) {
-            int64_t r = begin + first + i;
-            if (token) {
-                r = token[r];
-                if ((uint64_t)r >= (uint64_t)arows) continue;
+            for (int i = 0; i < 32; ++i) w[i] = *reinterpret_cast<const uint32_t*>(p + (int64_t)__builtin_amdgcn_readlane(row, i) * ld);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                v[0][i] = bf16lo_to_f32(w[i]);
+                v[1][i] = bf16hi_to_f32(w[i]);
             }
-            const T* p = A + r * ld + col;
-            if constexpr (sizeof(T) == 2) {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
-                v[0][i] = bf16lo_to_f32(w);
-                v[1][i] = bf16hi_to_f32(w);
-            } else {
-                const float2 w = *reinterpret_cast<const float2*>(p);
-                v[0][i] = w.x;
-                v[1][i] = w.y;
+        } else {
+            float2 w[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = *reinterpret_cast<const float2*>(p + (int64_t)__builtin_amdgcn_readlane(row, i) * ld);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                v[0][i] = w[i].x;
+                v[1][i] = w[i].y;
             }
         }
-    }
+        if (left < 32) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        uint32_t byte;
-        const ew_u4 w = mx_block(v[c], byte);
-        const int64_t at = base + (col + c) * stride + first;
-        *reinterpret_cast<ew_u4*>(codes + at / 2) = w;
-        scales[at / 32] = (uint8_t)byte;
+            for (int i = 0; i < 32; ++i) {
+                v[0][i] = i < left ? v[0][i] : 0.0f;
+                v[1][i] = i < left ? v[1][i] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            uint32_t byte;
+            *reinterpret_cast<ew_u4*>(s_codes + (2 * lane + c) * QT_ROW + 16 * wave) = mx_block(v[c], byte);
+            s_scales[(2 * lane + c) * 8 + wave] = (uint8_t)byte;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = 64 * i + (tid >> 3), b = tid & 7;
+        if (col0 + c < cols && first + 32 * b < written)
+            *reinterpret_cast<ew_u4*>(codes + (base + (col0 + c) * stride + first + 32 * b) / 2) =
+                *reinterpret_cast<const ew_u4*>(s_codes + c * QT_ROW + 16 * b);
+    }
+    if (offsets) {
+        if (tid < 128 && col0 + tid < cols)
+            *reinterpret_cast<ew_u2*>(scales + base / 32 + (first / 256 * cols + col0 + tid) * 8) = *reinterpret_cast<const ew_u2*>(s_scales + 8 * tid);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = 64 * i + (tid >> 3), b = tid & 7;
+            if (col0 + c < cols && first + 32 * b < written) scales[(base + (col0 + c) * stride + first) / 32 + b] = s_scales[8 * c + b];
+        }
     }
 }
 
@@ -134,18 +167,52 @@ k_experts_few(MxRows A, int64_t arows, MxRows W, const int32_t* __restrict__ off
 
 #include "experts_stream.h"
 
-// ---- rows quantized for the products: [rows, K] -> codes in rows of `units` * 4 bytes, K filled up with zeros to a multiple of 256 ----
-// A lane per 8 elements, four lanes per block of 32.
-template <typename T>
+// ---- rows quantized for the products ----
+// [rows, K] -> codes, in rows of Kp elements (K filled up with zeros), and scales.  A lane per 8 elements, four lanes per block of 32.
+// UNITS: Kp is a multiple of 256, and the scales go in units to the rows' slots: a lane of the 16 that hold four blocks writes their bytes for
+// one choice.  The workgroups behind the rows' put the weights' scales in units.
+struct RowScales {
+    uint8_t* to;
+    const int32_t* slot;                          // [rows, k]: the slots of a row; null: its own number
+    int64_t S;
+    int k;
+};
+struct WeightScales {
+    const uint8_t* from;                          // [rows, have]
+    uint8_t* to;
+    int64_t rows;
+    int have, units;
+};
+__device__ __forceinline__ void lay_scales(const WeightScales& w, int64_t block) {
+    const int64_t row = block * 64 + (threadIdx.x & 63);
+    if (row >= w.rows) return;
+    for (int u = threadIdx.x >> 6; u < w.units; u += 4) {
+        ew_u2 v;
+        const uint8_t* p = w.from + row * w.have + 8 * u;
+        if (w.have % 8 == 0) {
+            v = *reinterpret_cast<const ew_u2*>(p);
+        } else {
+            v = ew_u2{0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i >> 2] |= (8 * u + i < w.have ? (uint32_t)p[i] : 127u) << (8 * (i & 3));
+        }
+        *reinterpret_cast<ew_u2*>(w.to + (u * w.rows + row) * 8) = v;
+    }
+}
+template <typename T, bool UNITS>
 __global__ void __launch_bounds__(256)
 k_quantize_rows(const T* __restrict__ A, int64_t ld, int64_t K, uint64_t total, FastDiv units, uint8_t* __restrict__ codes,
-                uint8_t* __restrict__ scales) {
+                RowScales rs, WeightScales ws, uint32_t row_blocks) {
+    if (UNITS && blockIdx.x >= row_blocks) {
+        lay_scales(ws, blockIdx.x - row_blocks);
+        return;
+    }
     const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (n >= total) return;                                               // total is a multiple of 4: whole blocks leave
+    if (n >= total) return;                                               // total is a multiple of 4 (UNITS: 32): whole blocks (units) leave
     const uint64_t row = div_by(units, n);
-    const int64_t c = 8 * (int64_t)(n - row * units.d);
+    const uint32_t unit = (uint32_t)(n - row * units.d);
     float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (c < K) load_row<8>(A + row * ld + c, v);
+    if (8 * (int64_t)unit < K) load_row<8>(A + row * ld + 8 * (int64_t)unit, v);
     float amax = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[i]));
@@ -154,19 +221,18 @@ k_quantize_rows(const T* __restrict__ A, int64_t ld, int64_t K, uint64_t total, 
     const uint32_t byte = mx_scale(amax);
     const float inv = mx_inverse(byte);
     *reinterpret_cast<uint32_t*>(codes + 4 * n) = mx_pack8(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
-    if ((threadIdx.x & 3) == 0) scales[n >> 2] = (uint8_t)byte;
-}
-
-// the weights' scales in rows of whole units of 8
-__global__ void __launch_bounds__(256)
-k_pad_scales(const uint8_t* __restrict__ from, uint64_t rows, uint32_t have, uint8_t* __restrict__ to, FastDiv words) {
-    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = div_by(words, n);
-    if (row >= rows) return;
-    const uint32_t c = 4u * (uint32_t)(n - row * words.d);
-    uint32_t w = 0u;
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) w |= (c + i < have ? (uint32_t)from[row * have + c + i] : 127u) << (8 * i);
-    *reinterpret_cast<uint32_t*>(to + 4 * n) = w;
+    if constexpr (UNITS) {
+        uint32_t w = byte << (8 * (threadIdx.x >> 2 & 3));
+        w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x124, 0xF, 0xF, true);         // around the 16 lanes by 4, then by 8
+        w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x128, 0xF, 0xF, true);
+        const int j = threadIdx.x & 15;
+        if (j < rs.k) {
+            const int64_t s = rs.slot ? rs.slot[row * rs.k + j] : (int64_t)row;
+            if ((uint64_t)s < (uint64_t)rs.S) *reinterpret_cast<uint32_t*>(rs.to + ((unit >> 5) * rs.S + s) * 8 + 4 * (unit >> 4 & 1)) = w;
+        }
+    } else {
+        if ((threadIdx.x & 3) == 0) rs.to[n >> 2] = (uint8_t)byte;
+    }
 }
 
 int experts_plan_status(const metis_expert_plan* p) {
@@ -182,9 +248,9 @@ int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_p
     const int64_t units = p ? most_units(S, p->experts, SLOT_ALIGN) : A->rows / rows * ceil_div64(rows, SLOT_ALIGN);
     const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
     const dim3 grid((unsigned)ceil_div64(A->cols, 128), (unsigned)gy, (unsigned)gz);
-    if (gz > 65535) return METIS_UNSUPPORTED;
+    if (gz > 65535 || A->rows > 0x7FFFFFFF) return METIS_UNSUPPORTED;
     auto launch = [&](auto kern, auto zero) {
-        hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->rows, A->cols, p ? p->offsets : nullptr,
+        hipLaunchKernelGGL(kern, grid, dim3(512), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->rows, A->cols, p ? p->offsets : nullptr,
                            p ? p->experts : 0, S, gather ? p->token : nullptr, rows, codes, scales);
     };
     if (A->dtype == METIS_BF16) launch(k_quantize_mx_t<bf16_t>, bf16_t());
@@ -193,8 +259,8 @@ int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_p
     return METIS_OK;
 }
 int64_t padded_slots(int64_t S, int E) { return most_units(S, E, SLOT_ALIGN) * SLOT_ALIGN; }
-// (a last unit of the stream reaches up to 128 bytes behind a row)
-size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * cols / 2, 256) + align_up((size_t)rows * cols / 32 + 128, 256); }
+// (a tile reads the scales of 256 rows wherever its own end)
+size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * cols / 2, 256) + align_up((size_t)rows * cols / 32, 256) + 2048; }
 
 // The stream takes products of tiles that it can fill; the rest goes straight from memory.
 bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
@@ -204,28 +270,29 @@ bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
 }
 struct ProductPlace {
     int64_t Kp;                                   // K as the quantized rows have it
-    size_t scales, wscales, bytes;                // of the rows, of the weights in whole units (0: as they are), in all
+    size_t scales, wscales, bytes;                // places of the rows' scales and of the weights', and the end
 };
-ProductPlace product_place(bool stream, int64_t rows, int E, int64_t N, int64_t K) {
+// (a tile reads the scales of 256 rows wherever its own end)
+ProductPlace product_place(bool stream, int64_t rows, int64_t S, int E, int64_t N, int64_t K) {
     const int64_t Kp = stream ? (K + 255) / 256 * 256 : K;
     ProductPlace p = {Kp, align_up((size_t)rows * Kp / 2, 256), 0, 0};
-    p.bytes = p.scales + align_up((size_t)rows * Kp / 32, 256);
-    if (Kp != K) {
-        p.wscales = p.bytes;
-        p.bytes += align_up((size_t)E * N * Kp / 32, 256);
-    }
+    p.wscales = p.bytes = p.scales + align_up((size_t)(stream ? S : rows) * Kp / 32, 256);
+    if (stream) p.bytes = p.wscales + 2048 + align_up((size_t)E * N * Kp / 32, 256) + 2048;
     return p;
 }
-int launch_quantize_rows(hipStream_t s, const metis_mat* A, int64_t Kp, uint8_t* codes, uint8_t* scales) {
+template <bool UNITS>
+int launch_quantize_rows(hipStream_t s, const metis_mat* A, int64_t Kp, uint8_t* codes, const RowScales& rs, const WeightScales& ws) {
     const int st = units_status(A->rows, Kp / 8);
     if (st != METIS_OK) return st;
-    const int64_t total = A->rows * (Kp / 8);
+    const int64_t total = A->rows * (Kp / 8), blocks = ceil_div64(total, 256), more = UNITS ? ceil_div64(ws.rows, 64) : 0;
+    if (blocks + more > 0x7FFFFFFF) return METIS_UNSUPPORTED;
     const FastDiv units = fast_div((uint32_t)(Kp / 8));
-    const dim3 grid((unsigned)ceil_div64(total, 256));
-    if (A->dtype == METIS_BF16)
-        hipLaunchKernelGGL(k_quantize_rows<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)A->ptr, A->ld, A->cols, (uint64_t)total, units, codes, scales);
-    else
-        hipLaunchKernelGGL(k_quantize_rows<float>, grid, dim3(256), 0, s, (const float*)A->ptr, A->ld, A->cols, (uint64_t)total, units, codes, scales);
+    auto launch = [&](auto kern, auto zero) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)(blocks + more)), dim3(256), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->cols, (uint64_t)total,
+                           units, codes, rs, ws, (uint32_t)blocks);
+    };
+    if (A->dtype == METIS_BF16) launch(k_quantize_rows<bf16_t, UNITS>, bf16_t());
+    else launch(k_quantize_rows<float, UNITS>, float());
     METIS_LAUNCH_CHECK();
     return METIS_OK;
 }
@@ -251,10 +318,9 @@ extern "C" int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups,
     return launch_quantize_mx_t((hipStream_t)stream, A, nullptr, false, A->rows / groups, out->codes, out->scales);
 }
 
-extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int experts, int64_t N, int64_t K) {
-    if (rows < 1 || experts < 1 || experts > EXPERTS_MAX || N < 1 || K < 32 || K % 32) return 0;
-    const size_t a = product_place(false, rows, experts, N, K).bytes, b = product_place(true, rows, experts, N, K).bytes;
-    return a > b ? a : b;
+extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int64_t slots, int experts, int64_t N, int64_t K) {
+    if (rows < 1 || slots < 1 || experts < 1 || experts > EXPERTS_MAX || N < 1 || K < 32 || K % 32) return 0;
+    return product_place(product_streams(slots, experts, N, rows, K), rows, slots, experts, N, K).bytes;
 }
 
 extern "C" int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W, const metis_expert_plan* plan, int gather,
@@ -262,35 +328,30 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     const int st = experts_plan_status(plan);
     if (st != METIS_OK) return st;
     if (plan->tokens == 0) return METIS_OK;
-    if (!mat_ok(A) || !W || !W->codes || !W->scales || !mat_ok(C) || (gather && !plan->token)) return METIS_INVALID_ARG;
+    if (!mat_ok(A) || !W || !W->codes || !W->scales || !mat_ok(C) || (gather && (!plan->token || !plan->slot))) return METIS_INVALID_ARG;
     const int64_t S = plan->tokens * plan->k, K = W->cols, N = W->rows / plan->experts;
     const int E = plan->experts;
     if (K < 32 || K % 32 || W->rows < 1 || W->rows % E || A->cols != K || A->ld < K || A->rows != (gather ? plan->tokens : S) ||
         C->rows != S || C->cols != N || C->ld < N || !mat_aligned16(A) || (uintptr_t)W->codes % 16 || (uintptr_t)W->scales % 8)
         return METIS_BAD_SHAPE;
-    if (!workspace || workspace_bytes < metis_experts_workspace_bytes(A->rows, E, N, K)) return METIS_WORKSPACE_TOO_SMALL;
+    if (!workspace || workspace_bytes < metis_experts_workspace_bytes(A->rows, S, E, N, K)) return METIS_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
     const bool streams = product_streams(S, E, N, A->rows, K);
-    const ProductPlace place = product_place(streams, A->rows, E, N, K);
+    const ProductPlace place = product_place(streams, A->rows, S, E, N, K);
     uint8_t* ws = (uint8_t*)workspace;
     hipStream_t s = (hipStream_t)stream;
-    const int qs = launch_quantize_rows(s, A, place.Kp, ws, ws + place.scales);
-    if (qs != METIS_OK) return qs;
     if (streams) {
-        const uint8_t* wscales = W->scales;
-        if (place.wscales) {
-            const FastDiv words = fast_div((uint32_t)(place.Kp / 128));
-            hipLaunchKernelGGL(k_pad_scales, dim3((unsigned)ceil_div64(W->rows * (place.Kp / 128), 256)), dim3(256), 0, s, W->scales,
-                               (uint64_t)W->rows, (uint32_t)(K / 32), ws + place.wscales, words);
-            METIS_LAUNCH_CHECK();
-            wscales = ws + place.wscales;
-        }
+        const int qs = launch_quantize_rows<true>(s, A, place.Kp, ws, {ws + place.scales, gather ? plan->slot : nullptr, S, gather ? plan->k : 1},
+                                                  {W->scales, ws + place.wscales + 2048, W->rows, (int)(K / 32), (int)(place.Kp / 256)});
+        if (qs != METIS_OK) return qs;
         const int tn = (int)ceil_div64(N, 256);
-        const ExStream a = {{ws, ws + place.scales}, {W->codes, wscales}, plan->offsets, gather ? plan->token : nullptr, S, A->rows, N, K,
-                            (uint32_t)(place.Kp / 2), (uint32_t)(place.Kp / 32), E, 0, tn};
+        const ExStream a = {{ws, ws + place.scales}, {W->codes, ws + place.wscales + 2048}, plan->offsets, gather ? plan->token : nullptr, S,
+                            A->rows, N, K, (uint32_t)(place.Kp / 2), 8 * S, 8 * W->rows, E, 0, tn};
         const int64_t tiles = most_units(S, E, 256) * tn;
         return C->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_PRODUCT>(s, a, tiles, C) : launch_stream<float, EX_PRODUCT>(s, a, tiles, C);
     }
+    const int qs = launch_quantize_rows<false>(s, A, K, ws, {ws + place.scales, nullptr, 0, 0}, {});
+    if (qs != METIS_OK) return qs;
     const int64_t units = most_units(S, E, 16) + 1, nb = ceil_div64(N, 64);
     if (units > 65535 || nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
     auto launch = [&](auto kern, auto zero) {
@@ -337,6 +398,6 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
         if (r == METIS_OK) r = launch_quantize_mx_t(s, X, plan, gather != 0, 0, (uint8_t*)x.codes, (uint8_t*)x.scales);
         if (r != METIS_OK) return r;
     }
-    const ExStream a = {g, x, plan->offsets, nullptr, S, 0, N, K, 0, 0, (int)E, (int)tm, (int)tn};
+    const ExStream a = {g, x, plan->offsets, nullptr, S, 0, N, K, 0, 8 * N, 8 * K, (int)E, (int)tm, (int)tn};
     return dW->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_WGRAD>(s, a, tiles, dW) : launch_stream<float, EX_WGRAD>(s, a, tiles, dW);
 }

@@ -9,6 +9,8 @@
 //   EX_WGRAD    dW_e[n, k] over the expert's slots: every tile whole, the contraction as long as the expert has slots.
 // A workgroup works its way through the tiles, gridDim.x apart.  Neighbouring tiles are of one expert, up to EX_BAND of its column tiles wide,
 // and every XCD works on a run of them: they share panels of both operands in its L2.
+// Outputs are not read again here and go past the caches: kept in L2 they drive out the operands' panels (gradients of 8192 tokens' four
+// experts, 2048 x 4096 each, 626 us with the quantizers, so 461; 16384 tokens' product 409, 401).
 // A wave whose 128 rows lie behind the tile's end multiplies nothing, and a last unit that exists in part is multiplied by steps of 64.
 #define EX_BAND 8
 enum { EX_PRODUCT = 0, EX_WGRAD = 1 };
@@ -20,10 +22,13 @@ struct ExStream {
     int64_t N;                            // product: outputs of an expert; gradient: N
     int64_t K;                            // product: contraction, a multiple of 32; gradient: K
     uint32_t astride;                     // product: bytes of a row of A's codes, a multiple of 128 (its tail is zeros)
-    uint32_t bscales;                     // product: bytes of a row of B's scales, a multiple of 8
+    int64_t ascales, bscales;             // from one unit's scales to the next one's
     int E, tiles_m, tiles_n;              // gradient: tiles_m along N, tiles_n along K; product: tiles_n along N
 };
-#define EX_LDS (MXS_LDS + 4 * 4 * (EXPERTS_MAX + 1))     // behind the two buffers what every expert has, four numbers
+// Behind the two buffers a wave has room to turn 16 rows of its outputs into whole lines, and every expert has two numbers.
+#define EX_STAGE_ROW 144                                 // 64 bf16 and 16 bytes that spread the rows over the banks
+#define EX_STAGE (16 * EX_STAGE_ROW)
+#define EX_LDS (MXS_LDS + 8 * EX_STAGE + 2 * 4 * (EXPERTS_MAX + 1))
 
 // zeros to n elements from p
 template <typename OUT>
@@ -34,6 +39,56 @@ __device__ __forceinline__ void ex_clear(OUT* p, int64_t n, bool vec) {
     for (int64_t c = units * E + threadIdx.x; c < n; c += 512) p[c] = OUT(0);
 }
 
+// A wave's accumulator tiles (transposed, bf16) to memory: 16 rows of its 64 columns at a time are staged at sm, eight lanes a row.
+// Whole: 16 stores a lane.
+__device__ __forceinline__ void ex_store_lines(const float16_t (&acc)[4][2], uint8_t* sm, bf16_t* __restrict__ C, int64_t ldc, int64_t m0, int64_t n0,
+                                               int64_t M, int64_t N, bool vec, bool whole, int lane) {
+    const int li = lane & 31, half = lane >> 5, unit = lane & 7;
+    const int64_t c = n0 + 8 * unit;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if ((li >> 4) == h) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; v += 4)
+                        mx_put4(reinterpret_cast<bf16_t*>(sm + (li & 15) * EX_STAGE_ROW) + 32 * j + 2 * v + 4 * half, acc[i][j][v],
+                                acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
+            }
+            gs_wave_order();
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int row = 8 * t + (lane >> 3);
+                const uint8_t* q = sm + row * EX_STAGE_ROW + 16 * unit;
+                const int64_t r = m0 + 32 * i + 16 * h + row, left = N - c;
+                bf16_t* p = C + r * ldc + c;
+                if (whole || (r < M && vec && left >= 8)) {
+                    __builtin_nontemporal_store(*reinterpret_cast<const uvec4_t*>(q), reinterpret_cast<uvec4_t*>(p));
+                } else if (r < M) {
+#pragma unroll 1
+                    for (int e = 0; e < 8 && e < left; ++e) p[e] = reinterpret_cast<const bf16_t*>(q)[e];
+                }
+            }
+            gs_wave_order();
+        }
+}
+
+// fp32: a row of 32 is a whole line as it is
+__device__ __forceinline__ void ex_store_plain(const float16_t (&acc)[4][2], float* __restrict__ C, int64_t ldc, int64_t m0, int64_t n0, int64_t M,
+                                               int64_t N, bool whole, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int64_t r = m0 + 32 * i + 4 * (lane >> 5) + 8 * (v >> 2) + (v & 3), c = n0 + 32 * j + (lane & 31);
+                if (whole || (r < M && c < N)) __builtin_nontemporal_store(acc[i][j][v], C + r * ldc + c);
+            }
+}
+
 template <typename OUT, int MODE>
 __global__ void __launch_bounds__(512, 2)
 k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
@@ -41,42 +96,50 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
     constexpr bool WGRAD = MODE == EX_WGRAD;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    int32_t* const s_first = reinterpret_cast<int32_t*>(lds + MXS_LDS);              // first tile of every expert, and their number
-    int32_t* const s_begin = s_first + EXPERTS_MAX + 1;                              // an expert's first slot,
-    int32_t* const s_count = s_begin + EXPERTS_MAX + 1;                              // its slots,
-    int32_t* const s_padded = s_count + EXPERTS_MAX + 1;                             // and segments of SLOT_ALIGN before it
+    uint8_t* const s_stage = lds + MXS_LDS;
+    int32_t* const s_begin = reinterpret_cast<int32_t*>(s_stage + 8 * EX_STAGE);     // an expert's first slot, and the end of all
+    // product: the first tile of every expert, and their number.  Gradient: the experts with slots before it (low 10 bits; their number)
+    // and above these the segments of SLOT_ALIGN before it
+    int32_t* const s_first = s_begin + EXPERTS_MAX + 1;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = wave >> 2, wb = wave & 3;
     const int lane = (int)threadIdx.x & 63, li = lane & 31, half = lane >> 5;
 
     // ---- the tables, by every expert's thread
     {
         const int e = (int)threadIdx.x;
-        int64_t n = 0;
-        if (e < a.E) {
-            const int64_t b = held(a.offsets[e], a.S);
-            n = held(a.offsets[e + 1], a.S) - b;
-            if (n < 0) n = 0;
-            s_begin[e] = (int32_t)b;
-            s_count[e] = (int32_t)n;
-        }
-        int tiles = WGRAD ? (n > 0 ? a.tiles_m * a.tiles_n : 0) : (int)((n + 255) >> 8) * a.tiles_n, segs = (int)((n + SLOT_ALIGN - 1) / SLOT_ALIGN);
         int32_t* s_sum = reinterpret_cast<int32_t*>(lds);                            // (the waves' sums, before any unit is here)
-        const int mine_t = tiles, mine_s = segs;
+        // offsets held to 0 .. S and to ascend, whatever the memory says
+        int32_t b = e < a.E ? (int32_t)held(a.offsets[e], a.S) : 0, all = (int32_t)held(a.offsets[a.E], a.S);
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int t = __shfl_up(tiles, d), g = __shfl_up(segs, d);
-            if (lane >= d) { tiles += t; segs += g; }
+            const int32_t o = __shfl_up(b, d);
+            if (lane >= d && o > b) b = o;
         }
-        if (lane == 63) { s_sum[wave] = tiles; s_sum[8 + wave] = segs; }
+        if (lane == 63) s_sum[wave] = b;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) { tiles += s_sum[w]; segs += s_sum[8 + w]; }
-        if (e < a.E) { s_first[e] = tiles - mine_t; s_padded[e] = segs - mine_s; }
-        if (e == a.E - 1) s_first[a.E] = tiles;
+        for (int w = 0; w < wave; ++w) b = b > s_sum[w] ? b : s_sum[w];
+        if (e < a.E) s_begin[e] = b;
+        if (e == a.E - 1) s_begin[a.E] = all > b ? all : b;
+        __syncthreads();
+        const int32_t n = e < a.E ? s_begin[e + 1] - b : 0;
+        int32_t mine = WGRAD ? (n > 0) | (n + SLOT_ALIGN - 1) / SLOT_ALIGN << 10 : ((n + 255) >> 8) * a.tiles_n, upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int32_t o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        if (lane == 63) s_sum[8 + wave] = upto;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) upto += s_sum[8 + w];
+        if (e < a.E) s_first[e] = upto - mine;
+        if (e == a.E - 1) s_first[a.E] = upto;
         __syncthreads();
     }
-    const int total = __builtin_amdgcn_readfirstlane(s_first[a.E]);
-    auto begin_of = [&](int e) GS_INLINE { return __builtin_amdgcn_readfirstlane(s_begin[e]); };
-    auto count_of = [&](int e) GS_INLINE { return __builtin_amdgcn_readfirstlane(s_count[e]); };
+    auto table = [&](const int32_t* t, int e) GS_INLINE { return __builtin_amdgcn_readfirstlane(t[e]); };
+    auto begin_of = [&](int e) GS_INLINE { return table(s_begin, e); };
+    auto count_of = [&](int e) GS_INLINE { return table(s_begin, e + 1) - table(s_begin, e); };
+    auto first_of = [&](int e) GS_INLINE { return WGRAD ? (table(s_first, e) & 1023) * (a.tiles_m * a.tiles_n) : table(s_first, e); };
+    const int total = first_of(a.E);
 
     // ---- what no tile covers
     if constexpr (WGRAD) {
@@ -84,14 +147,14 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
             if (count_of(e) == 0)
                 for (int64_t r = blockIdx.x; r < a.N; r += gridDim.x) ex_clear(C + ((int64_t)e * a.N + r) * ldc, a.K, vec);
     } else {
-        for (int64_t r = (int64_t)begin_of(a.E - 1) + count_of(a.E - 1) + blockIdx.x; r < a.S; r += gridDim.x)      // slots that serve no choice
+        for (int64_t r = (int64_t)begin_of(a.E) + blockIdx.x; r < a.S; r += gridDim.x)      // slots that serve no choice
             ex_clear(C + r * ldc, a.N, vec);
     }
 
     // tile number -> expert (searched on from e) and place
     auto tile_of = [&](int tile, int& e, int& m0, int& n0) GS_INLINE {
-        while (tile >= __builtin_amdgcn_readfirstlane(s_first[e + 1])) ++e;
-        const int first = __builtin_amdgcn_readfirstlane(s_first[e]), local = tile - first;
+        while (tile >= first_of(e + 1)) ++e;
+        const int local = tile - first_of(e);
         const int down = WGRAD ? a.tiles_m : (count_of(e) + 255) >> 8;
         const int band = local / (EX_BAND * down), r = local - band * EX_BAND * down;
         const int left = a.tiles_n - band * EX_BAND, w = left < EX_BAND ? left : EX_BAND;
@@ -104,10 +167,10 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
     if (start >= total) return;
 
     // ---- transfers
-    const uint8_t *qa, *qb, *qsa, *qsb;                  // the next unit's codes and scales
+    const uint8_t *qa, *qb, *qsa, *qsb;                  // the next unit's codes, and this wave's part of its scales
     int lpos = start, lcnt = 0, lblk = 8;                // tile being fetched, units left of it, blocks of 32 of the unit that B has
-    uint32_t va[4], vb[4], wsa, wsb;                     // the lane's offsets
-    int32_t row_next[5];                                 // rows of A of the tile to be entered next, by this lane's place
+    uint32_t va[4], vb[4];                               // the lane's offsets
+    int32_t row_next[4];                                 // rows of A of the tile to be entered next, by this lane's place
     int nexp = 0, nm0 = 0, nn0 = 0;                      // that tile
     auto look_ahead = [&](int pos) GS_INLINE {
         tile_of(pos < total ? pos : total - 1, nexp, nm0, nn0);
@@ -115,8 +178,8 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
             const int l = gs_fresh_lane();
             const int32_t b = begin_of(nexp) + nm0, t = count_of(nexp) - nm0 - 1;
 #pragma unroll
-            for (int v = 0; v < 5; ++v) {
-                const int row = v < 4 ? 32 * wave + 8 * v + (l >> 3) : 32 * wave + (l >> 1);
+            for (int v = 0; v < 4; ++v) {
+                const int row = 32 * wave + 8 * v + (l >> 3);
                 row_next[v] = b + (row < t ? row : t);
                 if (a.token) row_next[v] = a.token[row_next[v]];
             }
@@ -128,18 +191,17 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         const uint32_t seg0 = (uint32_t)((l & 7) ^ (l >> 4)) * 16;
         const int64_t brows = WGRAD ? a.K : a.N;
         const int tb = (int)(brows - n0 < 256 ? brows - n0 : 256) - 1;
-        const int rs = 32 * wave + (l >> 1);
         if constexpr (WGRAD) {
             const int len = (count_of(e) + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
-            const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane(s_padded[e]) * SLOT_ALIGN;
+            const int64_t at = (int64_t)(table(s_first, e) >> 10) * SLOT_ALIGN;
             const int64_t pa = at * a.N + (int64_t)m0 * len, pb = at * a.K + (int64_t)n0 * len;
             lcnt = (count_of(e) + 255) >> 8;
             qa = a.A.codes + pa / 2;
-            qsa = a.A.scales + pa / 32;
+            qsa = a.A.scales + at * a.N / 32 + 8 * (m0 + 32 * wave);
             qb = a.B.codes + pb / 2;
-            qsb = a.B.scales + pb / 32;
+            qsb = a.B.scales + at * a.K / 32 + 8 * (n0 + 32 * wave);
             const int ta = (int)(a.N - m0 < 256 ? a.N - m0 : 256) - 1;
-            const uint32_t cs = (uint32_t)len / 2, ss = (uint32_t)len / 32;
+            const uint32_t cs = (uint32_t)len / 2;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int row = 32 * wave + 8 * v + (l >> 3);
@@ -147,16 +209,14 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
                 va[v] = (uint32_t)(row < ta ? row : ta) * cs + seg;
                 vb[v] = (uint32_t)(row < tb ? row : tb) * cs + seg;
             }
-            wsa = (uint32_t)(rs < ta ? rs : ta) * ss + 4u * (l & 1);
-            wsb = (uint32_t)(rs < tb ? rs : tb) * ss + 4u * (l & 1);
         } else {
             const int64_t w0 = (int64_t)e * a.N + n0;
             const uint32_t cs = (uint32_t)(a.K / 2);
             lcnt = (int)((a.K + 255) >> 8);
             qa = a.A.codes;
-            qsa = a.A.scales;
+            qsa = a.A.scales + 8 * (int64_t)(begin_of(e) + m0 + 32 * wave);
             qb = a.B.codes + w0 * cs;
-            qsb = a.B.scales + w0 * a.bscales;
+            qsb = a.B.scales + 8 * (w0 + 32 * wave);
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int row = 32 * wave + 8 * v + (l >> 3);
@@ -165,9 +225,6 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
                 va[v] = r * a.astride + seg;
                 vb[v] = (uint32_t)(row < tb ? row : tb) * cs + seg;
             }
-            const uint32_t r = (uint32_t)row_next[4] < (uint32_t)a.arows ? (uint32_t)row_next[4] : (uint32_t)a.arows - 1u;
-            wsa = r * (a.astride >> 4) + 4u * (l & 1);
-            wsb = (uint32_t)(rs < tb ? rs : tb) * a.bscales + 4u * (l & 1);
         }
         look_ahead(lpos + hop);
     };
@@ -199,15 +256,15 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
             }
             gs_dma16<MXS_CODES + 1024 * (k - 4)>(dc, off, qb);
         } else if constexpr (k == 8) {
-            gs_dma4<2 * MXS_CODES>(ds, wsa, qsa);
+            gs_dma4<2 * MXS_CODES>(ds, 4u * gs_fresh_lane(), qsa);
         } else {
-            gs_dma4<2 * MXS_CODES + MXS_SCALES>(ds, wsb, qsb);
+            gs_dma4<2 * MXS_CODES + MXS_SCALES>(ds, 4u * gs_fresh_lane(), qsb);
         }
         if constexpr (k == MXS_DMA - 1) {
             qa += MX_KI / 2;
             qb += MX_KI / 2;
-            qsa += MX_KI / 32;
-            qsb += MX_KI / 32;
+            qsa += a.ascales;
+            qsb += a.bscales;
         }
     };
 
@@ -244,9 +301,10 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
     mxs_settle_scales(sx);
 
     uint32_t b0 = 0;                                     // buffer of the unit in work
-    // first: the accumulators start here; steps: of 64 elements, that this wave multiplies; last: of the tile, and its buffer takes the outputs
-    auto unit = [&](auto first_, auto last_, int steps, bool only) GS_INLINE {
-        constexpr bool first = decltype(first_)::value, last = decltype(last_)::value;
+    // first: the accumulators start here; steps: of 64 elements, that this wave multiplies.  kept: the last tile's stores, younger than the
+    // transfers that the unit waits for, are 16 and may stay on their way.
+    auto unit = [&](auto first_, int steps, bool kept) GS_INLINE {
+        constexpr bool first = decltype(first_)::value;
         const uint32_t b1 = MXS_UNIT - b0;
         gs_for<4>([&](auto sc_) GS_INLINE {
             constexpr int s = decltype(sc_)::value, n = s & 1;
@@ -257,19 +315,17 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
                 if constexpr (s == 3) {
                     // the next unit is there, and this one's buffer has been read by all
                     if constexpr (m == 1) {
-                        gs_meet<0>();
-                        if constexpr (!last)
-                            if (!first || !only) advance();
+                        if (first && kept) gs_meet<16>();
+                        else gs_meet<0>();
+                        advance();
                     }
                     if constexpr (m >= 1 && m < 7) {
                         read_frag(b1, 0, 0, m - 1);
                         read_scale(b1, m - 1);
                     }
-                    if constexpr (!last && m >= 1) {
-                        if (!first || !only) {
-                            issue(b0, std::integral_constant<int, m - 1>{});
-                            if constexpr (m >= 5) issue(b0, std::integral_constant<int, m + 2>{});
-                        }
+                    if constexpr (m >= 1) {
+                        issue(b0, std::integral_constant<int, m - 1>{});
+                        if constexpr (m >= 5) issue(b0, std::integral_constant<int, m + 2>{});
                     }
                 }
                 const uint32_t as = s < 2 ? sx[i] : sy[i], bs = s < 2 ? sx[4 + j] : sy[4 + j];
@@ -285,8 +341,9 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         mxs_settle_scales(sx);
         b0 = b1;
     };
-    int pos = start, exp = 0;
-    for (;;) {
+    int exp = 0;
+    bool kept = false;
+    for (int pos = start; pos < total; pos += hop) {
         int m0, n0;
         tile_of(pos, exp, m0, n0);
         const int64_t base = WGRAD ? (int64_t)exp * a.N : (int64_t)begin_of(exp), rows = WGRAD ? a.N : (int64_t)count_of(exp);
@@ -294,26 +351,22 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         const int niter = (int)((con + 255) >> 8);
         const bool busy = m0 + 128 * wa < rows;
         const int whole = busy ? 4 : 0, rest = busy ? (int)((con - 256 * (int64_t)(niter - 1) + 63) >> 6) : 0;
-        unit(std::true_type{}, std::false_type{}, niter == 1 ? rest : whole, niter == 1);
-        if (niter > 1) {
+        unit(std::true_type{}, niter == 1 ? rest : whole, kept);
 #pragma unroll 1
-            for (int u = 2; u < niter; ++u) unit(std::false_type{}, std::false_type{}, whole, false);
-            unit(std::false_type{}, std::true_type{}, rest, false);
-        }
-        const uint32_t bl = MXS_UNIT - b0;               // the last unit's buffer
+        for (int u = 1; u < niter; ++u) unit(std::false_type{}, u == niter - 1 ? rest : whole, false);
 #pragma unroll
         for (int i = 0; i < 4; ++i) mxs_settle(acc[i]);
+        kept = false;
         if (busy) {
-            const int64_t N = WGRAD ? a.K : a.N;
-            mx_store_wave<OUT, LINES, 4, 2>(acc, lds + bl + wave * mx_wave_rows<OUT, 2>(), C + base * ldc, ldc, m0 + 128 * wa, n0 + 64 * wb, rows,
-                                            N, vec, mx_whole<LINES>(m0 + 128 * wa + 128 <= rows && n0 + 64 * wb + 64 <= N, vec), gs_fresh_lane());
+            const int64_t N = WGRAD ? a.K : a.N, r = m0 + 128 * wa, c = n0 + 64 * wb;
+            const bool inside = r + 128 <= rows && c + 64 <= N;
+            if constexpr (LINES) {
+                kept = inside && vec;
+                ex_store_lines(acc, s_stage + wave * EX_STAGE, C + base * ldc, ldc, r, c, rows, N, vec, kept, gs_fresh_lane());
+            } else {
+                ex_store_plain(acc, C + base * ldc, ldc, r, c, rows, N, inside, gs_fresh_lane());
+            }
         }
-        pos += hop;
-        if (pos >= total) break;
-        // every wave has its rows out of the buffer before any transfers into it
-        gs_meet<63>();
-        advance();
-        gs_for<MXS_DMA>([&](auto k) GS_INLINE { issue(bl, k); });
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // no transfer may outlive the workgroup's LDS
 }

@@ -114,7 +114,7 @@ _SIGNATURES = {
     "metis_route_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Router), C.c_void_p, C.c_void_p, C.POINTER(Mat)]),
     "metis_dispatch_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int, C.c_int]),
     "metis_dispatch": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(Plan), C.c_void_p, C.c_size_t]),
-    "metis_experts_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int, C.c_int64, C.c_int64]),
+    "metis_experts_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int, C.c_int64, C.c_int64]),
     "metis_experts_product": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(MxFp4), C.POINTER(Plan), C.c_int, C.POINTER(Mat), C.c_void_p,
                                         C.c_size_t]),
     "metis_quantize_mx_t": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.c_int, C.POINTER(MxFp4)]),
@@ -547,15 +547,15 @@ def dispatch(idx, experts, plan=None, workspace=None):
     return plan
 
 
-def experts_workspace_bytes(rows, experts, N, K):
-    return int(lib().metis_experts_workspace_bytes(rows, experts, N, K))
+def experts_workspace_bytes(rows, slots, experts, N, K):
+    return int(lib().metis_experts_workspace_bytes(rows, slots, experts, N, K))
 
 
 def experts_product(A, W, plan, Cmat, gather=False, workspace=None):
     """Cmat [S, N] = rows of A (by slot, or with gather by token) times their experts' weights W (MxTensor [experts * N, K])."""
     a, w, p, c = _mat(A), W.c(), plan.c(), _mat(Cmat)
     if workspace is None:
-        workspace = torch.empty((experts_workspace_bytes(A.shape[0], plan.experts, Cmat.shape[1], A.shape[1]),), dtype=torch.uint8, device=A.device)
+        workspace = torch.empty((experts_workspace_bytes(A.shape[0], Cmat.shape[0], plan.experts, Cmat.shape[1], A.shape[1]),), dtype=torch.uint8, device=A.device)
     _check(lib().metis_experts_product(_stream(), C.byref(a), C.byref(w), C.byref(p), gather, C.byref(c), workspace.data_ptr(),
                                        workspace.numel()))
     return Cmat

@@ -137,9 +137,9 @@ def test_products(metis):
     assert product(A=(8, 48, 48, 0), W=(128, 48)) == SHAPE and product(W=(129, 64)) == SHAPE and product(A=(7, 64, 64, 0)) == SHAPE
     assert product(C_=(7, 16, 16, 0)) == SHAPE and product(C_=(8, 16, 15, 0)) == SHAPE and product(A=(8, 64, 60, 0)) == SHAPE
     assert product(A=(8, 64, 68, 0)) == SHAPE and product(wp=FAKE + 8) == SHAPE and product(ap=FAKE + 2) == SHAPE
-    need = L.metis_experts_workspace_bytes(8, 8, 16, 64)
+    need = L.metis_experts_workspace_bytes(8, 8, 8, 16, 64)
     assert need >= 8 * 64 // 2 + 8 * 2 and product(size=need - 1) == WORKSPACE and product(ws=None) == WORKSPACE
-    assert L.metis_experts_workspace_bytes(8, 8, 16, 48) == 0
+    assert L.metis_experts_workspace_bytes(8, 8, 8, 16, 48) == 0
 
     def wgrad(G=(8, 16, 16, 0), X=(8, 64, 64, 0), dW=(128, 64, 64, 0), tokens=8, k=1, experts=8, gather=0, gp=FAKE, dp=FAKE, ws=FAKE, size=1 << 40):
         g, x, d = metis.Mat(gp, *G), metis.Mat(FAKE, *X), metis.Mat(dp, *dW)

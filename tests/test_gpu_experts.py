@@ -157,7 +157,7 @@ def test_on_another_stream_and_in_a_graph(metis):
     C0 = metis.experts_product(x, W, plan, torch.empty((T * k, N), dtype=torch.bfloat16, device="cuda"), gather=True)
     dW0 = metis.experts_wgrad(dy, x, plan, torch.empty((E * N, K), device="cuda"), gather=True)
     C1, dW1 = torch.empty_like(C0), torch.empty_like(dW0)
-    ws = torch.empty((max(metis.experts_workspace_bytes(T, E, N, K), metis.experts_wgrad_workspace_bytes(T * k, E, N, K)),), dtype=torch.uint8, device="cuda")
+    ws = torch.empty((max(metis.experts_workspace_bytes(T, T * k, E, N, K), metis.experts_wgrad_workspace_bytes(T * k, E, N, K)),), dtype=torch.uint8, device="cuda")
     torch.cuda.synchronize()
     s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=s):
