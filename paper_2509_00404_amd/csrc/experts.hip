@@ -106,34 +106,63 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
     }
 }
 
-// ---- products straight from memory ----
-// A wave makes 16 x 16 outputs by v_mfma_scale_f32_16x16x128_f8f6f4: a lane's operand is the 32 codes (16 bytes) of row lane % 16,
-// contraction block lane / 16, and that block's scale.  X's rows (the first operand) are the outputs' fast axis: a lane ends with four
-// neighbouring ones.
+// ---- products for few slots an expert: straight from memory ----
+// What counts is that the weights stream: they pass through registers alone, and nothing waits for anybody.  A wave has 32 of the expert's N
+// (the first operand, so that a lane ends with runs of four neighbouring outputs) and up to 32 G slots, on v_mfma_scale_f32_32x32x64_f8f6f4:
+// a lane's operand is the 32 codes (16 bytes) of row lane % 32 and one block of either half of the step.  Which blocks a step takes is free as
+// long as both operands agree: over a run of 512 elements a lane takes the 8 blocks of its half one after the other, 128 bytes
+// that lie together, and their 8 scale bytes.  The weights of the next run are on their way while one is multiplied.
+// SPLIT: the workgroup's four waves share 32 outputs, take every fourth run, and add up in their order by way of LDS; else each has 32 of its own.
 struct MxRows {
     const uint8_t* codes;
     const uint8_t* scales;
 };
-// this lane's row of either operand, blocks of 32 (nblk >= 0 in all)
-__device__ __forceinline__ ex_f4 mx_product16(MxRows x, MxRows y, int64_t nblk) {
-    const int kb = ((int)threadIdx.x & 63) >> 4;
-    ex_f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t b = kb; b - kb < nblk; b += 4) {
-        ew_u4 p = {0u, 0u, 0u, 0u}, q = {0u, 0u, 0u, 0u};
-        int ps = 0x7F, qs = 0x7F;
-        if (b < nblk) {
-            p = *reinterpret_cast<const ew_u4*>(x.codes + 16 * b);
-            q = *reinterpret_cast<const ew_u4*>(y.codes + 16 * b);
-            ps = x.scales[b];
-            qs = y.scales[b];
+typedef uint32_t ex_u2_any __attribute__((ext_vector_type(2), aligned(1)));
+// Blocks r + 8 h .. r + 8 h + 7 of a row (h = lane / 32), r the run's first.  Of the last run, where it is short, what lies behind the row's
+// nblk blocks is the last block once more under some scale, and zeros where ZERO: one operand's zeros are enough.
+template <bool ZERO>
+__device__ __forceinline__ void few_load(const uint8_t* codes, const uint8_t* scales, int r, int nblk, int half, ew_u4 (&c)[8], uint32_t (&sc)[2]) {
+    const int b = r + 8 * half;
+    if (r + 16 <= nblk) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = *reinterpret_cast<const ew_u4*>(codes + 16 * (int64_t)b + 16 * i);
+        const ex_u2_any w = *reinterpret_cast<const ex_u2_any*>(scales + b);
+        sc[0] = w[0];
+        sc[1] = w[1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = *reinterpret_cast<const ew_u4*>(codes + 16 * (int64_t)(b + i < nblk ? b + i : nblk - 1));
+        if (ZERO) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = b + i < nblk ? c[i] : ew_u4{0u, 0u, 0u, 0u};
         }
-        const ex_i8 pa = {(int)p[0], (int)p[1], (int)p[2], (int)p[3], 0, 0, 0, 0}, qa = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0};
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(pa, qa, acc, 4, 4, 0, ps, 0, qs);
+        uint64_t w = 0;
+        if (nblk >= 8) {
+            const int at = b + 8 < nblk ? b : nblk - 8, off = b - at;
+            const ex_u2_any v = *reinterpret_cast<const ex_u2_any*>(scales + at);
+            w = ((uint64_t)v[1] << 32 | v[0]) >> (8 * (off < 7 ? off : 7));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w |= (uint64_t)scales[b + i < nblk ? b + i : nblk - 1] << (8 * i);
+        }
+        sc[0] = (uint32_t)w;
+        sc[1] = (uint32_t)(w >> 32);
     }
-    return acc;
 }
+template <int I>
+__device__ __forceinline__ void few_step(float16_t& acc, const ew_u4 (&w)[8], const uint32_t (&ws)[2], const ew_u4 (&t)[8], const uint32_t (&ts)[2]) {
+    const ex_i8 a = {(int)w[I][0], (int)w[I][1], (int)w[I][2], (int)w[I][3], 0, 0, 0, 0};
+    const ex_i8 b = {(int)t[I][0], (int)t[I][1], (int)t[I][2], (int)t[I][3], 0, 0, 0, 0};
+    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 4, I & 3, (int)ws[I >> 2], I & 3, (int)ts[I >> 2]);
+}
+// four neighbouring outputs of a row; vec: the row and the place allow one store
 template <typename OUT>
-__device__ __forceinline__ void put4(OUT* p, ex_f4 v, int64_t left) {
+__device__ __forceinline__ void put4(OUT* p, ex_f4 v, int64_t left, bool vec) {
+    if (vec && left >= 4) {
+        if constexpr (sizeof(OUT) == 2) *reinterpret_cast<ew_u2*>(p) = ew_u2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        else *reinterpret_cast<ex_f4*>(p) = v;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (i < left) {
@@ -142,27 +171,99 @@ __device__ __forceinline__ void put4(OUT* p, ex_f4 v, int64_t left) {
         }
 }
 
-// C[s, n] of up to 16 slots of one expert and 64 of its N outputs; behind the last unit of slots the workgroups clear the unused ones
-template <typename OUT>
-__global__ void __launch_bounds__(256)
+template <typename OUT, int G, bool SPLIT>
+__global__ void __launch_bounds__(256, 2)
 k_experts_few(MxRows A, int64_t arows, MxRows W, const int32_t* __restrict__ offsets, const int32_t* __restrict__ token, int E, int64_t S,
-              int64_t N, int64_t nblk, OUT* __restrict__ C, int64_t ldc) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15;
-    const SlotUnit u = find_unit(offsets, E, S, 16, blockIdx.y);
-    const int64_t n0 = ((int64_t)blockIdx.x * 4 + wave) * 16, nq = n0 + 4 * (lane >> 4);
-    if (u.expert < 0) {
-        const int64_t used = held(offsets[E], S), step = (int64_t)(gridDim.y - u.total) * 16;
-        for (int64_t s = used + ((int64_t)blockIdx.y - u.total) * 16 + li; s < S; s += step)
-            put4(C + s * ldc + nq, ex_f4{0.0f, 0.0f, 0.0f, 0.0f}, N - nq);
+              int64_t N, int nblk, OUT* __restrict__ C, int64_t ldc, bool vec, uint32_t nblocks, uint32_t most) {
+    __shared__ float s_part[SPLIT ? 3 * G * 16 * 64 : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), li = lane & 31, half = lane >> 5;
+    const uint32_t ub = blockIdx.x / nblocks, nb = blockIdx.x - ub * nblocks;
+    const SlotUnit u = find_unit(offsets, E, S, 32 * G, ub);
+    const int64_t n0 = SPLIT ? 32 * (int64_t)nb : 128 * (int64_t)nb + 32 * wave;
+    if (u.expert < 0) {                                  // behind the last unit of slots the workgroups clear the unused ones
+        const int64_t used = held(offsets[E], S), step = most - u.total, wide = SPLIT ? 32 : 128, c0 = wide * nb;
+        for (int64_t s = used + ub - u.total; s < S; s += step)
+            for (int64_t c = c0 + threadIdx.x; c < c0 + wide && c < N; c += 256) C[s * ldc + c] = OUT(0);
         return;
     }
-    if (n0 >= N) return;
-    const int64_t s = u.begin + 16 * (int64_t)u.local + li, sr = s < u.end ? s : u.end - 1;
-    uint64_t row = token ? (uint64_t)(uint32_t)token[sr] : (uint64_t)sr;
-    if (row >= (uint64_t)arows) row = arows - 1;
+    if (n0 >= N) return;                                 // (SPLIT: not for some waves of a workgroup alone)
+    const int64_t first = u.begin + 32 * G * (int64_t)u.local;
+    const int groups = G > 1 && first + 32 < u.end ? 2 : 1;
     const uint64_t n = (uint64_t)u.expert * N + (n0 + li < N ? n0 + li : N - 1);
-    const ex_f4 acc = mx_product16({W.codes + n * nblk * 16, W.scales + n * nblk}, {A.codes + row * nblk * 16, A.scales + row * nblk}, nblk);
-    if (s < u.end) put4(C + s * ldc + nq, acc, N - nq);
+    const uint8_t *wc = W.codes + n * nblk * 16, *wsc = W.scales + n * nblk;
+    const uint8_t *tc[G], *tsc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const int64_t s = first + 32 * g + li, sr = s < u.end ? s : u.end - 1;
+        uint64_t row = token ? (uint64_t)(uint32_t)token[sr] : (uint64_t)sr;
+        if (row >= (uint64_t)arows) row = arows - 1;
+        tc[g] = A.codes + row * nblk * 16;
+        tsc[g] = A.scales + row * nblk;
+    }
+    float16_t acc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[g][v] = 0.0f;
+    constexpr int hop = SPLIT ? 64 : 16;
+    ew_u4 w[2][8];
+    uint32_t ws[2][2];
+    int r = SPLIT ? 16 * wave : 0;
+    if (r < nblk) few_load<false>(wc, wsc, r, nblk, half, w[0], ws[0]);
+    auto run = [&](auto now_) __attribute__((always_inline)) {
+        constexpr int now = decltype(now_)::value;
+        ew_u4 t[G][8];
+        uint32_t ts[G][2];
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            if (g < groups) few_load<true>(tc[g], tsc[g], r, nblk, half, t[g], ts[g]);
+        if (r + hop < nblk) few_load<false>(wc, wsc, r + hop, nblk, half, w[now ^ 1], ws[now ^ 1]);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            if (g < groups) {
+                few_step<0>(acc[g], w[now], ws[now], t[g], ts[g]);
+                few_step<1>(acc[g], w[now], ws[now], t[g], ts[g]);
+                few_step<2>(acc[g], w[now], ws[now], t[g], ts[g]);
+                few_step<3>(acc[g], w[now], ws[now], t[g], ts[g]);
+                few_step<4>(acc[g], w[now], ws[now], t[g], ts[g]);
+                few_step<5>(acc[g], w[now], ws[now], t[g], ts[g]);
+                few_step<6>(acc[g], w[now], ws[now], t[g], ts[g]);
+                few_step<7>(acc[g], w[now], ws[now], t[g], ts[g]);
+            }
+        r += hop;
+    };
+#pragma unroll 1
+    while (r < nblk) {
+        run(std::integral_constant<int, 0>{});
+        if (r >= nblk) break;
+        run(std::integral_constant<int, 1>{});
+    }
+    if constexpr (SPLIT) {
+        if (wave > 0) {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s_part[(((wave - 1) * G + g) * 16 + v) * 64 + lane] = acc[g][v];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[g][v] += s_part[((p * G + g) * 16 + v) * 64 + lane];
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const int64_t s = first + 32 * g + li;
+        if (s >= u.end) continue;
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+            const int64_t c = n0 + 2 * v + 4 * half;
+            put4(C + s * ldc + c, ex_f4{acc[g][v], acc[g][v + 1], acc[g][v + 2], acc[g][v + 3]}, N - c, vec);
+        }
+    }
 }
 
 #include "experts_stream.h"
@@ -352,15 +453,25 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     }
     const int qs = launch_quantize_rows<false>(s, A, K, ws, {ws + place.scales, nullptr, 0, 0}, {});
     if (qs != METIS_OK) return qs;
-    const int64_t units = most_units(S, E, 16) + 1, nb = ceil_div64(N, 64);
-    if (units > 65535 || nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    const int g = S > 24 * (int64_t)E ? 2 : 1;
+    const int64_t most = most_units(S, E, 32 * g) + 1;
+    const bool split = most * ceil_div64(N, 32) < 4096;
+    const int64_t nb = ceil_div64(N, split ? 32 : 128);
+    if (most * nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    const int64_t size = mat_size(C);
+    const bool vec = (uintptr_t)C->ptr % (4 * size) == 0 && C->ld % 4 == 0;
     auto launch = [&](auto kern, auto zero) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)nb, (unsigned)units), dim3(256), 0, s, MxRows{ws, ws + place.scales}, A->rows,
-                           MxRows{W->codes, W->scales}, plan->offsets, gather ? plan->token : nullptr, E, S, N, K / 32,
-                           (decltype(zero)*)C->ptr, C->ld);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(most * nb)), dim3(256), 0, s, MxRows{ws, ws + place.scales}, A->rows, MxRows{W->codes, W->scales},
+                           plan->offsets, gather ? plan->token : nullptr, E, S, N, (int)(K / 32), (decltype(zero)*)C->ptr, C->ld, vec, (uint32_t)nb,
+                           (uint32_t)most);
     };
-    if (C->dtype == METIS_BF16) launch(k_experts_few<bf16_t>, bf16_t());
-    else launch(k_experts_few<float>, float());
+    auto by_shape = [&](auto zero) {
+        typedef decltype(zero) OUT;
+        if (g == 1) split ? launch(k_experts_few<OUT, 1, true>, zero) : launch(k_experts_few<OUT, 1, false>, zero);
+        else split ? launch(k_experts_few<OUT, 2, true>, zero) : launch(k_experts_few<OUT, 2, false>, zero);
+    };
+    if (C->dtype == METIS_BF16) by_shape(bf16_t());
+    else by_shape(float());
     METIS_LAUNCH_CHECK();
     return METIS_OK;
 }
