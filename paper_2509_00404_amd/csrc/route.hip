@@ -1,6 +1,6 @@
 // Routing to experts: scores, selection, weights, their gradient, and the plan that sorts the choices into slots.
 #include <type_traits>
-#include "common.h"
+#include "elementwise.h"
 
 #define ROUTE_LANES 16                    // lanes that share a token: one row of the wave, inside which data moves without LDS
 #define ROUTE_TOKENS 16                   // tokens of a workgroup
@@ -61,14 +61,18 @@ struct RouteArgs {
     float* weights;
     int E, k, groups, top_groups, renorm;
     float scale;
+    bool vec;                             // a lane's experts are all there or none, and their logits whole 16-byte units
 };
 
-// One row of 16 lanes per token; a lane holds the keys of V neighbouring experts, in the experts' order, and its best one.  A round of the
-// selection is the highest key of the row, its lowest lane, and a look through that lane's keys for the next.
+// One row of 16 lanes per token; a lane has the keys of V neighbouring experts, in the experts' order.  A round of the selection is the
+// highest key of the row and its lowest lane, which then looks for its next one.  With V > 4 the lane holds the highest of every four keys, and
+// the keys themselves are in LDS, so that a round looks at four keys and V / 4 maxima instead of V keys.
+// What bounds it: vector issue.  16384 tokens, 256 experts in 8 groups, 8 choices: ROUTE_T us, of which the logits' 16.8 MB would take 3.3.
 template <typename T, int V, bool SIGMOID>
 __global__ void __launch_bounds__(ROUTE_LANES * ROUTE_TOKENS)
 k_route(const T* __restrict__ logits, RouteArgs a) {
-    __shared__ uint32_t s_key[ROUTE_TOKENS][ROUTE_LANES * V];
+    constexpr int Q = V < 4 ? V : 4, NQ = V / Q;                           // keys of a quad, quads of a lane
+    __shared__ __attribute__((aligned(16))) uint32_t s_key[ROUTE_TOKENS][ROUTE_LANES * V];
     __shared__ uint32_t s_group[ROUTE_TOKENS][ROUTE_LANES * V];
     __shared__ int s_idx[ROUTE_TOKENS][ROUTE_MAX_K];
     const int lane = threadIdx.x & (ROUTE_LANES - 1), tok = threadIdx.x / ROUTE_LANES;
@@ -79,64 +83,158 @@ k_route(const T* __restrict__ logits, RouteArgs a) {
     uint32_t key[V];
     float x[V];
     const int e0 = lane * V;
+    // (16384 x 256 fp32: 16 loads a lane of 4 bytes cost ROUTE_V us more than 4 of 16, every lane having a line of its own)
+    bool loaded = false;
+    if constexpr (V * sizeof(T) >= 16) {
+        if (a.vec) {
+            loaded = true;
+            constexpr int N = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int u = 0; u < V / N; ++u) {
+                ew_u4 w = {0u, 0u, 0u, 0u};
+                if (e0 < a.E) w = *reinterpret_cast<const ew_u4*>(row + e0 + N * u);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    x[N * u + i] = e0 >= a.E ? -INFINITY : N == 4 ? __uint_as_float(w[i & 3]) : i & 1 ? bf16hi_to_f32(w[i >> 1 & 3]) : bf16lo_to_f32(w[i >> 1 & 3]);
+            }
+        }
+    }
+    if (!loaded) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = e0 + v < a.E ? load_f32(row + e0 + v) : -INFINITY;
+    }
+    float add[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) add[v] = 0.0f;
+    if (a.bias) {
+        if (V >= 4 && a.vec) {
+            if constexpr (V >= 4)
+#pragma unroll
+                for (int u = 0; u < V / 4; ++u) {
+                    const ew_f4 w = *reinterpret_cast<const ew_f4*>(a.bias + (e0 < a.E ? e0 : 0) + 4 * u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) add[4 * u + i] = w[i];
+                }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) add[v] = a.bias[e0 + v < a.E ? e0 + v : 0];
+        }
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int e = e0 + v;
-        x[v] = ok && e < a.E ? load_f32(row + e) : -INFINITY;
-        const float s = SIGMOID ? sigmoid_f32(x[v]) : x[v];
-        const float f = a.bias && e < a.E ? s + a.bias[e] : s;
+        if (!ok || !(x[v] > -INFINITY)) x[v] = -INFINITY;
+        const float f = (SIGMOID ? sigmoid_f32(x[v]) : x[v]) + add[v];
         key[v] = x[v] > -INFINITY && f > -INFINITY ? order_key(f) : 0u;
-        if (!(x[v] > -INFINITY)) x[v] = -INFINITY;
     }
     // groups: the best of them by score, ties to the lowest; the keys of the others go
     if (a.top_groups < a.groups) {
         const int size = a.E / a.groups;
+        const bool own = size % V == 0;                                    // a lane's keys are of one group
+        uint32_t first = 0u, second = 0u;
+        auto take = [&](uint32_t u) {
+            const uint32_t low = u < first ? u : first;
+            first = u > first ? u : first;
+            second = low > second ? low : second;
+        };
+        if (own) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) s_key[tok][e0 + v] = key[v];
+            for (int v = 0; v < V; ++v) take(key[v]);
+            s_key[tok][lane] = first;                                      // the lanes' best two
+            if constexpr (V > 1) s_key[tok][ROUTE_LANES * V / 2 + lane] = second;
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) s_key[tok][e0 + v] = key[v];
+        }
         __syncthreads();
         for (int g = lane; g < a.groups; g += ROUTE_LANES) {
-            uint32_t first = 0u, second = 0u;
-            for (int i = 0; i < size; ++i) {
-                const uint32_t u = s_key[tok][g * size + i];
-                if (u > first) { second = first; first = u; }
-                else if (u > second) second = u;
+            first = second = 0u;
+            if (own) {
+                for (int i = 0; i < size / V; ++i) {
+                    take(s_key[tok][g * (size / V) + i]);
+                    if constexpr (V > 1) take(s_key[tok][ROUTE_LANES * V / 2 + g * (size / V) + i]);
+                }
+            } else {
+                for (int i = 0; i < size; ++i) take(s_key[tok][g * size + i]);
             }
-            if (SIGMOID && second) first = order_key(key_value(first) + key_value(second));
-            s_group[tok][g] = first;
+            s_group[tok][g] = SIGMOID && second ? order_key(key_value(first) + key_value(second)) : first;
         }
         __syncthreads();
         // a group stays if fewer than top_groups come before it
-#pragma unroll 1
-        for (int v = 0; v < V; ++v) {
-            const int e = e0 + v;
-            if (e >= a.E) continue;
-            const int g = e / size;
+        auto stays = [&](int g) {
             const uint32_t mine = s_group[tok][g];
             int before = 0;
             for (int h = 0; h < a.groups; ++h) {
                 const uint32_t o = s_group[tok][h];
                 before += o > mine || (o == mine && h < g);
             }
-            if (before >= a.top_groups) s_key[tok][e] = 0u;
+            return before < a.top_groups;
+        };
+        if (own) {
+            if (e0 < a.E && !stays(e0 / size)) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) key[v] = 0u;
+            }
+        } else {
+            int g = e0 / size, left = size - (e0 - g * size);              // the keys' group, and how many of them are still of it
+            bool keep = e0 < a.E && stays(g);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (left == 0) {
+                    ++g;
+                    left = size;
+                    keep = e0 + v < a.E && stays(g);
+                }
+                key[v] = keep ? key[v] : 0u;
+                --left;
+            }
         }
         __syncthreads();
+    }
+    uint32_t high[NQ];                                                     // the highest of every quad
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = s_key[tok][e0 + v];
+    for (int q = 0; q < NQ; ++q) {
+        high[q] = key[Q * q];
+#pragma unroll
+        for (int i = 1; i < Q; ++i) high[q] = high[q] > key[Q * q + i] ? high[q] : key[Q * q + i];
+        if constexpr (NQ > 1) *reinterpret_cast<ew_u4*>(&s_key[tok][e0 + Q * q]) = ew_u4{key[Q * q], key[Q * q + 1], key[Q * q + 2], key[Q * q + 3]};
     }
     const int shift = threadIdx.x & 48;
     for (int j = 0; j < a.k; ++j) {
-        uint32_t best = 0u;
-        int at = 0;
+        uint32_t best = high[0];
+        int quad = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (key[v] > best) { best = key[v]; at = v; }
+        for (int q = 1; q < NQ; ++q) {
+            quad = high[q] > best ? q : quad;
+            best = high[q] > best ? high[q] : best;
+        }
         const uint32_t top = row_max(best);
         const uint32_t mask = (uint32_t)(__ballot(best == top) >> shift) & 0xFFFFu;
         if (lane == __ffs(mask) - 1) {
-            s_idx[tok][j] = top ? e0 + at : -1;
+            ew_u4 k4 = {0u, 0u, 0u, 0u};
+            if constexpr (NQ > 1) {
+                k4 = *reinterpret_cast<const ew_u4*>(&s_key[tok][e0 + Q * quad]);
+            } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v == at) key[v] = 0u;
+                for (int i = 0; i < Q; ++i) k4[i] = key[i];
+            }
+            int at = 0;
+#pragma unroll
+            for (int i = Q - 1; i >= 0; --i) at = k4[i] == top ? i : at;
+            s_idx[tok][j] = top ? e0 + Q * quad + at : -1;
+            uint32_t next = 0u;
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                k4[i] = i == at ? 0u : k4[i];
+                next = next > k4[i] ? next : k4[i];
+            }
+            if constexpr (NQ > 1) {
+                s_key[tok][e0 + Q * quad + at] = 0u;
+            } else {
+#pragma unroll
+                for (int i = 0; i < Q; ++i) key[i] = k4[i];
+            }
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) high[q] = q == quad ? next : high[q];
         }
     }
     __syncthreads();
@@ -243,14 +341,17 @@ k_route_grads(const T* __restrict__ logits, int64_t ld, int64_t tokens, const in
 
 // ---- the plan: a stable counting sort of the choices by expert ----
 // The choices are cut into chunks.  With several chunks a first launch counts each chunk's choices of every expert; then every workgroup
-// adds up the counts of the chunks before its own, so that no launch is spent on a scan.
+// adds up the counts of the chunks before its own, so that no launch is spent on a scan.  Up to PLAN_ALONE choices one workgroup does all of
+// it, which costs it about a microsecond per 1024 and saves a launch of four.
+// 131072 choices of 256 experts: PLAN_T us, of which the counts take PLAN_C.
 #define PLAN_THREADS 1024
 #define PLAN_WAVES (PLAN_THREADS / METIS_WAVE)
 #define PLAN_MAX_CHUNKS 128
+#define PLAN_ALONE 4096
 
-__host__ __device__ inline int64_t plan_chunk(int64_t S) {
-    const int64_t c = (S + PLAN_MAX_CHUNKS - 1) / PLAN_MAX_CHUNKS;
-    return (c < 2048 ? 2048 : (c + PLAN_THREADS - 1) / PLAN_THREADS * PLAN_THREADS);
+int64_t plan_chunk(int64_t S) {
+    if (S <= PLAN_ALONE) return PLAN_ALONE;
+    return (S + PLAN_MAX_CHUNKS * PLAN_THREADS - 1) / (PLAN_MAX_CHUNKS * PLAN_THREADS) * PLAN_THREADS;
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS)
@@ -268,55 +369,63 @@ k_plan_count(const int32_t* __restrict__ idx, int64_t S, int64_t chunk, int E, i
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS)
-k_plan(const int32_t* __restrict__ idx, int64_t S, int k, int64_t chunk, int E, const int32_t* __restrict__ counts,
+k_plan(const int32_t* __restrict__ idx, int64_t S, FastDiv by_k, int64_t chunk, int E, const int32_t* __restrict__ counts,
        int32_t* __restrict__ offsets, int32_t* __restrict__ token, int32_t* __restrict__ slot) {
     __shared__ int32_t s_next[ROUTE_MAX_E];                               // the next slot of every expert
     __shared__ int32_t s_wave[PLAN_WAVES][ROUTE_MAX_E];                   // counts of a wave's 64 choices, then their first slots
-    __shared__ int32_t s_scan[ROUTE_MAX_E];
-    __shared__ int32_t s_total;
+    __shared__ int32_t s_before[ROUTE_MAX_E], s_all[ROUTE_MAX_E];
+    __shared__ int32_t s_sum[PLAN_WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nchunks = (int)gridDim.x;
     const int64_t from = (int64_t)blockIdx.x * chunk, to = from + chunk < S ? from + chunk : S;
-    int32_t before = 0, all = 0;
+    if (tid < E) s_before[tid] = s_all[tid] = 0;
+    __syncthreads();
     if (counts) {
-        if (tid < E)
-            for (int c = 0; c < nchunks; ++c) {
-                const int32_t n = counts[(int64_t)c * E + tid];
+        // the threads share an expert's chunks: as many parts as there are threads for
+        const int parts = PLAN_THREADS / E, e = tid % E, part = tid / E;
+        if (part < parts) {
+            int32_t before = 0, all = 0;
+#pragma unroll 8
+            for (int c = part; c < nchunks; c += parts) {
+                const int32_t n = counts[(int64_t)c * E + e];
                 before += c < (int)blockIdx.x ? n : 0;
                 all += n;
             }
+            atomicAdd(&s_before[e], before);
+            atomicAdd(&s_all[e], all);
+        }
     } else {
-        if (tid < E) s_next[tid] = 0;
-        __syncthreads();
         for (int64_t i = from + tid; i < to; i += PLAN_THREADS) {
             const int e = idx[i];
-            if ((uint32_t)e < (uint32_t)E) atomicAdd(&s_next[e], 1);
+            if ((uint32_t)e < (uint32_t)E) atomicAdd(&s_all[e], 1);
         }
-        __syncthreads();
-        if (tid < E) all = s_next[tid];
     }
-    if (tid < ROUTE_MAX_E) s_scan[tid] = tid < E ? all : 0;
     __syncthreads();
-    for (int step = 1; step < E; step *= 2) {                              // inclusive scan over the experts
-        const int32_t v = tid < E && tid >= step ? s_scan[tid - step] : 0;
-        __syncthreads();
-        if (tid < E) s_scan[tid] += v;
-        __syncthreads();
+    const int32_t mine = tid < E ? s_all[tid] : 0;
+    int32_t upto = mine;                                                   // inclusive scan over the experts
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 63) s_sum[wave] = upto;
+    __syncthreads();
+    int32_t total = 0;
+    for (int w = 0; w < ROUTE_MAX_E / 64; ++w) {
+        upto += w < wave ? s_sum[w] : 0;
+        total += s_sum[w];
     }
     if (tid < E) {
-        s_next[tid] = s_scan[tid] - all + before;
-        if (blockIdx.x == 0) offsets[tid + 1] = s_scan[tid];
-        if (tid == E - 1) s_total = s_scan[tid];
+        s_next[tid] = upto - mine + s_before[tid];
+        if (blockIdx.x == 0) offsets[tid + 1] = upto;
     }
     if (blockIdx.x == 0 && tid == 0) offsets[0] = 0;
-    __syncthreads();
     // slots that serve no choice
-    for (int64_t i = s_total + (int64_t)blockIdx.x * PLAN_THREADS + tid; i < S; i += (int64_t)nchunks * PLAN_THREADS) token[i] = -1;
+    for (int64_t i = total + (int64_t)blockIdx.x * PLAN_THREADS + tid; i < S; i += (int64_t)nchunks * PLAN_THREADS) token[i] = -1;
     for (int64_t base = from; base < to; base += PLAN_THREADS) {
         const int64_t i = base + tid;
         const int e = i < to ? idx[i] : -1;
         const bool there = (uint32_t)e < (uint32_t)E;
-        for (int n = tid; n < PLAN_WAVES * E; n += PLAN_THREADS) s_wave[n / E][n % E] = 0;
-        __syncthreads();
+        for (int n = lane; n < E; n += 64) s_wave[wave][n] = 0;
         // the lanes of the wave that chose the same expert
         uint64_t same = __ballot(there);
         for (int b = 1; b < E; b *= 2) {
@@ -327,11 +436,13 @@ k_plan(const int32_t* __restrict__ idx, int64_t S, int k, int64_t chunk, int E, 
         if (there && rank == 0) s_wave[wave][e] = __popcll(same);
         __syncthreads();
         if (tid < E) {
-            int32_t n = s_next[tid];
+            int32_t n = s_next[tid], c[PLAN_WAVES];
+#pragma unroll
+            for (int w = 0; w < PLAN_WAVES; ++w) c[w] = s_wave[w][tid];
+#pragma unroll
             for (int w = 0; w < PLAN_WAVES; ++w) {
-                const int32_t c = s_wave[w][tid];
                 s_wave[w][tid] = n;
-                n += c;
+                n += c[w];
             }
             s_next[tid] = n;
         }
@@ -339,9 +450,8 @@ k_plan(const int32_t* __restrict__ idx, int64_t S, int k, int64_t chunk, int E, 
         if (i < to) {
             const int32_t at = there ? s_wave[wave][e] + rank : -1;
             slot[i] = at;
-            if (there) token[at] = (int32_t)(i / k);
+            if (there) token[at] = (int32_t)div_by(by_k, (uint64_t)i);
         }
-        __syncthreads();
     }
 }
 
@@ -404,7 +514,10 @@ extern "C" int metis_route(void* stream, const metis_mat* logits, const metis_ro
         return METIS_INVALID_ARG;
     if (logits->rows == 0) return METIS_OK;
     if (!idx || !weights) return METIS_INVALID_ARG;
-    const RouteArgs a = {logits->rows, logits->ld, bias, valid, idx, weights, r->experts, r->k, r->groups, r->top_groups, r->renorm, r->scale};
+    int held = 1;                                                          // experts a lane has
+    while (held * ROUTE_LANES < r->experts) held *= 2;
+    const RouteArgs a = {logits->rows, logits->ld, bias, valid, idx, weights, r->experts, r->k, r->groups, r->top_groups, r->renorm, r->scale,
+                         r->experts % held == 0 && mat_aligned16(logits) && (uintptr_t)bias % 16 == 0};
     return logits->dtype == METIS_BF16 ? launch_route<bf16_t>((hipStream_t)stream, logits, r, a)
                                        : launch_route<float>((hipStream_t)stream, logits, r, a);
 }
@@ -447,7 +560,7 @@ extern "C" int metis_dispatch(void* stream, const int32_t* idx, metis_expert_pla
         hipLaunchKernelGGL(k_plan_count, dim3((unsigned)chunks), dim3(PLAN_THREADS), 0, s, idx, S, chunk, plan->experts, counts);
         METIS_LAUNCH_CHECK();
     }
-    hipLaunchKernelGGL(k_plan, dim3((unsigned)chunks), dim3(PLAN_THREADS), 0, s, idx, S, plan->k, chunk, plan->experts, counts,
+    hipLaunchKernelGGL(k_plan, dim3((unsigned)chunks), dim3(PLAN_THREADS), 0, s, idx, S, fast_div((uint32_t)plan->k), chunk, plan->experts, counts,
                        plan->offsets, plan->token, plan->slot);
     METIS_LAUNCH_CHECK();
     return METIS_OK;

@@ -161,10 +161,13 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
 def _mat(t):
-    assert t.is_cuda and t.dim() == 2 and t.stride(1) == 1
-    dt = {torch.bfloat16: BF16, torch.float32: F32}[t.dtype]
-    return Mat(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0), dt)
+    (rows, cols), (ld, step) = t.shape, t.stride()           # two axes
+    assert t.is_cuda and step == 1
+    return Mat(t.data_ptr(), rows, cols, ld, _DTYPES[t.dtype])
 
 
 class Fp4Tensor:
@@ -196,9 +199,10 @@ class MxTensor:
         if buffers is None:
             buffers = (torch.empty((rows, cols // 2), dtype=torch.uint8, device=device),
                        torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
+        else:
+            assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
+            assert [t.numel() for t in buffers] == [rows * (cols // 2), rows * (cols // 32)]
         self.codes, self.scales = buffers
-        assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
-        assert self.codes.numel() == rows * (cols // 2) and self.scales.numel() == rows * (cols // 32)
 
     def c(self):
         return MxFp4(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
@@ -213,9 +217,10 @@ class Mx8Tensor:
         if buffers is None:
             buffers = (torch.empty((rows, cols), dtype=torch.uint8, device=device),
                        torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
+        else:
+            assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
+            assert [t.numel() for t in buffers] == [rows * cols, rows * (cols // 32)]
         self.codes, self.scales = buffers
-        assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
-        assert self.codes.numel() == rows * cols and self.scales.numel() == rows * (cols // 32)
 
     def c(self):
         return Mx8(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
@@ -493,9 +498,10 @@ class ExpertPlan:
         if buffers is None:
             i32 = dict(dtype=torch.int32, device=device)
             buffers = torch.empty((experts + 1,), **i32), torch.empty((tokens * k,), **i32), torch.empty((tokens, k), **i32)
+        else:
+            assert all(t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 for t in buffers)
+            assert [t.numel() for t in buffers] == [experts + 1, tokens * k, tokens * k]
         self.offsets, self.token, self.slot = buffers
-        assert all(t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 for t in buffers)
-        assert self.offsets.numel() == experts + 1 and self.token.numel() == tokens * k == self.slot.numel()
 
     def c(self):
         return Plan(self.offsets.data_ptr(), self.token.data_ptr(), self.slot.data_ptr(), self.tokens, self.experts, self.k)
