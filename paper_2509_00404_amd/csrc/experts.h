@@ -75,6 +75,17 @@ __device__ __forceinline__ uint32_t mx_pack8(float a, float b, float c, float d,
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e, f, 1.0f, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, g, h, 1.0f, 3);
 }
+// eight elements of a block that four lanes hold: their codes, and the block's scale
+__device__ __forceinline__ uint32_t mx_quad(const float (&v)[8], uint32_t& byte) {
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[i]));
+    amax = fmaxf(amax, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(amax), 0xB1, 0xF, 0xF, true)));    // lanes 1 0 3 2
+    amax = fmaxf(amax, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(amax), 0x4E, 0xF, 0xF, true)));    // lanes 2 3 0 1
+    byte = mx_scale(amax);
+    const float inv = mx_inverse(byte);
+    return mx_pack8(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+}
 // one block of a lane's own
 __device__ __forceinline__ ew_u4 mx_block(const float (&v)[32], uint32_t& byte) {
     float amax = 0.0f;

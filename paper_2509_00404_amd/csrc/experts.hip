@@ -113,6 +113,8 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
 // long as both operands agree: over a run of 512 elements a lane takes the 8 blocks of its half one after the other, 128 bytes
 // that lie together, and their 8 scale bytes.  The weights of the next run are on their way while one is multiplied.
 // SPLIT: the workgroup's four waves share 32 outputs, take every fourth run, and add up in their order by way of LDS; else each has 32 of its own.
+// FUSE: few elements a unit (a decode step).  The workgroup quantizes its slots' rows itself, into LDS, while its first weights travel; a launch
+// of the row quantizer in front costs more (figures where it is chosen).
 struct MxRows {
     const uint8_t* codes;
     const uint8_t* scales;
@@ -171,11 +173,35 @@ __device__ __forceinline__ void put4(OUT* p, ex_f4 v, int64_t left, bool vec) {
         }
 }
 
-template <typename OUT, int G, bool SPLIT>
+struct DenseRows {
+    const void* ptr;
+    int64_t ld;
+};
+// LDS of a quantized row: codes in whole runs and 16 bytes that spread the rows over the banks, then the scales
+__host__ __device__ inline int few_code_row(int nblk) { return (nblk + 15) / 16 * 256 + 16; }
+__host__ __device__ inline int few_scale_row(int nblk) { return (nblk + 15) / 16 * 16; }
+// `rows` rows of A quantized to LDS, by all 256 threads; row_of(i): A's row
+template <typename T, typename F>
+__device__ __forceinline__ void few_quantize(const T* A, int64_t ld, int rows, int nblk, uint8_t* codes, uint8_t* scales, const F& row_of) {
+    const int per = (nblk + 15) / 16 * 64;               // lanes a row: 8 elements each, four per block
+    for (int i = threadIdx.x; i < rows * per; i += 256) {
+        const int row = i / per, c = i - row * per;
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (c < 4 * nblk) load_row<8>(A + row_of(row) * ld + 8 * c, v);
+        uint32_t byte;
+        const uint32_t w = mx_quad(v, byte);
+        *reinterpret_cast<uint32_t*>(codes + row * few_code_row(nblk) + 4 * c) = w;
+        if ((i & 3) == 0) scales[row * few_scale_row(nblk) + (c >> 2)] = (uint8_t)byte;
+    }
+}
+
+template <typename OUT, int G, bool SPLIT, typename T = void>
 __global__ void __launch_bounds__(256, 2)
-k_experts_few(MxRows A, int64_t arows, MxRows W, const int32_t* __restrict__ offsets, const int32_t* __restrict__ token, int E, int64_t S,
+k_experts_few(MxRows A, DenseRows dense, int64_t arows, MxRows W, const int32_t* __restrict__ offsets, const int32_t* __restrict__ token, int E, int64_t S,
               int64_t N, int nblk, OUT* __restrict__ C, int64_t ldc, bool vec, uint32_t nblocks, uint32_t most) {
+    constexpr bool FUSE = !std::is_void<T>::value;
     __shared__ float s_part[SPLIT ? 3 * G * 16 * 64 : 1];
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_rows[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), li = lane & 31, half = lane >> 5;
     const uint32_t ub = blockIdx.x / nblocks, nb = blockIdx.x - ub * nblocks;
     const SlotUnit u = find_unit(offsets, E, S, 32 * G, ub);
@@ -186,19 +212,24 @@ k_experts_few(MxRows A, int64_t arows, MxRows W, const int32_t* __restrict__ off
             for (int64_t c = c0 + threadIdx.x; c < c0 + wide && c < N; c += 256) C[s * ldc + c] = OUT(0);
         return;
     }
-    if (n0 >= N) return;                                 // (SPLIT: not for some waves of a workgroup alone)
+    if (!FUSE && n0 >= N) return;                        // (SPLIT: not for some waves of a workgroup alone)
     const int64_t first = u.begin + 32 * G * (int64_t)u.local;
     const int groups = G > 1 && first + 32 < u.end ? 2 : 1;
     const uint64_t n = (uint64_t)u.expert * N + (n0 + li < N ? n0 + li : N - 1);
     const uint8_t *wc = W.codes + n * nblk * 16, *wsc = W.scales + n * nblk;
+    auto row_of = [&](int i) {                           // A's row of the unit's slot i
+        const int64_t s = first + i, sr = s < u.end ? s : u.end - 1;
+        const uint64_t row = token ? (uint64_t)(uint32_t)token[sr] : (uint64_t)sr;
+        return (int64_t)(row < (uint64_t)arows ? row : (uint64_t)arows - 1);
+    };
     const uint8_t *tc[G], *tsc[G];
+    if constexpr (!FUSE) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        const int64_t s = first + 32 * g + li, sr = s < u.end ? s : u.end - 1;
-        uint64_t row = token ? (uint64_t)(uint32_t)token[sr] : (uint64_t)sr;
-        if (row >= (uint64_t)arows) row = arows - 1;
-        tc[g] = A.codes + row * nblk * 16;
-        tsc[g] = A.scales + row * nblk;
+        for (int g = 0; g < G; ++g) {
+            const int64_t row = row_of(32 * g + li);
+            tc[g] = A.codes + row * nblk * 16;
+            tsc[g] = A.scales + row * nblk;
+        }
     }
     float16_t acc[G];
 #pragma unroll
@@ -210,13 +241,33 @@ k_experts_few(MxRows A, int64_t arows, MxRows W, const int32_t* __restrict__ off
     uint32_t ws[2][2];
     int r = SPLIT ? 16 * wave : 0;
     if (r < nblk) few_load<false>(wc, wsc, r, nblk, half, w[0], ws[0]);
+    const int mine = first + li < u.end ? li : (int)(u.end - 1 - first);
+    const uint8_t *lc = s_rows + mine * few_code_row(nblk), *lsc = nullptr;
+    if constexpr (FUSE) {
+        const int rows = u.end - first < 32 ? (int)(u.end - first) : 32;
+        lsc = s_rows + rows * few_code_row(nblk) + mine * few_scale_row(nblk);
+        few_quantize((const T*)dense.ptr, dense.ld, rows, nblk, s_rows, s_rows + rows * few_code_row(nblk), row_of);
+        __syncthreads();
+        if (n0 >= N) return;
+    }
     auto run = [&](auto now_) __attribute__((always_inline)) {
         constexpr int now = decltype(now_)::value;
         ew_u4 t[G][8];
         uint32_t ts[G][2];
 #pragma unroll
         for (int g = 0; g < G; ++g)
-            if (g < groups) few_load<true>(tc[g], tsc[g], r, nblk, half, t[g], ts[g]);
+            if (g < groups) {
+                if constexpr (FUSE) {
+                    const int b = r + 8 * half;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) t[g][i] = *reinterpret_cast<const ew_u4*>(lc + 16 * b + 16 * i);
+                    const ew_u2 x = *reinterpret_cast<const ew_u2*>(lsc + b);
+                    ts[g][0] = x[0];
+                    ts[g][1] = x[1];
+                } else {
+                    few_load<true>(tc[g], tsc[g], r, nblk, half, t[g], ts[g]);
+                }
+            }
         if (r + hop < nblk) few_load<false>(wc, wsc, r + hop, nblk, half, w[now ^ 1], ws[now ^ 1]);
 #pragma unroll
         for (int g = 0; g < G; ++g)
@@ -314,14 +365,8 @@ k_quantize_rows(const T* __restrict__ A, int64_t ld, int64_t K, uint64_t total, 
     const uint32_t unit = (uint32_t)(n - row * units.d);
     float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (8 * (int64_t)unit < K) load_row<8>(A + row * ld + 8 * (int64_t)unit, v);
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[i]));
-    amax = fmaxf(amax, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(amax), 0xB1, 0xF, 0xF, true)));
-    amax = fmaxf(amax, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(amax), 0x4E, 0xF, 0xF, true)));
-    const uint32_t byte = mx_scale(amax);
-    const float inv = mx_inverse(byte);
-    *reinterpret_cast<uint32_t*>(codes + 4 * n) = mx_pack8(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+    uint32_t byte;
+    *reinterpret_cast<uint32_t*>(codes + 4 * n) = mx_quad(v, byte);
     if constexpr (UNITS) {
         uint32_t w = byte << (8 * (threadIdx.x >> 2 & 3));
         w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x124, 0xF, 0xF, true);         // around the 16 lanes by 4, then by 8
@@ -451,24 +496,43 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
         const int64_t tiles = most_units(S, E, 256) * tn;
         return C->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_PRODUCT>(s, a, tiles, C) : launch_stream<float, EX_PRODUCT>(s, a, tiles, C);
     }
-    const int qs = launch_quantize_rows<false>(s, A, K, ws, {ws + place.scales, nullptr, 0, 0}, {});
-    if (qs != METIS_OK) return qs;
-    const int g = S > 24 * (int64_t)E ? 2 : 1;
+    const int nblk = (int)(K / 32), g = S > 24 * (int64_t)E ? 2 : 1;
     const int64_t most = most_units(S, E, 32 * g) + 1;
     const bool split = most * ceil_div64(N, 32) < 4096;
     const int64_t nb = ceil_div64(N, split ? 32 : 128);
     if (most * nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    const size_t row_lds = (size_t)few_code_row(nblk) + few_scale_row(nblk), lds = row_lds * (S < 32 ? S : 32);
+    // Quantized on the spot where an expert has 8192 elements or fewer on average, and the rows of a full unit leave room for four
+    // workgroups a CU.  us, with the quantizer's launch / on the spot, 2048 x 4096 with 64 experts of which a token takes four: one token
+    // 18.7 / 16.9, two 19.0 / 15.5, 64 64.0 / 68.6, 200 74.3 / 97.9; 4096 x 1024, 24 tokens 27.3 / 24.7.  Rows of 70 KB, 8 tokens: 25.7 / 43.0.
+    const bool fuse = g == 1 && S * K <= 8192 * (S < E ? S : E) && lds <= 24 * 1024;
+    if (!fuse) {
+        const int qs = launch_quantize_rows<false>(s, A, K, ws, {ws + place.scales, nullptr, 0, 0}, {});
+        if (qs != METIS_OK) return qs;
+    }
     const int64_t size = mat_size(C);
     const bool vec = (uintptr_t)C->ptr % (4 * size) == 0 && C->ld % 4 == 0;
-    auto launch = [&](auto kern, auto zero) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)(most * nb)), dim3(256), 0, s, MxRows{ws, ws + place.scales}, A->rows, MxRows{W->codes, W->scales},
-                           plan->offsets, gather ? plan->token : nullptr, E, S, N, (int)(K / 32), (decltype(zero)*)C->ptr, C->ld, vec, (uint32_t)nb,
-                           (uint32_t)most);
+    auto launch = [&](auto kern, auto zero, size_t dyn) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)(most * nb)), dim3(256), dyn, s, MxRows{ws, ws + place.scales}, DenseRows{A->ptr, A->ld}, A->rows,
+                           MxRows{W->codes, W->scales}, plan->offsets, gather ? plan->token : nullptr, E, S, N, nblk, (decltype(zero)*)C->ptr,
+                           C->ld, vec, (uint32_t)nb, (uint32_t)most);
+    };
+    auto fused = [&](auto zero, auto in, auto split_) {
+        typedef decltype(in) T;
+        auto kern = k_experts_few<decltype(zero), 1, decltype(split_)::value, T>;
+        launch(kern, zero, lds);
     };
     auto by_shape = [&](auto zero) {
         typedef decltype(zero) OUT;
-        if (g == 1) split ? launch(k_experts_few<OUT, 1, true>, zero) : launch(k_experts_few<OUT, 1, false>, zero);
-        else split ? launch(k_experts_few<OUT, 2, true>, zero) : launch(k_experts_few<OUT, 2, false>, zero);
+        if (fuse) {
+            const bool bf = A->dtype == METIS_BF16;
+            if (split) bf ? fused(zero, bf16_t(), std::true_type{}) : fused(zero, float(), std::true_type{});
+            else bf ? fused(zero, bf16_t(), std::false_type{}) : fused(zero, float(), std::false_type{});
+        } else if (g == 1) {
+            split ? launch(k_experts_few<OUT, 1, true>, zero, 0) : launch(k_experts_few<OUT, 1, false>, zero, 0);
+        } else {
+            split ? launch(k_experts_few<OUT, 2, true>, zero, 0) : launch(k_experts_few<OUT, 2, false>, zero, 0);
+        }
     };
     if (C->dtype == METIS_BF16) by_shape(bf16_t());
     else by_shape(float());

@@ -50,8 +50,8 @@ def _calls(metis):
     return {
         "route, softmax": (route(0), 1), "route, sigmoid": (route(1), 1), "route gradients": (route(0, True), 1),
         "plan, one workgroup": (dispatch(1000), 1), "plan, chunks": (dispatch(10000), 2),
-        "product, one token": (product(1, 64, 4, 2048, 4096, 1, metis.BF16), 2),
-        "product, few slots": (product(100, 64, 4, 2048, 1024, 0, metis.F32), 2),
+        "product, one token": (product(1, 64, 4, 2048, 4096, 1, metis.BF16), 1),
+        "product, few slots": (product(100, 64, 4, 2048, 4096, 0, metis.F32), 2),
         "product, many slots": (product(4000, 16, 4, 2048, 1056, 1, metis.BF16), 2),
         "weight gradient, bf16": (wgrad(metis.BF16), 3), "weight gradient, fp32": (wgrad(metis.F32), 3),
         "weights transposed": (lambda: L.metis_quantize_mx_t(None, mat(4 * 512, 1024), 4, ref(metis.MxFp4(FAKE, FAKE, 4 * 1024, 512))), 1),

@@ -58,6 +58,10 @@ CASES = [  # T, E, k, N, K, skew, missing
     (700, 4, 2, 513, 768, 0.8, 0.0),
     (2100, 2, 1, 256, 512, 0.0, 0.0),
     (40, 512, 8, 40, 64, 0.0, 0.0),
+    (2, 8, 4, 333, 1568, 0.0, 0.0),                            # a decode step, the contraction's last run short
+    (9, 8, 2, 1030, 2080, 0.5, 0.1),
+    (60, 16, 4, 200, 992, 0.9, 0.0),                           # few slots, too many to quantize on the spot
+    (100, 8, 2, 140, 1056, 0.3, 0.0),
     (64, 8, 2, 136, 256, 0.0, 1.0),                            # nobody has an expert
 ]
 
