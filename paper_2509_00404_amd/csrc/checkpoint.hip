@@ -50,7 +50,8 @@ __device__ __forceinline__ void mx8_decode(ew_u2 c, uint32_t byte, float (&v)[8]
     }
 }
 
-// a lane per 8 elements, four lanes per block; `units` of 8 a row
+// a lane per 8 elements, four lanes per block; `units` of 8 a row.  Memory bounds all four kernels here: 65536 x 1024 bf16 activations and their
+// checkpoint (541 MB moved) take 94 us, the gradients (674 MB) 115, 5.8 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_quantize_mx8(const T* __restrict__ A, int64_t ld, uint64_t total, FastDiv units, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {

@@ -17,7 +17,8 @@ namespace {
 // neighbouring columns, all of them in flight together; a workgroup's 8 waves have 256 rows of 128 columns, which leave by way of LDS as
 // whole lines.  With a plan the segments are the experts' slots, padded with zeros to a multiple of 64, in rows of whole units and with
 // scales in units, and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows` rows.
-// What bounds it: 32768 x 4096 gathered rows, 339 MB to be moved, take QT_X us, x 2048 by slot (170 MB) QT_G.
+// What bounds it: memory.  32768 x 4096 gathered rows, 339 MB to be moved, take 55 us, x 2048 by slot (170 MB) 36.  (Loads in branches, 16
+// bytes of a column stored at a time and scales byte by byte: 140 and 103.)
 #define QT_ROW 144                            // a column's 8 blocks of 16 bytes, and 16 that spread the columns over the banks
 template <typename T>
 __global__ void __launch_bounds__(512)
@@ -108,7 +109,7 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
 
 // ---- products for few slots an expert: straight from memory ----
 // What counts is that the weights stream: they pass through registers alone, and nothing waits for anybody.  A wave has 32 of the expert's N
-// (the first operand, so that a lane ends with runs of four neighbouring outputs) and up to 32 G slots, on v_mfma_scale_f32_32x32x64_f8f6f4:
+// (the first operand, so that a lane ends with runs of four neighbouring outputs) and up to 32 slots, on v_mfma_scale_f32_32x32x64_f8f6f4:
 // a lane's operand is the 32 codes (16 bytes) of row lane % 32 and one block of either half of the step.  Which blocks a step takes is free as
 // long as both operands agree: over a run of 512 elements a lane takes the 8 blocks of its half one after the other, 128 bytes
 // that lie together, and their 8 scale bytes.  The weights of the next run are on their way while one is multiplied.
@@ -195,16 +196,16 @@ __device__ __forceinline__ void few_quantize(const T* A, int64_t ld, int rows, i
     }
 }
 
-template <typename OUT, int G, bool SPLIT, typename T = void>
+template <typename OUT, bool SPLIT, typename T = void>
 __global__ void __launch_bounds__(256, 2)
 k_experts_few(MxRows A, DenseRows dense, int64_t arows, MxRows W, const int32_t* __restrict__ offsets, const int32_t* __restrict__ token, int E, int64_t S,
               int64_t N, int nblk, OUT* __restrict__ C, int64_t ldc, bool vec, uint32_t nblocks, uint32_t most) {
     constexpr bool FUSE = !std::is_void<T>::value;
-    __shared__ float s_part[SPLIT ? 3 * G * 16 * 64 : 1];
+    __shared__ float s_part[SPLIT ? 3 * 16 * 64 : 1];
     extern __shared__ __attribute__((aligned(16))) uint8_t s_rows[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), li = lane & 31, half = lane >> 5;
     const uint32_t ub = blockIdx.x / nblocks, nb = blockIdx.x - ub * nblocks;
-    const SlotUnit u = find_unit(offsets, E, S, 32 * G, ub);
+    const SlotUnit u = find_unit(offsets, E, S, 32, ub);
     const int64_t n0 = SPLIT ? 32 * (int64_t)nb : 128 * (int64_t)nb + 32 * wave;
     if (u.expert < 0) {                                  // behind the last unit of slots the workgroups clear the unused ones
         const int64_t used = held(offsets[E], S), step = most - u.total, wide = SPLIT ? 32 : 128, c0 = wide * nb;
@@ -213,8 +214,7 @@ k_experts_few(MxRows A, DenseRows dense, int64_t arows, MxRows W, const int32_t*
         return;
     }
     if (!FUSE && n0 >= N) return;                        // (SPLIT: not for some waves of a workgroup alone)
-    const int64_t first = u.begin + 32 * G * (int64_t)u.local;
-    const int groups = G > 1 && first + 32 < u.end ? 2 : 1;
+    const int64_t first = u.begin + 32 * (int64_t)u.local;
     const uint64_t n = (uint64_t)u.expert * N + (n0 + li < N ? n0 + li : N - 1);
     const uint8_t *wc = W.codes + n * nblk * 16, *wsc = W.scales + n * nblk;
     auto row_of = [&](int i) {                           // A's row of the unit's slot i
@@ -222,65 +222,50 @@ k_experts_few(MxRows A, DenseRows dense, int64_t arows, MxRows W, const int32_t*
         const uint64_t row = token ? (uint64_t)(uint32_t)token[sr] : (uint64_t)sr;
         return (int64_t)(row < (uint64_t)arows ? row : (uint64_t)arows - 1);
     };
-    const uint8_t *tc[G], *tsc[G];
-    if constexpr (!FUSE) {
+    const uint8_t *tc, *tsc;                             // this lane's slot's row
+    float16_t acc;
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int64_t row = row_of(32 * g + li);
-            tc[g] = A.codes + row * nblk * 16;
-            tsc[g] = A.scales + row * nblk;
-        }
-    }
-    float16_t acc[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[g][v] = 0.0f;
+    for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
     constexpr int hop = SPLIT ? 64 : 16;
     ew_u4 w[2][8];
     uint32_t ws[2][2];
     int r = SPLIT ? 16 * wave : 0;
     if (r < nblk) few_load<false>(wc, wsc, r, nblk, half, w[0], ws[0]);
-    const int mine = first + li < u.end ? li : (int)(u.end - 1 - first);
-    const uint8_t *lc = s_rows + mine * few_code_row(nblk), *lsc = nullptr;
     if constexpr (FUSE) {
-        const int rows = u.end - first < 32 ? (int)(u.end - first) : 32;
-        lsc = s_rows + rows * few_code_row(nblk) + mine * few_scale_row(nblk);
+        const int rows = u.end - first < 32 ? (int)(u.end - first) : 32, mine = li < rows ? li : rows - 1;
+        tc = s_rows + mine * few_code_row(nblk);
+        tsc = s_rows + rows * few_code_row(nblk) + mine * few_scale_row(nblk);
         few_quantize((const T*)dense.ptr, dense.ld, rows, nblk, s_rows, s_rows + rows * few_code_row(nblk), row_of);
         __syncthreads();
         if (n0 >= N) return;
+    } else {
+        const int64_t row = row_of(li);
+        tc = A.codes + row * nblk * 16;
+        tsc = A.scales + row * nblk;
     }
     auto run = [&](auto now_) __attribute__((always_inline)) {
         constexpr int now = decltype(now_)::value;
-        ew_u4 t[G][8];
-        uint32_t ts[G][2];
+        ew_u4 t[8];
+        uint32_t ts[2];
+        if constexpr (FUSE) {                            // (in whole runs, zeros behind the row)
+            const int b = r + 8 * half;
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-            if (g < groups) {
-                if constexpr (FUSE) {
-                    const int b = r + 8 * half;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) t[g][i] = *reinterpret_cast<const ew_u4*>(lc + 16 * b + 16 * i);
-                    const ew_u2 x = *reinterpret_cast<const ew_u2*>(lsc + b);
-                    ts[g][0] = x[0];
-                    ts[g][1] = x[1];
-                } else {
-                    few_load<true>(tc[g], tsc[g], r, nblk, half, t[g], ts[g]);
-                }
-            }
+            for (int i = 0; i < 8; ++i) t[i] = *reinterpret_cast<const ew_u4*>(tc + 16 * (b + i));
+            const ew_u2 x = *reinterpret_cast<const ew_u2*>(tsc + b);
+            ts[0] = x[0];
+            ts[1] = x[1];
+        } else {
+            few_load<true>(tc, tsc, r, nblk, half, t, ts);
+        }
         if (r + hop < nblk) few_load<false>(wc, wsc, r + hop, nblk, half, w[now ^ 1], ws[now ^ 1]);
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-            if (g < groups) {
-                few_step<0>(acc[g], w[now], ws[now], t[g], ts[g]);
-                few_step<1>(acc[g], w[now], ws[now], t[g], ts[g]);
-                few_step<2>(acc[g], w[now], ws[now], t[g], ts[g]);
-                few_step<3>(acc[g], w[now], ws[now], t[g], ts[g]);
-                few_step<4>(acc[g], w[now], ws[now], t[g], ts[g]);
-                few_step<5>(acc[g], w[now], ws[now], t[g], ts[g]);
-                few_step<6>(acc[g], w[now], ws[now], t[g], ts[g]);
-                few_step<7>(acc[g], w[now], ws[now], t[g], ts[g]);
-            }
+        few_step<0>(acc, w[now], ws[now], t, ts);
+        few_step<1>(acc, w[now], ws[now], t, ts);
+        few_step<2>(acc, w[now], ws[now], t, ts);
+        few_step<3>(acc, w[now], ws[now], t, ts);
+        few_step<4>(acc, w[now], ws[now], t, ts);
+        few_step<5>(acc, w[now], ws[now], t, ts);
+        few_step<6>(acc, w[now], ws[now], t, ts);
+        few_step<7>(acc, w[now], ws[now], t, ts);
         r += hop;
     };
 #pragma unroll 1
@@ -292,28 +277,21 @@ k_experts_few(MxRows A, DenseRows dense, int64_t arows, MxRows W, const int32_t*
     if constexpr (SPLIT) {
         if (wave > 0) {
 #pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s_part[(((wave - 1) * G + g) * 16 + v) * 64 + lane] = acc[g][v];
+            for (int v = 0; v < 16; ++v) s_part[((wave - 1) * 16 + v) * 64 + lane] = acc[v];
         }
         __syncthreads();
         if (wave > 0) return;
 #pragma unroll
         for (int p = 0; p < 3; ++p)
 #pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[g][v] += s_part[((p * G + g) * 16 + v) * 64 + lane];
+            for (int v = 0; v < 16; ++v) acc[v] += s_part[(p * 16 + v) * 64 + lane];
     }
+    const int64_t s = first + li;
+    if (s >= u.end) return;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        const int64_t s = first + 32 * g + li;
-        if (s >= u.end) continue;
-#pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-            const int64_t c = n0 + 2 * v + 4 * half;
-            put4(C + s * ldc + c, ex_f4{acc[g][v], acc[g][v + 1], acc[g][v + 2], acc[g][v + 3]}, N - c, vec);
-        }
+    for (int v = 0; v < 16; v += 4) {
+        const int64_t c = n0 + 2 * v + 4 * half;
+        put4(C + s * ldc + c, ex_f4{acc[v], acc[v + 1], acc[v + 2], acc[v + 3]}, N - c, vec);
     }
 }
 
@@ -408,7 +386,9 @@ int64_t padded_slots(int64_t S, int E) { return most_units(S, E, SLOT_ALIGN) * S
 // (a tile reads the scales of 256 rows wherever its own end)
 size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * cols / 2, 256) + align_up((size_t)rows * cols / 32, 256) + 2048; }
 
-// The stream takes products of tiles that it can fill; the rest goes straight from memory.
+// The stream takes products of 16 slots an expert and more; what it cannot address, and fewer, goes straight from memory.  us, from memory /
+// streamed, 2048 x 4096 with 64 experts of which a token takes four: 24 tokens 27 / 51 (4096 x 1024), 64 64 / 78, 200 74 / 80, 400 89 / 82, 1000
+// 161 / 86.
 bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
     const int64_t Kp = (K + 255) / 256 * 256;
     if (arows * (Kp / 2) > 0xFFFFFFFFll || K > (1 << 24) || most_units(S, E, 256) * ceil_div64(N, 256) > 0x3FFFFFFF) return false;
@@ -496,8 +476,10 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
         const int64_t tiles = most_units(S, E, 256) * tn;
         return C->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_PRODUCT>(s, a, tiles, C) : launch_stream<float, EX_PRODUCT>(s, a, tiles, C);
     }
-    const int nblk = (int)(K / 32), g = S > 24 * (int64_t)E ? 2 : 1;
-    const int64_t most = most_units(S, E, 32 * g) + 1;
+    const int nblk = (int)(K / 32);
+    const int64_t most = most_units(S, E, 32) + 1;
+    // The contraction is split where there are few waves (not counting that a unit may not exist).  us, split / not: one token of the above
+    // 17.6 / 30.9, 24 tokens' 4096 x 1024 39.7 / 26.8, 200 tokens 72.7 / 75.0.
     const bool split = most * ceil_div64(N, 32) < 4096;
     const int64_t nb = ceil_div64(N, split ? 32 : 128);
     if (most * nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
@@ -505,7 +487,7 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     // Quantized on the spot where an expert has 8192 elements or fewer on average, and the rows of a full unit leave room for four
     // workgroups a CU.  us, with the quantizer's launch / on the spot, 2048 x 4096 with 64 experts of which a token takes four: one token
     // 18.7 / 16.9, two 19.0 / 15.5, 64 64.0 / 68.6, 200 74.3 / 97.9; 4096 x 1024, 24 tokens 27.3 / 24.7.  Rows of 70 KB, 8 tokens: 25.7 / 43.0.
-    const bool fuse = g == 1 && S * K <= 8192 * (S < E ? S : E) && lds <= 24 * 1024;
+    const bool fuse = S * K <= 8192 * (S < E ? S : E) && lds <= 24 * 1024;
     if (!fuse) {
         const int qs = launch_quantize_rows<false>(s, A, K, ws, {ws + place.scales, nullptr, 0, 0}, {});
         if (qs != METIS_OK) return qs;
@@ -519,7 +501,7 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     };
     auto fused = [&](auto zero, auto in, auto split_) {
         typedef decltype(in) T;
-        auto kern = k_experts_few<decltype(zero), 1, decltype(split_)::value, T>;
+        auto kern = k_experts_few<decltype(zero), decltype(split_)::value, T>;
         launch(kern, zero, lds);
     };
     auto by_shape = [&](auto zero) {
@@ -528,10 +510,8 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
             const bool bf = A->dtype == METIS_BF16;
             if (split) bf ? fused(zero, bf16_t(), std::true_type{}) : fused(zero, float(), std::true_type{});
             else bf ? fused(zero, bf16_t(), std::false_type{}) : fused(zero, float(), std::false_type{});
-        } else if (g == 1) {
-            split ? launch(k_experts_few<OUT, 1, true>, zero, 0) : launch(k_experts_few<OUT, 1, false>, zero, 0);
         } else {
-            split ? launch(k_experts_few<OUT, 2, true>, zero, 0) : launch(k_experts_few<OUT, 2, false>, zero, 0);
+            split ? launch(k_experts_few<OUT, true>, zero, 0) : launch(k_experts_few<OUT, false>, zero, 0);
         }
     };
     if (C->dtype == METIS_BF16) by_shape(bf16_t());

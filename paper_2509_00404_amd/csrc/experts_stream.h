@@ -11,6 +11,12 @@
 // and every XCD works on a run of them: they share panels of both operands in its L2.
 // Outputs are not read again here and go past the caches: kept in L2 they drive out the operands' panels (gradients of 8192 tokens' four
 // experts, 2048 x 4096 each, 626 us with the quantizers, so 461; 16384 tokens' product 409, 401).
+// What bounds it: 16384 tokens' four experts, 2048 x 4096 each, 320 us (1.1 PFLOP, 3.4 PFLOP/s; an eighth of the tiles' rows is short tiles').
+// Without its transfers it takes 250, without its matrix instructions 250, without its stores 285: LDS takes a unit's 192 KB of
+// fragments and 68 KB of transfers while the matrix pipe has 2048 cycles of work.  Gradients of 8192 tokens' (1.07 GB out) 285 to 320, without
+// stores 165.  Tried: tiles of 32 rows fewer to multiply at a short tile's end, transfers left out there, bands of 4 and 16, no XCD order: 1 % up
+// or down; whole tiles of all experts before the short ones: 3 % slower, 4 % faster at 60 rows an expert; a lane's own 32-byte stores instead
+// of lines by way of LDS: 391 for 362 with the quantizers, gradients 546 for 378.
 // A wave whose 128 rows lie behind the tile's end multiplies nothing, and a last unit that exists in part is multiplied by steps of 64.
 #define EX_BAND 8
 enum { EX_PRODUCT = 0, EX_WGRAD = 1 };
