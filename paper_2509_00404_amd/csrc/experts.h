@@ -9,28 +9,38 @@ namespace {
 
 // Where unit u lies when every expert's slots are cut into units of `size` (the last of an expert may be short, an expert without slots has
 // none): the expert, its slots, and the unit's number among its own.  expert = -1 behind the last unit; `total` = units in all.  Every
-// wave looks for itself, its lanes holding neighbouring experts; offsets are held to 0 <= o <= S, whatever the memory says.
+// wave looks for itself, its lanes holding up to eight neighbouring experts; offsets are held to 0 <= o <= S, whatever the memory says.
 struct SlotUnit {
     int expert, local, total;
     int64_t begin, end;                   // the expert's slots
-    int64_t padded;                       // slots of the experts before it, each padded to whole units
+    int64_t padded;                       // slots of the experts before it, each padded to whole SLOT_ALIGN
 };
 __device__ __forceinline__ int64_t held(int32_t o, int64_t S) { return o < 0 ? 0 : o > S ? S : o; }
 __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offsets, int E, int64_t S, int size, int64_t u) {
-    const int lane = (int)threadIdx.x & 63, q = (E + 63) >> 6;
-    int mine = 0;
-    for (int i = 0; i < q; ++i) {
-        const int e = lane * q + i;
-        if (e < E) {
-            const int64_t n = held(offsets[e + 1], S) - held(offsets[e], S);
-            if (n > 0) mine += (int)((n + size - 1) / size);
+    constexpr int Q = EXPERTS_MAX / 64;
+    const int lane = (int)threadIdx.x & 63, q = (E + 63) >> 6, e0 = lane * q;
+    int32_t o[Q + 1];
+#pragma unroll
+    for (int i = 0; i <= Q; ++i) {
+        const int e = e0 + (i < q ? i : q);
+        o[i] = offsets[e < E ? e : E];
+    }
+    int mine = 0, pads = 0;
+#pragma unroll
+    for (int i = 0; i <= Q; ++i) o[i] = (int32_t)held(o[i], S);
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const int32_t n = o[i + 1] - o[i];
+        if (n > 0) {
+            mine += (n + size - 1) / size;
+            pads += (n + SLOT_ALIGN - 1) / SLOT_ALIGN;
         }
     }
-    int upto = mine;
+    int upto = mine, pads_upto = pads;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
+        const int a = __shfl_up(upto, d), b = __shfl_up(pads_upto, d);
+        if (lane >= d) { upto += a; pads_upto += b; }
     }
     SlotUnit r;
     r.total = __builtin_amdgcn_readlane(upto, 63);
@@ -38,25 +48,26 @@ __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offset
     r.local = 0;
     r.begin = r.end = r.padded = 0;
     if (u >= r.total) return r;
-    const uint64_t behind = __ballot(upto > u);
-    const int at = __ffsll((unsigned long long)behind) - 1;
-    int64_t before = __builtin_amdgcn_readlane(upto - mine, at);
-    for (int i = 0; i < q; ++i) {
-        const int e = at * q + i;
-        if (e >= E) break;
-        const int64_t b = held(offsets[e], S), n = held(offsets[e + 1], S) - b;
-        if (n <= 0) continue;
-        const int64_t units = (n + size - 1) / size;
-        if (u < before + units) {
-            r.expert = e;
-            r.local = (int)(u - before);
-            r.begin = b;
-            r.end = b + n;
-            r.padded = before * size;
-            return r;
-        }
+    // every lane looks through its own experts, and the one that has the unit says where
+    int before = upto - mine, pads_before = pads_upto - pads, expert = 0, local = 0, begin = 0, end = 0, padded = 0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const int32_t n = o[i + 1] - o[i], units = n > 0 ? (n + size - 1) / size : 0;
+        const bool here = u >= before && u < before + units;
+        expert = here ? e0 + i : expert;
+        local = here ? (int)(u - before) : local;
+        begin = here ? o[i] : begin;
+        end = here ? o[i + 1] : end;
+        padded = here ? pads_before : padded;
         before += units;
+        pads_before += n > 0 ? (n + SLOT_ALIGN - 1) / SLOT_ALIGN : 0;
     }
+    const int at = __ffsll((unsigned long long)__ballot(upto > u)) - 1;
+    r.expert = __builtin_amdgcn_readlane(expert, at);
+    r.local = __builtin_amdgcn_readlane(local, at);
+    r.begin = __builtin_amdgcn_readlane(begin, at);
+    r.end = __builtin_amdgcn_readlane(end, at);
+    r.padded = (int64_t)__builtin_amdgcn_readlane(padded, at) * SLOT_ALIGN;
     return r;
 }
 // units of `size` that S slots can fall into

@@ -17,27 +17,29 @@ namespace {
 // neighbouring columns, all of them in flight together; a workgroup's 8 waves have 256 rows of 128 columns, which leave by way of LDS as
 // whole lines.  With a plan the segments are the experts' slots, padded with zeros to a multiple of 64, in rows of whole units and with
 // scales in units, and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows` rows.
+// FLAT (a plan's segments): a workgroup has 64 rows of 512 columns instead, and its lanes store by themselves; for few slots an expert, whose
+// result has no whole lines, and of whose 256 rows most would not exist.
 // What bounds it: memory.  32768 x 4096 gathered rows, 339 MB to be moved, take 55 us, x 2048 by slot (170 MB) 36.  (Loads in branches, 16
 // bytes of a column stored at a time and scales byte by byte: 140 and 103.)
 #define QT_ROW 144                            // a column's 8 blocks of 16 bytes, and 16 that spread the columns over the banks
-template <typename T>
+template <typename T, bool FLAT>
 __global__ void __launch_bounds__(512)
 k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols, const int32_t* __restrict__ offsets, int E, int64_t S,
                 const int32_t* __restrict__ token, int64_t rows, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-    __shared__ __attribute__((aligned(16))) uint8_t s_codes[128 * QT_ROW];
-    __shared__ __attribute__((aligned(16))) uint8_t s_scales[128 * 8];
+    __shared__ __attribute__((aligned(16))) uint8_t s_codes[FLAT ? 16 : 128 * QT_ROW];
+    __shared__ __attribute__((aligned(16))) uint8_t s_scales[FLAT ? 8 : 128 * 8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t unit = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
     int64_t begin, count, stride, written, base, first;   // the segment's rows, the length of its result's rows and what is written of them, its place; the unit's first row
-    if (offsets) {
-        const SlotUnit u = find_unit(offsets, E, S, SLOT_ALIGN, unit);
+    if (FLAT || offsets) {
+        const SlotUnit u = find_unit(offsets, E, S, FLAT ? 64 : SLOT_ALIGN, unit);
         if (u.expert < 0) return;
         begin = u.begin;
         count = u.end - u.begin;
         stride = (count + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
         written = (count + 63) / 64 * 64;
         base = u.padded * cols;
-        first = (int64_t)u.local * SLOT_ALIGN;
+        first = (int64_t)u.local * (FLAT ? 64 : SLOT_ALIGN);
     } else {
         const int64_t per = (rows + SLOT_ALIGN - 1) / SLOT_ALIGN, g = unit / per;
         begin = g * rows;
@@ -45,7 +47,9 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
         base = begin * cols;
         first = (unit - g * per) * SLOT_ALIGN;
     }
-    const int64_t col0 = (int64_t)blockIdx.x * 128, col = col0 + 2 * lane, from = first + 32 * wave;
+    const int64_t col0 = FLAT ? (int64_t)blockIdx.x * 512 + 128 * (wave >> 1) : (int64_t)blockIdx.x * 128, col = col0 + 2 * lane;
+    const int64_t from = first + 32 * (FLAT ? wave & 1 : wave);
+    if (FLAT && col0 >= cols) return;
     if (from < written) {
         const int left = (int)(count - from < 32 ? count - from : 32);        // may be 0 or less: zeros
         int64_t r = from + (lane & 31);
@@ -83,10 +87,19 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             uint32_t byte;
-            *reinterpret_cast<ew_u4*>(s_codes + (2 * lane + c) * QT_ROW + 16 * wave) = mx_block(v[c], byte);
-            s_scales[(2 * lane + c) * 8 + wave] = (uint8_t)byte;
+            const ew_u4 w = mx_block(v[c], byte);
+            if constexpr (FLAT) {
+                if (col < cols) {
+                    *reinterpret_cast<ew_u4*>(codes + (base + (col + c) * stride + from) / 2) = w;
+                    scales[base / 32 + (from / 256 * cols + col + c) * 8 + from % 256 / 32] = (uint8_t)byte;
+                }
+            } else {
+                *reinterpret_cast<ew_u4*>(s_codes + (2 * lane + c) * QT_ROW + 16 * wave) = w;
+                s_scales[(2 * lane + c) * 8 + wave] = (uint8_t)byte;
+            }
         }
     }
+    if constexpr (FLAT) return;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -369,16 +382,17 @@ int experts_plan_status(const metis_expert_plan* p) {
 int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_plan* p, bool gather, int64_t rows, uint8_t* codes,
                          uint8_t* scales) {
     const int64_t S = p ? p->tokens * p->k : 0;
-    const int64_t units = p ? most_units(S, p->experts, SLOT_ALIGN) : A->rows / rows * ceil_div64(rows, SLOT_ALIGN);
+    const bool flat = p && S < 128 * (int64_t)p->experts;
+    const int64_t units = p ? most_units(S, p->experts, flat ? 64 : SLOT_ALIGN) : A->rows / rows * ceil_div64(rows, SLOT_ALIGN);
     const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
-    const dim3 grid((unsigned)ceil_div64(A->cols, 128), (unsigned)gy, (unsigned)gz);
+    const dim3 grid((unsigned)ceil_div64(A->cols, flat ? 512 : 128), (unsigned)gy, (unsigned)gz);
     if (gz > 65535 || A->rows > 0x7FFFFFFF) return METIS_UNSUPPORTED;
     auto launch = [&](auto kern, auto zero) {
         hipLaunchKernelGGL(kern, grid, dim3(512), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->rows, A->cols, p ? p->offsets : nullptr,
                            p ? p->experts : 0, S, gather ? p->token : nullptr, rows, codes, scales);
     };
-    if (A->dtype == METIS_BF16) launch(k_quantize_mx_t<bf16_t>, bf16_t());
-    else launch(k_quantize_mx_t<float>, float());
+    if (A->dtype == METIS_BF16) flat ? launch(k_quantize_mx_t<bf16_t, true>, bf16_t()) : launch(k_quantize_mx_t<bf16_t, false>, bf16_t());
+    else flat ? launch(k_quantize_mx_t<float, true>, float()) : launch(k_quantize_mx_t<float, false>, float());
     METIS_LAUNCH_CHECK();
     return METIS_OK;
 }

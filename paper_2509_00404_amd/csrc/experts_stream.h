@@ -31,11 +31,29 @@ struct ExStream {
     int64_t ascales, bscales;             // from one unit's scales to the next one's
     int E, tiles_m, tiles_n;              // gradient: tiles_m along N, tiles_n along K; product: tiles_n along N
 };
-// Behind the two buffers a wave has room to turn 16 rows of its outputs into whole lines, and every expert has two numbers.
+// Behind the two buffers a wave has room to turn 16 rows of its outputs into whole lines, every expert has two numbers, and the workgroup
+// its next tiles.
 #define EX_STAGE_ROW 144                                 // 64 bf16 and 16 bytes that spread the rows over the banks
 #define EX_STAGE (16 * EX_STAGE_ROW)
-#define EX_LDS (MXS_LDS + 8 * EX_STAGE + 2 * 4 * (EXPERTS_MAX + 1))
+#define EX_HALF 48                                       // tiles that are looked up at a time
+#define EX_LIST (MXS_LDS + 8 * EX_STAGE + 2 * 4 * (EXPERTS_MAX + 1) + 8)
+#define EX_LDS (EX_LIST + 2 * EX_HALF * 16)
+static_assert(EX_LIST % 16 == 0 && EX_LDS <= 160 * 1024, "fits a CU");
 
+// gs_meet with `stores` younger stores on their way, rounded down to an even number
+__device__ __forceinline__ void ex_meet(int stores) {
+    switch (stores >> 1) {
+        case 8: gs_meet<16>(); break;
+        case 7: gs_meet<14>(); break;
+        case 6: gs_meet<12>(); break;
+        case 5: gs_meet<10>(); break;
+        case 4: gs_meet<8>(); break;
+        case 3: gs_meet<6>(); break;
+        case 2: gs_meet<4>(); break;
+        case 1: gs_meet<2>(); break;
+        default: gs_meet<0>(); break;
+    }
+}
 // zeros to n elements from p
 template <typename OUT>
 __device__ __forceinline__ void ex_clear(OUT* p, int64_t n, bool vec) {
@@ -46,7 +64,7 @@ __device__ __forceinline__ void ex_clear(OUT* p, int64_t n, bool vec) {
 }
 
 // A wave's accumulator tiles (transposed, bf16) to memory: 16 rows of its 64 columns at a time are staged at sm, eight lanes a row.
-// Whole: 16 stores a lane.
+// A store for every eight rows: 16 where all are there.
 __device__ __forceinline__ void ex_store_lines(const float16_t (&acc)[4][2], uint8_t* sm, bf16_t* __restrict__ C, int64_t ldc, int64_t m0, int64_t n0,
                                                int64_t M, int64_t N, bool vec, bool whole, int lane) {
     const int li = lane & 31, half = lane >> 5, unit = lane & 7;
@@ -69,6 +87,7 @@ __device__ __forceinline__ void ex_store_lines(const float16_t (&acc)[4][2], uin
                 const int row = 8 * t + (lane >> 3);
                 const uint8_t* q = sm + row * EX_STAGE_ROW + 16 * unit;
                 const int64_t r = m0 + 32 * i + 16 * h + row, left = N - c;
+                if (!whole && r - (lane >> 3) >= M) continue;             // (for the whole wave)
                 bf16_t* p = C + r * ldc + c;
                 if (whole || (r < M && vec && left >= 8)) {
                     __builtin_nontemporal_store(*reinterpret_cast<const uvec4_t*>(q), reinterpret_cast<uvec4_t*>(p));
@@ -84,16 +103,24 @@ __device__ __forceinline__ void ex_store_lines(const float16_t (&acc)[4][2], uin
 // fp32: a row of 32 is a whole line as it is
 __device__ __forceinline__ void ex_store_plain(const float16_t (&acc)[4][2], float* __restrict__ C, int64_t ldc, int64_t m0, int64_t n0, int64_t M,
                                                int64_t N, bool whole, int lane) {
+    const int64_t c = n0 + (lane & 31), row = 4 * (lane >> 5);
+    const int rows = M - m0 < 128 ? (int)(M - m0) : 128, cols = N - c < 64 ? (int)(N - c) : 64;
+    float* p = C + (m0 + row) * ldc + c;                 // the lane's first; the next of its rows, the fifth one 8 behind the first
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int64_t r = m0 + 32 * i + 4 * (lane >> 5) + 8 * (v >> 2) + (v & 3), c = n0 + 32 * j + (lane & 31);
-                if (whole || (r < M && c < N)) __builtin_nontemporal_store(acc[i][j][v], C + r * ldc + c);
-            }
+        for (int v = 0; v < 16; ++v) {
+            const bool there = whole || 32 * i + (int)row + 8 * (v >> 2) + (v & 3) < rows;
+            if (there && (whole || 0 < cols)) __builtin_nontemporal_store(acc[i][0][v], p);
+            if (there && (whole || 32 < cols)) __builtin_nontemporal_store(acc[i][1][v], p + 32);
+            p += v % 4 == 3 ? 5 * ldc : ldc;
+        }
 }
+
+// a tile: its expert, its first row in the expert and column, and the expert's first slot (product) or slots (gradient)
+struct __attribute__((aligned(16))) ExTile {
+    int expert, m0, n0, at;
+};
 
 template <typename OUT, int MODE>
 __global__ void __launch_bounds__(512, 2)
@@ -157,51 +184,69 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
             ex_clear(C + r * ldc, a.N, vec);
     }
 
-    // tile number -> expert (searched on from e) and place
-    auto tile_of = [&](int tile, int& e, int& m0, int& n0) GS_INLINE {
-        while (tile >= first_of(e + 1)) ++e;
-        const int local = tile - first_of(e);
-        const int down = WGRAD ? a.tiles_m : (count_of(e) + 255) >> 8;
-        const int band = local / (EX_BAND * down), r = local - band * EX_BAND * down;
-        const int left = a.tiles_n - band * EX_BAND, w = left < EX_BAND ? left : EX_BAND;
-        const int tm = r / w;
-        m0 = 256 * tm;
-        n0 = 256 * (band * EX_BAND + r - tm * w);
-    };
+    // ---- this workgroup's tiles.  A tile's place takes a search and two divisions, some thousand cycles one after the other: 48 lanes do them
+    // for 48 tiles at once, two halves of a ring ahead (before, every wave for every tile: 1664 tiles of one unit 66 us without transfers or
+    // stores, so EX_AFTER).
     const int hop = (int)gridDim.x, xcds = (hop & 7) == 0 ? 8 : 1;
     const int start = ((int)blockIdx.x % xcds) * (hop / xcds) + (int)blockIdx.x / xcds;
     if (start >= total) return;
+    const int tiles = (total - start + hop - 1) / hop;
+    ExTile* const s_list = reinterpret_cast<ExTile*>(lds + EX_LIST);
+    auto fill = [&](int half_no) GS_INLINE {
+        const int i = (int)threadIdx.x, t = half_no * EX_HALF + i;
+        if (i >= EX_HALF || t >= tiles) return;
+        const int tile = start + t * hop, per = a.tiles_m * a.tiles_n;
+        auto first = [&](int e) GS_INLINE { return WGRAD ? (s_first[e] & 1023) * per : s_first[e]; };
+        int lo = 0, hi = a.E;                            // first(lo) <= tile < first(hi)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first(mid) <= tile) lo = mid;
+            else hi = mid;
+        }
+        const int local = tile - first(lo), count = s_begin[lo + 1] - s_begin[lo], down = WGRAD ? a.tiles_m : (count + 255) >> 8;
+        const int band = local / (EX_BAND * down), r = local - band * EX_BAND * down;
+        const int left = a.tiles_n - band * EX_BAND, w = left < EX_BAND ? left : EX_BAND, tm = r / w;
+        s_list[t % (2 * EX_HALF)] = {lo, 256 * tm, 256 * (band * EX_BAND + r - tm * w), WGRAD ? count : s_begin[lo]};
+    };
+    fill(0);
+    fill(1);
+    __syncthreads();
+    auto tile_at = [&](int t) GS_INLINE {
+        const uvec4_t v = *reinterpret_cast<const uvec4_t*>(s_list + t % (2 * EX_HALF));
+        return ExTile{__builtin_amdgcn_readfirstlane((int)v[0]), __builtin_amdgcn_readfirstlane((int)v[1]),
+                      __builtin_amdgcn_readfirstlane((int)v[2]), __builtin_amdgcn_readfirstlane((int)v[3])};
+    };
 
     // ---- transfers
     const uint8_t *qa, *qb, *qsa, *qsb;                  // the next unit's codes, and this wave's part of its scales
-    int lpos = start, lcnt = 0, lblk = 8;                // tile being fetched, units left of it, blocks of 32 of the unit that B has
+    int ltile = 0, lcnt = 0, lblk = 8;                   // tile being fetched, units left of it, blocks of 32 of the unit that B has
     uint32_t va[4], vb[4];                               // the lane's offsets
     int32_t row_next[4];                                 // rows of A of the tile to be entered next, by this lane's place
-    int nexp = 0, nm0 = 0, nn0 = 0;                      // that tile
-    auto look_ahead = [&](int pos) GS_INLINE {
-        tile_of(pos < total ? pos : total - 1, nexp, nm0, nn0);
+    ExTile next;                                         // that tile
+    auto look_ahead = [&](int t) GS_INLINE {
+        next = tile_at(t < tiles ? t : tiles - 1);       // (past the end: the last one again, unused)
         if constexpr (!WGRAD) {
             const int l = gs_fresh_lane();
-            const int32_t b = begin_of(nexp) + nm0, t = count_of(nexp) - nm0 - 1;
+            const int32_t b = next.at + next.m0, last = begin_of(next.expert + 1) - b - 1;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int row = 32 * wave + 8 * v + (l >> 3);
-                row_next[v] = b + (row < t ? row : t);
+                row_next[v] = b + (row < last ? row : last);
                 if (a.token) row_next[v] = a.token[row_next[v]];
             }
         }
     };
     auto enter = [&]() GS_INLINE {
-        const int e = nexp, m0 = nm0, n0 = nn0;
+        const int e = next.expert, m0 = next.m0, n0 = next.n0;
         const int l = gs_fresh_lane();
         const uint32_t seg0 = (uint32_t)((l & 7) ^ (l >> 4)) * 16;
         const int64_t brows = WGRAD ? a.K : a.N;
         const int tb = (int)(brows - n0 < 256 ? brows - n0 : 256) - 1;
         if constexpr (WGRAD) {
-            const int len = (count_of(e) + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
+            const int units = (next.at + SLOT_ALIGN - 1) / SLOT_ALIGN, len = units * SLOT_ALIGN;
             const int64_t at = (int64_t)(table(s_first, e) >> 10) * SLOT_ALIGN;
             const int64_t pa = at * a.N + (int64_t)m0 * len, pb = at * a.K + (int64_t)n0 * len;
-            lcnt = (count_of(e) + 255) >> 8;
+            lcnt = units;
             qa = a.A.codes + pa / 2;
             qsa = a.A.scales + at * a.N / 32 + 8 * (m0 + 32 * wave);
             qb = a.B.codes + pb / 2;
@@ -220,7 +265,7 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
             const uint32_t cs = (uint32_t)(a.K / 2);
             lcnt = (int)((a.K + 255) >> 8);
             qa = a.A.codes;
-            qsa = a.A.scales + 8 * (int64_t)(begin_of(e) + m0 + 32 * wave);
+            qsa = a.A.scales + 8 * (int64_t)(next.at + m0 + 32 * wave);
             qb = a.B.codes + w0 * cs;
             qsb = a.B.scales + 8 * (w0 + 32 * wave);
 #pragma unroll
@@ -232,13 +277,10 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
                 vb[v] = (uint32_t)(row < tb ? row : tb) * cs + seg;
             }
         }
-        look_ahead(lpos + hop);
+        look_ahead(++ltile);
     };
     auto advance = [&]() GS_INLINE {                     // before the first transfer of a unit
-        if (lcnt == 0) {
-            lpos += hop;
-            enter();
-        }
+        if (lcnt == 0) enter();
         --lcnt;
         // B's codes end with the contraction: what lies behind is some other row's, or nobody's.  A's rows are padded, the gradient's
         // operands have room behind them.
@@ -274,7 +316,7 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         }
     };
 
-    look_ahead(start);
+    look_ahead(0);
     enter();
     advance();
     gs_for<MXS_DMA>([&](auto k) GS_INLINE { issue(0, k); });
@@ -307,9 +349,9 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
     mxs_settle_scales(sx);
 
     uint32_t b0 = 0;                                     // buffer of the unit in work
-    // first: the accumulators start here; steps: of 64 elements, that this wave multiplies.  kept: the last tile's stores, younger than the
-    // transfers that the unit waits for, are 16 and may stay on their way.
-    auto unit = [&](auto first_, int steps, bool kept) GS_INLINE {
+    // first: the accumulators start here; steps: of 64 elements, that this wave multiplies.  kept: the last tile's stores, which are younger than the
+    // transfers that the unit waits for and may stay on their way.
+    auto unit = [&](auto first_, int steps, int kept) GS_INLINE {
         constexpr bool first = decltype(first_)::value;
         const uint32_t b1 = MXS_UNIT - b0;
         gs_for<4>([&](auto sc_) GS_INLINE {
@@ -321,7 +363,7 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
                 if constexpr (s == 3) {
                     // the next unit is there, and this one's buffer has been read by all
                     if constexpr (m == 1) {
-                        if (first && kept) gs_meet<16>();
+                        if constexpr (first) ex_meet(kept);
                         else gs_meet<0>();
                         advance();
                     }
@@ -347,28 +389,30 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         mxs_settle_scales(sx);
         b0 = b1;
     };
-    int exp = 0;
-    bool kept = false;
-    for (int pos = start; pos < total; pos += hop) {
-        int m0, n0;
-        tile_of(pos, exp, m0, n0);
-        const int64_t base = WGRAD ? (int64_t)exp * a.N : (int64_t)begin_of(exp), rows = WGRAD ? a.N : (int64_t)count_of(exp);
-        const int64_t con = WGRAD ? (int64_t)count_of(exp) : a.K;
+    int kept = 0;
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) {
+        // the half of the ring that the tiles before have left, which no wave reads any more
+        if (t > EX_HALF && t % EX_HALF == 1) fill(t / EX_HALF + 1);
+        const ExTile now = tile_at(t);
+        const int64_t base = WGRAD ? (int64_t)now.expert * a.N : (int64_t)now.at;
+        const int64_t rows = WGRAD ? a.N : (int64_t)(begin_of(now.expert + 1) - now.at), con = WGRAD ? (int64_t)now.at : a.K;
         const int niter = (int)((con + 255) >> 8);
-        const bool busy = m0 + 128 * wa < rows;
+        const int64_t r = now.m0 + 128 * wa, c = now.n0 + 64 * wb, N = WGRAD ? a.K : a.N;
+        const bool busy = r < rows && c < N;
         const int whole = busy ? 4 : 0, rest = busy ? (int)((con - 256 * (int64_t)(niter - 1) + 63) >> 6) : 0;
         unit(std::true_type{}, niter == 1 ? rest : whole, kept);
 #pragma unroll 1
-        for (int u = 1; u < niter; ++u) unit(std::false_type{}, u == niter - 1 ? rest : whole, false);
+        for (int u = 1; u < niter; ++u) unit(std::false_type{}, u == niter - 1 ? rest : whole, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) mxs_settle(acc[i]);
-        kept = false;
+        kept = 0;
         if (busy) {
-            const int64_t N = WGRAD ? a.K : a.N, r = m0 + 128 * wa, c = n0 + 64 * wb;
             const bool inside = r + 128 <= rows && c + 64 <= N;
             if constexpr (LINES) {
-                kept = inside && vec;
-                ex_store_lines(acc, s_stage + wave * EX_STAGE, C + base * ldc, ldc, r, c, rows, N, vec, kept, gs_fresh_lane());
+                ex_store_lines(acc, s_stage + wave * EX_STAGE, C + base * ldc, ldc, r, c, rows, N, vec, inside && vec, gs_fresh_lane());
+                // one store for every eight rows there are, where no row's end is stored piece by piece
+                if (vec && N % 8 == 0) kept = inside ? 16 : rows - r < 128 ? (int)((rows - r + 7) >> 3) : 16;
             } else {
                 ex_store_plain(acc, C + base * ldc, ldc, r, c, rows, N, inside, gs_fresh_lane());
             }
