@@ -5,6 +5,7 @@
 
 typedef int ex_i8 __attribute__((ext_vector_type(8)));
 typedef float ex_f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t ex_u2_any __attribute__((ext_vector_type(2), aligned(1)));
 
 namespace {
 
@@ -133,7 +134,6 @@ struct MxRows {
     const uint8_t* codes;
     const uint8_t* scales;
 };
-typedef uint32_t ex_u2_any __attribute__((ext_vector_type(2), aligned(1)));
 // Blocks r + 8 h .. r + 8 h + 7 of a row (h = lane / 32), r the run's first.  Of the last run, where it is short, what lies behind the row's
 // nblk blocks is the last block once more under some scale, and zeros where ZERO: one operand's zeros are enough.
 template <bool ZERO>
@@ -329,17 +329,19 @@ struct WeightScales {
 __device__ __forceinline__ void lay_scales(const WeightScales& w, int64_t block) {
     const int64_t row = block * 64 + (threadIdx.x & 63);
     if (row >= w.rows) return;
+    const uint8_t* p = w.from + row * w.have;
+    const int64_t left = (w.rows - row) * w.have;        // bytes that may be read from p on
     for (int u = threadIdx.x >> 6; u < w.units; u += 4) {
-        ew_u2 v;
-        const uint8_t* p = w.from + row * w.have + 8 * u;
-        if (w.have % 8 == 0) {
-            v = *reinterpret_cast<const ew_u2*>(p);
+        const int n = w.have - 8 * u;                    // of the row's in this unit, 8 or more: all
+        uint64_t v = 0;
+        if (8 * u + 8 <= left) {
+            const ex_u2_any x = *reinterpret_cast<const ex_u2_any*>(p + 8 * u);
+            v = (uint64_t)x[1] << 32 | x[0];
         } else {
-            v = ew_u2{0u, 0u};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i >> 2] |= (8 * u + i < w.have ? (uint32_t)p[i] : 127u) << (8 * (i & 3));
+            for (int i = 0; i < n; ++i) v |= (uint64_t)p[8 * u + i] << (8 * i);
         }
-        *reinterpret_cast<ew_u2*>(w.to + (u * w.rows + row) * 8) = v;
+        if (n < 8) v = (v & ~(~0ull << (8 * n))) | 0x7F7F7F7F7F7F7F7Full << (8 * n);
+        *reinterpret_cast<uint64_t*>(w.to + (u * w.rows + row) * 8) = v;
     }
 }
 template <typename T, bool UNITS>
@@ -439,13 +441,17 @@ int launch_quantize_rows(hipStream_t s, const metis_mat* A, int64_t Kp, uint8_t*
 template <typename OUT, int MODE>
 int launch_stream(hipStream_t s, const ExStream& a, int64_t tiles, metis_mat* C) {
     const int cus = device_cu_count();
-    static LdsLimitCache lds_set;
-    auto kern = k_experts_stream<OUT, MODE>;
-    if (cus < 1 || !ensure_dyn_lds((const void*)kern, EX_LDS, lds_set)) return METIS_HIP_ERROR;
-    const bool vec = mat_aligned16(C);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles < cus ? tiles : cus)), dim3(512), EX_LDS, s, a, (OUT*)C->ptr, C->ld, vec);
-    METIS_LAUNCH_CHECK();
-    return METIS_OK;
+    if (cus < 1) return METIS_HIP_ERROR;
+    auto launch = [&](auto kern, LdsLimitCache& lds_set) -> int {
+        if (!ensure_dyn_lds((const void*)kern, EX_LDS, lds_set)) return METIS_HIP_ERROR;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(tiles < cus ? tiles : cus)), dim3(512), EX_LDS, s, a, (OUT*)C->ptr, C->ld, mat_aligned16(C));
+        METIS_LAUNCH_CHECK();
+        return METIS_OK;
+    };
+    static LdsLimitCache lds_set[2];
+    if constexpr (MODE == EX_WGRAD)
+        if ((uintptr_t)C->ptr % 128 || C->ld * sizeof(OUT) % 128) return launch(k_experts_stream<OUT, MODE, false>, lds_set[0]);
+    return launch(k_experts_stream<OUT, MODE, true>, lds_set[1]);
 }
 
 }  // namespace

@@ -10,7 +10,9 @@
 // A workgroup works its way through the tiles, gridDim.x apart.  Neighbouring tiles are of one expert, up to EX_BAND of its column tiles wide,
 // and every XCD works on a run of them: they share panels of both operands in its L2.
 // Outputs are not read again here and go past the caches: kept in L2 they drive out the operands' panels (gradients of 8192 tokens' four
-// experts, 2048 x 4096 each, 626 us with the quantizers, so 461; 16384 tokens' product 409, 401).
+// experts, 2048 x 4096 each, 529 us with the quantizers, so 378; 16384 tokens' product 409, 401).  Gradients whose rows do not start on
+// cache lines stay in L2, where the parts of a line meet (1384 x 2456 each, 403 tokens' five of 64 experts 152, past it 246; products,
+// which write less, are 3 % better past it all the same).
 // What bounds it: 16384 tokens' four experts, 2048 x 4096 each, 320 us (1.1 PFLOP, 3.4 PFLOP/s; an eighth of the tiles' rows is short tiles').
 // Without its transfers it takes 250, without its matrix instructions 250, without its stores 285: LDS takes a unit's 192 KB of
 // fragments and 68 KB of transfers while the matrix pipe has 2048 cycles of work.  Gradients of 8192 tokens' (1.07 GB out) 285 to 320, without
@@ -65,6 +67,7 @@ __device__ __forceinline__ void ex_clear(OUT* p, int64_t n, bool vec) {
 
 // A wave's accumulator tiles (transposed, bf16) to memory: 16 rows of its 64 columns at a time are staged at sm, eight lanes a row.
 // A store for every eight rows: 16 where all are there.
+template <bool PAST>
 __device__ __forceinline__ void ex_store_lines(const float16_t (&acc)[4][2], uint8_t* sm, bf16_t* __restrict__ C, int64_t ldc, int64_t m0, int64_t n0,
                                                int64_t M, int64_t N, bool vec, bool whole, int lane) {
     const int li = lane & 31, half = lane >> 5, unit = lane & 7;
@@ -90,7 +93,9 @@ __device__ __forceinline__ void ex_store_lines(const float16_t (&acc)[4][2], uin
                 if (!whole && r - (lane >> 3) >= M) continue;             // (for the whole wave)
                 bf16_t* p = C + r * ldc + c;
                 if (whole || (r < M && vec && left >= 8)) {
-                    __builtin_nontemporal_store(*reinterpret_cast<const uvec4_t*>(q), reinterpret_cast<uvec4_t*>(p));
+                    const uvec4_t w = *reinterpret_cast<const uvec4_t*>(q);
+                    if constexpr (PAST) __builtin_nontemporal_store(w, reinterpret_cast<uvec4_t*>(p));
+                    else *reinterpret_cast<uvec4_t*>(p) = w;
                 } else if (r < M) {
 #pragma unroll 1
                     for (int e = 0; e < 8 && e < left; ++e) p[e] = reinterpret_cast<const bf16_t*>(q)[e];
@@ -101,6 +106,7 @@ __device__ __forceinline__ void ex_store_lines(const float16_t (&acc)[4][2], uin
 }
 
 // fp32: a row of 32 is a whole line as it is
+template <bool PAST>
 __device__ __forceinline__ void ex_store_plain(const float16_t (&acc)[4][2], float* __restrict__ C, int64_t ldc, int64_t m0, int64_t n0, int64_t M,
                                                int64_t N, bool whole, int lane) {
     const int64_t c = n0 + (lane & 31), row = 4 * (lane >> 5);
@@ -111,8 +117,13 @@ __device__ __forceinline__ void ex_store_plain(const float16_t (&acc)[4][2], flo
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const bool there = whole || 32 * i + (int)row + 8 * (v >> 2) + (v & 3) < rows;
-            if (there && (whole || 0 < cols)) __builtin_nontemporal_store(acc[i][0][v], p);
-            if (there && (whole || 32 < cols)) __builtin_nontemporal_store(acc[i][1][v], p + 32);
+            if constexpr (PAST) {
+                if (there && (whole || 0 < cols)) __builtin_nontemporal_store(acc[i][0][v], p);
+                if (there && (whole || 32 < cols)) __builtin_nontemporal_store(acc[i][1][v], p + 32);
+            } else {
+                if (there && (whole || 0 < cols)) p[0] = acc[i][0][v];
+                if (there && (whole || 32 < cols)) p[32] = acc[i][1][v];
+            }
             p += v % 4 == 3 ? 5 * ldc : ldc;
         }
 }
@@ -122,7 +133,8 @@ struct __attribute__((aligned(16))) ExTile {
     int expert, m0, n0, at;
 };
 
-template <typename OUT, int MODE>
+// PAST: outputs go past the caches
+template <typename OUT, int MODE, bool PAST>
 __global__ void __launch_bounds__(512, 2)
 k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
     constexpr bool LINES = sizeof(OUT) == 2;             // outputs by way of LDS, accumulator tiles transposed
@@ -410,11 +422,11 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         if (busy) {
             const bool inside = r + 128 <= rows && c + 64 <= N;
             if constexpr (LINES) {
-                ex_store_lines(acc, s_stage + wave * EX_STAGE, C + base * ldc, ldc, r, c, rows, N, vec, inside && vec, gs_fresh_lane());
+                ex_store_lines<PAST>(acc, s_stage + wave * EX_STAGE, C + base * ldc, ldc, r, c, rows, N, vec, inside && vec, gs_fresh_lane());
                 // one store for every eight rows there are, where no row's end is stored piece by piece
                 if (vec && N % 8 == 0) kept = inside ? 16 : rows - r < 128 ? (int)((rows - r + 7) >> 3) : 16;
             } else {
-                ex_store_plain(acc, C + base * ldc, ldc, r, c, rows, N, inside, gs_fresh_lane());
+                ex_store_plain<PAST>(acc, C + base * ldc, ldc, r, c, rows, N, inside, gs_fresh_lane());
             }
         }
     }
