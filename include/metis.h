@@ -488,7 +488,7 @@ int metis_experts_wgrad(void* stream, const metis_mat* G, const metis_mat* X, co
  * y [tokens, D] = sum over j of weights[t, j] * rows[slot[t, j], :], in fp32, the choices in their order, rounded once.  Choices without a
  * slot add nothing.  weights: device fp32 [tokens, k], or null for ones (the input gradient of gathered rows).  rows [tokens * k, D]
  * and y: bf16 or fp32 each; any D and row strides (whole 16-byte units where both allow them).  plan->slot is read alone.
- * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (k > 16, or more than 2^25 columns or units).
+ * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (k > 16, or more than 2^28 columns).
  */
 int metis_combine(void* stream, const metis_mat* rows, const metis_expert_plan* plan, const float* weights, metis_mat* y);
 

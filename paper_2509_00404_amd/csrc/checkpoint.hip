@@ -59,7 +59,7 @@ k_quantize_mx8(const T* __restrict__ A, int64_t ld, uint64_t total, FastDiv unit
     if (n >= total) return;                                               // total is a multiple of 4: whole blocks leave
     const uint64_t row = div_by(units, n), c = n - row * units.d;
     float v[8];
-    load_row<8>(A + row * ld + 8 * c, v);
+    load_row(A + row * ld + 8 * c, v);
     uint32_t byte;
     const ew_u2 w = mx8_encode(v, byte);
     *reinterpret_cast<ew_u2*>(codes + 8 * n) = w;
@@ -75,7 +75,7 @@ k_dequantize_mx8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ 
     const uint64_t row = div_by(units, n), c = n - row * units.d;
     float v[8];
     mx8_decode(*reinterpret_cast<const ew_u2*>(codes + 8 * n), scales[n >> 2], v);
-    store_row<8>(A + row * ld + 8 * c, v);
+    store_row(A + row * ld + 8 * c, v);
 }
 
 // sigmoid: for bf16 results the hardware's exponential and reciprocal, one unit in the last place each, as against a rounding to 8 bits
@@ -93,11 +93,11 @@ k_swiglu(const T* __restrict__ gu, int64_t ldg, uint64_t total, FastDiv units, T
     if (n >= total) return;
     const uint64_t row = div_by(units, n), c = n - row * units.d, F = 8ull * units.d;
     float g[8], u[8], a[8];
-    load_row<8>(gu + row * ldg + 8 * c, g);
-    load_row<8>(gu + row * ldg + F + 8 * c, u);
+    load_row(gu + row * ldg + 8 * c, g);
+    load_row(gu + row * ldg + F + 8 * c, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = g[i] * gate<T>(g[i]) * u[i];
-    store_row<8>(act + row * lda + 8 * c, a);
+    store_row(act + row * lda + 8 * c, a);
     if constexpr (SAVE) {
         uint32_t bg, bu;
         const ew_u2 wg = mx8_encode(g, bg), wu = mx8_encode(u, bu);
@@ -122,7 +122,7 @@ k_swiglu_grads(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ sc
     const uint8_t* p = codes + row * 2 * F + 8 * c;
     const uint8_t* q = scales + row * (F / 16) + c / 4;
     float g[8], u[8], d[8], a[8];
-    load_row<8>(dact + row * ldd + 8 * c, d);
+    load_row(dact + row * ldd + 8 * c, d);
     mx8_decode(*reinterpret_cast<const ew_u2*>(p), q[0], g);
     mx8_decode(*reinterpret_cast<const ew_u2*>(p + F), q[F / 32], u);
 #pragma unroll
@@ -132,9 +132,9 @@ k_swiglu_grads(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ sc
         g[i] = d[i] * u[i] * (s * (1.0f + g[i] * (1.0f - s)));
         u[i] = d[i] * gs;
     }
-    store_row<8>(dgu + row * ldg + 8 * c, g);
-    store_row<8>(dgu + row * ldg + F + 8 * c, u);
-    if (act) store_row<8>(act + row * lda + 8 * c, a);
+    store_row(dgu + row * ldg + 8 * c, g);
+    store_row(dgu + row * ldg + F + 8 * c, u);
+    if (act) store_row(act + row * lda + 8 * c, a);
 }
 
 bool mx8_ok(const metis_mx8* q) { return q && q->codes && q->scales && q->rows >= 1 && q->cols >= 32 && q->cols % 32 == 0; }

@@ -6,33 +6,33 @@
 
 namespace {
 
-// A lane per W columns of a token, its choices' rows in flight together.  Memory: 16384 tokens' four rows of 4096 bf16 (672 MB) 126 us, 5.3 TB/s.
-template <typename T, typename O, int W>
+// A lane per eight columns of a token, its choices' rows in flight together.  ANY: rows of any length and alignment.  Memory: 16384 tokens' four
+// rows of 4096 bf16 (672 MB) 126 us, 5.3 TB/s; 3668 tokens' seven rows of 1388 22 us (82 MB; a column a lane 49).
+template <typename T, typename O, bool ANY>
 __global__ void __launch_bounds__(256)
-k_combine(const T* __restrict__ rows, int64_t ldr, int64_t S, const int32_t* __restrict__ slot, const float* __restrict__ weights, int k,
-          O* __restrict__ y, int64_t ldy, uint64_t total, FastDiv units) {
+k_combine(const T* __restrict__ rows, int64_t ldr, int64_t S, int64_t cols, const int32_t* __restrict__ slot, const float* __restrict__ weights,
+          int k, O* __restrict__ y, int64_t ldy, uint64_t total, FastDiv units) {
     const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
     if (n >= total) return;
-    const uint64_t t = div_by(units, n), c = (n - t * units.d) * W;
-    float acc[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) acc[i] = 0.0f;
+    const uint64_t t = div_by(units, n), c = 8 * (n - t * units.d);
+    const int64_t left = cols - (int64_t)c;
+    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
     for (int j = 0; j < k; ++j) {
         const int32_t s = slot[t * k + j];
         if ((uint32_t)s >= (uint64_t)S) continue;
         const float w = weights ? weights[t * k + j] : 1.0f;
-        float v[W];
-        load_row<W>(rows + s * ldr + c, v);
+        float v[8];
+        load_part<T, ANY>(rows + s * ldr + c, left, v);
 #pragma unroll
-        for (int i = 0; i < W; ++i) acc[i] = fmaf(w, v[i], acc[i]);
+        for (int i = 0; i < 8; ++i) acc[i] = fmaf(w, v[i], acc[i]);
     }
-    store_row<W>(y + t * ldy + c, acc);
+    store_part<O, ANY>(y + t * ldy + c, left, acc);
 }
 
 // A workgroup per token: its gradient row is read once for all its choices.  The products with the rows are added up per lane, then over
 // the wave, then over the waves, always in the same order.  Memory: 8192 tokens' four rows of 4096 bf16 (604 MB) 126 us, 4.8 TB/s.
-template <typename T, typename D, int W, int K>
+template <typename T, typename D, bool ANY, int K>
 __global__ void __launch_bounds__(256)
 k_combine_grads(const D* __restrict__ dy, int64_t ldy, const T* __restrict__ rows, int64_t ldr, int64_t S, int64_t cols,
                 const int32_t* __restrict__ offsets, int E, const int32_t* __restrict__ slot, const float* __restrict__ weights, int k,
@@ -49,20 +49,21 @@ k_combine_grads(const D* __restrict__ dy, int64_t ldy, const T* __restrict__ row
         w[j] = s[j] >= 0 ? weights[t * k + j] : 0.0f;
         dot[j] = 0.0f;
     }
-    for (int64_t c = (int64_t)threadIdx.x * W; c < cols; c += (int64_t)blockDim.x * W) {
-        float d[W];
-        load_row<W>(dy + t * ldy + c, d);
+    for (int64_t c = (int64_t)threadIdx.x * 8; c < cols; c += (int64_t)blockDim.x * 8) {
+        const int64_t left = cols - c;
+        float d[8];
+        load_part<D, ANY>(dy + t * ldy + c, left, d);
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             if (s[j] < 0) continue;
-            float v[W];
-            load_row<W>(rows + s[j] * ldr + c, v);
+            float v[8];
+            load_part<T, ANY>(rows + s[j] * ldr + c, left, v);
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 dot[j] = fmaf(d[i], v[i], dot[j]);
                 v[i] = w[j] * d[i];
             }
-            store_row<W>(drows + s[j] * ldd + c, v);
+            store_part<T, ANY>(drows + s[j] * ldd + c, left, v);
         }
     }
 #pragma unroll
@@ -78,10 +79,10 @@ k_combine_grads(const D* __restrict__ dy, int64_t ldy, const T* __restrict__ row
         dweights[t * k + threadIdx.x] = sum;
     }
     // the slots that serve no choice
-    const float zero[W] = {};
+    const float zero[8] = {};
     const int64_t used = offsets[E] > 0 ? offsets[E] : 0;
     for (int64_t r = used + t; r < S; r += gridDim.x)
-        for (int64_t c = (int64_t)threadIdx.x * W; c < cols; c += (int64_t)blockDim.x * W) store_row<W>(drows + r * ldd + c, zero);
+        for (int64_t c = (int64_t)threadIdx.x * 8; c < cols; c += (int64_t)blockDim.x * 8) store_part<T, ANY>(drows + r * ldd + c, cols - c, zero);
 }
 
 int plan_rows_status(const metis_mat* rows, const metis_expert_plan* p) {
@@ -94,13 +95,13 @@ int plan_rows_status(const metis_mat* rows, const metis_expert_plan* p) {
 
 template <typename T, typename O>
 int launch_combine(hipStream_t s, const metis_mat* rows, const metis_expert_plan* p, const float* weights, metis_mat* y) {
-    const bool vec = rows->cols % 8 == 0 && mat_aligned16(rows) && mat_aligned16(y);
-    const int64_t units = vec ? rows->cols / 8 : rows->cols, total = p->tokens * units;
+    const bool whole = rows->cols % 8 == 0 && mat_aligned16(rows) && mat_aligned16(y);
+    const int64_t units = ceil_div64(rows->cols, 8), total = p->tokens * units;
     const int st = units_status(p->tokens, units);
     if (st != METIS_OK) return st;
-    auto kern = vec ? k_combine<T, O, 8> : k_combine<T, O, 1>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div64(total, 256)), dim3(256), 0, s, (const T*)rows->ptr, rows->ld, rows->rows, p->slot,
-                       weights, p->k, (O*)y->ptr, y->ld, (uint64_t)total, fast_div((uint32_t)units));
+    auto kern = whole ? k_combine<T, O, false> : k_combine<T, O, true>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div64(total, 256)), dim3(256), 0, s, (const T*)rows->ptr, rows->ld, rows->rows, rows->cols,
+                       p->slot, weights, p->k, (O*)y->ptr, y->ld, (uint64_t)total, fast_div((uint32_t)units));
     METIS_LAUNCH_CHECK();
     return METIS_OK;
 }
@@ -108,9 +109,9 @@ int launch_combine(hipStream_t s, const metis_mat* rows, const metis_expert_plan
 template <typename T, typename D, int K>
 int launch_combine_grads(hipStream_t s, const metis_mat* dy, const metis_mat* rows, const metis_expert_plan* p, const float* weights,
                          metis_mat* drows, float* dweights) {
-    const bool vec = rows->cols % 8 == 0 && mat_aligned16(rows) && mat_aligned16(drows) && mat_aligned16(dy);
-    const int64_t units = vec ? rows->cols / 8 : rows->cols;
-    auto kern = vec ? k_combine_grads<T, D, 8, K> : k_combine_grads<T, D, 1, K>;
+    const bool whole = rows->cols % 8 == 0 && mat_aligned16(rows) && mat_aligned16(drows) && mat_aligned16(dy);
+    const int64_t units = ceil_div64(rows->cols, 8);
+    auto kern = whole ? k_combine_grads<T, D, false, K> : k_combine_grads<T, D, true, K>;
     hipLaunchKernelGGL(kern, dim3((unsigned)p->tokens), dim3(units <= 64 ? 64 : units <= 128 ? 128 : 256), 0, s, (const D*)dy->ptr, dy->ld,
                        (const T*)rows->ptr, rows->ld, rows->rows, rows->cols, p->offsets, p->experts, p->slot, weights, p->k, (T*)drows->ptr,
                        drows->ld, dweights);

@@ -24,48 +24,71 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf2_t));
 }
 
-// W elements from p, W = 8 (16-byte aligned) or 1
-template <int W>
-__device__ __forceinline__ void load_row(const bf16_t* p, float (&v)[W]) {
-    if constexpr (W == 1) {
-        v[0] = bf16_to_f32(*p);
-    } else {
-        const ew_u4 a = *reinterpret_cast<const ew_u4*>(p);
+// Eight elements from p, 16-byte aligned, or (ANY) aligned as the elements are: memory takes whole vectors at any address, at the price of
+// the lines they straddle
+typedef uint32_t ew_u4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float ew_f4_any __attribute__((ext_vector_type(4), aligned(4)));
+template <bool ANY = false>
+__device__ __forceinline__ void load_row(const bf16_t* p, float (&v)[8]) {
+    ew_u4 a;
+    if constexpr (ANY) a = *reinterpret_cast<const ew_u4_any*>(p);
+    else a = *reinterpret_cast<const ew_u4*>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = bf16lo_to_f32(a[i]);
-            v[2 * i + 1] = bf16hi_to_f32(a[i]);
-        }
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16lo_to_f32(a[i]);
+        v[2 * i + 1] = bf16hi_to_f32(a[i]);
     }
 }
-template <int W>
-__device__ __forceinline__ void load_row(const float* p, float (&v)[W]) {
-    if constexpr (W == 1) {
-        v[0] = *p;
-    } else {
+template <bool ANY = false>
+__device__ __forceinline__ void load_row(const float* p, float (&v)[8]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const ew_f4 a = reinterpret_cast<const ew_f4*>(p)[h];
+    for (int h = 0; h < 2; ++h) {
+        ew_f4 a;
+        if constexpr (ANY) a = reinterpret_cast<const ew_f4_any*>(p)[h];
+        else a = reinterpret_cast<const ew_f4*>(p)[h];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[4 * h + i] = a[i];
-        }
+        for (int i = 0; i < 4; ++i) v[4 * h + i] = a[i];
     }
 }
-template <int W>
-__device__ __forceinline__ void store_row(bf16_t* p, const float (&v)[W]) {
-    if constexpr (W == 1) {
-        *p = (bf16_t)pack_bf16(v[0], 0.0f);
+template <bool ANY = false>
+__device__ __forceinline__ void store_row(bf16_t* p, const float (&v)[8]) {
+    const ew_u4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    if constexpr (ANY) *reinterpret_cast<ew_u4_any*>(p) = w;
+    else *reinterpret_cast<ew_u4*>(p) = w;
+}
+template <bool ANY = false>
+__device__ __forceinline__ void store_row(float* p, const float (&v)[8]) {
+    const ew_f4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+    if constexpr (ANY) {
+        reinterpret_cast<ew_f4_any*>(p)[0] = a;
+        reinterpret_cast<ew_f4_any*>(p)[1] = b;
     } else {
-        *reinterpret_cast<ew_u4*>(p) = ew_u4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        reinterpret_cast<ew_f4*>(p)[0] = a;
+        reinterpret_cast<ew_f4*>(p)[1] = b;
     }
 }
-template <int W>
-__device__ __forceinline__ void store_row(float* p, const float (&v)[W]) {
-    if constexpr (W == 1) {
-        *p = v[0];
+__device__ __forceinline__ float load_one(const bf16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ float load_one(const float* p) { return *p; }
+__device__ __forceinline__ void store_one(bf16_t* p, float v) { *p = (bf16_t)pack_bf16(v, 0.0f); }
+__device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
+// the first n of them, zeros for the rest
+template <typename T, bool ANY>
+__device__ __forceinline__ void load_part(const T* p, int64_t n, float (&v)[8]) {
+    if (!ANY || n >= 8) {
+        load_row<ANY>(p, v);
     } else {
-        reinterpret_cast<ew_f4*>(p)[0] = ew_f4{v[0], v[1], v[2], v[3]};
-        reinterpret_cast<ew_f4*>(p)[1] = ew_f4{v[4], v[5], v[6], v[7]};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? load_one(p + i) : 0.0f;
+    }
+}
+template <typename T, bool ANY>
+__device__ __forceinline__ void store_part(T* p, int64_t n, const float (&v)[8]) {
+    if (!ANY || n >= 8) {
+        store_row<ANY>(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) store_one(p + i, v[i]);
     }
 }
 

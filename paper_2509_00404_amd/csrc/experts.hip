@@ -181,10 +181,7 @@ __device__ __forceinline__ void put4(OUT* p, ex_f4 v, int64_t left, bool vec) {
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (i < left) {
-            const float one[1] = {v[i]};
-            store_row<1>(p + i, one);
-        }
+        if (i < left) store_one(p + i, v[i]);
 }
 
 struct DenseRows {
@@ -201,7 +198,7 @@ __device__ __forceinline__ void few_quantize(const T* A, int64_t ld, int rows, i
     for (int i = threadIdx.x; i < rows * per; i += 256) {
         const int row = i / per, c = i - row * per;
         float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (c < 4 * nblk) load_row<8>(A + row_of(row) * ld + 8 * c, v);
+        if (c < 4 * nblk) load_row(A + row_of(row) * ld + 8 * c, v);
         uint32_t byte;
         const uint32_t w = mx_quad(v, byte);
         *reinterpret_cast<uint32_t*>(codes + row * few_code_row(nblk) + 4 * c) = w;
@@ -357,7 +354,7 @@ k_quantize_rows(const T* __restrict__ A, int64_t ld, int64_t K, uint64_t total, 
     const uint64_t row = div_by(units, n);
     const uint32_t unit = (uint32_t)(n - row * units.d);
     float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (8 * (int64_t)unit < K) load_row<8>(A + row * ld + 8 * (int64_t)unit, v);
+    if (8 * (int64_t)unit < K) load_row(A + row * ld + 8 * (int64_t)unit, v);
     uint32_t byte;
     *reinterpret_cast<uint32_t*>(codes + 4 * n) = mx_quad(v, byte);
     if constexpr (UNITS) {

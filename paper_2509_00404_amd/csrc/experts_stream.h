@@ -197,8 +197,8 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
     }
 
     // ---- this workgroup's tiles.  A tile's place takes a search and two divisions, some thousand cycles one after the other: 48 lanes do them
-    // for 48 tiles at once, two halves of a ring ahead (before, every wave for every tile: 1664 tiles of one unit 66 us without transfers or
-    // stores, so EX_AFTER).
+    // for 48 tiles at once, a half of a ring ahead.  (Done by every wave for every tile, 1664 tiles of a single unit took 37 us without any
+    // transfer or store; 533 tokens' gradients, 128 experts of 80 x 3240, 90 us instead of 67.)
     const int hop = (int)gridDim.x, xcds = (hop & 7) == 0 ? 8 : 1;
     const int start = ((int)blockIdx.x % xcds) * (hop / xcds) + (int)blockIdx.x / xcds;
     if (start >= total) return;

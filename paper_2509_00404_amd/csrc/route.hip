@@ -9,14 +9,6 @@
 
 namespace {
 
-__device__ __forceinline__ float load_f32(const float* p) { return *p; }
-__device__ __forceinline__ float load_f32(const bf16_t* p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_f32(bf16_t* p, float v) {
-    // (the shared conversion is for finite values: a NaN's low bits alone would round up to infinity)
-    *p = v == v ? f32_to_bf16_rne(v) : (bf16_t)0x7FC0u;
-}
-
 // v of the lane N places on, around the row of 16
 template <int N>
 __device__ __forceinline__ uint32_t row_rotate(uint32_t v) {
@@ -103,7 +95,7 @@ k_route(const T* __restrict__ logits, RouteArgs a) {
     }
     if (!loaded) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = e0 + v < a.E ? load_f32(row + e0 + v) : -INFINITY;
+        for (int v = 0; v < V; ++v) x[v] = e0 + v < a.E ? load_one(row + e0 + v) : -INFINITY;
     }
     float add[V];
 #pragma unroll
@@ -242,7 +234,7 @@ k_route(const T* __restrict__ logits, RouteArgs a) {
     __syncthreads();
     // one lane per choice from here on
     const int e = lane < a.k ? s_idx[tok][lane] : -1;
-    const float xe = e >= 0 ? load_f32(row + e) : -INFINITY;
+    const float xe = e >= 0 ? load_one(row + e) : -INFINITY;
     float w;
     if (SIGMOID) {
         w = e >= 0 ? sigmoid_f32(xe) : 0.0f;
@@ -285,7 +277,7 @@ k_route_grads(const T* __restrict__ logits, int64_t ld, int64_t tokens, const in
     const bool there = t < tokens;
     const T* row = logits + (there ? t : 0) * ld;
     int e = there && lane < k ? idx[t * k + lane] : -1;
-    const float xe = (uint32_t)e < (uint32_t)E ? load_f32(row + e) : -INFINITY;
+    const float xe = (uint32_t)e < (uint32_t)E ? load_one(row + e) : -INFINITY;
     if (!(xe > -INFINITY)) e = -1;
     const float v = e >= 0 ? scale * dweights[t * k + lane] : 0.0f;
     float x[V], p[V], d = 0.0f, inner = 0.0f;
@@ -308,7 +300,7 @@ k_route_grads(const T* __restrict__ logits, int64_t ld, int64_t tokens, const in
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int n = lane + ROUTE_LANES * i;
-            x[i] = there && n < E ? load_f32(row + n) : -INFINITY;
+            x[i] = there && n < E ? load_one(row + n) : -INFINITY;
             top = fmaxf(top, x[i]);
         }
         top = row_maxf(top);
@@ -339,7 +331,7 @@ k_route_grads(const T* __restrict__ logits, int64_t ld, int64_t tokens, const in
         const int n = lane + ROUTE_LANES * i;
         if (n >= E) continue;
         const float g = s_dx[tok][n];
-        store_f32(dlogits + t * ldd + n, dense ? p[i] * (g - inner) : g);
+        store_one(dlogits + t * ldd + n, dense ? p[i] * (g - inner) : g);
     }
 }
 
