@@ -215,8 +215,8 @@ class Mx8Tensor:
     def __init__(self, rows, cols, device="cuda", buffers=None):
         self.rows, self.cols = rows, cols
         if buffers is None:
-            buffers = (torch.empty((rows, cols), dtype=torch.uint8, device=device),
-                       torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
+            buffers = (torch.empty(rows, cols, dtype=torch.uint8, device=device),
+                       torch.empty(rows, cols // 32, dtype=torch.uint8, device=device))
         else:
             assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
             assert [t.numel() for t in buffers] == [rows * cols, rows * (cols // 32)]
@@ -496,8 +496,9 @@ class ExpertPlan:
     def __init__(self, tokens, experts, k, buffers=None, device="cuda"):
         self.tokens, self.experts, self.k = tokens, experts, k
         if buffers is None:
-            i32 = dict(dtype=torch.int32, device=device)
-            buffers = torch.empty((experts + 1,), **i32), torch.empty((tokens * k,), **i32), torch.empty((tokens, k), **i32)
+            # (sizes as plain numbers: a tuple costs the host 0.4 us more, a third of what these calls take)
+            slot = torch.empty(tokens, k, dtype=torch.int32, device=device)
+            buffers = torch.empty(experts + 1, dtype=torch.int32, device=device), torch.empty(tokens * k, dtype=torch.int32, device=device), slot
         else:
             assert all(t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 for t in buffers)
             assert [t.numel() for t in buffers] == [experts + 1, tokens * k, tokens * k]
@@ -511,15 +512,15 @@ def _ptr(t, dtype, shape):
     """Address of a contiguous device tensor of that type and shape (None stays None)."""
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and tuple(t.shape) == shape
+    assert t.shape == shape and t.dtype == dtype and t.is_cuda and t.is_contiguous()
     return t.data_ptr()
 
 
 def route(logits, k, bias=None, valid=None, scores="softmax", groups=1, top_groups=1, renorm=True, scale=1.0):
     """Chosen experts idx [T, k] int32 and weights [T, k] fp32 of logits [T, experts] (see metis_route)."""
     T, E = logits.shape
-    idx = torch.empty((T, k), dtype=torch.int32, device=logits.device)
-    weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    idx = torch.empty(T, k, dtype=torch.int32, device=logits.device)
+    weights = torch.empty_like(idx, dtype=torch.float32)
     m, r = _mat(logits), Router(E, k, SCORES[scores], groups, top_groups, renorm, scale)
     _check(lib().metis_route(_stream(), C.byref(m), C.byref(r), _ptr(bias, torch.float32, (E,)), _ptr(valid, torch.uint8, (T,)),
                              idx.data_ptr(), weights.data_ptr()))
@@ -531,7 +532,7 @@ def route_grads(logits, idx, dweights, scores="softmax", renorm=True, scale=1.0,
     T, E = logits.shape
     k = idx.shape[1]
     if out is None:
-        out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+        out = torch.empty(T, E, dtype=logits.dtype, device=logits.device)
     m, o, r = _mat(logits), _mat(out), Router(E, k, SCORES[scores], 1, 1, renorm, scale)
     _check(lib().metis_route_grads(_stream(), C.byref(m), C.byref(r), _ptr(idx, torch.int32, (T, k)),
                                    _ptr(dweights, torch.float32, (T, k)), C.byref(o)))
@@ -545,7 +546,7 @@ def dispatch(idx, experts, plan=None, workspace=None):
         plan = ExpertPlan(T, experts, k, device=idx.device)
     if workspace is None:
         nbytes = int(lib().metis_dispatch_workspace_bytes(T, experts, k))
-        workspace = torch.empty((nbytes,), dtype=torch.uint8, device=idx.device) if nbytes else None
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=idx.device) if nbytes else None
     p = plan.c()
     _check(lib().metis_dispatch(_stream(), _ptr(idx, torch.int32, (plan.tokens, plan.k)), C.byref(p),
                                 workspace.data_ptr() if workspace is not None else None,
@@ -561,7 +562,7 @@ def experts_product(A, W, plan, Cmat, gather=False, workspace=None):
     """Cmat [S, N] = rows of A (by slot, or with gather by token) times their experts' weights W (MxTensor [experts * N, K])."""
     a, w, p, c = _mat(A), W.c(), plan.c(), _mat(Cmat)
     if workspace is None:
-        workspace = torch.empty((experts_workspace_bytes(A.shape[0], Cmat.shape[0], plan.experts, Cmat.shape[1], A.shape[1]),), dtype=torch.uint8, device=A.device)
+        workspace = torch.empty(experts_workspace_bytes(a.rows, c.rows, plan.experts, c.cols, a.cols), dtype=torch.uint8, device=A.device)
     _check(lib().metis_experts_product(_stream(), C.byref(a), C.byref(w), C.byref(p), gather, C.byref(c), workspace.data_ptr(),
                                        workspace.numel()))
     return Cmat
@@ -582,8 +583,7 @@ def experts_wgrad(G, X, plan, dW, gather=False, workspace=None):
     """dW [experts * N, K] of G [S, N] and X (by slot, or with gather by token), quantized along the slots of each expert."""
     g, x, p, d = _mat(G), _mat(X), plan.c(), _mat(dW)
     if workspace is None:
-        workspace = torch.empty((experts_wgrad_workspace_bytes(G.shape[0], plan.experts, G.shape[1], X.shape[1]),), dtype=torch.uint8,
-                                device=dW.device)
+        workspace = torch.empty(experts_wgrad_workspace_bytes(g.rows, plan.experts, g.cols, x.cols), dtype=torch.uint8, device=dW.device)
     _check(lib().metis_experts_wgrad(_stream(), C.byref(g), C.byref(x), C.byref(p), gather, C.byref(d), workspace.data_ptr(),
                                      workspace.numel()))
     return dW
@@ -599,9 +599,9 @@ def combine(rows, plan, y, weights=None):
 def combine_grads(dy, rows, plan, weights, drows=None, dweights=None):
     """Gradients (drows like rows, dweights [T, k] fp32) of combine."""
     if drows is None:
-        drows = torch.empty(rows.shape, dtype=rows.dtype, device=rows.device)
+        drows = torch.empty(*rows.shape, dtype=rows.dtype, device=rows.device)
     if dweights is None:
-        dweights = torch.empty((plan.tokens, plan.k), dtype=torch.float32, device=rows.device)
+        dweights = torch.empty(plan.tokens, plan.k, dtype=torch.float32, device=rows.device)
     d, r, p, o, shape = _mat(dy), _mat(rows), plan.c(), _mat(drows), (plan.tokens, plan.k)
     _check(lib().metis_combine_grads(_stream(), C.byref(d), C.byref(r), C.byref(p), _ptr(weights, torch.float32, shape), C.byref(o),
                                      _ptr(dweights, torch.float32, shape)))

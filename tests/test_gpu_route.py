@@ -72,6 +72,29 @@ def test_route(metis, T, E, k, groups, top_groups, scores, renorm):
         _close_rows(w.double().cpu().numpy()[same], rw[same], 1e-5)
 
 
+@pytest.mark.parametrize("T,E,k,groups,top_groups", [(65, 256, 8, 8, 4), (40, 512, 16, 16, 3), (33, 128, 4, 1, 1), (20, 384, 5, 3, 2), (9, 248, 6, 1, 1)])
+@pytest.mark.parametrize("scores", ["softmax", "sigmoid"])
+def test_route_bf16_wide(metis, T, E, k, groups, top_groups, scores):
+    """Many experts in bf16: whole 16-byte loads where the rows allow them, single ones in a view off 16 bytes."""
+    x = _logits(T, E, E, torch.bfloat16)
+    bias = (0.0625 * torch.arange(E) % 1.0)
+    ri, rw = oe.route(x.double().numpy(), k, bias.double().numpy(), None, scores, groups, top_groups)
+    same = np.ones(T, dtype=bool)
+    for t in range(T):
+        key = oe.selection_keys(x[t].double().numpy(), bias.double().numpy(), scores)
+        vals = np.concatenate([key, oe.group_scores(key, groups, scores)])
+        gap = np.diff(np.unique(vals[vals > -np.inf]))
+        same[t] = scores == "softmax" or not np.any(gap < 1e-6)
+    assert same.mean() > 0.3
+    wide = torch.zeros((T, E + 8), dtype=torch.bfloat16, device="cuda")
+    for left in (0, 3):
+        wide[:, left:left + E] = x.cuda()
+        for xd in (x.cuda(), wide[:, left:left + E]):
+            idx, w = metis.route(xd, k, bias=bias.cuda(), scores=scores, groups=groups, top_groups=top_groups)
+            assert np.array_equal(idx.cpu().numpy()[same], ri[same])
+            _close_rows(w.double().cpu().numpy()[same], rw[same], 1e-5)
+
+
 def test_route_bf16_strided_logits(metis):
     T, E, k = 70, 24, 3
     x = _logits(T, E, 3, torch.bfloat16)
