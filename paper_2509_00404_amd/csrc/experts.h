@@ -13,7 +13,6 @@ namespace {
 struct SlotUnit {
     int expert, local, total;
     int64_t begin, end;                   // the expert's slots
-    int64_t padded;                       // slots of the experts before it, each padded to whole SLOT_ALIGN
 };
 __device__ __forceinline__ int64_t held(int32_t o, int64_t S) { return o < 0 ? 0 : o > S ? S : o; }
 __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offsets, int E, int64_t S, int size, int64_t u) {
@@ -25,31 +24,28 @@ __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offset
         const int e = e0 + (i < q ? i : q);
         o[i] = offsets[e < E ? e : E];
     }
-    int mine = 0, pads = 0;
+    int mine = 0;
 #pragma unroll
     for (int i = 0; i <= Q; ++i) o[i] = (int32_t)held(o[i], S);
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
         const int32_t n = o[i + 1] - o[i];
-        if (n > 0) {
-            mine += (n + size - 1) / size;
-            pads += (n + SLOT_ALIGN - 1) / SLOT_ALIGN;
-        }
+        if (n > 0) mine += (n + size - 1) / size;
     }
-    int upto = mine, pads_upto = pads;
+    int upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int a = __shfl_up(upto, d), b = __shfl_up(pads_upto, d);
-        if (lane >= d) { upto += a; pads_upto += b; }
+        const int a = __shfl_up(upto, d);
+        if (lane >= d) upto += a;
     }
     SlotUnit r;
     r.total = __builtin_amdgcn_readlane(upto, 63);
     r.expert = -1;
     r.local = 0;
-    r.begin = r.end = r.padded = 0;
+    r.begin = r.end = 0;
     if (u >= r.total) return r;
     // every lane looks through its own experts, and the one that has the unit says where
-    int before = upto - mine, pads_before = pads_upto - pads, expert = 0, local = 0, begin = 0, end = 0, padded = 0;
+    int before = upto - mine, expert = 0, local = 0, begin = 0, end = 0;
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
         const int32_t n = o[i + 1] - o[i], units = n > 0 ? (n + size - 1) / size : 0;
@@ -58,17 +54,35 @@ __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offset
         local = here ? (int)(u - before) : local;
         begin = here ? o[i] : begin;
         end = here ? o[i + 1] : end;
-        padded = here ? pads_before : padded;
         before += units;
-        pads_before += n > 0 ? (n + SLOT_ALIGN - 1) / SLOT_ALIGN : 0;
     }
     const int at = __ffsll((unsigned long long)__ballot(upto > u)) - 1;
     r.expert = __builtin_amdgcn_readlane(expert, at);
     r.local = __builtin_amdgcn_readlane(local, at);
     r.begin = __builtin_amdgcn_readlane(begin, at);
     r.end = __builtin_amdgcn_readlane(end, at);
-    r.padded = (int64_t)__builtin_amdgcn_readlane(padded, at) * SLOT_ALIGN;
     return r;
+}
+// units of `size` of the experts before e
+__device__ __forceinline__ int64_t units_before(const int32_t* __restrict__ offsets, int E, int64_t S, int size, int e) {
+    constexpr int Q = EXPERTS_MAX / 64;
+    const int lane = (int)threadIdx.x & 63;
+    int32_t o[Q][2];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const int x = 64 * i + lane;                     // (those from e on: nothing)
+        o[i][0] = offsets[x < e ? x : e];
+        o[i][1] = offsets[x < e ? x + 1 : e];
+    }
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const int64_t n = held(o[i][1], S) - held(o[i][0], S);
+        if (n > 0) sum += (int)((n + size - 1) / size);
+    }
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
+    return __builtin_amdgcn_readfirstlane(sum);
 }
 // units of `size` that S slots can fall into
 inline int64_t most_units(int64_t S, int E, int size) { return S / size + (E < S ? E : S); }

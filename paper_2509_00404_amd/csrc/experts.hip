@@ -18,8 +18,8 @@ namespace {
 // neighbouring columns, all of them in flight together; a workgroup's 8 waves have 256 rows of 128 columns, which leave by way of LDS as
 // whole lines.  With a plan the segments are the experts' slots, padded with zeros to a multiple of 64, in rows of whole units and with
 // scales in units, and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows` rows.
-// FLAT (a plan's segments): a workgroup has 64 rows of 512 columns instead, and its lanes store by themselves; for few slots an expert, whose
-// result has no whole lines, and of whose 256 rows most would not exist.
+// FLAT (a plan's segments, for the gradients of few slots): rows of whole 64 slots and scales row by row, as k_experts_short reads them; a
+// workgroup has 64 rows of 512 columns, and its lanes store by themselves.
 // What bounds it: memory.  32768 x 4096 gathered rows, 339 MB to be moved, take 55 us, x 2048 by slot (170 MB) 36.  (Loads in branches, 16
 // bytes of a column stored at a time and scales byte by byte: 140 and 103.)
 #define QT_ROW 144                            // a column's 8 blocks of 16 bytes, and 16 that spread the columns over the banks
@@ -33,14 +33,15 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
     const int64_t unit = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
     int64_t begin, count, stride, written, base, first;   // the segment's rows, the length of its result's rows and what is written of them, its place; the unit's first row
     if (FLAT || offsets) {
-        const SlotUnit u = find_unit(offsets, E, S, FLAT ? 64 : SLOT_ALIGN, unit);
+        constexpr int UNIT = FLAT ? 64 : SLOT_ALIGN;
+        const SlotUnit u = find_unit(offsets, E, S, UNIT, unit);
         if (u.expert < 0) return;
         begin = u.begin;
         count = u.end - u.begin;
-        stride = (count + SLOT_ALIGN - 1) / SLOT_ALIGN * SLOT_ALIGN;
+        stride = (count + UNIT - 1) / UNIT * UNIT;
         written = (count + 63) / 64 * 64;
-        base = u.padded * cols;
-        first = (int64_t)u.local * (FLAT ? 64 : SLOT_ALIGN);
+        base = (unit - u.local) * UNIT * cols;
+        first = (int64_t)u.local * UNIT;
     } else {
         const int64_t per = (rows + SLOT_ALIGN - 1) / SLOT_ALIGN, g = unit / per;
         begin = g * rows;
@@ -91,8 +92,9 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
             const ew_u4 w = mx_block(v[c], byte);
             if constexpr (FLAT) {
                 if (col < cols) {
-                    *reinterpret_cast<ew_u4*>(codes + (base + (col + c) * stride + from) / 2) = w;
-                    scales[base / 32 + (from / 256 * cols + col + c) * 8 + from % 256 / 32] = (uint8_t)byte;
+                    const int64_t at = base + (col + c) * stride + from;
+                    *reinterpret_cast<ew_u4*>(codes + at / 2) = w;
+                    scales[at / 32] = (uint8_t)byte;
                 }
             } else {
                 *reinterpret_cast<ew_u4*>(s_codes + (2 * lane + c) * QT_ROW + 16 * wave) = w;
@@ -307,6 +309,67 @@ k_experts_few(MxRows A, DenseRows dense, int64_t arows, MxRows W, const int32_t*
 
 #include "experts_stream.h"
 
+// ---- gradients of few slots an expert ----
+// dW is what is written and bounds it; the contraction is a step or two.  A wave has 128 x 64 outputs, a workgroup 128 x 256; operands come
+// straight from memory and nothing waits for anybody, so that one wave's stores and another's loads overlap (on the stream, a tile of a single
+// unit waits for its transfers, then for its stores).  Operands as the quantizer's FLAT form leaves them.
+template <typename OUT, bool PAST>
+__global__ void __launch_bounds__(256, 2)
+k_experts_short(MxRows G, MxRows X, const int32_t* __restrict__ offsets, int E, int64_t S, int64_t N, int64_t K, OUT* __restrict__ dW, int64_t ldw,
+                bool vec, uint32_t tiles_k) {
+    constexpr bool LINES = sizeof(OUT) == 2;             // outputs by way of LDS, accumulator tiles transposed
+    __shared__ __attribute__((aligned(16))) uint8_t s_stage[LINES ? 4 * EX_STAGE : 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), li = lane & 31, half = lane >> 5;
+    const int e = blockIdx.y;
+    const uint32_t tn = blockIdx.x / tiles_k, tk = blockIdx.x - tn * tiles_k;
+    const int64_t n0 = 128 * (int64_t)tn, k0 = 256 * (int64_t)tk + 64 * wave;
+    if (k0 >= K) return;
+    const int64_t before = units_before(offsets, E, S, 64, e);
+    const int64_t count = held(offsets[e + 1], S) - held(offsets[e], S);
+    const int steps = count > 0 ? (int)((count + 63) >> 6) : 0;
+    const int64_t len = 64 * (int64_t)steps;
+    float16_t acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    int64_t at[6];                                       // of this lane's rows: 0 .. 3 of G, 4 and 5 of X
+#pragma unroll
+    for (int x = 0; x < 6; ++x) {
+        const int64_t rows = x < 4 ? N : K, r = (x < 4 ? n0 + 32 * x : k0 + 32 * (x - 4)) + li;
+        at[x] = 64 * before * rows + (r < rows ? r : rows - 1) * len + 32 * half;
+    }
+    for (int s = 0; s < steps; ++s) {
+        ew_u4 f[6];
+        int sc[6];
+#pragma unroll
+        for (int x = 0; x < 6; ++x) {
+            const MxRows& m = x < 4 ? G : X;
+            f[x] = *reinterpret_cast<const ew_u4*>(m.codes + at[x] / 2);
+            sc[x] = m.scales[at[x] / 32];
+            at[x] += 64;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (n0 + 32 * i >= N) continue;
+            const ex_i8 g = {(int)f[i][0], (int)f[i][1], (int)f[i][2], (int)f[i][3], 0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const ew_u4 y = f[4 + j];
+                const ex_i8 x = {(int)y[0], (int)y[1], (int)y[2], (int)y[3], 0, 0, 0, 0};
+                if constexpr (LINES) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, g, acc[i][j], 4, 4, 0, sc[4 + j], 0, sc[i]);
+                else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(g, x, acc[i][j], 4, 4, 0, sc[i], 0, sc[4 + j]);
+            }
+        }
+    }
+    OUT* C = dW + (int64_t)e * N * ldw;
+    const bool inside = n0 + 128 <= N && k0 + 64 <= K;
+    if constexpr (LINES) ex_store_lines<PAST>(acc, s_stage + wave * EX_STAGE, C, ldw, n0, k0, N, K, vec, inside && vec, lane);
+    else ex_store_plain<PAST>(acc, C, ldw, n0, k0, N, K, inside, lane);
+}
+
 // ---- rows quantized for the products ----
 // [rows, K] -> codes, in rows of Kp elements (K filled up with zeros), and scales.  A lane per 8 elements, four lanes per block of 32.
 // UNITS: Kp is a multiple of 256, and the scales go in units to the rows' slots: a lane of the 16 that hold four blocks writes their bytes for
@@ -377,11 +440,14 @@ int experts_plan_status(const metis_expert_plan* p) {
     if (p->tokens > 0x7FFFFFFFll / p->k) return METIS_BAD_SHAPE;
     return METIS_OK;
 }
+// Gradients of few slots an expert go without the stream.  us with the quantizers, without / with it: bf16, 2 slots an expert of 256 (2464 x
+// 400) 176 / 256, 17 of 128 (80 x 3240) 42 / 75, 112 of 160 (128 x 6888) 178 / 211, 150 of 64 (2048 x 4096) 263 / 224; fp32, 31 of 64 (1384 x
+// 2456) 238 / 240, 100 of 64 (1024 x 2040) 184 / 162.
+bool wgrad_short(int64_t S, int E, int dtype) { return S < (dtype == METIS_BF16 ? 128 : 64) * (int64_t)E; }
 // quantize A^T by segments of a plan (token may be null) or of `rows` rows
-int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_plan* p, bool gather, int64_t rows, uint8_t* codes,
+int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_plan* p, bool gather, bool flat, int64_t rows, uint8_t* codes,
                          uint8_t* scales) {
     const int64_t S = p ? p->tokens * p->k : 0;
-    const bool flat = p && S < 128 * (int64_t)p->experts;
     const int64_t units = p ? most_units(S, p->experts, flat ? 64 : SLOT_ALIGN) : A->rows / rows * ceil_div64(rows, SLOT_ALIGN);
     const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
     const dim3 grid((unsigned)ceil_div64(A->cols, flat ? 512 : 128), (unsigned)gy, (unsigned)gz);
@@ -436,7 +502,7 @@ int launch_quantize_rows(hipStream_t s, const metis_mat* A, int64_t Kp, uint8_t*
     return METIS_OK;
 }
 template <typename OUT, int MODE>
-int launch_stream(hipStream_t s, const ExStream& a, int64_t tiles, metis_mat* C) {
+int launch_stream(hipStream_t s, const ExStream& a, int64_t tiles, metis_mat* C, bool past) {
     const int cus = device_cu_count();
     if (cus < 1) return METIS_HIP_ERROR;
     auto launch = [&](auto kern, LdsLimitCache& lds_set) -> int {
@@ -447,7 +513,7 @@ int launch_stream(hipStream_t s, const ExStream& a, int64_t tiles, metis_mat* C)
     };
     static LdsLimitCache lds_set[2];
     if constexpr (MODE == EX_WGRAD)
-        if ((uintptr_t)C->ptr % 128 || C->ld * sizeof(OUT) % 128) return launch(k_experts_stream<OUT, MODE, false>, lds_set[0]);
+        if (!past) return launch(k_experts_stream<OUT, MODE, false>, lds_set[0]);
     return launch(k_experts_stream<OUT, MODE, true>, lds_set[1]);
 }
 
@@ -458,7 +524,7 @@ extern "C" int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups,
     if (A->rows % groups || A->rows / groups % 32 || A->cols % 8 || A->ld < A->cols || !mat_aligned16(A) || (uintptr_t)out->codes % 16 ||
         out->rows != groups * A->cols || out->cols != A->rows / groups)
         return METIS_BAD_SHAPE;
-    return launch_quantize_mx_t((hipStream_t)stream, A, nullptr, false, A->rows / groups, out->codes, out->scales);
+    return launch_quantize_mx_t((hipStream_t)stream, A, nullptr, false, false, A->rows / groups, out->codes, out->scales);
 }
 
 extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int64_t slots, int experts, int64_t N, int64_t K) {
@@ -491,7 +557,7 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
         const ExStream a = {{ws, ws + place.scales}, {W->codes, ws + place.wscales + 2048}, plan->offsets, gather ? plan->token : nullptr, S,
                             A->rows, N, K, (uint32_t)(place.Kp / 2), 8 * S, 8 * W->rows, E, 0, tn};
         const int64_t tiles = most_units(S, E, 256) * tn;
-        return C->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_PRODUCT>(s, a, tiles, C) : launch_stream<float, EX_PRODUCT>(s, a, tiles, C);
+        return C->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_PRODUCT>(s, a, tiles, C, true) : launch_stream<float, EX_PRODUCT>(s, a, tiles, C, true);
     }
     const int nblk = (int)(K / 32);
     const int64_t most = most_units(S, E, 32) + 1;
@@ -565,11 +631,24 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
     w += mx_bytes(N, P);
     const MxRows x = {w, w + align_up((size_t)K * P / 2, 256)};
     hipStream_t s = (hipStream_t)stream;
+    const bool brief = wgrad_short(S, (int)E, dW->dtype);
     if (S > 0) {
-        int r = launch_quantize_mx_t(s, G, plan, false, 0, (uint8_t*)g.codes, (uint8_t*)g.scales);
-        if (r == METIS_OK) r = launch_quantize_mx_t(s, X, plan, gather != 0, 0, (uint8_t*)x.codes, (uint8_t*)x.scales);
+        int r = launch_quantize_mx_t(s, G, plan, false, brief, 0, (uint8_t*)g.codes, (uint8_t*)g.scales);
+        if (r == METIS_OK) r = launch_quantize_mx_t(s, X, plan, gather != 0, brief, 0, (uint8_t*)x.codes, (uint8_t*)x.scales);
         if (r != METIS_OK) return r;
     }
+    const bool past = (uintptr_t)dW->ptr % 128 == 0 && dW->ld * mat_size(dW) % 128 == 0;
+    if (brief) {
+        const int64_t sn = ceil_div64(N, 128), sk = ceil_div64(K, 256);
+        auto launch = [&](auto kern, auto zero) {
+            hipLaunchKernelGGL(kern, dim3((unsigned)(sn * sk), (unsigned)E), dim3(256), 0, s, g, x, plan->offsets, (int)E, S, N, K,
+                               (decltype(zero)*)dW->ptr, dW->ld, mat_aligned16(dW), (uint32_t)sk);
+        };
+        if (dW->dtype == METIS_BF16) past ? launch(k_experts_short<bf16_t, true>, bf16_t()) : launch(k_experts_short<bf16_t, false>, bf16_t());
+        else past ? launch(k_experts_short<float, true>, float()) : launch(k_experts_short<float, false>, float());
+        METIS_LAUNCH_CHECK();
+        return METIS_OK;
+    }
     const ExStream a = {g, x, plan->offsets, nullptr, S, 0, N, K, 0, 8 * N, 8 * K, (int)E, (int)tm, (int)tn};
-    return dW->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_WGRAD>(s, a, tiles, dW) : launch_stream<float, EX_WGRAD>(s, a, tiles, dW);
+    return dW->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_WGRAD>(s, a, tiles, dW, past) : launch_stream<float, EX_WGRAD>(s, a, tiles, dW, past);
 }

@@ -35,7 +35,8 @@ def test_product_over_many_tiles(metis, T, E, k, N, K, skew, out):
     _check(C, ref, big, out)
 
 
-@pytest.mark.parametrize("T,E,k,N,K,skew", [(1500, 6, 2, 2312, 3000, 0.3), (700, 20, 4, 1032, 1800, 0.0)])
+@pytest.mark.parametrize("T,E,k,N,K,skew", [(1500, 6, 2, 2312, 3000, 0.3), (700, 20, 4, 1032, 1800, 0.0),
+                                               (300, 40, 4, 1096, 1160, 0.5)])
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
 def test_weight_gradient_over_many_tiles(metis, T, E, k, N, K, skew, out):
     plan, g = _plan(metis, T, E, k, 12, skew, 0.05)
