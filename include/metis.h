@@ -458,7 +458,7 @@ int metis_dispatch(void* stream, const int32_t* idx, metis_expert_plan* plan, vo
  * The plan is read on the device: its offsets, and token and slot with gather.
  *   K % 32 == 0; A's rows 16-byte aligned; W's codes 16-byte, scales 8-byte aligned; workspace 256-byte aligned, metis_experts_workspace_bytes(A->rows, S, ...) bytes.
  * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (experts > 512, k > 16,
- * a grid of more than 2^31 - 1 workgroups).
+ * K > 2^28, a grid of more than 2^31 - 1 workgroups).
  */
 size_t metis_experts_workspace_bytes(int64_t rows, int64_t slots, int experts, int64_t N, int64_t K);
 int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W, const metis_expert_plan* plan, int gather, metis_mat* C,
@@ -476,7 +476,7 @@ int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups, metis_mxfp
  * X by slot ([S, K]) or, with gather, by token ([tokens, K]).  Both (bf16 or fp32) are quantized to MXFP4 in blocks of 32 consecutive
  * slots of one expert, from its first; what its last block lacks is zeros.  An expert without slots gets 0.
  *   N, K multiples of 8; G's and X's rows 16-byte aligned; workspace 256-byte aligned, metis_experts_wgrad_workspace_bytes(S, ...) bytes.
- * Errors: as for metis_experts_product, and METIS_UNSUPPORTED for more than 2^25 slots.
+ * Errors: as for metis_experts_product, and METIS_UNSUPPORTED for more than 2^25 slots or 2^28 rows or columns.
  */
 size_t metis_experts_wgrad_workspace_bytes(int64_t slots, int experts, int64_t N, int64_t K);
 int metis_experts_wgrad(void* stream, const metis_mat* G, const metis_mat* X, const metis_expert_plan* plan, int gather, metis_mat* dW,

@@ -528,7 +528,7 @@ extern "C" int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups,
 }
 
 extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int64_t slots, int experts, int64_t N, int64_t K) {
-    if (rows < 1 || slots < 1 || experts < 1 || experts > EXPERTS_MAX || N < 1 || K < 32 || K % 32) return 0;
+    if (rows < 1 || slots < 1 || experts < 1 || experts > EXPERTS_MAX || N < 1 || N > (1ll << 40) || K < 32 || K % 32 || K > (1 << 28)) return 0;
     return product_place(product_streams(slots, experts, N, rows, K), rows, slots, experts, N, K).bytes;
 }
 
@@ -543,6 +543,7 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     if (K < 32 || K % 32 || W->rows < 1 || W->rows % E || A->cols != K || A->ld < K || A->rows != (gather ? plan->tokens : S) ||
         C->rows != S || C->cols != N || C->ld < N || !mat_aligned16(A) || (uintptr_t)W->codes % 16 || (uintptr_t)W->scales % 8)
         return METIS_BAD_SHAPE;
+    if (K > (1 << 28) || N > (1ll << 40)) return METIS_UNSUPPORTED;
     if (!workspace || workspace_bytes < metis_experts_workspace_bytes(A->rows, S, E, N, K)) return METIS_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
     const bool streams = product_streams(S, E, N, A->rows, K);
@@ -604,7 +605,7 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
 }
 
 extern "C" size_t metis_experts_wgrad_workspace_bytes(int64_t slots, int experts, int64_t N, int64_t K) {
-    if (slots < 1 || experts < 1 || experts > EXPERTS_MAX || N < 1 || K < 1) return 0;
+    if (slots < 1 || slots > (1 << 25) || experts < 1 || experts > EXPERTS_MAX || N < 1 || N > (1 << 28) || K < 1 || K > (1 << 28)) return 0;
     const int64_t P = padded_slots(slots, experts);
     return mx_bytes(N, P) + mx_bytes(K, P);
 }
@@ -620,8 +621,9 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
         dW->ld < K)
         return METIS_BAD_SHAPE;
     if (S > 0 && (G->ld < N || X->ld < K || !mat_aligned16(G) || !mat_aligned16(X))) return METIS_BAD_SHAPE;
+    if (S > (1 << 25) || N > (1 << 28) || K > (1 << 28)) return METIS_UNSUPPORTED;
     const int64_t tm = ceil_div64(N, 256), tn = ceil_div64(K, 256), tiles = E * tm * tn;
-    if (S > (1 << 25) || N > (1 << 30) || K > (1 << 30) || tiles > 0x3FFFFFFF) return METIS_UNSUPPORTED;
+    if (tiles > 0x3FFFFFFF) return METIS_UNSUPPORTED;
     const size_t need = metis_experts_wgrad_workspace_bytes(S, (int)E, N, K);
     if (workspace_bytes < need || (need && !workspace)) return METIS_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;

@@ -149,6 +149,9 @@ def test_products(metis):
     assert wgrad(gp=None) == INVALID and wgrad(dp=None) == INVALID and wgrad(ws=FAKE + 16) == INVALID
     assert wgrad(G=(8, 12, 16, 0), dW=(96, 64, 64, 0)) == SHAPE and wgrad(G=(7, 16, 16, 0)) == SHAPE and wgrad(X=(4, 64, 64, 0)) == SHAPE
     assert wgrad(dW=(127, 64, 64, 0)) == SHAPE and wgrad(dW=(128, 64, 63, 0)) == SHAPE and wgrad(G=(8, 16, 20, 0)) == SHAPE
+    huge = 1 << 29
+    assert wgrad(X=(8, huge, huge, 0), dW=(128, huge, huge, 0)) == UNSUPPORTED and L.metis_experts_wgrad_workspace_bytes(8, 8, 16, huge) == 0
+    assert product(A=(8, huge, huge, 0), W=(128, huge)) == UNSUPPORTED and L.metis_experts_workspace_bytes(8, 8, 8, 16, huge) == 0
     need = L.metis_experts_wgrad_workspace_bytes(8, 8, 16, 64)
     assert need > 0 and wgrad(size=need - 1) == WORKSPACE and wgrad(ws=None) == WORKSPACE
 

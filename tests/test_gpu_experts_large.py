@@ -104,3 +104,53 @@ def test_checkpoints_past_32_bits(metis):
     assert torch.equal(dgu[-n:], dgu1) and torch.equal(again[-n:], again1)
     back = metis.dequantize_mx8(q, dgu)
     assert torch.equal(back[-n:], metis.dequantize_mx8(q1, dgu1))
+
+
+def _values(codes, scales):
+    """fp64 values of MXFP4 rows on the GPU"""
+    grid = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
+    v = grid[torch.stack((codes & 15, codes >> 4), -1).flatten(-2).int()]
+    return (v.unflatten(-1, (-1, 32)) * torch.exp2(scales.double() - 127)[..., None]).flatten(-2)
+
+
+def test_product_over_more_tiles_than_are_looked_up_at_once(metis):
+    T, E, N, K = 1100, 64, 98304, 64                           # about a hundred tiles a workgroup
+    g = torch.Generator(device="cuda").manual_seed(3)
+    codes = torch.randint(0, 256, (E * N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(120, 126, (E * N, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+    W = metis.MxTensor(E * N, K, buffers=(codes, scales))
+    x = torch.randn((T, K), generator=g, device="cuda").to(torch.bfloat16)
+    idx = torch.randint(0, E, (T, 1), generator=g, device="cuda", dtype=torch.int32)
+    plan = metis.dispatch(idx, E)
+    C = torch.full((T, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+    metis.experts_product(x, W, plan, C, gather=True)
+    X = metis.quantize_mx(x, metis.MxTensor(T, K))
+    xv = _values(X.codes, X.scales)[plan.token.long()]
+    expert = idx[plan.token.long(), 0].long()
+    cols = torch.cat((torch.arange(600, device="cuda"), torch.randint(0, N, (600,), generator=g, device="cuda"), torch.arange(N - 600, N, device="cuda")))
+    assert bool(torch.isfinite(C).all())
+    for e in range(E):
+        s = (expert == e).nonzero()[:, 0]
+        wv = _values(codes[e * N + cols], scales[e * N + cols])
+        ref, big = xv[s] @ wv.T, xv[s].abs() @ wv.abs().T
+        assert bool(((C[s][:, cols].double() - ref).abs() <= 2e-6 * big + 2.0 ** -8 * ref.abs()).all()), e
+
+
+def test_weight_gradient_over_more_tiles_than_are_looked_up_at_once(metis):
+    T, E, N, K = 300, 2, 28416, 28672
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, dy = (torch.randn((T, n), generator=g, device="cuda").to(torch.bfloat16) for n in (K, N))
+    plan = metis.dispatch((torch.rand((T, 1), generator=g, device="cuda") < 0.4).to(torch.int32), E)
+    dW = torch.full((E * N, K), float("nan"), dtype=torch.bfloat16, device="cuda")
+    metis.experts_wgrad(dy, x, plan, dW, gather=True)
+    ends = plan.offsets.tolist()
+    assert min(ends[1], T - ends[1]) > 64
+    rows = torch.cat((torch.arange(300, device="cuda"), torch.randint(0, N, (300,), generator=g, device="cuda"), torch.arange(N - 300, N, device="cuda")))
+    for e in range(E):
+        s = torch.arange(ends[e], ends[e + 1], device="cuda")
+        pad = (0, 0, 0, -len(s) % 32)
+        q = [torch.nn.functional.pad(t, pad).t().contiguous() for t in (dy[s][:, rows], x[plan.token[s].long()])]
+        v = [_values(m.codes, m.scales) for m in (metis.quantize_mx(t, metis.MxTensor(*t.shape)) for t in q)]
+        ref, big = v[0] @ v[1].T, v[0].abs() @ v[1].abs().T
+        got = dW[e * N + rows].double()
+        assert bool(torch.isfinite(got).all()) and bool(((got - ref).abs() <= 2e-6 * big + 2.0 ** -8 * ref.abs()).all()), e
