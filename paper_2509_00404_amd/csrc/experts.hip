@@ -434,6 +434,41 @@ k_quantize_rows(const T* __restrict__ A, int64_t ld, int64_t K, uint64_t total, 
     }
 }
 
+#define PARTS_MAX 8
+// The parts of a contraction (sums of part p: rows p S and on of P, ld columns, a multiple of 4) added up in their order; slots from the end of
+// the experts' on get zeros.
+template <typename OUT>
+__global__ void __launch_bounds__(256)
+k_experts_join(const float* __restrict__ P, int64_t ld, int parts, const int32_t* __restrict__ offsets, int E, int64_t S, int64_t N, uint64_t total,
+             FastDiv quads, OUT* __restrict__ C, int64_t ldc, bool vec) {
+    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= total) return;
+    const int64_t row = (int64_t)div_by(quads, n), c = 4 * (int64_t)(n - (uint64_t)row * quads.d);
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (row < held(offsets[E], S)) {
+        const float* p = P + row * ld + c;
+        ew_f4 x[PARTS_MAX] = {};
+#pragma unroll
+        for (int i = 0; i < PARTS_MAX; ++i, p += S * ld)
+            if (i < parts) x[i] = *reinterpret_cast<const ew_f4*>(p);     // all on their way at once
+#pragma unroll
+        for (int i = 0; i < PARTS_MAX; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += x[i][j];
+    }
+    OUT* q = C + row * ldc + c;
+    if (vec && c + 4 <= N) {
+        mx_put4(q, v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < N) {
+                if constexpr (sizeof(OUT) == 2) q[i] = (bf16_t)pack_bf16(v[i], 0.0f);
+                else q[i] = v[i];
+            }
+    }
+}
+
 int experts_plan_status(const metis_expert_plan* p) {
     if (!p || !p->offsets || p->tokens < 0 || p->k < 1 || p->experts < 1) return METIS_INVALID_ARG;
     if (p->experts > EXPERTS_MAX || p->k > 16) return METIS_UNSUPPORTED;
@@ -473,16 +508,40 @@ bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
     if (arows * (Kp / 2) > 0xFFFFFFFFll || K > (1 << 24) || most_units(S, E, 256) * ceil_div64(N, 256) > 0x3FFFFFFF) return false;
     return S >= 16 * (int64_t)E;
 }
+// A streamed product whose tiles (as many as evenly filled experts have) fill half the chip or less has its contraction cut into parts, where
+// the units that a tile is spared (1.1 us each, 1.6 where all CUs fetch other weights) outweigh the launch that joins them (5 us) and what
+// the sums are written and read at.  us, cut / whole: 4 experts of 4096 x 14336, 64 slots each 44 / 79; 8 of 512 x 8192, 350 slots
+// 39 / 64; 64 of 128 x 7520, 114 slots 40 / 60; 16 of 1024 x 4096, 64 slots 28 / 32; 8 of 1384 x 5312, 345 slots 47 / 51; and those left whole:
+// 4 of 1024 x 4096, 1500 slots 48 / 43; 8 of 1024 x 2048, 150 slots 27 / 24.  Parts of 3 and 6 units at least: as 4; 1 to 2 us slower.
+#define PART_LEAST 4                              // units
+int64_t parts_ld(int64_t N) { return (N + 3) / 4 * 4; }
+struct Parts {
+    int count, units;                             // count 1: not cut
+};
+Parts product_parts(int64_t S, int E, int64_t N, int64_t K) {
+    const int64_t units = (K + 255) / 256, tiles = E * ceil_div64(S, 256 * (int64_t)E) * ceil_div64(N, 256);
+    const int64_t room = 256 / tiles, most = units / PART_LEAST, want = room < most ? room : most;
+    if (want < 2) return {1, (int)units};
+    const int64_t per = ceil_div64(units, want < PARTS_MAX ? want : PARTS_MAX);
+    const int64_t count = ceil_div64(units, per);
+    if (2 * (units - per - 6) < (count * S * N) >> 20) return {1, (int)units};
+    return {(int)count, (int)per};
+}
 struct ProductPlace {
     int64_t Kp;                                   // K as the quantized rows have it
-    size_t scales, wscales, bytes;                // places of the rows' scales and of the weights', and the end
+    size_t scales, wscales, parts, bytes;         // places of the rows' scales, of the weights' and of the parts' sums, and the end
+    Parts cut;
 };
 // (a tile reads the scales of 256 rows wherever its own end)
 ProductPlace product_place(bool stream, int64_t rows, int64_t S, int E, int64_t N, int64_t K) {
     const int64_t Kp = stream ? (K + 255) / 256 * 256 : K;
-    ProductPlace p = {Kp, align_up((size_t)rows * Kp / 2, 256), 0, 0};
+    ProductPlace p = {Kp, align_up((size_t)rows * Kp / 2, 256), 0, 0, 0, {1, 0}};
     p.wscales = p.bytes = p.scales + align_up((size_t)(stream ? S : rows) * Kp / 32, 256);
-    if (stream) p.bytes = p.wscales + 2048 + align_up((size_t)E * N * Kp / 32, 256) + 2048;
+    if (stream) {
+        p.cut = product_parts(S, E, N, K);
+        p.parts = p.bytes = p.wscales + 2048 + align_up((size_t)E * N * Kp / 32, 256) + 2048;
+        if (p.cut.count > 1) p.bytes += (size_t)p.cut.count * S * parts_ld(N) * 4;
+    }
     return p;
 }
 template <bool UNITS>
@@ -512,9 +571,10 @@ int launch_stream(hipStream_t s, const ExStream& a, int64_t tiles, metis_mat* C,
         return METIS_OK;
     };
     static LdsLimitCache lds_set[2];
-    if constexpr (MODE == EX_WGRAD)
+    if constexpr (MODE != EX_PRODUCT)
         if (!past) return launch(k_experts_stream<OUT, MODE, false>, lds_set[0]);
-    return launch(k_experts_stream<OUT, MODE, true>, lds_set[1]);
+    if constexpr (MODE != EX_PARTS) return launch(k_experts_stream<OUT, MODE, true>, lds_set[1]);
+    return METIS_INVALID_ARG;
 }
 
 }  // namespace
@@ -556,8 +616,29 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
         if (qs != METIS_OK) return qs;
         const int tn = (int)ceil_div64(N, 256);
         const ExStream a = {{ws, ws + place.scales}, {W->codes, ws + place.wscales + 2048}, plan->offsets, gather ? plan->token : nullptr, S,
-                            A->rows, N, K, (uint32_t)(place.Kp / 2), 8 * S, 8 * W->rows, E, 0, tn};
-        const int64_t tiles = most_units(S, E, 256) * tn;
+                            A->rows, N, K, (uint32_t)(place.Kp / 2), 8 * S, 8 * W->rows, E, 0, tn, place.cut.count, place.cut.units};
+        const int64_t tiles = most_units(S, E, 256) * tn * place.cut.count;
+        if (place.cut.count > 1) {
+            const int64_t ld = parts_ld(N), total = S * (ld / 4);
+            const int us = units_status(S, ld / 4);
+            if (us != METIS_OK) return us;
+            float* const sums = (float*)(ws + place.parts);
+            metis_mat P = *C;
+            P.ptr = sums;
+            P.ld = ld;
+            const int ss = launch_stream<float, EX_PARTS>(s, a, tiles, &P, false);
+            if (ss != METIS_OK) return ss;
+            auto join = [&](auto zero) {
+                typedef decltype(zero) OUT;
+                hipLaunchKernelGGL(k_experts_join<OUT>, dim3((unsigned)ceil_div64(total, 256)), dim3(256), 0, s, sums, ld, place.cut.count,
+                                   plan->offsets, E, S, N, (uint64_t)total, fast_div((uint32_t)(ld / 4)), (OUT*)C->ptr, C->ld,
+                                   (uintptr_t)C->ptr % (4 * sizeof(OUT)) == 0 && C->ld % 4 == 0);
+            };
+            if (C->dtype == METIS_BF16) join(bf16_t());
+            else join(float());
+            METIS_LAUNCH_CHECK();
+            return METIS_OK;
+        }
         return C->dtype == METIS_BF16 ? launch_stream<bf16_t, EX_PRODUCT>(s, a, tiles, C, true) : launch_stream<float, EX_PRODUCT>(s, a, tiles, C, true);
     }
     const int nblk = (int)(K / 32);

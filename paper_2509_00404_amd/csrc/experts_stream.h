@@ -6,6 +6,8 @@
 // one ends.  What is different is where tiles lie and how long they are, which the device alone knows:
 //   EX_PRODUCT  C[s, n]: the expert's slots against its N outputs; its last tile of slots is short.  The first operand's rows are the
 //               slots', or the tokens' by way of token[]: those of the next tile are fetched while this one is multiplied.
+//   EX_PARTS    EX_PRODUCT with the contraction cut into parts of part_units units, a tile for each: fp32 sums of part p go to rows p S and on
+//               of C, and k_experts_join adds them up.  For products whose tiles are fewer than half the chip.
 //   EX_WGRAD    dW_e[n, k] over the expert's slots: every tile whole, the contraction as long as the expert has slots.
 // A workgroup works its way through the tiles, gridDim.x apart.  Neighbouring tiles are of one expert, up to EX_BAND of its column tiles wide,
 // and every XCD works on a run of them: they share panels of both operands in its L2.
@@ -21,7 +23,7 @@
 // of lines by way of LDS: 391 for 362 with the quantizers, gradients 546 for 378.
 // A wave whose 128 rows lie behind the tile's end multiplies nothing, and a last unit that exists in part is multiplied by steps of 64.
 #define EX_BAND 8
-enum { EX_PRODUCT = 0, EX_WGRAD = 1 };
+enum { EX_PRODUCT = 0, EX_WGRAD = 1, EX_PARTS = 2 };
 struct ExStream {
     MxRows A, B;                          // first operand (slots, or N), second (weights, or K)
     const int32_t* offsets;
@@ -32,6 +34,7 @@ struct ExStream {
     uint32_t astride;                     // product: bytes of a row of A's codes, a multiple of 128 (its tail is zeros)
     int64_t ascales, bscales;             // from one unit's scales to the next one's
     int E, tiles_m, tiles_n;              // gradient: tiles_m along N, tiles_n along K; product: tiles_n along N
+    int parts, part_units;                // EX_PARTS: the parts, none of them empty, and the units of each but the last
 };
 // Behind the two buffers a wave has room to turn 16 rows of its outputs into whole lines, every expert has two numbers, and the workgroup
 // its next tiles.
@@ -128,7 +131,7 @@ __device__ __forceinline__ void ex_store_plain(const float16_t (&acc)[4][2], flo
         }
 }
 
-// a tile: its expert, its first row in the expert and column, and the expert's first slot (product) or slots (gradient)
+// a tile: its expert, its first row in the expert and column, and the expert's first slot (product) or slots (gradient), or its part
 struct __attribute__((aligned(16))) ExTile {
     int expert, m0, n0, at;
 };
@@ -138,7 +141,7 @@ template <typename OUT, int MODE, bool PAST>
 __global__ void __launch_bounds__(512, 2)
 k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
     constexpr bool LINES = sizeof(OUT) == 2;             // outputs by way of LDS, accumulator tiles transposed
-    constexpr bool WGRAD = MODE == EX_WGRAD;
+    constexpr bool WGRAD = MODE == EX_WGRAD, PARTS = MODE == EX_PARTS;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     uint8_t* const s_stage = lds + MXS_LDS;
@@ -167,7 +170,7 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         if (e == a.E - 1) s_begin[a.E] = all > b ? all : b;
         __syncthreads();
         const int32_t n = e < a.E ? s_begin[e + 1] - b : 0;
-        int32_t mine = WGRAD ? (n > 0) | (n + SLOT_ALIGN - 1) / SLOT_ALIGN << 10 : ((n + 255) >> 8) * a.tiles_n, upto = mine;
+        int32_t mine = WGRAD ? (n > 0) | (n + SLOT_ALIGN - 1) / SLOT_ALIGN << 10 : ((n + 255) >> 8) * a.tiles_n * (PARTS ? a.parts : 1), upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int32_t o = __shfl_up(upto, d);
@@ -191,7 +194,7 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         for (int e = 0; e < a.E; ++e)                                                // experts without slots
             if (count_of(e) == 0)
                 for (int64_t r = blockIdx.x; r < a.N; r += gridDim.x) ex_clear(C + ((int64_t)e * a.N + r) * ldc, a.K, vec);
-    } else {
+    } else if constexpr (!PARTS) {
         for (int64_t r = (int64_t)begin_of(a.E) + blockIdx.x; r < a.S; r += gridDim.x)      // slots that serve no choice
             ex_clear(C + r * ldc, a.N, vec);
     }
@@ -215,10 +218,15 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
             if (first(mid) <= tile) lo = mid;
             else hi = mid;
         }
-        const int local = tile - first(lo), count = s_begin[lo + 1] - s_begin[lo], down = WGRAD ? a.tiles_m : (count + 255) >> 8;
+        const int count = s_begin[lo + 1] - s_begin[lo], down = WGRAD ? a.tiles_m : (count + 255) >> 8;
+        int local = tile - first(lo), part = 0;
+        if constexpr (PARTS) {
+            part = local / (down * a.tiles_n);
+            local -= part * (down * a.tiles_n);
+        }
         const int band = local / (EX_BAND * down), r = local - band * EX_BAND * down;
         const int left = a.tiles_n - band * EX_BAND, w = left < EX_BAND ? left : EX_BAND, tm = r / w;
-        s_list[t % (2 * EX_HALF)] = {lo, 256 * tm, 256 * (band * EX_BAND + r - tm * w), WGRAD ? count : s_begin[lo]};
+        s_list[t % (2 * EX_HALF)] = {lo, 256 * tm, 256 * (band * EX_BAND + r - tm * w), WGRAD ? count : PARTS ? part : s_begin[lo]};
     };
     fill(0);
     fill(1);
@@ -229,9 +237,12 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
                       __builtin_amdgcn_readfirstlane((int)v[2]), __builtin_amdgcn_readfirstlane((int)v[3])};
     };
 
+    auto slots_at = [&](const ExTile& t) GS_INLINE { return PARTS ? begin_of(t.expert) : t.at; };
+
     // ---- transfers
     const uint8_t *qa, *qb, *qsa, *qsb;                  // the next unit's codes, and this wave's part of its scales
     int ltile = 0, lcnt = 0, lblk = 8;                   // tile being fetched, units left of it, blocks of 32 of the unit that B has
+    bool lends = true;                                   // whether its last unit is the contraction's
     uint32_t va[4], vb[4];                               // the lane's offsets
     int32_t row_next[4];                                 // rows of A of the tile to be entered next, by this lane's place
     ExTile next;                                         // that tile
@@ -239,7 +250,7 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         next = tile_at(t < tiles ? t : tiles - 1);       // (past the end: the last one again, unused)
         if constexpr (!WGRAD) {
             const int l = gs_fresh_lane();
-            const int32_t b = next.at + next.m0, last = begin_of(next.expert + 1) - b - 1;
+            const int32_t b = slots_at(next) + next.m0, last = begin_of(next.expert + 1) - b - 1;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int row = 32 * wave + 8 * v + (l >> 3);
@@ -277,9 +288,18 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
             const uint32_t cs = (uint32_t)(a.K / 2);
             lcnt = (int)((a.K + 255) >> 8);
             qa = a.A.codes;
-            qsa = a.A.scales + 8 * (int64_t)(next.at + m0 + 32 * wave);
+            qsa = a.A.scales + 8 * (int64_t)(slots_at(next) + m0 + 32 * wave);
             qb = a.B.codes + w0 * cs;
             qsb = a.B.scales + 8 * (w0 + 32 * wave);
+            if constexpr (PARTS) {
+                const int u0 = next.at * a.part_units, left = lcnt - u0;
+                lends = left <= a.part_units;
+                lcnt = lends ? left : a.part_units;
+                qa += (int64_t)u0 * (MX_KI / 2);
+                qb += (int64_t)u0 * (MX_KI / 2);
+                qsa += u0 * a.ascales;
+                qsb += u0 * a.bscales;
+            }
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int row = 32 * wave + 8 * v + (l >> 3);
@@ -296,7 +316,7 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         --lcnt;
         // B's codes end with the contraction: what lies behind is some other row's, or nobody's.  A's rows are padded, the gradient's
         // operands have room behind them.
-        lblk = !WGRAD && lcnt == 0 ? (int)((a.K >> 5) - 8 * (((a.K + 255) >> 8) - 1)) : 8;
+        lblk = !WGRAD && lcnt == 0 && lends ? (int)((a.K >> 5) - 8 * (((a.K + 255) >> 8) - 1)) : 8;
         qa = gs_uniform(qa);
         qb = gs_uniform(qb);
         qsa = gs_uniform(qsa);
@@ -407,8 +427,14 @@ k_experts_stream(ExStream a, OUT* __restrict__ C, int64_t ldc, bool vec) {
         // the half of the ring that the tiles before have left, which no wave reads any more
         if (t > EX_HALF && t % EX_HALF == 1) fill(t / EX_HALF + 1);
         const ExTile now = tile_at(t);
-        const int64_t base = WGRAD ? (int64_t)now.expert * a.N : (int64_t)now.at;
-        const int64_t rows = WGRAD ? a.N : (int64_t)(begin_of(now.expert + 1) - now.at), con = WGRAD ? (int64_t)now.at : a.K;
+        const int64_t base = WGRAD ? (int64_t)now.expert * a.N : (int64_t)slots_at(now) + (PARTS ? now.at * a.S : 0);
+        const int64_t rows = WGRAD ? a.N : (int64_t)(begin_of(now.expert + 1) - slots_at(now));
+        int64_t con = WGRAD ? (int64_t)now.at : a.K;
+        if constexpr (PARTS) {
+            const int64_t long_ = 256 * (int64_t)a.part_units;
+            con -= now.at * long_;
+            con = con < long_ ? con : long_;
+        }
         const int niter = (int)((con + 255) >> 8);
         const int64_t r = now.m0 + 128 * wa, c = now.n0 + 64 * wb, N = WGRAD ? a.K : a.N;
         const bool busy = r < rows && c < N;

@@ -53,6 +53,8 @@ def _calls(metis):
         "product, one token": (product(1, 64, 4, 2048, 4096, 1, metis.BF16), 1),
         "product, few slots": (product(100, 64, 4, 2048, 4096, 0, metis.F32), 2),
         "product, many slots": (product(4000, 16, 4, 2048, 1056, 1, metis.BF16), 2),
+        "product, contraction in parts, bf16": (product(256, 16, 4, 1024, 4096, 1, metis.BF16), 3),
+        "product, contraction in parts, fp32": (product(256, 16, 4, 1024, 4096, 0, metis.F32), 3),
         "weight gradient, bf16": (wgrad(metis.BF16), 3), "weight gradient, fp32": (wgrad(metis.F32), 3),
         "weight gradient, few slots, bf16": (wgrad(metis.BF16, 100), 3), "weight gradient, few slots, fp32": (wgrad(metis.F32, 100), 3),
         "weights transposed": (lambda: L.metis_quantize_mx_t(None, mat(4 * 512, 1024), 4, ref(metis.MxFp4(FAKE, FAKE, 4 * 1024, 512))), 1),
