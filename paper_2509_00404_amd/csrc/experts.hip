@@ -22,11 +22,26 @@ namespace {
 // workgroup has 64 rows of 512 columns, and its lanes store by themselves.
 // What bounds it: memory.  32768 x 4096 gathered rows, 339 MB to be moved, take 55 us, x 2048 by slot (170 MB) 36.  (Loads in branches, 16
 // bytes of a column stored at a time and scales byte by byte: 140 and 103.)
+// Both operands of a gradient go in one launch, side by side along the columns: every workgroup takes up one of the two, `side`.
+struct TurnSide {
+    const void* A;
+    const int32_t* token;
+    uint8_t* codes;
+    uint8_t* scales;
+    int64_t ld, arows, cols;
+    uint32_t blocks;                          // workgroups along its columns
+};
 #define QT_ROW 144                            // a column's 8 blocks of 16 bytes, and 16 that spread the columns over the banks
 template <typename T, bool FLAT>
 __global__ void __launch_bounds__(512)
-k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols, const int32_t* __restrict__ offsets, int E, int64_t S,
-                const int32_t* __restrict__ token, int64_t rows, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+k_quantize_mx_t(TurnSide one, TurnSide two, const int32_t* __restrict__ offsets, int E, int64_t S, int64_t rows) {
+    const bool other = blockIdx.x >= one.blocks;
+    const T* __restrict__ A = (const T*)(other ? two.A : one.A);
+    const int32_t* __restrict__ token = other ? two.token : one.token;
+    uint8_t* __restrict__ codes = other ? two.codes : one.codes;
+    uint8_t* __restrict__ scales = other ? two.scales : one.scales;
+    const int64_t ld = other ? two.ld : one.ld, arows = other ? two.arows : one.arows, cols = other ? two.cols : one.cols;
+    const uint32_t bx = other ? blockIdx.x - one.blocks : blockIdx.x;
     __shared__ __attribute__((aligned(16))) uint8_t s_codes[FLAT ? 16 : 128 * QT_ROW];
     __shared__ __attribute__((aligned(16))) uint8_t s_scales[FLAT ? 8 : 128 * 8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -49,7 +64,7 @@ k_quantize_mx_t(const T* __restrict__ A, int64_t ld, int64_t arows, int64_t cols
         base = begin * cols;
         first = (unit - g * per) * SLOT_ALIGN;
     }
-    const int64_t col0 = FLAT ? (int64_t)blockIdx.x * 512 + 128 * (wave >> 1) : (int64_t)blockIdx.x * 128, col = col0 + 2 * lane;
+    const int64_t col0 = FLAT ? (int64_t)bx * 512 + 128 * (wave >> 1) : (int64_t)bx * 128, col = col0 + 2 * lane;
     const int64_t from = first + 32 * (FLAT ? wave & 1 : wave);
     if (FLAT && col0 >= cols) return;
     if (from < written) {
@@ -479,20 +494,19 @@ int experts_plan_status(const metis_expert_plan* p) {
 // 400) 176 / 256, 17 of 128 (80 x 3240) 42 / 75, 112 of 160 (128 x 6888) 178 / 211, 150 of 64 (2048 x 4096) 263 / 224; fp32, 31 of 64 (1384 x
 // 2456) 238 / 240, 100 of 64 (1024 x 2040) 184 / 162.
 bool wgrad_short(int64_t S, int E, int dtype) { return S < (dtype == METIS_BF16 ? 128 : 64) * (int64_t)E; }
-// quantize A^T by segments of a plan (token may be null) or of `rows` rows
-int launch_quantize_mx_t(hipStream_t s, const metis_mat* A, const metis_expert_plan* p, bool gather, bool flat, int64_t rows, uint8_t* codes,
-                         uint8_t* scales) {
+// quantize A^T, and B^T of the same rows and type where there is a B, by segments of a plan (gathered where a token list is there) or of `rows` rows
+TurnSide turn_side(const metis_mat* A, const int32_t* token, bool flat, uint8_t* codes, uint8_t* scales) {
+    return {A->ptr, token, codes, scales, A->ld, A->rows, A->cols, (uint32_t)ceil_div64(A->cols, flat ? 512 : 128)};
+}
+int launch_quantize_mx_t(hipStream_t s, const TurnSide& one, const TurnSide& two, int dtype, const metis_expert_plan* p, bool flat, int64_t rows) {
     const int64_t S = p ? p->tokens * p->k : 0;
-    const int64_t units = p ? most_units(S, p->experts, flat ? 64 : SLOT_ALIGN) : A->rows / rows * ceil_div64(rows, SLOT_ALIGN);
+    const int64_t units = p ? most_units(S, p->experts, flat ? 64 : SLOT_ALIGN) : one.arows / rows * ceil_div64(rows, SLOT_ALIGN);
     const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
-    const dim3 grid((unsigned)ceil_div64(A->cols, flat ? 512 : 128), (unsigned)gy, (unsigned)gz);
-    if (gz > 65535 || A->rows > 0x7FFFFFFF) return METIS_UNSUPPORTED;
-    auto launch = [&](auto kern, auto zero) {
-        hipLaunchKernelGGL(kern, grid, dim3(512), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->rows, A->cols, p ? p->offsets : nullptr,
-                           p ? p->experts : 0, S, gather ? p->token : nullptr, rows, codes, scales);
-    };
-    if (A->dtype == METIS_BF16) flat ? launch(k_quantize_mx_t<bf16_t, true>, bf16_t()) : launch(k_quantize_mx_t<bf16_t, false>, bf16_t());
-    else flat ? launch(k_quantize_mx_t<float, true>, float()) : launch(k_quantize_mx_t<float, false>, float());
+    const dim3 grid(one.blocks + two.blocks, (unsigned)gy, (unsigned)gz);
+    if (gz > 65535 || one.arows > 0x7FFFFFFF || two.arows > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, s, one, two, p ? p->offsets : nullptr, p ? p->experts : 0, S, rows); };
+    if (dtype == METIS_BF16) flat ? launch(k_quantize_mx_t<bf16_t, true>) : launch(k_quantize_mx_t<bf16_t, false>);
+    else flat ? launch(k_quantize_mx_t<float, true>) : launch(k_quantize_mx_t<float, false>);
     METIS_LAUNCH_CHECK();
     return METIS_OK;
 }
@@ -584,7 +598,8 @@ extern "C" int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups,
     if (A->rows % groups || A->rows / groups % 32 || A->cols % 8 || A->ld < A->cols || !mat_aligned16(A) || (uintptr_t)out->codes % 16 ||
         out->rows != groups * A->cols || out->cols != A->rows / groups)
         return METIS_BAD_SHAPE;
-    return launch_quantize_mx_t((hipStream_t)stream, A, nullptr, false, false, A->rows / groups, out->codes, out->scales);
+    return launch_quantize_mx_t((hipStream_t)stream, turn_side(A, nullptr, false, out->codes, out->scales), {}, A->dtype, nullptr, false,
+                                A->rows / groups);
 }
 
 extern "C" size_t metis_experts_workspace_bytes(int64_t rows, int64_t slots, int experts, int64_t N, int64_t K) {
@@ -716,8 +731,11 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
     hipStream_t s = (hipStream_t)stream;
     const bool brief = wgrad_short(S, (int)E, dW->dtype);
     if (S > 0) {
-        int r = launch_quantize_mx_t(s, G, plan, false, brief, 0, (uint8_t*)g.codes, (uint8_t*)g.scales);
-        if (r == METIS_OK) r = launch_quantize_mx_t(s, X, plan, gather != 0, brief, 0, (uint8_t*)x.codes, (uint8_t*)x.scales);
+        const TurnSide sg = turn_side(G, nullptr, brief, (uint8_t*)g.codes, (uint8_t*)g.scales);
+        const TurnSide sx = turn_side(X, gather ? plan->token : nullptr, brief, (uint8_t*)x.codes, (uint8_t*)x.scales);
+        const bool same = G->dtype == X->dtype;
+        int r = launch_quantize_mx_t(s, sg, same ? sx : TurnSide{}, G->dtype, plan, brief, 0);
+        if (r == METIS_OK && !same) r = launch_quantize_mx_t(s, sx, {}, X->dtype, plan, brief, 0);
         if (r != METIS_OK) return r;
     }
     const bool past = (uintptr_t)dW->ptr % 128 == 0 && dW->ld * mat_size(dW) % 128 == 0;

@@ -43,8 +43,8 @@ def _calls(metis):
         w = ref(metis.MxFp4(FAKE, FAKE, E * N, K))
         return lambda: L.metis_experts_product(None, mat(T if gather else T * k, K), w, plan(T, E, k), gather, mat(T * k, N, out), FAKE, 1 << 40)
 
-    def wgrad(out, T=1000):
-        return lambda: L.metis_experts_wgrad(None, mat(4 * T, 512), mat(T, 1024), plan(T, 16, 4), 1, mat(16 * 512, 1024, out), FAKE, 1 << 40)
+    def wgrad(out, T=1000, g=metis.BF16):
+        return lambda: L.metis_experts_wgrad(None, mat(4 * T, 512, g), mat(T, 1024), plan(T, 16, 4), 1, mat(16 * 512, 1024, out), FAKE, 1 << 40)
 
     mx8 = lambda rows, cols: ref(metis.Mx8(FAKE, FAKE, rows, cols))
     return {
@@ -55,8 +55,9 @@ def _calls(metis):
         "product, many slots": (product(4000, 16, 4, 2048, 1056, 1, metis.BF16), 2),
         "product, contraction in parts, bf16": (product(256, 16, 4, 1024, 4096, 1, metis.BF16), 3),
         "product, contraction in parts, fp32": (product(256, 16, 4, 1024, 4096, 0, metis.F32), 3),
-        "weight gradient, bf16": (wgrad(metis.BF16), 3), "weight gradient, fp32": (wgrad(metis.F32), 3),
-        "weight gradient, few slots, bf16": (wgrad(metis.BF16, 100), 3), "weight gradient, few slots, fp32": (wgrad(metis.F32, 100), 3),
+        "weight gradient, bf16": (wgrad(metis.BF16), 2), "weight gradient, fp32": (wgrad(metis.F32), 2),
+        "weight gradient, operands of two types": (wgrad(metis.BF16, g=metis.F32), 3),
+        "weight gradient, few slots, bf16": (wgrad(metis.BF16, 100), 2), "weight gradient, few slots, fp32": (wgrad(metis.F32, 100), 2),
         "weights transposed": (lambda: L.metis_quantize_mx_t(None, mat(4 * 512, 1024), 4, ref(metis.MxFp4(FAKE, FAKE, 4 * 1024, 512))), 1),
         "combine": (lambda: L.metis_combine(None, mat(400, 512), plan(100, 16, 4), FAKE, mat(100, 512, metis.F32)), 1),
         "combine gradients": (lambda: L.metis_combine_grads(None, mat(100, 512), mat(400, 512), plan(100, 16, 4), FAKE, mat(400, 512), FAKE), 1),

@@ -142,6 +142,20 @@ def test_weight_gradient(metis, T, E, k, N, K, skew, missing, gather, dtype, out
         assert torch.isnan(dW[:, :pad]).all()
 
 
+@pytest.mark.parametrize("T", [40, 900])
+@pytest.mark.parametrize("gt,xt", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+def test_weight_gradient_of_two_types(metis, T, gt, xt):
+    E, k, N, K = 5, 2, 136, 328
+    plan, g = _plan(metis, T, E, k, T, 0.3, 0.1)
+    x, dy = _dense(g, T, K, xt), _dense(g, T * k, N, gt)
+    offsets, token = plan.offsets.cpu().numpy(), plan.token.cpu().numpy()
+    ref = oe.experts_wgrad(dy.double().numpy(), x.double().numpy(), offsets, token, True)
+    big = oe.experts_wgrad(dy.double().abs().numpy(), x.double().abs().numpy(), offsets, token, True)
+    dW = torch.full((E * N, K), float("nan"), device="cuda")
+    metis.experts_wgrad(dy.cuda(), x.cuda(), plan, dW, gather=True)
+    _check(dW, ref, big, torch.float32)
+
+
 def test_no_tokens(metis):
     plan = metis.dispatch(torch.empty((0, 2), dtype=torch.int32, device="cuda"), 8)
     e = lambda n: torch.empty((0, n), dtype=torch.bfloat16, device="cuda")
