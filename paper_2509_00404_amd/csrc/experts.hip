@@ -490,9 +490,9 @@ int experts_plan_status(const metis_expert_plan* p) {
     if (p->tokens > 0x7FFFFFFFll / p->k) return METIS_BAD_SHAPE;
     return METIS_OK;
 }
-// Gradients of few slots an expert go without the stream.  us with the quantizers, without / with it: bf16, 2 slots an expert of 256 (2464 x
-// 400) 176 / 256, 17 of 128 (80 x 3240) 42 / 75, 112 of 160 (128 x 6888) 178 / 211, 150 of 64 (2048 x 4096) 263 / 224; fp32, 31 of 64 (1384 x
-// 2456) 238 / 240, 100 of 64 (1024 x 2040) 184 / 162.
+// Gradients of few slots an expert go without the stream.  us with the quantizer, without / with it: bf16, 2 slots an expert of 256 (2464 x
+// 400) 182 / 257, 17 of 128 (80 x 3240) 38 / 72, 112 of 160 (128 x 6888) 174 / 211, 150 of 64 (2048 x 4096) 253 / 213; fp32, 31 of 64 (1384 x
+// 2456) 258 / 252, 100 of 64 (1024 x 2040) 182 / 154.
 bool wgrad_short(int64_t S, int E, int dtype) { return S < (dtype == METIS_BF16 ? 128 : 64) * (int64_t)E; }
 // quantize A^T, and B^T of the same rows and type where there is a B, by segments of a plan (gathered where a token list is there) or of `rows` rows
 TurnSide turn_side(const metis_mat* A, const int32_t* token, bool flat, uint8_t* codes, uint8_t* scales) {
