@@ -517,10 +517,13 @@ size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * col
 // The stream takes products of 16 slots an expert and more; what it cannot address, and fewer, goes straight from memory.  us, from memory /
 // streamed, 2048 x 4096 with 64 experts of which a token takes four: 24 tokens 27 / 51 (4096 x 1024), 64 64 / 78, 200 74 / 80, 400 89 / 82, 1000
 // 161 / 86.
+// And so do products of less than 2^20 outputs and 2^31 multiplications, which end before the stream has begun in earnest: from memory / streamed, 64
+// experts of 136 x 5376, 35 slots each 20 / 27; 8 of 1024 x 4096, 40 slots 18 / 24; 2 of 512 x 8192, 150 slots 18 / 26; 1 of 256 x 2048, 2000 slots
+// 18 / 25; 96 of 72 x 800, 92 slots 18 / 21; and beyond: 2.0 M outputs of 992 22 / 21, 8.2 M of 256 31 / 20; 2048 x 7168, 40 slots 35 / 30.
 bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
     const int64_t Kp = (K + 255) / 256 * 256;
     if (arows * (Kp / 2) > 0xFFFFFFFFll || K > (1 << 24) || most_units(S, E, 256) * ceil_div64(N, 256) > 0x3FFFFFFF) return false;
-    return S >= 16 * (int64_t)E;
+    return S >= 16 * (int64_t)E && (S * N >= (1 << 20) || S * N >= (1ll << 31) / K);
 }
 // A streamed product whose tiles (as many as evenly filled experts have) fill half the chip or less has its contraction cut into parts, where
 // the units that a tile is spared (1.1 us each, 1.6 where all CUs fetch other weights) outweigh the launch that joins them (5 us) and what

@@ -62,6 +62,10 @@ CASES = [  # T, E, k, N, K, skew, missing
     (9, 8, 2, 1030, 2080, 0.5, 0.1),
     (60, 16, 4, 200, 992, 0.9, 0.0),                           # few slots, too many to quantize on the spot
     (100, 8, 2, 140, 1056, 0.3, 0.0),
+    (1100, 4, 2, 520, 160, 0.8, 0.1),                          # enough outputs for the stream, whatever the contraction
+    (2200, 2, 1, 513, 544, 0.0, 0.0),
+    (900, 60, 6, 203, 96, 0.9, 0.05),
+    (4200, 3, 1, 264, 1056, 0.3, 0.0),
     (64, 8, 2, 136, 256, 0.0, 1.0),                            # nobody has an expert
 ]
 

@@ -20,12 +20,12 @@ def metis():
 
 
 CASES = [  # T, E, k, N, K, skew, missing
-    (200, 4, 2, 260, 4096, 0.0, 0.0),
-    (70, 2, 1, 130, 14304, 0.0, 0.0),                          # as many parts as there are at most, the last unit short
-    (300, 8, 2, 513, 3680, 0.8, 0.2),                          # an expert without slots, slots without an expert
-    (520, 1, 1, 64, 3104, 0.0, 0.0),                           # the last part's units fewer; a unit of one block
-    (64, 4, 4, 1, 8352, 0.0, 0.0),
-    (128, 3, 2, 40, 4640, 0.0, 1.0),                           # nobody has an expert
+    (600, 4, 2, 514, 4096, 0.0, 0.0),
+    (300, 2, 1, 513, 14304, 0.0, 0.0),                         # as many parts as there are at most, the last unit short
+    (900, 8, 2, 330, 3680, 0.8, 0.2),                          # an expert without slots, slots without an expert
+    (2100, 1, 1, 344, 3104, 0.0, 0.0),                          # the last part's units fewer; a unit of one block
+    (2000, 4, 4, 33, 8352, 0.0, 0.0),
+    (640, 3, 2, 400, 4640, 0.0, 1.0),                          # nobody has an expert
     (5000, 120, 6, 64, 4096, 0.9, 0.0),                        # more tiles than the chip has CUs
 ]
 
