@@ -34,7 +34,7 @@ struct TurnSide {
 #define QT_ROW 144                            // a column's 8 blocks of 16 bytes, and 16 that spread the columns over the banks
 template <typename T, bool FLAT>
 __global__ void __launch_bounds__(512)
-k_quantize_mx_t(TurnSide one, TurnSide two, const int32_t* __restrict__ offsets, int E, int64_t S, int64_t rows) {
+k_quantize_mx_t(TurnSide one, TurnSide two, const int32_t* __restrict__ offsets, int E, int64_t S, int64_t rows, int64_t units) {
     const bool other = blockIdx.x >= one.blocks;
     const T* __restrict__ A = (const T*)(other ? two.A : one.A);
     const int32_t* __restrict__ token = other ? two.token : one.token;
@@ -46,6 +46,7 @@ k_quantize_mx_t(TurnSide one, TurnSide two, const int32_t* __restrict__ offsets,
     __shared__ __attribute__((aligned(16))) uint8_t s_scales[FLAT ? 8 : 128 * 8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t unit = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
+    if (unit >= units) return;            // gridDim.y and z multiply to more than there are
     int64_t begin, count, stride, written, base, first;   // the segment's rows, the length of its result's rows and what is written of them, its place; the unit's first row
     if (FLAT || offsets) {
         constexpr int UNIT = FLAT ? 64 : SLOT_ALIGN;
@@ -504,7 +505,7 @@ int launch_quantize_mx_t(hipStream_t s, const TurnSide& one, const TurnSide& two
     const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
     const dim3 grid(one.blocks + two.blocks, (unsigned)gy, (unsigned)gz);
     if (gz > 65535 || one.arows > 0x7FFFFFFF || two.arows > 0x7FFFFFFF) return METIS_UNSUPPORTED;
-    auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, s, one, two, p ? p->offsets : nullptr, p ? p->experts : 0, S, rows); };
+    auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, s, one, two, p ? p->offsets : nullptr, p ? p->experts : 0, S, rows, units); };
     if (dtype == METIS_BF16) flat ? launch(k_quantize_mx_t<bf16_t, true>) : launch(k_quantize_mx_t<bf16_t, false>);
     else flat ? launch(k_quantize_mx_t<float, true>) : launch(k_quantize_mx_t<float, false>);
     METIS_LAUNCH_CHECK();
