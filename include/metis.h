@@ -456,6 +456,8 @@ int metis_dispatch(void* stream, const int32_t* idx, metis_expert_plan* plan, vo
  * other (rows = experts * N, cols = K).  A (bf16 or fp32) is quantized to MXFP4 on the way, as metis_quantize_mx does; the products are exact
  * and accumulate in fp32.  C: bf16 or fp32; its rows of slots that serve no choice become 0.  With W of metis_quantize_mx_t this is the input gradient.
  * The plan is read on the device: its offsets, and token and slot with gather.
+ * Offsets that do not ascend are read as their running maximum, held to 0 .. S, and tokens and slots outside the rows are not followed: no plan,
+ * whatever is in it, leads outside the operands.
  *   K % 32 == 0; A's rows 16-byte aligned; W's codes 16-byte, scales 8-byte aligned; workspace 256-byte aligned, metis_experts_workspace_bytes(A->rows, S, ...) bytes.
  * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (experts > 512, k > 16,
  * K > 2^28, a grid of more than 2^31 - 1 workgroups).

@@ -9,10 +9,13 @@ namespace {
 
 // Where unit u lies when every expert's slots are cut into units of `size` (the last of an expert may be short, an expert without slots has
 // none): the expert, its slots, and the unit's number among its own.  expert = -1 behind the last unit; `total` = units in all.  Every
-// wave looks for itself, its lanes holding up to eight neighbouring experts; offsets are held to 0 <= o <= S, whatever the memory says.
+// wave looks for itself, its lanes holding up to eight neighbouring experts.  Offsets are held to 0 <= o <= S and to ascend, whatever the
+// memory says: one that is smaller than one before it counts as the largest before it, so that segments never overlap and all of them
+// together are at most S slots.  (Whether any descends is one ballot; the scan that mends it runs only then.)
 struct SlotUnit {
     int expert, local, total;
     int64_t begin, end;                   // the expert's slots
+    int64_t used;                         // the end of all experts' slots
 };
 __device__ __forceinline__ int64_t held(int32_t o, int64_t S) { return o < 0 ? 0 : o > S ? S : o; }
 __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offsets, int E, int64_t S, int size, int64_t u) {
@@ -25,8 +28,25 @@ __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offset
         o[i] = offsets[e < E ? e : E];
     }
     int mine = 0;
+    bool descends = false;
 #pragma unroll
-    for (int i = 0; i <= Q; ++i) o[i] = (int32_t)held(o[i], S);
+    for (int i = 0; i <= Q; ++i) {
+        o[i] = (int32_t)held(o[i], S);
+        descends |= i > 0 && o[i] < o[i > 0 ? i - 1 : 0];
+    }
+    if (__any(descends)) {
+#pragma unroll
+        for (int i = 1; i <= Q; ++i) o[i] = o[i] > o[i - 1] ? o[i] : o[i - 1];
+        int32_t top = o[Q];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int32_t a = __shfl_up(top, d);
+            if (lane >= d && a > top) top = a;
+        }
+        const int32_t before = __shfl_up(top, 1);
+#pragma unroll
+        for (int i = 0; i <= Q; ++i) o[i] = lane > 0 && before > o[i] ? before : o[i];
+    }
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
         const int32_t n = o[i + 1] - o[i];
@@ -43,6 +63,7 @@ __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offset
     r.expert = -1;
     r.local = 0;
     r.begin = r.end = 0;
+    r.used = __builtin_amdgcn_readlane(o[Q], 63);
     if (u >= r.total) return r;
     // every lane looks through its own experts, and the one that has the unit says where
     int before = upto - mine, expert = 0, local = 0, begin = 0, end = 0;
@@ -63,8 +84,11 @@ __device__ __forceinline__ SlotUnit find_unit(const int32_t* __restrict__ offset
     r.end = __builtin_amdgcn_readlane(end, at);
     return r;
 }
-// units of `size` of the experts before e
-__device__ __forceinline__ int64_t units_before(const int32_t* __restrict__ offsets, int E, int64_t S, int size, int e) {
+// expert e's slots, and the units of `size` of the experts before it (offsets held as above)
+struct ExpertSlots {
+    int64_t units_before, count;
+};
+__device__ __forceinline__ ExpertSlots slots_of(const int32_t* __restrict__ offsets, int E, int64_t S, int size, int e) {
     constexpr int Q = EXPERTS_MAX / 64;
     const int lane = (int)threadIdx.x & 63;
     int32_t o[Q][2];
@@ -74,15 +98,30 @@ __device__ __forceinline__ int64_t units_before(const int32_t* __restrict__ offs
         o[i][0] = offsets[x < e ? x : e];
         o[i][1] = offsets[x < e ? x + 1 : e];
     }
+    int64_t begin = held(offsets[e], S), end = held(offsets[e + 1], S);
+    bool descends = end < begin;
     int sum = 0;
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
         const int64_t n = held(o[i][1], S) - held(o[i][0], S);
+        descends |= n < 0;
         if (n > 0) sum += (int)((n + size - 1) / size);
+    }
+    if (__any(descends)) {
+        int64_t all = 0;
+        begin = held(offsets[0], S);
+        for (int x = 0; x < e; ++x) {
+            end = held(offsets[x + 1], S);
+            end = end > begin ? end : begin;
+            all += (end - begin + size - 1) / size;
+            begin = end;
+        }
+        end = held(offsets[e + 1], S);
+        return {all, end > begin ? end - begin : 0};
     }
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
-    return __builtin_amdgcn_readfirstlane(sum);
+    return {__builtin_amdgcn_readfirstlane(sum), end - begin};
 }
 // units of `size` that S slots can fall into
 inline int64_t most_units(int64_t S, int E, int size) { return S / size + (E < S ? E : S); }

@@ -236,8 +236,8 @@ k_experts_few(MxRows A, DenseRows dense, int64_t arows, MxRows W, const int32_t*
     const SlotUnit u = find_unit(offsets, E, S, 32, ub);
     const int64_t n0 = SPLIT ? 32 * (int64_t)nb : 128 * (int64_t)nb + 32 * wave;
     if (u.expert < 0) {                                  // behind the last unit of slots the workgroups clear the unused ones
-        const int64_t used = held(offsets[E], S), step = most - u.total, wide = SPLIT ? 32 : 128, c0 = wide * nb;
-        for (int64_t s = used + ub - u.total; s < S; s += step)
+        const int64_t step = most - u.total, wide = SPLIT ? 32 : 128, c0 = wide * nb;
+        for (int64_t s = u.used + ub - u.total; s < S; s += step)
             for (int64_t c = c0 + threadIdx.x; c < c0 + wide && c < N; c += 256) C[s * ldc + c] = OUT(0);
         return;
     }
@@ -340,9 +340,9 @@ k_experts_short(MxRows G, MxRows X, const int32_t* __restrict__ offsets, int E, 
     const uint32_t tn = blockIdx.x / tiles_k, tk = blockIdx.x - tn * tiles_k;
     const int64_t n0 = 128 * (int64_t)tn, k0 = 256 * (int64_t)tk + 64 * wave;
     if (k0 >= K) return;
-    const int64_t before = units_before(offsets, E, S, 64, e);
-    const int64_t count = held(offsets[e + 1], S) - held(offsets[e], S);
-    const int steps = count > 0 ? (int)((count + 63) >> 6) : 0;
+    const ExpertSlots own = slots_of(offsets, E, S, 64, e);
+    const int64_t before = own.units_before;
+    const int steps = (int)((own.count + 63) >> 6);
     const int64_t len = 64 * (int64_t)steps;
     float16_t acc[4][2];
 #pragma unroll
