@@ -402,7 +402,8 @@ int metis_mxfp4_gemm_nt(void* stream, const metis_mxfp4* A, const metis_mxfp4* B
  *            a softmax over the chosen logits (0 where that sum is 0).
  * Limits: 1 <= experts <= 512, 1 <= k <= 16, groups divides experts, 1 <= top_groups <= groups, k <= top_groups * experts / groups.
  * Errors: METIS_INVALID_ARG (null pointer, dtype, unknown scores, parameters outside these rules), METIS_BAD_SHAPE (logits->cols !=
- * experts, ld < cols, more than 2^31 - 1 choices), METIS_UNSUPPORTED (experts > 512, k > 16).  T = 0 is no work and no error.
+ * experts, ld < cols, more than 2^31 - 1 choices), METIS_UNSUPPORTED (experts > 512, k > 16, 2^28 - 15 tokens or more).
+ * T = 0 is no work and no error.
  */
 enum { METIS_SCORES_SOFTMAX = 0, METIS_SCORES_SIGMOID = 1 };
 typedef struct {
@@ -460,7 +461,8 @@ int metis_dispatch(void* stream, const int32_t* idx, metis_expert_plan* plan, vo
  * whatever is in it, leads outside the operands.
  *   K % 32 == 0; A's rows 16-byte aligned; W's codes 16-byte, scales 8-byte aligned; workspace 256-byte aligned, metis_experts_workspace_bytes(A->rows, S, ...) bytes.
  * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (experts > 512, k > 16,
- * K > 2^28, a grid of more than 2^31 - 1 workgroups).
+ * K > 2^28, or a launch of 2^32 threads and more: A->rows * K of 2^35, rows of W of 2^30, and, where few slots an expert go straight from memory,
+ * (S / 32 + experts) * N of some 2^31).
  */
 size_t metis_experts_workspace_bytes(int64_t rows, int64_t slots, int experts, int64_t N, int64_t K);
 int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W, const metis_expert_plan* plan, int gather, metis_mat* C,
@@ -469,7 +471,8 @@ int metis_experts_product(void* stream, const metis_mat* A, const metis_mxfp4* W
 /*
  * MXFP4 with blocks along the rows: A [groups * M, cols] (bf16 or fp32) is `groups` matrices [M, cols], each of which is transposed and
  * quantized along its M.  out [groups * cols, M].  For the input gradient the experts' stacked weights [experts * N, K] become [experts * K, N].
- * M % 32 == 0, cols % 8 == 0, A's rows and out's codes 16-byte aligned.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED.
+ * M % 32 == 0, cols % 8 == 0, A's rows and out's codes 16-byte aligned.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (2^30
+ * columns or 2^31 rows and more).
  */
 int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups, metis_mxfp4* out);
 
@@ -490,14 +493,16 @@ int metis_experts_wgrad(void* stream, const metis_mat* G, const metis_mat* X, co
  * y [tokens, D] = sum over j of weights[t, j] * rows[slot[t, j], :], in fp32, the choices in their order, rounded once.  Choices without a
  * slot add nothing.  weights: device fp32 [tokens, k], or null for ones (the input gradient of gathered rows).  rows [tokens * k, D]
  * and y: bf16 or fp32 each; any D and row strides (whole 16-byte units where both allow them).  plan->slot is read alone.
- * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (k > 16, or more than 2^28 columns).
+ * No tokens is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (k > 16, more than 2^28 columns,
+ * or y of some 2^35 elements and more).
  */
 int metis_combine(void* stream, const metis_mat* rows, const metis_expert_plan* plan, const float* weights, metis_mat* y);
 
 /*
  * Gradients of metis_combine from dy [tokens, D]: drows[slot[t, j], :] = weights[t, j] * dy[t, :], zeros in the slots that serve no
  * choice; dweights [tokens, k] (fp32) = <dy[t, :], rows[slot[t, j], :]>, 0 without a slot; the sums in fp32, in an order that depends on D
- * alone.  rows and drows share a type, dy has its own.  drows must not overlap rows.  Errors as above.
+ * alone.  rows and drows share a type, dy has its own.  drows must not overlap rows.  Errors as above; METIS_UNSUPPORTED for 2^24 tokens and more (up to
+ * 1024 columns 2^25, up to 512 2^26).
  */
 int metis_combine_grads(void* stream, const metis_mat* dy, const metis_mat* rows, const metis_expert_plan* plan, const float* weights,
                         metis_mat* drows, float* dweights);
@@ -520,7 +525,8 @@ typedef struct {
 
 /*
  * Save A [rows, cols] (bf16 or fp32) into out; restore A into out.  cols % 32 == 0; the dense matrix's rows 16-byte aligned, codes 8-byte
- * aligned.  No rows is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (rows of more than 2^28 columns).
+ * aligned.  No rows is no work.  Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (rows of more than 2^28
+ * columns, or some 2^35 elements and more).
  */
 int metis_quantize_mx8(void* stream, const metis_mat* A, metis_mx8* out);
 int metis_dequantize_mx8(void* stream, const metis_mx8* A, metis_mat* out);

@@ -138,11 +138,12 @@ k_swiglu_grads(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ sc
 }
 
 bool mx8_ok(const metis_mx8* q) { return q && q->codes && q->scales && q->rows >= 1 && q->cols >= 32 && q->cols % 32 == 0; }
-// blocks of 32 of a row in one go: 16-byte loads of A, 8-byte loads of the codes; the units of a launch fit its grid
-int mx8_status(const metis_mat* A, const metis_mx8* q) {
+// blocks of 32 of a row in one go: 16-byte loads of A, 8-byte loads of the codes; the units of a launch (a lane has one, or one of either half
+// of the row) fit its grid
+int mx8_status(const metis_mat* A, const metis_mx8* q, bool halves = false) {
     if (!mat_ok(A) || !mx8_ok(q)) return METIS_INVALID_ARG;
     if (A->rows != q->rows || A->cols != q->cols || A->ld < A->cols || !mat_aligned16(A) || (uintptr_t)q->codes % 8) return METIS_BAD_SHAPE;
-    return units_status(q->rows, q->cols / 8);
+    return units_status(q->rows, q->cols / (halves ? 16 : 8));
 }
 dim3 unit_grid(int64_t units) { return dim3((unsigned)ceil_div64(units, 256)); }
 
@@ -192,7 +193,7 @@ extern "C" int metis_swiglu(void* stream, const metis_mat* gate_up, metis_mat* a
     if (act->rows < 1 || act->cols < 32 || act->cols % 32 || gate_up->ld < gate_up->cols || !mat_aligned16(gate_up) || !half_of(act, gate_up))
         return METIS_BAD_SHAPE;
     if (saved) {
-        const int st = mx8_status(gate_up, saved);
+        const int st = mx8_status(gate_up, saved, true);
         if (st != METIS_OK) return st;
     }
     const int big = units_status(act->rows, act->cols / 8);
@@ -214,7 +215,7 @@ extern "C" int metis_swiglu(void* stream, const metis_mat* gate_up, metis_mat* a
 extern "C" int metis_swiglu_grads(void* stream, const metis_mx8* saved, const metis_mat* dact, metis_mat* dgate_up, metis_mat* act) {
     if (saved && dact && dgate_up && saved->rows == 0 && dact->rows == 0 && dgate_up->rows == 0) return METIS_OK;
     if (!mat_ok(dact) || (act && !mat_ok(act))) return METIS_INVALID_ARG;
-    const int st = mx8_status(dgate_up, saved);
+    const int st = mx8_status(dgate_up, saved, true);
     if (st != METIS_OK) return st;
     if (dact->cols < 32 || dact->cols % 32 || !half_of(dact, dgate_up) || (act && !half_of(act, dgate_up))) return METIS_BAD_SHAPE;
     const FastDiv units = fast_div((uint32_t)(dact->cols / 8));

@@ -111,8 +111,10 @@ int launch_combine_grads(hipStream_t s, const metis_mat* dy, const metis_mat* ro
                          metis_mat* drows, float* dweights) {
     const bool whole = rows->cols % 8 == 0 && mat_aligned16(rows) && mat_aligned16(drows) && mat_aligned16(dy);
     const int64_t units = ceil_div64(rows->cols, 8);
+    const int threads = units <= 64 ? 64 : units <= 128 ? 128 : 256;
+    if (!grid_fits(p->tokens, threads)) return METIS_UNSUPPORTED;
     auto kern = whole ? k_combine_grads<T, D, false, K> : k_combine_grads<T, D, true, K>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)p->tokens), dim3(units <= 64 ? 64 : units <= 128 ? 128 : 256), 0, s, (const D*)dy->ptr, dy->ld,
+    hipLaunchKernelGGL(kern, dim3((unsigned)p->tokens), dim3(threads), 0, s, (const D*)dy->ptr, dy->ld,
                        (const T*)rows->ptr, rows->ld, rows->rows, rows->cols, p->offsets, p->experts, p->slot, weights, p->k, (T*)drows->ptr,
                        drows->ld, dweights);
     METIS_LAUNCH_CHECK();

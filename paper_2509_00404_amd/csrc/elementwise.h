@@ -92,9 +92,11 @@ __device__ __forceinline__ void store_part(T* p, int64_t n, const float (&v)[8])
     }
 }
 
+// HIP takes fewer than 2^32 threads along an axis of a grid
+inline bool grid_fits(int64_t workgroups, int threads) { return workgroups <= 0xFFFFFFFFll / threads; }
 // rows of `units` that a kernel takes a lane each, 256 a workgroup: they fit its grid, and fast_div is exact
 inline int units_status(int64_t rows, int64_t units) {
-    return units > (1 << 25) || rows > (int64_t)256 * 0x7FFFFFFF / units ? METIS_UNSUPPORTED : METIS_OK;
+    return units > (1 << 25) || rows > 0xFFFFFFFFll / 256 * 256 / units ? METIS_UNSUPPORTED : METIS_OK;
 }
 inline bool mat_ok(const metis_mat* m) { return m && m->ptr && (m->dtype == METIS_BF16 || m->dtype == METIS_F32); }
 inline int64_t mat_size(const metis_mat* m) { return m->dtype == METIS_BF16 ? 2 : 4; }

@@ -504,7 +504,8 @@ int launch_quantize_mx_t(hipStream_t s, const TurnSide& one, const TurnSide& two
     const int64_t units = p ? most_units(S, p->experts, flat ? 64 : SLOT_ALIGN) : one.arows / rows * ceil_div64(rows, SLOT_ALIGN);
     const int64_t gy = units < 32768 ? units : 32768, gz = ceil_div64(units, gy);
     const dim3 grid(one.blocks + two.blocks, (unsigned)gy, (unsigned)gz);
-    if (gz > 65535 || one.arows > 0x7FFFFFFF || two.arows > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    const int64_t blocks = ceil_div64(one.cols, flat ? 512 : 128) + ceil_div64(two.cols, flat ? 512 : 128);
+    if (!grid_fits(blocks, 512) || gz > 65535 || one.arows > 0x7FFFFFFF || two.arows > 0x7FFFFFFF) return METIS_UNSUPPORTED;
     auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, s, one, two, p ? p->offsets : nullptr, p ? p->experts : 0, S, rows, units); };
     if (dtype == METIS_BF16) flat ? launch(k_quantize_mx_t<bf16_t, true>) : launch(k_quantize_mx_t<bf16_t, false>);
     else flat ? launch(k_quantize_mx_t<float, true>) : launch(k_quantize_mx_t<float, false>);
@@ -567,7 +568,7 @@ int launch_quantize_rows(hipStream_t s, const metis_mat* A, int64_t Kp, uint8_t*
     const int st = units_status(A->rows, Kp / 8);
     if (st != METIS_OK) return st;
     const int64_t total = A->rows * (Kp / 8), blocks = ceil_div64(total, 256), more = UNITS ? ceil_div64(ws.rows, 64) : 0;
-    if (blocks + more > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    if (!grid_fits(blocks + more, 256)) return METIS_UNSUPPORTED;
     const FastDiv units = fast_div((uint32_t)(Kp / 8));
     auto launch = [&](auto kern, auto zero) {
         hipLaunchKernelGGL(kern, dim3((unsigned)(blocks + more)), dim3(256), 0, s, (const decltype(zero)*)A->ptr, A->ld, A->cols, (uint64_t)total,
@@ -599,6 +600,7 @@ int launch_stream(hipStream_t s, const ExStream& a, int64_t tiles, metis_mat* C,
 
 extern "C" int metis_quantize_mx_t(void* stream, const metis_mat* A, int groups, metis_mxfp4* out) {
     if (!mat_ok(A) || !out || !out->codes || !out->scales || groups < 1 || A->rows < 1 || A->cols < 1) return METIS_INVALID_ARG;
+    if (A->cols >= 1ll << 30) return METIS_UNSUPPORTED;
     if (A->rows % groups || A->rows / groups % 32 || A->cols % 8 || A->ld < A->cols || !mat_aligned16(A) || (uintptr_t)out->codes % 16 ||
         out->rows != groups * A->cols || out->cols != A->rows / groups)
         return METIS_BAD_SHAPE;
@@ -630,6 +632,8 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     uint8_t* ws = (uint8_t*)workspace;
     hipStream_t s = (hipStream_t)stream;
     if (streams) {
+        const int us = place.cut.count > 1 ? units_status(S, parts_ld(N) / 4) : METIS_OK;
+        if (us != METIS_OK) return us;
         const int qs = launch_quantize_rows<true>(s, A, place.Kp, ws, {ws + place.scales, gather ? plan->slot : nullptr, S, gather ? plan->k : 1},
                                                   {W->scales, ws + place.wscales + 2048, W->rows, (int)(K / 32), (int)(place.Kp / 256)});
         if (qs != METIS_OK) return qs;
@@ -639,8 +643,6 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
         const int64_t tiles = most_units(S, E, 256) * tn * place.cut.count;
         if (place.cut.count > 1) {
             const int64_t ld = parts_ld(N), total = S * (ld / 4);
-            const int us = units_status(S, ld / 4);
-            if (us != METIS_OK) return us;
             float* const sums = (float*)(ws + place.parts);
             metis_mat P = *C;
             P.ptr = sums;
@@ -666,7 +668,7 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     // 17.6 / 30.9, 24 tokens' 4096 x 1024 39.7 / 26.8, 200 tokens 72.7 / 75.0.
     const bool split = most * ceil_div64(N, 32) < 4096;
     const int64_t nb = ceil_div64(N, split ? 32 : 128);
-    if (most * nb > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    if (!grid_fits(most * nb, 256)) return METIS_UNSUPPORTED;
     const size_t row_lds = (size_t)few_code_row(nblk) + few_scale_row(nblk), lds = row_lds * (S < 32 ? S : 32);
     // Quantized on the spot where an expert has 8192 elements or fewer on average, and the rows of a full unit leave room for four
     // workgroups a CU.  us, with the quantizer's launch / on the spot, 2048 x 4096 with 64 experts of which a token takes four: one token
@@ -723,7 +725,8 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
     if (S > 0 && (G->ld < N || X->ld < K || !mat_aligned16(G) || !mat_aligned16(X))) return METIS_BAD_SHAPE;
     if (S > (1 << 25) || N > (1 << 28) || K > (1 << 28)) return METIS_UNSUPPORTED;
     const int64_t tm = ceil_div64(N, 256), tn = ceil_div64(K, 256), tiles = E * tm * tn;
-    if (tiles > 0x3FFFFFFF) return METIS_UNSUPPORTED;
+    const bool brief = wgrad_short(S, (int)E, dW->dtype);
+    if (tiles > 0x3FFFFFFF || (brief && !grid_fits(ceil_div64(N, 128) * tn, 256))) return METIS_UNSUPPORTED;
     const size_t need = metis_experts_wgrad_workspace_bytes(S, (int)E, N, K);
     if (workspace_bytes < need || (need && !workspace)) return METIS_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
@@ -733,7 +736,6 @@ extern "C" int metis_experts_wgrad(void* stream, const metis_mat* G, const metis
     w += mx_bytes(N, P);
     const MxRows x = {w, w + align_up((size_t)K * P / 2, 256)};
     hipStream_t s = (hipStream_t)stream;
-    const bool brief = wgrad_short(S, (int)E, dW->dtype);
     if (S > 0) {
         const TurnSide sg = turn_side(G, nullptr, brief, (uint8_t*)g.codes, (uint8_t*)g.scales);
         const TurnSide sx = turn_side(X, gather ? plan->token : nullptr, brief, (uint8_t*)x.codes, (uint8_t*)x.scales);

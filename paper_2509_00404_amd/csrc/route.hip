@@ -460,6 +460,7 @@ int router_status(const metis_mat* logits, const metis_router* r) {
     if (r->experts > ROUTE_MAX_E || r->k > ROUTE_MAX_K) return METIS_UNSUPPORTED;
     if (logits->rows < 0 || logits->cols != r->experts || logits->ld < logits->cols) return METIS_BAD_SHAPE;
     if (logits->rows > 0x7FFFFFFFll / r->k) return METIS_BAD_SHAPE;
+    if (!grid_fits(ceil_div64(logits->rows, ROUTE_TOKENS), ROUTE_LANES * ROUTE_TOKENS)) return METIS_UNSUPPORTED;
     return METIS_OK;
 }
 
