@@ -501,7 +501,7 @@ int metis_combine(void* stream, const metis_mat* rows, const metis_expert_plan* 
 /*
  * Gradients of metis_combine from dy [tokens, D]: drows[slot[t, j], :] = weights[t, j] * dy[t, :], zeros in the slots that serve no
  * choice; dweights [tokens, k] (fp32) = <dy[t, :], rows[slot[t, j], :]>, 0 without a slot; the sums in fp32, in an order that depends on D
- * alone.  rows and drows share a type, dy has its own.  drows must not overlap rows.  Errors as above; METIS_UNSUPPORTED for 2^24 tokens and more (up to
+ * alone.  plan->slot and offsets are read.  rows and drows share a type, dy has its own.  drows must not overlap rows.  Errors as above; METIS_UNSUPPORTED for 2^24 tokens and more (up to
  * 1024 columns 2^25, up to 512 2^26).
  */
 int metis_combine_grads(void* stream, const metis_mat* dy, const metis_mat* rows, const metis_expert_plan* plan, const float* weights,

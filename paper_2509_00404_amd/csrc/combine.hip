@@ -86,7 +86,7 @@ k_combine_grads(const D* __restrict__ dy, int64_t ldy, const T* __restrict__ row
 }
 
 int plan_rows_status(const metis_mat* rows, const metis_expert_plan* p) {
-    if (!mat_ok(rows) || !p || !p->offsets || !p->slot || p->tokens < 1 || p->k < 1 || p->experts < 1) return METIS_INVALID_ARG;
+    if (!mat_ok(rows) || !p || !p->slot || p->tokens < 1 || p->k < 1 || p->experts < 1) return METIS_INVALID_ARG;
     if (p->k > COMBINE_MAX_K) return METIS_UNSUPPORTED;
     if (p->tokens > 0x7FFFFFFFll / p->k || rows->rows != p->tokens * p->k || rows->cols < 1 || rows->cols > 0x7FFFFFFF || rows->ld < rows->cols)
         return METIS_BAD_SHAPE;
@@ -140,7 +140,7 @@ extern "C" int metis_combine_grads(void* stream, const metis_mat* dy, const meti
     if (plan && plan->tokens == 0) return METIS_OK;
     const int st = plan_rows_status(rows, plan);
     if (st != METIS_OK) return st;
-    if (!mat_ok(dy) || !mat_ok(drows) || !weights || !dweights || drows->dtype != rows->dtype) return METIS_INVALID_ARG;
+    if (!plan->offsets || !mat_ok(dy) || !mat_ok(drows) || !weights || !dweights || drows->dtype != rows->dtype) return METIS_INVALID_ARG;
     if (dy->rows != plan->tokens || dy->cols != rows->cols || dy->ld < dy->cols) return METIS_BAD_SHAPE;
     if (drows->rows != rows->rows || drows->cols != rows->cols || drows->ld < drows->cols) return METIS_BAD_SHAPE;
     hipStream_t s = (hipStream_t)stream;
