@@ -544,6 +544,7 @@ def dispatch(idx, experts, plan=None, workspace=None):
     T, k = idx.shape
     if plan is None:
         plan = ExpertPlan(T, experts, k, device=idx.device)
+    assert plan.experts == experts
     if workspace is None:
         nbytes = int(lib().metis_dispatch_workspace_bytes(T, experts, k))
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=idx.device) if nbytes else None

@@ -1,0 +1,19 @@
+"""What the Python bindings of the mixture-of-experts calls refuse before the library sees it."""
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def metis():
+    from paper_2509_00404_amd import metis as m
+    return m
+
+
+@pytest.mark.gpu
+def test_dispatch_into_a_plan_of_other_experts(metis):
+    """(its choices of the experts that the plan does not have would be left out without a word)"""
+    idx = torch.arange(64, device="cuda", dtype=torch.int32).view(32, 2)
+    with pytest.raises(AssertionError):
+        metis.dispatch(idx, 64, plan=metis.ExpertPlan(32, 8, 2))
+    plan = metis.ExpertPlan(32, 64, 2)
+    assert metis.dispatch(idx, 64, plan=plan) is plan and plan.offsets.tolist() == list(range(65))
