@@ -200,7 +200,7 @@ class MxTensor:
             buffers = (torch.empty((rows, cols // 2), dtype=torch.uint8, device=device),
                        torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
         else:
-            assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
+            assert all(t.is_cuda and t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
             assert [t.numel() for t in buffers] == [rows * (cols // 2), rows * (cols // 32)]
         self.codes, self.scales = buffers
 
@@ -218,7 +218,7 @@ class Mx8Tensor:
             buffers = (torch.empty(rows, cols, dtype=torch.uint8, device=device),
                        torch.empty(rows, cols // 32, dtype=torch.uint8, device=device))
         else:
-            assert all(t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
+            assert all(t.is_cuda and t.is_contiguous() and t.dtype == torch.uint8 for t in buffers)
             assert [t.numel() for t in buffers] == [rows * cols, rows * (cols // 32)]
         self.codes, self.scales = buffers
 
