@@ -8,8 +8,6 @@ import numpy as np
 
 from . import mx as omx
 
-SLOT_ALIGN = 64                                    # an expert's segment of slots, in a matrix quantized along the slots, is padded to this
-
 
 # ---- routing ----------------------------------------------------------------------------------------------------------------------
 
