@@ -390,7 +390,7 @@ int metis_mxfp4_gemm_nt(void* stream, const metis_mxfp4* A, const metis_mxfp4* B
 /*
  * Routing of T tokens to experts.  x = logits [T, experts] (bf16 or fp32), evaluated in fp32:
  *   score    softmax over the row's experts, or sigmoid(x) = 1 / (1 + exp(-x)) of each expert
- *   key      what the selection compares: x + bias (softmax: the order of p * exp(bias)), score + bias (sigmoid).  bias (device fp32
+ *   key      what the selection compares: x + bias (softmax: the order of p * exp(bias), not that of p + bias), score + bias (sigmoid).  bias (device fp32
  *            [experts], optional) balances the load; it enters the selection alone, not the weights.  An expert whose logit is
  *            -inf or NaN, or whose key is -inf, is not available; a token with valid[t] == 0 (device uint8 [T], optional) has no
  *            expert at all.
@@ -430,7 +430,7 @@ int metis_route_grads(void* stream, const metis_mat* logits, const metis_router*
 
 /*
  * The plan of a batch: its S = tokens * k choices sorted into slots, expert by expert and within an expert in the order of the choices
- * (a stable counting sort; no atomics, the same bits every time).  Expert e has the slots offsets[e] .. offsets[e + 1) - 1.
+ * (a stable counting sort of whole numbers: the same bits every time).  Expert e has the slots offsets[e] .. offsets[e + 1) - 1.
  *   offsets  device int32 [experts + 1]
  *   token    device int32 [S]: the token that a slot serves; -1 for the slots at and behind offsets[experts], which serve none
  *   slot     device int32 [tokens, k]: the slot of a choice, -1 where idx is -1 (or outside the experts)

@@ -20,7 +20,8 @@ namespace {
 // scales in units, and row s of the segment is A's row token[s] where they are gathered; else they are runs of `rows` rows.
 // FLAT (a plan's segments, for the gradients of few slots): rows of whole 64 slots and scales row by row, as k_experts_short reads them; a
 // workgroup has 64 rows of 512 columns, and its lanes store by themselves.
-// What bounds it: memory.  32768 x 4096 gathered rows, 339 MB to be moved, take 55 us, x 2048 by slot (170 MB) 36.  (Loads in branches, 16
+// What bounds it: vector issue, 0.94 of the clocks, and memory alike.  32768 x 4096 gathered rows, 339 MB to be moved, take 55 us, x 2048 by slot
+// (170 MB) 36, both in one launch 80 (6.3 TB/s).  (Loads in branches, 16
 // bytes of a column stored at a time and scales byte by byte: 140 and 103.)
 // Both operands of a gradient go in one launch, side by side along the columns: every workgroup takes up one of the two, `side`.
 struct TurnSide {
@@ -491,9 +492,14 @@ int experts_plan_status(const metis_expert_plan* p) {
     if (p->tokens > 0x7FFFFFFFll / p->k) return METIS_BAD_SHAPE;
     return METIS_OK;
 }
-// Gradients of few slots an expert go without the stream.  us with the quantizer, without / with it: bf16, 2 slots an expert of 256 (2464 x
-// 400) 182 / 257, 17 of 128 (80 x 3240) 38 / 72, 112 of 160 (128 x 6888) 174 / 211, 150 of 64 (2048 x 4096) 253 / 213; fp32, 31 of 64 (1384 x
-// 2456) 258 / 252, 100 of 64 (1024 x 2040) 182 / 154.
+// Gradients of few slots an expert go without the stream.  us with the quantizer, without / with it, by slots an expert:
+//   bf16  64 experts of 1024 x 2048    31 67 / 72     100 77 / 73    160 86 / 77       64 of 1384 x 2456   31 148 / 155   126 175 / 151
+//         128 of 80 x 3240             31 37 / 72     126 63 / 85    160 73 / 94       256 of 2464 x 400   31 185 / 254   126 269 / 282   160 302 / 296
+//   fp32  64 of 1024 x 2048            31 100 / 111   62 101 / 111   100 108 / 113     64 of 1384 x 2456   31 258 / 252   62 259 / 251
+//         128 of 80 x 3240             31 44 / 79     62 52 / 85     100 63 / 96       256 of 2464 x 400   31 261 / 334   62 262 / 335    100 286 / 342
+//         64 of 1024 x 2040            31 176 / 155   62 178 / 154   100 184 / 159     64 of 512 x 1000    31 34 / 43     62 36 / 43      100 40 / 44
+// The limits are between what gains and what loses: fp32 gradients of half a GB and more whose rows do not start on cache lines lose up to 15 %
+// below theirs, others would gain as much above it.
 bool wgrad_short(int64_t S, int E, int dtype) { return S < (dtype == METIS_BF16 ? 128 : 64) * (int64_t)E; }
 // quantize A^T, and B^T of the same rows and type where there is a B, by segments of a plan (gathered where a token list is there) or of `rows` rows
 TurnSide turn_side(const metis_mat* A, const int32_t* token, bool flat, uint8_t* codes, uint8_t* scales) {
@@ -517,11 +523,12 @@ int64_t padded_slots(int64_t S, int E) { return most_units(S, E, SLOT_ALIGN) * S
 size_t mx_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * cols / 2, 256) + align_up((size_t)rows * cols / 32, 256) + 2048; }
 
 // The stream takes products of 16 slots an expert and more; what it cannot address, and fewer, goes straight from memory.  us, from memory /
-// streamed, 2048 x 4096 with 64 experts of which a token takes four: 24 tokens 27 / 51 (4096 x 1024), 64 64 / 78, 200 74 / 80, 400 89 / 82, 1000
-// 161 / 86.
+// streamed, 2048 x 4096 with 64 experts of which a token takes four: 24 tokens 57 / 69 (4096 x 1024: 26 / 44), 64 66 / 73, 200 75 / 74, 250
+// 81 / 75, 400 103 / 77, 1000 184 / 83.  The average decides: where all tokens share one expert beside their others, 100 tokens 73 / 72, 200 84 / 76.
 // And so do products of less than 2^20 outputs and 2^31 multiplications, which end before the stream has begun in earnest: from memory / streamed, 64
 // experts of 136 x 5376, 35 slots each 20 / 27; 8 of 1024 x 4096, 40 slots 18 / 24; 2 of 512 x 8192, 150 slots 18 / 26; 1 of 256 x 2048, 2000 slots
-// 18 / 25; 96 of 72 x 800, 92 slots 18 / 21; and beyond: 2.0 M outputs of 992 22 / 21, 8.2 M of 256 31 / 20; 2048 x 7168, 40 slots 35 / 30.
+// 18 / 25; 96 of 72 x 800, 92 slots 18 / 21; and beyond: 2.0 M outputs of 992 22 / 21, 8.2 M of 256 31 / 20; 2048 x 7168, 40 slots 35 / 30 (24 slots
+// 22 / 29, streamed all the same).
 bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
     const int64_t Kp = (K + 255) / 256 * 256;
     if (arows * (Kp / 2) > 0xFFFFFFFFll || K > (1 << 24) || most_units(S, E, 256) * ceil_div64(N, 256) > 0x3FFFFFFF) return false;
@@ -533,13 +540,14 @@ bool product_streams(int64_t S, int E, int64_t N, int64_t arows, int64_t K) {
 // 39 / 64; 64 of 128 x 7520, 114 slots 40 / 60; 16 of 1024 x 4096, 64 slots 28 / 32; 8 of 1384 x 5312, 345 slots 47 / 51; and those left whole:
 // 4 of 1024 x 4096, 1500 slots 48 / 43; 8 of 1024 x 2048, 150 slots 27 / 24.  Parts of 3 and 6 units at least: as 4; 1 to 2 us slower.
 #define PART_LEAST 4                              // units
+#define PART_TILES 256                            // tiles of all parts: a CU each, and the same on any chip, so that results are the same
 int64_t parts_ld(int64_t N) { return (N + 3) / 4 * 4; }
 struct Parts {
     int count, units;                             // count 1: not cut
 };
 Parts product_parts(int64_t S, int E, int64_t N, int64_t K) {
     const int64_t units = (K + 255) / 256, tiles = E * ceil_div64(S, 256 * (int64_t)E) * ceil_div64(N, 256);
-    const int64_t room = 256 / tiles, most = units / PART_LEAST, want = room < most ? room : most;
+    const int64_t room = PART_TILES / tiles, most = units / PART_LEAST, want = room < most ? room : most;
     if (want < 2) return {1, (int)units};
     const int64_t per = ceil_div64(units, want < PARTS_MAX ? want : PARTS_MAX);
     const int64_t count = ceil_div64(units, per);
@@ -664,8 +672,10 @@ extern "C" int metis_experts_product(void* stream, const metis_mat* A, const met
     }
     const int nblk = (int)(K / 32);
     const int64_t most = most_units(S, E, 32) + 1;
-    // The contraction is split where there are few waves (not counting that a unit may not exist).  us, split / not: one token of the above
-    // 17.6 / 30.9, 24 tokens' 4096 x 1024 39.7 / 26.8, 200 tokens 72.7 / 75.0.
+    // The contraction is split where there are few waves (not counting that a unit may not exist).  us, split / not, 8 experts of 2048 x 7168,
+    // two a token: one token 13.7 / 19.7, 8 18.2 / 29.0, 64 20.4 / 32.7; 64 of 2048 x 4096, four a token: 2 tokens 13.9 / 15.5, 8 29.1 /
+    // 29.2, 16 45.9 / 41.8, 24 58.3 / 56.5, 200 83.4 / 74.1; 4096 x 1024, 24 tokens 44.2 / 26.6; and 128 of 1024 x 2048, eight a token, where it
+    // loses a little: 8 tokens 23.4 / 19.0.
     const bool split = most * ceil_div64(N, 32) < 4096;
     const int64_t nb = ceil_div64(N, split ? 32 : 128);
     if (!grid_fits(most * nb, 256)) return METIS_UNSUPPORTED;

@@ -17,7 +17,8 @@
 // which write less, are 3 % better past it all the same).
 // What bounds it: 16384 tokens' four experts, 2048 x 4096 each, 320 us (1.1 PFLOP, 3.4 PFLOP/s; an eighth of the tiles' rows is short tiles').
 // Without its transfers it takes 250, without its matrix instructions 250, without its stores 285: LDS takes a unit's 192 KB of
-// fragments and 68 KB of transfers while the matrix pipe has 2048 cycles of work.  Gradients of 8192 tokens' (1.07 GB out) 285 to 320, without
+// fragments and 68 KB of transfers while the matrix pipe has 2048 cycles of work.  The matrix pipe is busy 0.48 of the clocks (1.8 GHz held), LDS
+// reads 0.27, and the waves wait 0.39 of their time where units meet; at 60 rows an expert 0.23, 0.22 and 0.57.  Gradients of 8192 tokens' (1.07 GB out) 285 to 320, without
 // stores 165.  Tried: tiles of 32 rows fewer to multiply at a short tile's end, transfers left out there, bands of 4 and 16, no XCD order: 1 % up
 // or down; whole tiles of all experts before the short ones: 3 % slower, 4 % faster at 60 rows an expert; a lane's own 32-byte stores instead
 // of lines by way of LDS: 391 for 362 with the quantizers, gradients 546 for 378.

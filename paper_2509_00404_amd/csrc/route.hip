@@ -59,8 +59,8 @@ struct RouteArgs {
 // One row of 16 lanes per token; a lane has the keys of V neighbouring experts, in the experts' order.  A round of the selection is the
 // highest key of the row and its lowest lane, which then looks for its next one.  With V > 4 the lane holds the highest of every four keys, and
 // the keys themselves are in LDS, so that a round looks at four keys and V / 4 maxima instead of V keys.
-// What bounds it: vector issue.  16384 tokens, 256 experts in 8 groups, 8 choices: 14.0 us, of which the logits' 16.8 MB would take
-// 3.3.  (All of a lane's keys looked at in every round, and every key's group by itself: 39.)
+// What bounds it: vector issue, two thirds of the clocks with the four waves a SIMD that 16384 tokens make, and between them the rounds' steps,
+// which depend on one another.  16384 tokens, 256 experts in 8 groups, 8 choices: 14.4 us, of which the logits' 16.8 MB would take 3.3.  (All of a lane's keys looked at in every round, and every key's group by itself: 39.)
 template <typename T, int V, bool SIGMOID>
 __global__ void __launch_bounds__(ROUTE_LANES * ROUTE_TOKENS)
 k_route(const T* __restrict__ logits, RouteArgs a) {
@@ -339,7 +339,7 @@ k_route_grads(const T* __restrict__ logits, int64_t ld, int64_t tokens, const in
 // The choices are cut into chunks.  With several chunks a first launch counts each chunk's choices of every expert; then every workgroup
 // adds up the counts of the chunks before its own, so that no launch is spent on a scan.  Up to PLAN_ALONE choices one workgroup does all of
 // it, which costs it about a microsecond per 1024 and saves a launch of four.
-// 131072 choices of 256 experts: 2.9 us for the counts and 8.0 for the rest, latency of its steps (one thread per expert adding up the
+// 131072 choices of 256 experts: 2.8 us for the counts and 7.8 for the rest, latency of its steps (waves wait 0.63 of their time; one thread per expert adding up the
 // counts, and chunks of 2048: 21).
 #define PLAN_THREADS 1024
 #define PLAN_WAVES (PLAN_THREADS / METIS_WAVE)
