@@ -545,6 +545,96 @@ int metis_dequantize_mx8(void* stream, const metis_mx8* A, metis_mat* out);
 int metis_swiglu(void* stream, const metis_mat* gate_up, metis_mat* act, metis_mx8* saved);
 int metis_swiglu_grads(void* stream, const metis_mx8* saved, const metis_mat* dact, metis_mat* dgate_up, metis_mat* act);
 
+/* ---- around the products of a block: dropout, epilogues, layer norm ------------------------------ */
+
+/*
+ * A dropout mask that is computed wherever it is needed and never stored.  Element (i, j) of a matrix has the 16-bit number j % 8 (low halves
+ * first) of the Philox4x32-10 block with counter (j / 8, i, 16, step mod 2^32) and key `seed`.  It is dropped where that number is below
+ * t = floor(65536 p + 1/2), so with a probability within 2^-17 of p, and multiplied by 65536 / (65536 - t) elsewhere.  A dropped element is 0 whatever
+ * it was.  The mask goes by an element's row and column alone: strides, types and the kernel that applies it change nothing, and the backward pass
+ * computes it again.
+ *   p     0 <= p < 1, and t < 65536; 0 drops nothing
+ *   seed  a layer's own; masks share no numbers with the library's other draws under the same seed
+ *   step  device memory, 8-byte aligned, or null (0): read when the work runs, so that a captured graph draws another mask on every replay
+ *         once the program counts it up in between
+ */
+typedef struct {
+    double         p;
+    uint64_t       seed;
+    const int64_t* step;
+} metis_dropout_mask;
+
+/*
+ * y = residual + m x, m the mask's factors (residual optional); dx = m dy is the same call.  x, residual, y: [rows, cols], one type (bf16 or fp32),
+ * any row strides and alignments of elements; y may be x or residual itself, and must not overlap them otherwise.  The sum is formed in fp32 and
+ * rounded once.  No rows is no work.  Errors: METIS_INVALID_ARG (null pointer, types, a mask outside these rules), METIS_BAD_SHAPE,
+ * METIS_UNSUPPORTED (more than 2^28 columns, or some 2^35 elements and more).
+ */
+int metis_dropout(void* stream, const metis_mat* x, const metis_dropout_mask* mask, const metis_mat* residual, metis_mat* y);
+
+/*
+ * Y [rows, N] = residual + m act(Q(X) W^T + bias): metis_mxfp4_gemm_nt with an epilogue.  The products are exact and accumulate in fp32; the
+ * epilogue is fp32 too, and its result is rounded once.
+ *   X, Xq      exactly one of them: X [rows, K] (bf16 or fp32, rows 16-byte aligned), quantized to MXFP4 on the way as metis_quantize_mx does, or
+ *              Xq, quantized already
+ *   W          [N, K]; K % 32 == 0
+ *   e          null: no epilogue.  bias: device fp32 [N], or null.  act: see below.  pre: null, or an output of Y's shape and type: Q(X) W^T + bias,
+ *              rounded (the activation is applied to what is not rounded yet).  mask: null, or a dropout.  residual: null, or a matrix of Y's
+ *              shape and type, which may be Y itself; Y, pre and residual must not overlap otherwise.
+ *   workspace  with X: metis_mxfp4_linear_workspace_bytes bytes, 256-byte aligned; also without it, where that many bytes let few rows
+ *              run faster (a call without is right too).  Calls that may run at the same time have workspaces of their own.
+ *   act        relu max(z, 0); gelu z Phi(z), Phi the normal distribution; gelu_tanh z sigmoid(2 sqrt(2 / pi) (z + 0.044715 z^3)); silu
+ *              z sigmoid(z).  For bf16 outputs their exponentials are the hardware's: results are within 4e-5, relatively.
+ * Any strides of Y, pre, residual, and alignments of their elements.  No rows is no work.
+ * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL (with X), METIS_UNSUPPORTED (an operand larger than 4 GiB of codes).
+ */
+enum { METIS_ACT_NONE = 0, METIS_ACT_RELU = 1, METIS_ACT_GELU = 2, METIS_ACT_GELU_TANH = 3, METIS_ACT_SILU = 4 };
+typedef struct {
+    const float*              bias;
+    int                       act;
+    const metis_mat*          pre;
+    const metis_dropout_mask* mask;
+    const metis_mat*          residual;
+} metis_epilogue;
+size_t metis_mxfp4_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K);
+int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_mxfp4* Xq, const metis_mxfp4* W, const metis_epilogue* epilogue, metis_mat* Y,
+                       void* workspace, size_t workspace_bytes);
+
+/*
+ * Gradient of that epilogue: dZ = act'(pre) m dY, of what the activation is applied to, and dbias (device fp32 [cols]) = the sum of dZ's rows,
+ * of its values before they are rounded, in an order that depends on the shape alone.  (The residual's gradient is dY itself.)  relu' (0) = 0.
+ *   pre        as the forward pass left it; not looked at for METIS_ACT_NONE
+ *   mask       the forward pass's, or null
+ *   dZ, dbias  either may be null; dZ may be dY or pre itself
+ *   workspace  metis_linear_grads_workspace_bytes bytes where dbias is wanted, 256-byte aligned (may be null where that is 0)
+ * dY, pre, dZ: [rows, cols], one type (bf16 or fp32), any strides and alignments of elements.  Without rows dbias becomes 0.
+ * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (more than 2^28 columns or 2^32 - 1 rows).
+ */
+size_t metis_linear_grads_workspace_bytes(int64_t rows, int64_t cols);
+int metis_linear_grads(void* stream, const metis_mat* dY, const metis_mat* pre, int act, const metis_dropout_mask* mask, metis_mat* dZ, float* dbias,
+                       void* workspace, size_t workspace_bytes);
+
+/*
+ * Layer norm of the rows of x [rows, cols]: y = (x - mean) rstd weight + bias, mean and variance of the row in fp32 (the variance from the
+ * differences), rstd = 1 / sqrt(variance + eps).  weight, bias: device fp32 [cols], each may be null (ones, zeros).  stats: null, or device fp32
+ * [rows, 2], 8-byte aligned: mean and rstd, for the backward pass.  x, y: one type (bf16 or fp32), any strides and alignments of elements; y may be x itself.
+ * eps >= 0 (with 0, a row of equal elements is NaN).  No rows is no work.
+ * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (more than 2^28 columns or 2^32 - 1 rows).
+ */
+int metis_layernorm(void* stream, const metis_mat* x, const float* weight, const float* bias, float eps, metis_mat* y, float* stats);
+
+/*
+ * Its gradients, with xh = (x - mean) rstd from `stats` and g = dy weight:
+ *   dx = add + rstd (g - mean of g - xh * mean of g xh)    add: null, or the gradient that reaches x past the norm
+ *   dweight, dbias (device fp32 [cols], each may be null) = sums over the rows of dy xh and of dy, in an order that depends on the shape alone
+ * dy, x, add, dx: one type (bf16 or fp32), any strides and alignments of elements; dx may be dy, x or add itself.
+ * workspace: metis_layernorm_grads_workspace_bytes bytes where dweight or dbias is wanted, 256-byte aligned.  Without rows both become 0.
+ * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (as above).
+ */
+size_t metis_layernorm_grads_workspace_bytes(int64_t rows, int64_t cols);
+int metis_layernorm_grads(void* stream, const metis_mat* dy, const metis_mat* x, const float* stats, const float* weight, const metis_mat* add,
+                          metis_mat* dx, float* dweight, float* dbias, void* workspace, size_t workspace_bytes);
+
 /* ---- measurement aid ---------------------------------------------------------------------- */
 
 /*

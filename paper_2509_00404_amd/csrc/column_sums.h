@@ -1,0 +1,44 @@
+// Sums over rows, as partial sums side by side that a second launch adds in their order: the same bits every time.
+#pragma once
+#include <type_traits>
+#include "elementwise.h"
+
+namespace {
+
+// out[c] = sum over p of P[p, c] (parts rows of n).  Columns from `split` on go to `out2`.  A workgroup has 64 columns, its four waves every
+// fourth part.
+__global__ void __launch_bounds__(256)
+k_join_sums(const float* __restrict__ P, int64_t parts, int64_t n, float* __restrict__ out, int64_t split, float* __restrict__ out2) {
+    __shared__ float s_sum[3 * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = 64 * (int64_t)blockIdx.x + lane;
+    float sum = 0.0f;
+    if (c < n) {
+#pragma unroll 8
+        for (int64_t p = wave; p < parts; p += 4) sum += P[p * n + c];
+    }
+    if (wave > 0) s_sum[64 * (wave - 1) + lane] = sum;
+    __syncthreads();
+    if (wave > 0 || c >= n) return;
+    sum += s_sum[lane] + s_sum[64 + lane] + s_sum[128 + lane];
+    if (c < split) { if (out) out[c] = sum; }
+    else if (out2) out2[c - split] = sum;
+}
+__global__ void __launch_bounds__(256)
+k_clear(float* __restrict__ p, int64_t n) {
+    const int64_t i = 256 * (int64_t)blockIdx.x + threadIdx.x;
+    if (i < n) p[i] = 0.0f;
+}
+
+int launch_join(hipStream_t s, const float* P, int64_t parts, int64_t n, float* out, int64_t split, float* out2) {
+    hipLaunchKernelGGL(k_join_sums, dim3((unsigned)ceil_div64(n, 64)), dim3(256), 0, s, P, parts, n, out, split, out2);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+int launch_clear(hipStream_t s, float* p, int64_t n) {
+    hipLaunchKernelGGL(k_clear, dim3((unsigned)ceil_div64(n, 256)), dim3(256), 0, s, p, n);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+
+}  // namespace

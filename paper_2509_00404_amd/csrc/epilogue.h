@@ -1,0 +1,227 @@
+// What a product's outputs go through on their way to memory -- bias, activation, dropout, residual -- eight neighbouring elements of a row at a
+// time, and the pieces of it that other kernels share: the activations with their slopes, and the dropout mask.
+#pragma once
+#include "mx_tile.h"
+#include "elementwise.h"
+
+namespace {
+
+// ---- dropout masks ----
+// Element (i, j) has number j % 8 of the eight 16-bit numbers of Philox block (j / 8, i, MASK_TAG, step) under `seed`, low halves first: a
+// lane's eight elements cost one block, whatever the rows' stride, and the sixteen bits set p in steps of 2^-16 (32 bits an element would be
+// two blocks: the generator, not memory, would then bound the plain dropout).  The third counter word keeps the masks apart from the library's
+// other draws under the same seed.
+#define MASK_TAG 16u
+struct MaskKey {
+    uint64_t seed;
+    const int64_t* step;                      // device memory, or null: 0
+    uint32_t dropped;                         // numbers below this one are dropped; 0: no dropout
+    float keep;                               // factor of the others
+};
+inline int mask_status(const metis_dropout_mask* m) {
+    if (!m) return METIS_OK;
+    if (!(m->p >= 0.0) || !(m->p < 1.0) || (uintptr_t)m->step % 8) return METIS_INVALID_ARG;
+    return (uint32_t)(65536.0 * m->p + 0.5) < 65536u ? METIS_OK : METIS_INVALID_ARG;
+}
+inline MaskKey mask_key(const metis_dropout_mask* m) {
+    if (!m) return {0, nullptr, 0, 1.0f};
+    const uint32_t t = (uint32_t)(65536.0 * m->p + 0.5);
+    return {m->seed, m->step, t, (float)(65536.0 / (65536.0 - t))};
+}
+__device__ __forceinline__ uint32_t mask_step(const MaskKey& k) { return k.dropped && k.step ? (uint32_t)*k.step : 0u; }
+// The block of unit j / 8 of row i.  A round is two products and two three-input xors (the plain rounds compile to twice the xors).
+__device__ __forceinline__ u32x4 mask_block(const MaskKey& key, uint32_t step, uint32_t unit, uint32_t row) {
+    const uint32_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u, W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
+    const uint32_t k0 = (uint32_t)key.seed, k1 = (uint32_t)(key.seed >> 32);
+    uint32_t x = unit, y = row, z = MASK_TAG, w = step;
+#pragma unroll
+    for (uint32_t r = 0; r < 10; ++r) {
+        const uint64_t p0 = (uint64_t)M0 * x, p1 = (uint64_t)M1 * z;
+        x = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), y, k0 + r * W0, 0x96);
+        z = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), w, k1 + r * W1, 0x96);
+        y = (uint32_t)p1;
+        w = (uint32_t)p0;
+    }
+    return {x, y, z, w};
+}
+// v = kept ? keep v : 0 (dropped elements are 0 whatever they were)
+__device__ __forceinline__ void mask_apply(const MaskKey& key, uint32_t step, uint32_t unit, uint32_t row, float (&v)[8]) {
+    const u32x4 b = mask_block(key, step, unit, row);
+    const uint32_t w[4] = {b.x, b.y, b.z, b.w}, high = key.dropped << 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = (w[i] & 0xFFFFu) >= key.dropped ? v[2 * i] * key.keep : 0.0f;
+        v[2 * i + 1] = w[i] >= high ? v[2 * i + 1] * key.keep : 0.0f;
+    }
+}
+
+// ---- activations ----
+// FAST (bf16 results): the hardware's exponential and reciprocal, one unit in the last place of fp32 each, as against a rounding to 8 bits.
+__device__ __forceinline__ float act_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+template <bool FAST>
+__device__ __forceinline__ float logistic(float x) {
+    if constexpr (FAST) return __builtin_amdgcn_rcpf(1.0f + act_exp(-x));
+    else return 1.0f / (1.0f + expf(-x));
+}
+// Upper tail of the normal distribution at a = |z|: exp(-a^2 / 2) R(a), R(a) = erfcx(a / sqrt 2) / 2.  R is smooth and falls from 1/2 as 1 / a; in
+// t = 1 / (1 + 0.36 a) a polynomial of degree 5, fitted for the least relative error, is within 1.4e-5 of it for a <= 14, beyond which the
+// exponential is below fp32's range: the result keeps its relative accuracy however small it is.
+__device__ __forceinline__ float normal_tail(float a, float& bell) {
+    bell = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.36f, a, 1.0f));
+    float p = fmaf(-0.0985156898f, t, 0.254387546f);
+    p = fmaf(p, t, 0.0351163301f);
+    p = fmaf(p, t, 0.168695796f);
+    p = fmaf(p, t, 0.140124069f);
+    p = fmaf(p, t, 0.000191289818f);
+    return bell * p;
+}
+#define GELU_C 0.797884561f                       // sqrt(2 / pi)
+template <bool FAST>
+__device__ __forceinline__ float act_value(int act, float z) {
+    switch (act) {
+        case METIS_ACT_RELU: return z < 0.0f ? 0.0f : z;                          // (NaN stays)
+        case METIS_ACT_GELU:
+            if constexpr (FAST) {
+                float bell;
+                const float q = normal_tail(fabsf(z), bell);
+                return z * (z < 0.0f ? q : 1.0f - q);
+            } else {
+                return 0.5f * z * erfcf(z * -0.707106781f);
+            }
+        case METIS_ACT_GELU_TANH: return z * logistic<FAST>(2.0f * GELU_C * z * fmaf(0.044715f * z, z, 1.0f));
+        case METIS_ACT_SILU: return z * logistic<FAST>(z);
+        default: return z;
+    }
+}
+// s = sigmoid(x) and s (1 - s), the latter from exp(-|x|) so that it keeps its relative accuracy where s is near 1
+template <bool FAST>
+__device__ __forceinline__ float logistic_slope(float x, float& s) {
+    float e, d;
+    if constexpr (FAST) {
+        e = act_exp(-fabsf(x));
+        d = __builtin_amdgcn_rcpf(1.0f + e);
+    } else {
+        e = expf(-fabsf(x));
+        d = 1.0f / (1.0f + e);
+    }
+    s = x < 0.0f ? e * d : d;
+    return e * d * d;
+}
+template <bool FAST>
+__device__ __forceinline__ float act_slope(int act, float z) {
+    switch (act) {
+        case METIS_ACT_RELU: return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+        case METIS_ACT_GELU:
+            if constexpr (FAST) {
+                float bell;
+                const float q = normal_tail(fabsf(z), bell);
+                return fmaf(0.5f * GELU_C * z, bell, z < 0.0f ? q : 1.0f - q);
+            } else {
+                return fmaf(0.5f * GELU_C * z, expf(-0.5f * z * z), 0.5f * erfcf(z * -0.707106781f));
+            }
+        case METIS_ACT_GELU_TANH: {
+            // (beyond |z| = 20 the slope is 0 or 1, and z^2 would overflow beyond 1e19)
+            float s;
+            const float c = fminf(fmaxf(z, -20.0f), 20.0f), d = logistic_slope<FAST>(2.0f * GELU_C * c * fmaf(0.044715f * c, c, 1.0f), s);
+            return z != z ? z : fmaf(c * d * (2.0f * GELU_C), fmaf(3.0f * 0.044715f * c, c, 1.0f), s);
+        }
+        case METIS_ACT_SILU: {
+            float s;
+            const float d = logistic_slope<FAST>(z, s);
+            return fmaf(z, d, s);
+        }
+        default: return 1.0f;
+    }
+}
+// `act` is uniform: one branch for the eight
+template <bool FAST>
+__device__ __forceinline__ void act_values(int act, float (&v)[8]) {
+    auto all = [&](int a) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act_value<FAST>(a, v[i]);
+    };
+    switch (act) {
+        case METIS_ACT_RELU: all(METIS_ACT_RELU); break;
+        case METIS_ACT_GELU: all(METIS_ACT_GELU); break;
+        case METIS_ACT_GELU_TANH: all(METIS_ACT_GELU_TANH); break;
+        case METIS_ACT_SILU: all(METIS_ACT_SILU); break;
+        default: break;
+    }
+}
+inline bool act_ok(int act) { return act >= METIS_ACT_NONE && act <= METIS_ACT_SILU; }
+
+// ---- the epilogue ----
+struct MxPlain {};                                // a product's outputs as they are
+template <typename T>
+struct MxFinish {
+    typedef T type;
+    T* y;                                         // (residual may be y: no restrict)
+    int64_t ldy;
+    const float* bias;                            // null: none
+    T* pre;                                       // null: not wanted
+    int64_t ldp;
+    const T* residual;                            // null: none
+    int64_t ldr;
+    MaskKey mask;
+    int act;
+};
+// n <= 8 elements (row r, columns c .. c + n - 1, c a multiple of 8) whose bias is in b; step: mask_step(f.mask)
+template <typename T>
+__device__ __forceinline__ void finish_unit(const MxFinish<T>& f, uint32_t step, int64_t r, int64_t c, int64_t n, const float (&b)[8], float (&v)[8]) {
+    float res[8];
+    if (f.residual) load_part<T, true>(f.residual + r * f.ldr + c, n, res);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += b[i];
+    if (f.pre) store_part<T, true>(f.pre + r * f.ldp + c, n, v);
+    act_values<sizeof(T) == 2>(f.act, v);
+    if (f.mask.dropped) mask_apply(f.mask, step, (uint32_t)(c >> 3), (uint32_t)r, v);
+    if (f.residual) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += res[i];
+    }
+    store_part<T, true>(f.y + r * f.ldy + c, n, v);
+}
+template <typename T>
+__device__ __forceinline__ void finish_bias(const MxFinish<T>& f, int64_t c, int64_t N, float (&b)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+    if (f.bias && c < N) load_part<float, true>(f.bias + c, N - c, b);
+}
+
+// A wave's TM x TN accumulator tiles, transposed (a lane holds runs of four columns of one row), through the epilogue.  32 rows of its columns at
+// a time are staged at sm as fp32 (mx_wave_rows<float, TN> bytes), and a lane takes eight neighbouring columns of a row: one block of the
+// mask's numbers, and 16 bytes of every bf16 operand.
+template <int TM, int TN, typename T>
+__device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T>& f, int64_t m0, int64_t n0, int64_t M,
+                                               int64_t N, int lane) {
+    constexpr int LROW = 32 * TN * 4 + 16, UNITS = 4 * TN, ROWS = 64 / UNITS;
+    const int li = lane & 31, half = lane >> 5, unit = lane % UNITS;
+    const int64_t c = n0 + 8 * unit;
+    const uint32_t step = mask_step(f.mask);
+    float b[8];
+    finish_bias(f, c, N, b);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4)
+                mx_put4(reinterpret_cast<float*>(sm + li * LROW) + 32 * j + 2 * v + 4 * half, acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2],
+                        acc[i][j][v + 3]);
+        gs_wave_order();
+#pragma unroll 1
+        for (int t = 0; t < 32 / ROWS; ++t) {
+            const int row = ROWS * t + lane / UNITS;
+            const int64_t r = m0 + 32 * i + row;
+            if (r < M && c < N) {
+                float v[8];
+                load_row(reinterpret_cast<const float*>(sm + row * LROW + 32 * unit), v);
+                finish_unit(f, step, r, c, N - c, b, v);
+            }
+        }
+        gs_wave_order();
+    }
+}
+
+}  // namespace

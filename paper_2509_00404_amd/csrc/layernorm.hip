@@ -1,0 +1,420 @@
+// Layer norm of rows, and its gradients.
+#include "column_sums.h"
+
+namespace {
+
+// A row belongs to RT threads, each of which holds U units of eight neighbouring elements in registers: unit u of thread t starts at column
+// 8 (t + RT u).  RT 64: a workgroup of 256 has four rows, else one.  Workgroups go through the rows with the weights in registers.
+template <int RT>
+struct RowGroup {
+    static constexpr int THREADS = RT < 256 ? 256 : RT, ROWS = THREADS / RT, WAVES = RT / 64;
+};
+// the wave's sum, the same in all lanes: within each 16 lanes by swaps, then the four in their order
+__device__ __forceinline__ float wave_sum(float v) {
+    auto add = [&](auto ctrl) __attribute__((always_inline)) {
+        v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    add(std::integral_constant<int, 0xB1>{});                     // lanes 1 0 3 2
+    add(std::integral_constant<int, 0x4E>{});                     // 2 3 0 1
+    add(std::integral_constant<int, 0x141>{});                    // halves of eight mirrored
+    add(std::integral_constant<int, 0x140>{});                    // sixteen mirrored
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 16 * i + 15));
+    return s;
+}
+// Sums of N values over a row's threads.  slot: LDS of N * WAVES floats, not written again before the workgroup has met once more.
+template <int RT, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* slot) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (RT > 64) {
+        constexpr int W = RT / 64;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) slot[i * W + wave] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) s += slot[i * W + w];
+            v[i] = s;
+        }
+    }
+}
+template <int U>
+__device__ __forceinline__ void load_factors(const float* p, float none, int64_t cols, int t, int rt, float (&v)[U][8]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t c = 8 * (int64_t)(t + rt * u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = none;
+        if (p && c < cols) load_part<float, true>(p + c, cols - c, v[u]);
+    }
+}
+template <typename T, int RT, int U>
+__global__ void __launch_bounds__(RowGroup<RT>::THREADS)
+k_layernorm(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
+            float2* __restrict__ stats, int64_t rows, int64_t cols) {
+    typedef RowGroup<RT> G;
+    __shared__ float s_mean[G::WAVES], s_var[G::WAVES];
+    const int t = RT == 64 ? (int)threadIdx.x & 63 : (int)threadIdx.x;
+    const int own = RT == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
+    const float n = (float)cols;
+    float w[U][8], b[U][8];
+    load_factors<U>(weight, 1.0f, cols, t, RT, w);
+    load_factors<U>(bias, 0.0f, cols, t, RT, b);
+    for (int64_t r = (int64_t)blockIdx.x * G::ROWS + own; r < rows; r += (int64_t)gridDim.x * G::ROWS) {
+        float v[U][8], sum[1] = {0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = 8 * (int64_t)(t + RT * u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
+            if (c < cols) load_part<T, true>(x + r * ldx + c, cols - c, v[u]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] += v[u][i];
+        }
+        row_sums<RT>(sum, s_mean);
+        const float mean = sum[0] / n;
+        sum[0] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = 8 * (int64_t)(t + RT * u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[u][i] -= mean;
+                if (c + i < cols) sum[0] = fmaf(v[u][i], v[u][i], sum[0]);
+            }
+        }
+        row_sums<RT>(sum, s_var);
+        const float rstd = 1.0f / sqrtf(sum[0] / n + eps);
+        if (stats && t == 0) stats[r] = make_float2(mean, rstd);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = 8 * (int64_t)(t + RT * u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = fmaf(v[u][i] * rstd, w[u][i], b[u][i]);
+            if (c < cols) store_part<T, true>(y + r * ldy + c, cols - c, v[u]);
+        }
+    }
+}
+
+// Rows longer than what registers hold: three passes over the row, which stays in the caches.
+template <typename T>
+__global__ void __launch_bounds__(1024)
+k_layernorm_long(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
+                 float2* __restrict__ stats, int64_t rows, int64_t cols) {
+    __shared__ float s_mean[16], s_var[16];
+    const float n = (float)cols;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        float sum[1] = {0.0f}, v[8];
+        auto each = [&](auto f) __attribute__((always_inline)) {
+            for (int64_t c = 8 * (int64_t)threadIdx.x; c < cols; c += 8192) {
+                load_part<T, true>(x + r * ldx + c, cols - c, v);
+                f(c);
+            }
+        };
+        each([&](int64_t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] += v[i];
+        });
+        row_sums<1024>(sum, s_mean);
+        const float mean = sum[0] / n;
+        sum[0] = 0.0f;
+        each([&](int64_t c) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < cols) sum[0] = fmaf(v[i] - mean, v[i] - mean, sum[0]);
+        });
+        row_sums<1024>(sum, s_var);
+        const float rstd = 1.0f / sqrtf(sum[0] / n + eps);
+        if (stats && threadIdx.x == 0) stats[r] = make_float2(mean, rstd);
+        each([&](int64_t c) {
+            float w[8] = {1, 1, 1, 1, 1, 1, 1, 1}, b[8] = {};
+            if (weight) load_part<float, true>(weight + c, cols - c, w);
+            if (bias) load_part<float, true>(bias + c, cols - c, b);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - mean) * rstd, w[i], b[i]);
+            store_part<T, true>(y + r * ldy + c, cols - c, v);
+        });
+    }
+}
+
+// ---- gradients ----
+// xh = (x - mean) rstd, g = dy w:  dx = add + rstd (g - mean of g - xh * mean of g xh).  Both means come from one pass over what the registers
+// hold; the columns' sums of dy xh and dy stay in registers over all the rows of a workgroup, and leave as one row of `sums` [gridDim.x, 2 cols].
+template <typename T, int RT, int U>
+__global__ void __launch_bounds__(RowGroup<RT>::THREADS)
+k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
+                  const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows, int64_t cols, float* __restrict__ sums) {
+    typedef RowGroup<RT> G;
+    __shared__ float s_sum[2][2 * G::WAVES], s_join[RT == 64 ? 3 * 512 : 1];
+    const int t = RT == 64 ? (int)threadIdx.x & 63 : (int)threadIdx.x;
+    const int own = RT == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
+    const float n = (float)cols;
+    float w[U][8], dw[U][8], db[U][8];
+    load_factors<U>(weight, 1.0f, cols, t, RT, w);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[u][i] = db[u][i] = 0.0f;
+    int turn = 0;
+    for (int64_t r = (int64_t)blockIdx.x * G::ROWS + own; r < rows; r += (int64_t)gridDim.x * G::ROWS, turn ^= 1) {
+        float xh[U][8], g[U][8], sum[2] = {0.0f, 0.0f};
+        const float2 st = stats[r];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = 8 * (int64_t)(t + RT * u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) xh[u][i] = st.x, g[u][i] = 0.0f;                  // (xh becomes 0)
+            if (c < cols) {
+                load_part<T, true>(x + r * ldx + c, cols - c, xh[u]);
+                load_part<T, true>(dy + r * ldd + c, cols - c, g[u]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                xh[u][i] = (xh[u][i] - st.x) * st.y;
+                dw[u][i] = fmaf(g[u][i], xh[u][i], dw[u][i]);
+                db[u][i] += g[u][i];
+                g[u][i] *= w[u][i];
+                sum[0] += g[u][i];
+                sum[1] = fmaf(g[u][i], xh[u][i], sum[1]);
+            }
+        }
+        row_sums<RT>(sum, s_sum[turn]);
+        const float mg = sum[0] / n, mx = sum[1] / n;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = 8 * (int64_t)(t + RT * u);
+            if (c >= cols) continue;
+            float a[8] = {};
+            if (add) load_part<T, true>(add + r * lda + c, cols - c, a);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = fmaf(st.y, g[u][i] - mg - xh[u][i] * mx, a[i]);
+            store_part<T, true>(dx + r * ldo + c, cols - c, a);
+        }
+    }
+    if (!sums) return;
+    float* out = sums + (int64_t)blockIdx.x * 2 * cols;
+    auto leave = [&](float (&s)[U][8], float* to) __attribute__((always_inline)) {
+        if constexpr (RT == 64) {                                                     // the four waves' sums in their order
+            __syncthreads();
+            if (own > 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s_join[(own - 1) * 512 + 64 * i + t] = s[0][i];
+            }
+            __syncthreads();
+            if (own > 0) return;
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[0][i] += s_join[p * 512 + 64 * i + t];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = 8 * (int64_t)(t + RT * u);
+            if (c < cols) store_part<float, true>(to + c, cols - c, s[u]);
+        }
+    };
+    leave(dw, out);
+    leave(db, out + cols);
+}
+
+// Long rows: two passes over a row for its gradient, and the columns' sums by a kernel that goes down the columns.
+template <typename T>
+__global__ void __launch_bounds__(1024)
+k_layernorm_grads_long(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
+                       const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows, int64_t cols) {
+    __shared__ float s_sum[2][32];
+    const float n = (float)cols;
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x, turn ^= 1) {
+        const float2 st = stats[r];
+        float sum[2] = {0.0f, 0.0f}, xh[8], g[8];
+        auto each = [&](auto f) __attribute__((always_inline)) {
+            for (int64_t c = 8 * (int64_t)threadIdx.x; c < cols; c += 8192) {
+                float w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+                load_part<T, true>(x + r * ldx + c, cols - c, xh);
+                load_part<T, true>(dy + r * ldd + c, cols - c, g);                   // (zeros behind the row)
+                if (weight) load_part<float, true>(weight + c, cols - c, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    xh[i] = (xh[i] - st.x) * st.y;
+                    g[i] = c + i < cols ? g[i] * w[i] : 0.0f;
+                }
+                f(c);
+            }
+        };
+        each([&](int64_t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sum[0] += g[i];
+                sum[1] = fmaf(g[i], xh[i], sum[1]);
+            }
+        });
+        row_sums<1024>(sum, s_sum[turn]);
+        const float mg = sum[0] / n, mx = sum[1] / n;
+        each([&](int64_t c) {
+            float a[8] = {};
+            if (add) load_part<T, true>(add + r * lda + c, cols - c, a);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = fmaf(st.y, g[i] - mg - xh[i] * mx, a[i]);
+            store_part<T, true>(dx + r * ldo + c, cols - c, a);
+        });
+    }
+}
+// a workgroup has 512 columns of `chunk` rows
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_layernorm_columns(const T* __restrict__ dy, int64_t ldd, const T* __restrict__ x, int64_t ldx, const float2* __restrict__ stats, int64_t rows,
+                    int64_t cols, int64_t chunk, float* __restrict__ sums) {
+    __shared__ float s_join[2 * 3 * 512];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t c = 512 * (int64_t)blockIdx.x + 8 * lane, n = cols - c;
+    const int64_t first = chunk * blockIdx.y, end = first + chunk < rows ? first + chunk : rows;
+    float s[2][8] = {};
+    if (n > 0) {
+        for (int64_t r = first + wave; r < end; r += 4) {
+            const float2 st = stats[r];
+            float v[8], g[8];
+            load_part<T, true>(x + r * ldx + c, n, v);
+            load_part<T, true>(dy + r * ldd + c, n, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[0][i] = fmaf(g[i], (v[i] - st.x) * st.y, s[0][i]);
+                s[1][i] += g[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (wave > 0) s_join[(3 * k + wave - 1) * 512 + 64 * i + lane] = s[k][i];
+    __syncthreads();
+    if (wave > 0 || n <= 0) return;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[k][i] += s_join[(3 * k + p) * 512 + 64 * i + lane];
+        store_part<float, true>(sums + (blockIdx.y * 2 + k) * cols + c, n, s[k]);
+    }
+}
+
+#define NORM_REGS 16384                           // longest row whose gradient's kernel keeps it, and its columns' sums, in registers
+#define NORM_PARTS 512                            // rows of partial sums at most, the same on any chip so that the sums have the same order
+
+int64_t norm_rows(int64_t cols) { return cols <= 512 ? 4 : 1; }          // rows of a workgroup at a time
+int64_t norm_parts(int64_t rows, int64_t cols) {
+    const int64_t groups = ceil_div64(rows, norm_rows(cols));
+    return groups < NORM_PARTS ? groups : NORM_PARTS;
+}
+int64_t column_chunk(int64_t rows, int64_t cols) {                       // rows of a workgroup of k_layernorm_columns
+    const int64_t chunks = ceil_div64(2048, ceil_div64(cols, 512)), chunk = ceil_div64(rows, chunks);
+    return chunk < 32 ? 32 : chunk;
+}
+int64_t sum_rows(int64_t rows, int64_t cols) {
+    return cols <= NORM_REGS ? norm_parts(rows, cols) : ceil_div64(rows, column_chunk(rows, cols));
+}
+// the threads of a row and the units of a thread: f(threads, units)
+template <typename F>
+void by_length(int64_t cols, F f) {
+    if (cols <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+    else if (cols <= 2048) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+    else if (cols <= 4096) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+    else if (cols <= 8192) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+    else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+}
+bool norm_mat(const metis_mat* m, const metis_mat* like) {
+    return m->rows == like->rows && m->cols == like->cols && m->ld >= m->cols;
+}
+int norm_limits(int64_t rows, int64_t cols) { return cols > (1 << 28) || rows > 0xFFFFFFFFll ? METIS_UNSUPPORTED : METIS_OK; }
+
+}  // namespace
+
+extern "C" int metis_layernorm(void* stream, const metis_mat* x, const float* weight, const float* bias, float eps, metis_mat* y, float* stats) {
+    if (!x || !y || !(eps >= 0.0f) || (uintptr_t)weight % 4 || (uintptr_t)bias % 4 || (uintptr_t)stats % 8) return METIS_INVALID_ARG;
+    if (x->rows == 0 && y->rows == 0) return METIS_OK;
+    if (!mat_ok(x) || !mat_ok(y) || x->dtype != y->dtype) return METIS_INVALID_ARG;
+    if (x->rows < 1 || x->cols < 1 || !norm_mat(x, x) || !norm_mat(y, x)) return METIS_BAD_SHAPE;
+    const int64_t rows = x->rows, cols = x->cols;
+    const int st = norm_limits(rows, cols);
+    if (st != METIS_OK) return st;
+    hipStream_t s = (hipStream_t)stream;
+    auto launch = [&](auto zero) {
+        typedef decltype(zero) T;
+        auto go = [&](auto kern, int threads, int64_t groups, int64_t most) {
+            hipLaunchKernelGGL(kern, dim3((unsigned)(groups < most ? groups : most)), dim3(threads), 0, s, (const T*)x->ptr, x->ld, (T*)y->ptr,
+                               y->ld, weight, bias, eps, (float2*)stats, rows, cols);
+        };
+        if (cols > NORM_REGS) return go(k_layernorm_long<T>, 1024, rows, 512);
+        by_length(cols, [&](auto rt, auto u) {
+            constexpr int RT = decltype(rt)::value;
+            go(k_layernorm<T, RT, decltype(u)::value>, RowGroup<RT>::THREADS, ceil_div64(rows, RowGroup<RT>::ROWS), RT == 1024 ? 512 : 2048);
+        });
+    };
+    if (x->dtype == METIS_BF16) launch(bf16_t());
+    else launch(float());
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+
+extern "C" size_t metis_layernorm_grads_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 1 || cols < 1 || norm_limits(rows, cols) != METIS_OK) return 0;
+    return align_up((size_t)sum_rows(rows, cols) * 2 * cols * 4, 256);
+}
+
+extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const metis_mat* x, const float* stats, const float* weight,
+                                     const metis_mat* add, metis_mat* dx, float* dweight, float* dbias, void* workspace, size_t workspace_bytes) {
+    if (!dy || !x || !dx || (uintptr_t)weight % 4 || (uintptr_t)dweight % 4 || (uintptr_t)dbias % 4 || (uintptr_t)stats % 8) return METIS_INVALID_ARG;
+    const int64_t rows = x->rows, cols = x->cols;
+    const bool columns = dweight || dbias;
+    hipStream_t s = (hipStream_t)stream;
+    if (rows == 0 && dy->rows == 0 && dx->rows == 0) {
+        if (cols < 1 || cols > (1 << 28)) return cols < 1 ? METIS_BAD_SHAPE : METIS_UNSUPPORTED;
+        int r = dweight ? launch_clear(s, dweight, cols) : METIS_OK;
+        if (r == METIS_OK && dbias) r = launch_clear(s, dbias, cols);
+        return r;
+    }
+    if (!mat_ok(x) || !mat_ok(dy) || !mat_ok(dx) || !stats || (add && !mat_ok(add)) || x->dtype != dy->dtype || x->dtype != dx->dtype ||
+        (add && add->dtype != x->dtype))
+        return METIS_INVALID_ARG;
+    if (rows < 1 || cols < 1 || !norm_mat(x, x) || !norm_mat(dy, x) || !norm_mat(dx, x) || (add && !norm_mat(add, x))) return METIS_BAD_SHAPE;
+    const int st = norm_limits(rows, cols);
+    if (st != METIS_OK) return st;
+    if (columns && (!workspace || workspace_bytes < metis_layernorm_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;
+    if (columns && (uintptr_t)workspace % 256) return METIS_INVALID_ARG;
+    float* sums = columns ? (float*)workspace : nullptr;
+    auto launch = [&](auto zero) {
+        typedef decltype(zero) T;
+        const T *pd = (const T*)dy->ptr, *px = (const T*)x->ptr, *pa = add ? (const T*)add->ptr : nullptr;
+        const int64_t la = add ? add->ld : 0;
+        if (cols > NORM_REGS) {
+            if (columns) {
+                const int64_t chunk = column_chunk(rows, cols);
+                hipLaunchKernelGGL(k_layernorm_columns<T>, dim3((unsigned)ceil_div64(cols, 512), (unsigned)ceil_div64(rows, chunk)), dim3(256), 0, s,
+                                   pd, dy->ld, px, x->ld, (const float2*)stats, rows, cols, chunk, sums);
+                if (hipGetLastError() != hipSuccess) return METIS_HIP_ERROR;
+            }
+            hipLaunchKernelGGL(k_layernorm_grads_long<T>, dim3((unsigned)(rows < 512 ? rows : 512)), dim3(1024), 0, s, pd, dy->ld, px, x->ld,
+                               (const float2*)stats, weight, pa, la, (T*)dx->ptr, dx->ld, rows, cols);
+        } else {
+            by_length(cols, [&](auto rt, auto u) {
+                constexpr int RT = decltype(rt)::value;
+                auto kern = k_layernorm_grads<T, RT, decltype(u)::value>;
+                hipLaunchKernelGGL(kern, dim3((unsigned)norm_parts(rows, cols)), dim3(RowGroup<RT>::THREADS), 0, s, pd, dy->ld, px, x->ld,
+                                   (const float2*)stats, weight, pa, la, (T*)dx->ptr, dx->ld, rows, cols, sums);
+            });
+        }
+        return hipGetLastError() == hipSuccess ? METIS_OK : METIS_HIP_ERROR;
+    };
+    const int ls = x->dtype == METIS_BF16 ? launch(bf16_t()) : launch(float());
+    if (ls != METIS_OK || !columns) return ls;
+    return launch_join(s, sums, sum_rows(rows, cols), 2 * cols, dweight, cols, dbias);
+}

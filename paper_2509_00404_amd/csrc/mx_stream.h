@@ -1,4 +1,4 @@
-// The MXFP4 GEMM for large outputs (included by mxfp4.hip, inside its namespace).
+// The MXFP4 GEMM for large outputs (included by mx_gemm.h, inside its namespace).
 #pragma once
 
 // 256 x 256 tiles, 8 waves of 128 x 64, two per SIMD; a unit is 256 contraction elements, 128 bytes of every row = whole cache lines.
@@ -14,10 +14,11 @@
 // two steps ahead and its buffer given back a step earlier, the transfers' offsets then formed where they are issued, 277; starts of the
 // workgroups staggered by 0.5 to 2 us, stores past the caches: no difference.
 // LDS: two buffers of a unit (mx_tile.h).
-template <typename OUT>
+template <typename OUT, typename END = MxPlain>
 __global__ void __launch_bounds__(512, 2)
-k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C, int64_t ldc, bool vec, MxOrder order, int total) {
-    constexpr bool LINES = sizeof(OUT) == 2;             // outputs by way of LDS, accumulator tiles transposed
+k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C, int64_t ldc, bool vec, MxOrder order, int total, END end) {
+    constexpr bool PLAIN = std::is_same<END, MxPlain>::value;
+    constexpr bool LINES = !PLAIN || sizeof(OUT) == 2;   // outputs by way of LDS, accumulator tiles transposed
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int niter = (int)(K / MX_KI);                  // at least 2
@@ -162,8 +163,11 @@ k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C,
         const uint32_t bl = MXS_UNIT - b0;               // the last unit's buffer
         int m0, n0;
         tile_of(pos, m0, n0);
-        mx_store_wave<OUT, LINES, 4, 2>(acc, lds + bl + wave * mx_wave_rows<OUT, 2>(), C, ldc, m0 + 128 * wa, n0 + 64 * wb, A.rows, B.rows,
-                                        vec, mx_whole<LINES>(m0 + 256 <= A.rows && n0 + 256 <= B.rows, vec), gs_fresh_lane());
+        if constexpr (PLAIN)
+            mx_store_wave<OUT, LINES, 4, 2>(acc, lds + bl + wave * mx_wave_rows<OUT, 2>(), C, ldc, m0 + 128 * wa, n0 + 64 * wb, A.rows, B.rows,
+                                            vec, mx_whole<LINES>(m0 + 256 <= A.rows && n0 + 256 <= B.rows, vec), gs_fresh_lane());
+        else
+            mx_finish_wave<4, 2>(acc, lds + bl + wave * mx_wave_rows<float, 2>(), end, m0 + 128 * wa, n0 + 64 * wb, A.rows, B.rows, gs_fresh_lane());
         pos += (int)gridDim.x;
         if (pos >= total) break;
         // every wave has its rows out of the buffer before any transfers into it

@@ -48,6 +48,14 @@ class Mx8(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64)]
 
 
+class Mask(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_void_p)]
+
+
+class Epilogue(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("act", C.c_int), ("pre", C.POINTER(Mat)), ("mask", C.POINTER(Mask)), ("residual", C.POINTER(Mat))]
+
+
 class DecomposeJob(C.Structure):
     _fields_ = [("A", C.POINTER(Mat)), ("k", C.c_int), ("oversample", C.c_int), ("sample_rate", C.c_double),
                 ("seed", C.c_uint64), ("U", C.c_void_p), ("S", C.c_void_p), ("V", C.c_void_p), ("amax_out", C.c_void_p),
@@ -127,6 +135,17 @@ _SIGNATURES = {
     "metis_dequantize_mx8": (C.c_int, [C.c_void_p, C.POINTER(Mx8), C.POINTER(Mat)]),
     "metis_swiglu": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Mx8)]),
     "metis_swiglu_grads": (C.c_int, [C.c_void_p, C.POINTER(Mx8), C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Mat)]),
+    "metis_dropout": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mask), C.POINTER(Mat), C.POINTER(Mat)]),
+    "metis_mxfp4_linear_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "metis_mxfp4_linear": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(MxFp4), C.POINTER(MxFp4), C.POINTER(Epilogue), C.POINTER(Mat),
+                                     C.c_void_p, C.c_size_t]),
+    "metis_linear_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "metis_linear_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.c_int, C.POINTER(Mask), C.POINTER(Mat), C.c_void_p,
+                                     C.c_void_p, C.c_size_t]),
+    "metis_layernorm": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.c_void_p, C.c_void_p, C.c_float, C.POINTER(Mat), C.c_void_p]),
+    "metis_layernorm_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "metis_layernorm_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.c_void_p, C.c_void_p, C.POINTER(Mat), C.POINTER(Mat),
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t]),
     "metis_factor_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int]),
     "metis_fp4_factor_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Split), C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_size_t]),
@@ -633,6 +652,93 @@ def swiglu_grads(saved, dact, dgate_up, act=None):
     q, d, o, a = saved.c(), _mat(dact), _mat(dgate_up), _mat(act) if act is not None else None
     _check(lib().metis_swiglu_grads(_stream(), C.byref(q), C.byref(d), C.byref(o), C.byref(a) if a is not None else None))
     return dgate_up
+
+
+class DropoutMask:
+    """The mask of a dropout (see metis_dropout_mask): probability p, the layer's seed, and an int64 tensor on the device that counts the steps
+    (None: 0).  The mask depends on these and an element's place alone, so the backward pass is given the same object."""
+
+    def __init__(self, p, seed, step=None):
+        assert step is None or (step.is_cuda and step.dtype == torch.int64 and step.numel() == 1)
+        self.p, self.seed, self.step = p, seed, step
+
+    def c(self):
+        return Mask(self.p, self.seed & 0xFFFFFFFFFFFFFFFF, self.step.data_ptr() if self.step is not None else None)
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _ref(x):
+    return C.byref(x) if x is not None else None
+
+
+def _scratch(nbytes, like):
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+def dropout(x, y, mask, residual=None):
+    """y = residual + m x, m the factors of `mask` (a DropoutMask)."""
+    a, o, k, r = _mat(x), _mat(y), mask.c(), _mat(residual) if residual is not None else None
+    _check(lib().metis_dropout(_stream(), C.byref(a), C.byref(k), _ref(r), C.byref(o)))
+    return y
+
+
+def mxfp4_linear_workspace_bytes(rows, N, K):
+    return int(lib().metis_mxfp4_linear_workspace_bytes(rows, N, K))
+
+
+def mxfp4_linear(X, W, Y, bias=None, act="none", pre=None, mask=None, residual=None, workspace=None):
+    """Y [T, N] = residual + m act(Q(X) W^T + bias); X an MxTensor or a dense tensor, pre: output for what act is applied to."""
+    w, y = W.c(), _mat(Y)
+    dense = isinstance(X, torch.Tensor)
+    x = _mat(X) if dense else X.c()
+    p, k, r = _mat(pre) if pre is not None else None, mask.c() if mask is not None else None, _mat(residual) if residual is not None else None
+    e = Epilogue(_ptr(bias, torch.float32, (w.rows,)), ACTIVATIONS[act], C.pointer(p) if p is not None else None,
+                 C.pointer(k) if k is not None else None, C.pointer(r) if r is not None else None)
+    if workspace is None:
+        workspace = _scratch(mxfp4_linear_workspace_bytes(x.rows, w.rows, w.cols), Y)
+    _check(lib().metis_mxfp4_linear(_stream(), C.byref(x) if dense else None, None if dense else C.byref(x), C.byref(w), C.byref(e), C.byref(y),
+                                    workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0))
+    return Y
+
+
+def linear_grads_workspace_bytes(rows, cols):
+    return int(lib().metis_linear_grads_workspace_bytes(rows, cols))
+
+
+def linear_grads(dY, dZ=None, pre=None, act="none", mask=None, dbias=None, workspace=None):
+    """dZ = act'(pre) m dY, and dbias [cols] fp32 = its column sums; either may be None."""
+    d, z, p, k = _mat(dY), _mat(dZ) if dZ is not None else None, _mat(pre) if pre is not None else None, mask.c() if mask is not None else None
+    if workspace is None and dbias is not None:
+        workspace = _scratch(linear_grads_workspace_bytes(d.rows, d.cols), dY)
+    _check(lib().metis_linear_grads(_stream(), C.byref(d), _ref(p), ACTIVATIONS[act], _ref(k), _ref(z), _ptr(dbias, torch.float32, (d.cols,)),
+                                    workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0))
+    return dZ
+
+
+def layernorm(x, y, weight=None, bias=None, eps=1e-5, stats=None):
+    """y = (x - mean) rstd weight + bias by rows; stats [rows, 2] fp32: mean and rstd, for the backward pass."""
+    a, o = _mat(x), _mat(y)
+    _check(lib().metis_layernorm(_stream(), C.byref(a), _ptr(weight, torch.float32, (a.cols,)), _ptr(bias, torch.float32, (a.cols,)), eps,
+                                 C.byref(o), _ptr(stats, torch.float32, (a.rows, 2))))
+    return y
+
+
+def layernorm_grads_workspace_bytes(rows, cols):
+    return int(lib().metis_layernorm_grads_workspace_bytes(rows, cols))
+
+
+def layernorm_grads(dy, x, stats, dx, weight=None, dweight=None, dbias=None, add=None, workspace=None):
+    """dx (with `add`, the gradient that reaches x past the norm) and, where given, dweight and dbias [cols] fp32."""
+    d, a, o, r = _mat(dy), _mat(x), _mat(dx), _mat(add) if add is not None else None
+    col = (a.cols,)
+    if workspace is None and (dweight is not None or dbias is not None):
+        workspace = _scratch(layernorm_grads_workspace_bytes(a.rows, a.cols), x)
+    _check(lib().metis_layernorm_grads(_stream(), C.byref(d), C.byref(a), _ptr(stats, torch.float32, (a.rows, 2)), _ptr(weight, torch.float32, col),
+                                       _ref(r), C.byref(o), _ptr(dweight, torch.float32, col), _ptr(dbias, torch.float32, col),
+                                       workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0))
+    return dx
 
 
 def ceiling_copy(src, dst):

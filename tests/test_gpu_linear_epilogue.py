@@ -1,0 +1,228 @@
+"""GPU parity of the MXFP4 linear layer with an epilogue, and of the epilogue's gradient, with the fp64 oracle.
+
+Bounds, element by element.  z = Q(X) W^T + bias sums K exact products and one more term in fp32: off by at most (K + 2) 2^-24 (|Q(X)| |W|^T + |bias|).
+The activations' slopes are below 1.13 and they are within 4e-5 of their values (the bf16 forms; the fp32 ones are nearer), the smallest fp32
+normal number standing in for what the exponentials flush.  A mask's factor, its product and the residual's sum round once each (2^-24), and the
+result once more: 2^-8 for bf16, 2^-24 for fp32."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import epilogue as oep
+from oracle import mx as omx
+
+pytestmark = pytest.mark.gpu
+ROUND = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+TINY = 2.0 ** -126
+
+
+@pytest.fixture(scope="module")
+def metis():
+    from paper_2509_00404_amd import metis as m
+    assert torch.cuda.is_available()
+    m.lib()
+    return m
+
+
+def _f64(t):
+    return t.double().cpu().numpy()
+
+
+def _offset(rows, cols, dtype, pad):
+    """A matrix whose rows start `pad` elements behind 16 bytes; what is around it holds 7."""
+    whole = torch.full((rows, cols + 2 * pad), 7.0, dtype=dtype, device="cuda")
+    return whole, whole[:, pad:pad + cols]
+
+
+class _Layer:
+    def __init__(self, metis, T, N, K, dtype, seed):
+        g = torch.Generator().manual_seed(seed)
+        self.metis, self.T, self.N, self.K, self.dtype = metis, T, N, K, dtype
+        x = torch.randn((T, K), generator=g)
+        x[:, ::37] *= 20
+        self.x = x.to(torch.bfloat16).cuda()
+        self.w = (torch.randn((N, K), generator=g) * K ** -0.5).to(torch.bfloat16).cuda()
+        self.W, self.X = metis.MxTensor(N, K), metis.MxTensor(T, K)
+        metis.quantize_mx(self.w, self.W)
+        metis.quantize_mx(self.x, self.X)
+        self.bias = (0.3 * torch.randn(N, generator=g)).cuda()
+        self.res = torch.randn((T, N), generator=g).to(dtype).cuda()
+        self.step = torch.tensor([5 + (1 << 33)], dtype=torch.int64, device="cuda")
+        self.rows = np.arange(T) if T <= 700 else np.unique(np.concatenate([np.arange(0, T, max(1, T // 97)), np.arange(T - 40, T)]))
+        xq = omx.dequantize_mx(*omx.quantize_mx(_f64(self.x)[self.rows]))
+        wq = omx.dequantize_mx(*omx.quantize_mx(_f64(self.w)))
+        on = lambda a: torch.from_numpy(a).cuda()
+        self.z = (on(xq) @ on(wq).t()).cpu().numpy()
+        self.big = (on(np.abs(xq)) @ on(np.abs(wq)).t()).cpu().numpy()
+
+    def check(self, act="none", bias=True, pre=False, p=0.0, residual=False, dense=False, pad=0, inplace=False, workspace=None):
+        T, N, dtype = self.T, self.N, self.dtype
+        whole, Y = _offset(T, N, dtype, pad)
+        wpre, P = _offset(T, N, dtype, pad) if pre else (None, None)
+        mask = self.metis.DropoutMask(p, 0x123456789ABC, self.step) if p else None
+        res = self.res if residual else None
+        if inplace:
+            Y.copy_(self.res)
+            res = Y
+        out = self.metis.mxfp4_linear(self.x if dense else self.X, self.W, Y, bias=self.bias if bias else None, act=act, pre=P, mask=mask,
+                                      residual=res, workspace=workspace)
+        assert out is Y
+        b = _f64(self.bias)[None, :] if bias else 0.0
+        z = self.z + b
+        ez = (self.K + 2) * 2.0 ** -24 * (self.big + np.abs(b))
+        a = oep.act(act, z)
+        ea = 1.13 * ez + 4e-5 * np.abs(a) + TINY if act not in ("none", "relu") else ez
+        m = oep.mask(p, 0x123456789ABC, 5, self.rows, N) if p else 1.0
+        r = _f64(self.res)[self.rows] if residual or inplace else 0.0
+        ref = r + m * a
+        err = m * ea + 4 * 2.0 ** -24 * (np.abs(r) + np.abs(m * a))
+        err = err + ROUND[dtype] * (np.abs(ref) + err)
+        got = _f64(Y)[self.rows]
+        assert np.all(np.abs(got - ref) <= err), float(np.max(np.abs(got - ref) / err))
+        if pre:
+            assert np.all(np.abs(_f64(P)[self.rows] - z) <= ez + ROUND[dtype] * (np.abs(z) + ez))
+        for t in (whole, wpre):
+            if t is not None and pad:
+                assert (t[:, :pad] == 7).all() and (t[:, N + pad:] == 7).all()
+        return Y
+
+
+SIZES = [(1, 64, 32), (1, 14, 64), (5, 1, 32), (1, 1000, 4096), (2, 33, 1056), (33, 257, 96), (16, 48, 2048), (17, 100, 544), (48, 130, 8192),
+         (100, 1000, 288), (128, 128, 256), (129, 777, 2080), (300, 520, 512), (513, 640, 1024), (1000, 264, 4096)]
+EPILOGUES = [dict(act="gelu", pre=True), dict(act="none", p=0.1, residual=True), dict(act="silu", p=0.5, residual=True, pre=True, dense=True),
+             dict(act="gelu_tanh", bias=False), dict(act="relu", dense=True, inplace=True), dict(bias=False)]
+
+
+@pytest.mark.parametrize("T,N,K", SIZES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_linear(metis, T, N, K, dtype):
+    layer = _Layer(metis, T, N, K, dtype, T + N)
+    for e in EPILOGUES:
+        for pad in (0, 3):
+            layer.check(pad=pad, **e)
+
+
+@pytest.mark.parametrize("T,N,K", [(4352, 4112, 512), (3000, 6001, 1024), (4100, 4096, 96), (4096, 4096, 800), (2048, 8192, 2048)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_linear_of_many_tiles(metis, T, N, K, dtype):
+    layer = _Layer(metis, T, N, K, dtype, K)
+    layer.check(act="gelu", pre=True)
+    layer.check(act="silu", p=0.1, residual=True, pad=1)
+    layer.check(p=0.3, inplace=True, dense=True)
+
+
+def test_plain_product_is_the_gemm_without_an_epilogue(metis):
+    """An epilogue of nothing rounds what metis_mxfp4_gemm_nt rounds."""
+    for T, N, K in [(300, 520, 512), (4352, 4112, 512), (4096, 4096, 96)]:
+        layer = _Layer(metis, T, N, K, torch.bfloat16, 3)
+        y = layer.check(bias=False)
+        ref = metis.mxfp4_gemm_nt(layer.X, layer.W, torch.empty((T, N), dtype=torch.bfloat16, device="cuda"))
+        assert torch.equal(y, ref)
+
+
+def test_dense_rows_are_quantized_as_by_the_quantizer(metis):
+    for T, N, K in [(1, 200, 4096), (3, 64, 32), (20, 96, 1024), (40, 500, 2080), (200, 300, 512)]:
+        for dtype in (torch.bfloat16, torch.float32):
+            layer = _Layer(metis, T, N, K, torch.float32, T)
+            x = (layer.x.float() * 1.01).to(dtype)
+            x[0, :32] = 0.0                                      # a block of zeros
+            if K > 64:
+                x[0, 32:64] = 1e-39                              # a block below the normal numbers
+            q = metis.quantize_mx(x, metis.MxTensor(T, K))
+            a = metis.mxfp4_linear(x, layer.W, torch.empty((T, N), device="cuda"), bias=layer.bias)
+            b = metis.mxfp4_linear(q, layer.W, torch.empty((T, N), device="cuda"), bias=layer.bias)
+            assert (a - b).abs().max() <= 1e-5 * b.abs().max()
+            wide = torch.zeros((T, K + 16), dtype=dtype, device="cuda")
+            wide[:, 8:8 + K] = x
+            assert torch.equal(metis.mxfp4_linear(wide[:, 8:8 + K], layer.W, torch.empty((T, N), device="cuda"), bias=layer.bias), a)
+
+
+def test_large_and_missing_values(metis):
+    """Activations far from zero, infinities and NaN; a dropped element is 0 whatever it was."""
+    N, K = 96, 32
+    w = torch.zeros((N, K), device="cuda")
+    w[:, 0] = 1.0
+    W = metis.quantize_mx(w, metis.MxTensor(N, K))
+    x = torch.zeros((1, K), device="cuda")
+    far = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 5.0, -5.0, 12.0, -12.0, 30.0, -30.0, 1e4, -1e4, 1e12, -1e12, 3e38, -3e38], device="cuda")
+    bias = far.repeat(6)
+    for dtype in (torch.float32, torch.bfloat16):
+        for act in ("none", "relu", "gelu", "gelu_tanh", "silu"):
+            y = _f64(metis.mxfp4_linear(x, W, torch.empty((1, N), dtype=dtype, device="cuda"), bias=bias, act=act))[0]
+            z = _f64(bias)
+            with np.errstate(over="ignore", invalid="ignore"):
+                ref = np.nan_to_num(oep.act(act, z), nan=0.0)
+            ref = np.where((act != "none") & (z < -100), 0.0, np.where((act != "none") & (z > 100), z, ref))
+            assert np.all(np.abs(y - ref) <= (ROUND[dtype] + 4e-5) * np.abs(ref) + 1e-36), (act, y, ref)
+    bias[5], bias[7], bias[9] = float("nan"), float("inf"), float("-inf")
+    for act in ("none", "relu", "gelu", "silu"):
+        y = _f64(metis.mxfp4_linear(x, W, torch.empty((1, N), device="cuda"), bias=bias, act=act))[0]
+        assert np.isnan(y[5]) and y[7] == np.inf and np.isfinite(np.delete(y, [5, 7, 9])).all()
+    mask = metis.DropoutMask(0.5, 3)
+    m = oep.mask(0.5, 3, 0, [0], N)[0]
+    y = _f64(metis.mxfp4_linear(x, W, torch.empty((1, N), device="cuda"), bias=torch.full((N,), float("nan"), device="cuda"), mask=mask))[0]
+    assert np.isnan(y[m > 0]).all() and (y[m == 0] == 0).all() and (m == 0).any()
+
+
+@pytest.mark.parametrize("T,N", [(1, 8), (1, 1), (3, 515), (32, 512), (33, 1000), (200, 77), (1000, 2056), (4097, 40)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradient_of_the_epilogue(metis, T, N, dtype):
+    """dz: its slope's two terms are within 4e-5 of their values, three products round (2^-24 each), the result once more.  dbias: sums of T terms,
+    at most T + 160 roundings (a workgroup's rows one after the other, then its waves, then the workgroups' parts)."""
+    g = torch.Generator().manual_seed(T + N)
+    dy, z = torch.randn((T, N), generator=g).to(dtype), (2 * torch.randn((T, N), generator=g)).to(dtype)
+    for act, p, pad, inplace in (("none", 0.0, 0, False), ("gelu", 0.0, 0, False), ("gelu", 0.2, 3, True), ("relu", 0.1, 0, True), ("silu", 0.0, 1, False),
+                                 ("gelu_tanh", 0.3, 0, False), ("none", 0.5, 0, False)):
+        mask = metis.DropoutMask(p, 9, torch.tensor([7], device="cuda")) if p else None
+        wd, d = _offset(T, N, dtype, pad)
+        d.copy_(dy)
+        wz, dz = (wd, d) if inplace else _offset(T, N, dtype, pad)
+        wp, pre = _offset(T, N, dtype, pad)
+        pre.copy_(z)
+        db = torch.full((N,), 3.0, device="cuda")
+        assert metis.linear_grads(d, dz, pre=pre if act != "none" else None, act=act, mask=mask, dbias=db) is dz
+        m = oep.mask(p, 9, 7, np.arange(T), N) if p else 1.0
+        s1, s2 = oep.slope_terms(act, _f64(z))
+        d64 = _f64(dy) * m
+        ref = d64 * (s1 + s2)
+        err = np.abs(d64) * (4e-5 * (np.abs(s1) + np.abs(s2)) + 3 * 2.0 ** -24 * np.abs(s1 + s2)) + TINY
+        if act in ("none", "relu"):
+            err = 3 * 2.0 ** -24 * np.abs(ref)
+        got = _f64(dz)
+        assert np.all(np.abs(got - ref) <= err + ROUND[dtype] * (np.abs(ref) + err)), act
+        eb = err.sum(0) + (T + 160) * 2.0 ** -24 * np.abs(ref).sum(0)
+        assert np.all(np.abs(_f64(db) - ref.sum(0)) <= eb), act
+        if pad:
+            assert (wz[:, :pad] == 7).all() and (wz[:, N + pad:] == 7).all()
+        # one of the two alone, and the same bits every time
+        if not inplace:
+            again = torch.empty_like(db)
+            metis.linear_grads(d, None, pre=pre, act=act, mask=mask, dbias=again)
+            assert torch.equal(again, db)
+            alone = torch.empty_like(dy, device="cuda")
+            metis.linear_grads(d, alone, pre=pre, act=act, mask=mask)
+            assert torch.equal(alone, dz)
+
+
+def test_gradient_is_the_forward_pass_differences(metis):
+    """dz against differences of the forward pass itself: fp32, a step of 2^-7 (second-order error 2^-14 / 6 of a third derivative below 2, results
+    of magnitude up to 8 rounded to 2^-21, over 2^-6)."""
+    N, K, h = 256, 32, 2.0 ** -7
+    w = torch.zeros((N, K), device="cuda")
+    W, x = metis.quantize_mx(w, metis.MxTensor(N, K)), torch.zeros((1, K), device="cuda")
+    z = torch.linspace(-4, 4, N, device="cuda") + 0.01
+    mask = metis.DropoutMask(0.25, 11)
+    for act in ("gelu", "gelu_tanh", "silu"):
+        f = lambda b: metis.mxfp4_linear(x, W, torch.empty((1, N), device="cuda"), bias=b, act=act, mask=mask).double()
+        diff = (f(z + h) - f(z - h)) / (2 * h)
+        dz = metis.linear_grads(torch.ones((1, N), device="cuda"), torch.empty((1, N), device="cuda"), pre=z[None, :], act=act, mask=mask)
+        assert (diff - dz.double()).abs().max() < 4 / 3 * 2 * 2.0 ** -14 / 6 * 3 + 2.0 ** -15 * 4
+
+
+def test_no_rows(metis):
+    W = metis.MxTensor(16, 32)
+    e = torch.empty((0, 16), device="cuda")
+    metis.mxfp4_linear(torch.empty((0, 32), device="cuda"), W, e)
+    db = torch.ones(16, device="cuda")
+    metis.linear_grads(e, e, dbias=db)
+    assert (db == 0).all()
