@@ -1,30 +1,323 @@
 // A linear layer on MXFP4 operands whose epilogue adds a bias, applies an activation, drops elements and adds a residual; and the gradient of
 // that epilogue.
 #include "mx_gemm.h"
+#include "experts.h"
 #include "column_sums.h"
 
 namespace {
 
-struct LinearPlace {
-    size_t scales, bytes;                         // place of the rows' scales behind their codes, and the end
+// ---- few rows: the weights stream through registers ----
+// A workgroup has 16 OF outputs (the first operand of v_mfma_scale_f32_16x16x128_f8f6f4, so that a lane ends with four neighbouring outputs of a
+// row) and all rows, up to 16 TG.  Its waves share the contraction: a run of 512 elements is 16 blocks of a row, 256 bytes, read 64 at a time by the four
+// lanes that hold them; a wave takes every `waves`-th run, with the next one's weights on their way.  The waves' sums meet in LDS, added in their order, and
+// eight neighbouring outputs of a row go through the epilogue together.
+// FUSE (a type): the workgroup quantizes the rows itself, into LDS, while its first weights travel.
+struct DenseRows {
+    const void* ptr;
+    int64_t ld;
 };
-LinearPlace linear_place(int64_t rows, int64_t K) {
-    const size_t scales = align_up((size_t)rows * (K / 2), 256);
-    return {scales, scales + align_up((size_t)rows * (K / 32), 256)};
+typedef uint32_t lf_u4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef float lf_f4 __attribute__((ext_vector_type(4)));
+typedef int lf_i8 __attribute__((ext_vector_type(8)));
+#define FEW_ROWS 64
+constexpr int few_waves(int tg, int of) { return tg * of <= 2 ? 16 : 8; }         // at most: more rows need more registers a wave
+__host__ __device__ inline int few_runs(int nblk) { return (nblk + 15) / 16; }
+__host__ __device__ inline int few_codes_row(int nblk) { return few_runs(nblk) * 256 + 16; }        // 16 more spread the rows over the banks
+__host__ __device__ inline int few_scales_row(int nblk) { return few_runs(nblk) * 16; }
+// The lane's blocks 4 i + g of run r (c[i]) with their scale bytes (s[i], the lowest).  Behind the row: its last block, zeros where ZERO (one
+// operand's are enough).
+template <bool ZERO>
+__device__ __forceinline__ void run_load(const uint8_t* codes, const uint8_t* scales, int r, int nblk, int g, uvec4_t (&c)[4], uint32_t (&s)[4]) {
+    const int b = 16 * r;
+    if (b + 16 <= nblk) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const uvec4_t*>(codes + 16 * (int64_t)(b + g) + 64 * i);
+        const lf_u4_any w = *reinterpret_cast<const lf_u4_any*>(scales + b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = w[i] >> (8 * g);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int x = b + 4 * i + g, at = x < nblk ? x : nblk - 1;
+            c[i] = *reinterpret_cast<const uvec4_t*>(codes + 16 * (int64_t)at);
+            s[i] = scales[at];
+            if (ZERO && x >= nblk) c[i] = uvec4_t{0u, 0u, 0u, 0u};
+        }
+    }
+}
+
+template <typename OUT, int TG, int OF, typename T = void>
+__global__ void __launch_bounds__(64 * few_waves(TG, OF))
+k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> f) {
+    constexpr bool FUSE = !std::is_void<T>::value;
+    constexpr int PROW = 16 * OF + 4;                    // floats of a row's sums of one wave
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int li = lane & 15, g = lane >> 4, rows = (int)X.rows, runs = few_runs(nblk);
+    const int64_t N = W.rows, n0 = 16 * OF * (int64_t)blockIdx.x;
+    const uint8_t *wc[OF], *wsc[OF];
+#pragma unroll
+    for (int o = 0; o < OF; ++o) {
+        const int64_t n = n0 + 16 * o + li < N ? n0 + 16 * o + li : N - 1;
+        wc[o] = W.codes + n * nblk * 16;
+        wsc[o] = W.scales + n * nblk;
+    }
+    uvec4_t w[2][OF][4];
+    uint32_t ws[2][OF][4];
+    int r = wave;                                        // (waves <= runs)
+#pragma unroll
+    for (int o = 0; o < OF; ++o) run_load<false>(wc[o], wsc[o], r, nblk, g, w[0][o], ws[0][o]);
+    const uint8_t *tc[TG], *tsc[TG];                     // this lane's rows
+    if constexpr (FUSE) {
+        uint8_t* s_scales = s_mem + rows * few_codes_row(nblk);
+        const int per = runs * 64;                       // lanes a row: 8 elements each, four per block
+        for (int i = threadIdx.x; i < rows * per; i += blockDim.x) {
+            const int row = i / per, c = i - row * per;
+            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (c < 4 * nblk) load_row((const T*)dense.ptr + row * dense.ld + 8 * c, v);
+            uint32_t byte;
+            *reinterpret_cast<uint32_t*>(s_mem + row * few_codes_row(nblk) + 4 * c) = mx_quad(v, byte);
+            if ((i & 3) == 0) s_scales[row * few_scales_row(nblk) + (c >> 2)] = (uint8_t)byte;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int t = 0; t < TG; ++t) {
+        const int row = 16 * t + li < rows ? 16 * t + li : rows - 1;
+        if constexpr (FUSE) {
+            tc[t] = s_mem + row * few_codes_row(nblk);
+            tsc[t] = s_mem + rows * few_codes_row(nblk) + row * few_scales_row(nblk);
+        } else {
+            tc[t] = X.codes + (int64_t)row * nblk * 16;
+            tsc[t] = X.scales + (int64_t)row * nblk;
+        }
+    }
+    lf_f4 acc[OF][TG];
+#pragma unroll
+    for (int o = 0; o < OF; ++o)
+#pragma unroll
+        for (int t = 0; t < TG; ++t) acc[o][t] = lf_f4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto run = [&](auto now_) __attribute__((always_inline)) {
+        constexpr int now = decltype(now_)::value;
+        if (r + waves < runs) {
+#pragma unroll
+            for (int o = 0; o < OF; ++o) run_load<false>(wc[o], wsc[o], r + waves, nblk, g, w[now ^ 1][o], ws[now ^ 1][o]);
+        }
+#pragma unroll
+        for (int t = 0; t < TG; ++t) {
+            uvec4_t x[4];
+            uint32_t xs[4];
+            if constexpr (FUSE) {                        // (in whole runs, zeros behind the row)
+                const uvec4_t s = *reinterpret_cast<const uvec4_t*>(tsc[t] + 16 * r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = *reinterpret_cast<const uvec4_t*>(tc[t] + 256 * r + 64 * i + 16 * g);
+                    xs[i] = s[i] >> (8 * g);
+                }
+            } else {
+                run_load<true>(tc[t], tsc[t], r, nblk, g, x, xs);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const lf_i8 b = {(int)x[i].x, (int)x[i].y, (int)x[i].z, (int)x[i].w, 0, 0, 0, 0};
+#pragma unroll
+                for (int o = 0; o < OF; ++o) {
+                    const uvec4_t y = w[now][o][i];
+                    const lf_i8 a = {(int)y.x, (int)y.y, (int)y.z, (int)y.w, 0, 0, 0, 0};
+                    acc[o][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[o][t], 4, 4, 0, (int)ws[now][o][i], 0, (int)xs[i]);
+                }
+            }
+        }
+        r += waves;
+    };
+#pragma unroll 1
+    while (r < runs) {
+        run(std::integral_constant<int, 0>{});
+        if (r >= runs) break;
+        run(std::integral_constant<int, 1>{});
+    }
+    if constexpr (FUSE) __syncthreads();                 // the sums take the rows' place
+    float* s_part = reinterpret_cast<float*>(s_mem);
+#pragma unroll
+    for (int o = 0; o < OF; ++o)
+#pragma unroll
+        for (int t = 0; t < TG; ++t)
+            *reinterpret_cast<lf_f4*>(s_part + ((wave * TG + t) * 16 + li) * PROW + 16 * o + 4 * g) = acc[o][t];
+    __syncthreads();
+    const uint32_t step = mask_step(f.mask);
+    for (int u = threadIdx.x; u < rows * 2 * OF; u += blockDim.x) {
+        const int row = u / (2 * OF), unit = u % (2 * OF);
+        const int64_t c = n0 + 8 * unit;
+        if (c >= N) continue;
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}, b[8];
+        finish_bias(f, c, N, b);
+        for (int p = 0; p < waves; ++p) {
+            const lf_f4* q = reinterpret_cast<const lf_f4*>(s_part + (p * TG * 16 + row) * PROW + 8 * unit);
+            const lf_f4 lo = q[0], hi = q[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] += lo[i];
+                v[4 + i] += hi[i];
+            }
+        }
+        finish_unit(f, step, row, c, N - c, b, v);
+    }
+}
+
+// ---- few tiles: the contraction in parts ----
+#define PARTS_MAX 16
+// The parts' sums (fp32, rows of ld, a multiple of 8) added up in their order, through the epilogue.  A lane per eight outputs.
+template <typename OUT>
+__global__ void __launch_bounds__(256)
+k_linear_join(const float* __restrict__ sums, int64_t ld, int64_t stride, int parts, uint64_t total, FastDiv units, int64_t N, MxFinish<OUT> f) {
+    const uint64_t u = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (u >= total) return;
+    const int64_t r = (int64_t)div_by(units, u), c = 8 * (int64_t)(u - (uint64_t)r * units.d);
+    const float* p = sums + r * ld + c;
+    float v[8], b[8];
+    finish_bias(f, c, N, b);
+    load_row(p, v);
+    int i = 1;
+    for (; i + 3 < parts; i += 4) {
+        float x[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load_row(p + (i + k) * stride, x[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += x[k][e];
+    }
+    for (; i < parts; ++i) {
+        float x[8];
+        load_row(p + i * stride, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+    finish_unit(f, mask_step(f.mask), r, c, N - c, b, v);
+}
+
+struct LinearParts {
+    int count, units;                             // count 1: not cut
+    int64_t ld, stride;                           // of the sums
+};
+// A stage of a lone workgroup a CU takes 1.4 us where its weights come from memory (its loads are one stage ahead), the joining launch 3.5, and
+// an output's sum of a part is written and read at some 400 of them a ns.  us, whole / cut in 2 / 4 / 8, without the quantizer: 128 x 4096 x 14336 85.5 /
+// 48.7 / 30.5 / 23.1; 256 rows 78.8 / 46.5 / 31.2 / 37.3; 512 72.8 / 46.6 / 50.2 / 63.1; 128 x 14336 x 4096 29.3 / 24.4 / 30.5 / 41.9, 256 rows 28.3 / 38.7;
+// 128 x 4096 x 4096 18.4 / 15.0 / 14.8 / 18.8, 256 rows 17.9 / 17.6 / 20.2.
+LinearParts linear_parts(int64_t rows, int64_t N, int64_t K) {
+    const int64_t tiles = ceil_div64(rows, 128) * ceil_div64(N, 128), units = ceil_div64(K, MX_KI), ld = (N + 7) / 8 * 8;
+    LinearParts p = {1, (int)units, ld, (rows * ld + 63) / 64 * 64};
+    if (rows <= FEW_ROWS || tiles > 128) return p;
+    double least = 1.4 * units;
+    for (int64_t n = 2; n <= PARTS_MAX && n <= units / 2 && n * tiles <= 256; ++n) {
+        const int64_t per = ceil_div64(units, n);
+        const double t = 1.4 * per + 3.5 + n * rows * ld / 400e3;
+        if (t >= least) continue;
+        least = t;
+        p.units = (int)per;
+        p.count = (int)ceil_div64(units, per);
+    }
+    return p;
+}
+template <typename T>
+int launch_parts(hipStream_t s, const MxOperand& x, const MxOperand& w, int64_t K, const LinearParts& p, float* sums, const MxFinish<T>& f) {
+    constexpr size_t LDS = 2 * 256 * (size_t)(MX_CROW + MX_SROW);
+    const int64_t tm = ceil_div64(x.rows, 128), tn = ceil_div64(w.rows, 128), units = p.ld / 8;
+    const int us = units_status(x.rows, units);
+    if (us != METIS_OK) return us;
+    const MxOrder order = mx_order(tm, tn, K, 128);
+    auto launch = [&](auto kern, LdsLimitCache& lds_set) {
+        if (!ensure_dyn_lds((const void*)kern, LDS, lds_set)) return false;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn), (unsigned)p.count), dim3(512), LDS, s, x, w, K, sums, p.ld, true, order,
+                           MxParts{p.units, p.stride});
+        return true;
+    };
+    static LdsLimitCache lds_set[2];
+    const bool ok = K % MX_KI == 0 ? launch(k_mxfp4_gemm_nt<float, MX_WHOLE, 128, MxParts>, lds_set[0])
+                                   : launch(k_mxfp4_gemm_nt<float, MX_TAIL, 128, MxParts>, lds_set[1]);
+    if (!ok) return METIS_HIP_ERROR;
+    METIS_LAUNCH_CHECK();
+    const int64_t total = x.rows * units;
+    hipLaunchKernelGGL(k_linear_join<T>, dim3((unsigned)ceil_div64(total, 256)), dim3(256), 0, s, sums, p.ld, p.stride, p.count, (uint64_t)total,
+                       fast_div((uint32_t)units), w.rows, f);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+
+struct LinearPlace {
+    size_t scales, sums, bytes;                   // places of the rows' scales behind their codes and of the parts' sums, and the end
+    LinearParts parts;
+};
+LinearPlace linear_place(int64_t rows, int64_t N, int64_t K) {
+    LinearPlace p;
+    p.parts = linear_parts(rows, N, K);
+    p.scales = align_up((size_t)rows * (K / 2), 256);
+    p.sums = p.scales + align_up((size_t)rows * (K / 32), 256);
+    p.bytes = p.sums + (p.parts.count > 1 ? (size_t)p.parts.count * p.parts.stride * 4 : 0);
+    return p;
 }
 
 template <typename T>
-int launch_linear(hipStream_t s, const MxOperand& x, const MxOperand& w, int64_t K, const metis_epilogue* e, const metis_mat* Y) {
-    const MxFinish<T> f = {(T*)Y->ptr,
-                           Y->ld,
-                           e ? e->bias : nullptr,
-                           e && e->pre ? (T*)e->pre->ptr : nullptr,
-                           e && e->pre ? e->pre->ld : 0,
-                           e && e->residual ? (const T*)e->residual->ptr : nullptr,
-                           e && e->residual ? e->residual->ld : 0,
-                           mask_key(e ? e->mask : nullptr),
-                           e ? e->act : METIS_ACT_NONE};
-    return launch_mx_gemm<T>(s, x, w, K, f.y, f.ldy, f);
+MxFinish<T> finish_of(const metis_epilogue* e, const metis_mat* Y) {
+    return {(T*)Y->ptr,
+            Y->ld,
+            e ? e->bias : nullptr,
+            e && e->pre ? (T*)e->pre->ptr : nullptr,
+            e && e->pre ? e->pre->ld : 0,
+            e && e->residual ? (const T*)e->residual->ptr : nullptr,
+            e && e->residual ? e->residual->ld : 0,
+            mask_key(e ? e->mask : nullptr),
+            e ? e->act : METIS_ACT_NONE};
+}
+
+// How few rows are shared out: 16 or 32 outputs a workgroup, and as many waves as let a CU hold its share of the workgroups at once (16 waves a CU, or 8
+// where they need more registers; four at least).  us, 16 / 32 outputs: one row 14336 x 4096 11.6 / 10.3, 4096 x 14336 10.5 / 16.0; 64 rows 35.5 / 18.8,
+// 23.3 / 27.6.  24 rows of 14336 x 4096 with four waves 13.2, with eight (half of the workgroups wait) 15.9.
+struct FewShape {
+    int tg, of, waves;
+};
+FewShape few_shape(int64_t rows, int64_t N, int64_t K) {
+    const int tg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, of = N >= 8192 ? 2 : 1;
+    const int64_t wgs = ceil_div64(N, 16 * of);
+    // waves that a CU holds at once, over the workgroups that it has to hold
+    const int64_t room = 256 * (tg == 1 ? 16 : tg == 2 && of == 1 ? 16 : 8) / wgs;
+    const int64_t runs = few_runs((int)(K / 32));
+    int64_t most = room < few_waves(tg, of) ? room : few_waves(tg, of);
+    most = most < 4 ? 4 : most;
+    const int64_t per = (runs + most - 1) / most;
+    return {tg, of, (int)((runs + per - 1) / per)};
+}
+// Quantized on the spot up to 16384 elements in all.  us, with the quantizer's launch / on the spot, 14336 x 4096: one row 13.0 / 10.9, four 14.9 / 15.1,
+// eight 15.7 / 19.6; 4096 x 14336: one row 13.3 / 11.3, four 13.7 / 15.6.
+bool few_fused(int64_t rows, int64_t K) { return rows <= 16 && rows * K <= 16384; }
+template <typename OUT, int TG, int OF, typename IN>
+int launch_few(hipStream_t s, const MxOperand& x, const metis_mat* dense, const MxOperand& w, int64_t K, const MxFinish<OUT>& f, int waves) {
+    constexpr bool FUSE = !std::is_void<IN>::value;
+    const int nblk = (int)(K / 32);
+    const size_t sums = (size_t)waves * TG * 16 * (16 * OF + 4) * 4, rows = FUSE ? (size_t)x.rows * (few_codes_row(nblk) + few_scales_row(nblk)) : 0;
+    const size_t lds = sums > rows ? sums : rows;
+    auto kern = k_linear_few<OUT, TG, OF, IN>;
+    static LdsLimitCache lds_set;
+    if (!ensure_dyn_lds((const void*)kern, lds, lds_set)) return METIS_HIP_ERROR;
+    hipLaunchKernelGGL(kern, dim3((unsigned)ceil_div64(w.rows, 16 * OF)), dim3(64 * waves), lds, s, x,
+                       DenseRows{FUSE ? dense->ptr : nullptr, FUSE ? dense->ld : 0}, w, nblk, f);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+// dense: rows that the kernel quantizes itself, or null
+template <typename OUT>
+int launch_few_shape(hipStream_t s, const MxOperand& x, const metis_mat* dense, const MxOperand& w, int64_t K, const MxFinish<OUT>& f) {
+    const FewShape p = few_shape(x.rows, w.rows, K);
+    auto by_type = [&](auto tg, auto of) {
+        constexpr int TG = decltype(tg)::value, OF = decltype(of)::value;
+        if (!dense) return launch_few<OUT, TG, OF, void>(s, x, dense, w, K, f, p.waves);
+        if constexpr (TG == 1) return dense->dtype == METIS_BF16 ? launch_few<OUT, TG, OF, bf16_t>(s, x, dense, w, K, f, p.waves) : launch_few<OUT, TG, OF, float>(s, x, dense, w, K, f, p.waves);
+        else return (int)METIS_INVALID_ARG;
+    };
+    auto by_of = [&](auto tg) {
+        return p.of == 1 ? by_type(tg, std::integral_constant<int, 1>{}) : by_type(tg, std::integral_constant<int, 2>{});
+    };
+    return p.tg == 1 ? by_of(std::integral_constant<int, 1>{}) : p.tg == 2 ? by_of(std::integral_constant<int, 2>{}) : by_of(std::integral_constant<int, 4>{});
 }
 
 // ---- gradient of the epilogue ----
@@ -94,7 +387,7 @@ bool same_layout(const metis_mat* a, const metis_mat* b) { return a->rows == b->
 
 extern "C" size_t metis_mxfp4_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K) {
     if (rows < 1 || N < 1 || K < 32 || K % 32 || rows > 0xFFFFFFFFll / (K / 2) || N > 0xFFFFFFFFll / (K / 2)) return 0;
-    return linear_place(rows, K).bytes;
+    return linear_place(rows, N, K).bytes;
 }
 
 extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_mxfp4* Xq, const metis_mxfp4* W, const metis_epilogue* e,
@@ -110,20 +403,29 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
     if (e && ((e->pre && !same_layout(e->pre, Y)) || (e->residual && !same_layout(e->residual, Y)))) return METIS_BAD_SHAPE;
     if (X && (X->ld < K || !mat_aligned16(X))) return METIS_BAD_SHAPE;
     uint8_t* ws = (uint8_t*)workspace;
-    const LinearPlace place = linear_place(rows, K);
+    const LinearPlace place = linear_place(rows, N, K);
     metis_mxfp4 q = X ? metis_mxfp4{ws, ws + place.scales, rows, K} : *Xq;
     const int st = mx_operands_status(X ? W : &q, W);
     if (st != METIS_OK) return st;
+    const bool few = rows <= FEW_ROWS, fused = few && X && few_fused(rows, K);
     if (X) {
         if (rows * (K / 2) > 0xFFFFFFFFll) return METIS_UNSUPPORTED;
         if (!workspace || workspace_bytes < place.bytes) return METIS_WORKSPACE_TOO_SMALL;
         if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
-        const int qs = metis_quantize_mx(stream, X, &q);
+        const int qs = fused ? METIS_OK : metis_quantize_mx(stream, X, &q);
         if (qs != METIS_OK) return qs;
     }
+    const bool cut = place.parts.count > 1 && workspace && workspace_bytes >= place.bytes && (uintptr_t)workspace % 256 == 0;
     const MxOperand x = {q.codes, q.scales, rows}, w = {W->codes, W->scales, N};
     hipStream_t s = (hipStream_t)stream;
-    return Y->dtype == METIS_BF16 ? launch_linear<bf16_t>(s, x, w, K, e, Y) : launch_linear<float>(s, x, w, K, e, Y);
+    auto launch = [&](auto zero) {
+        typedef decltype(zero) T;
+        const MxFinish<T> f = finish_of<T>(e, Y);
+        if (few) return launch_few_shape<T>(s, x, fused ? X : nullptr, w, K, f);
+        if (cut) return launch_parts<T>(s, x, w, K, place.parts, (float*)(ws + place.sums), f);
+        return launch_mx_gemm<T>(s, x, w, K, f.y, f.ldy, f);
+    };
+    return Y->dtype == METIS_BF16 ? launch(bf16_t()) : launch(float());
 }
 
 extern "C" size_t metis_linear_grads_workspace_bytes(int64_t rows, int64_t cols) {
