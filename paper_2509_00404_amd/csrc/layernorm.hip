@@ -4,7 +4,11 @@
 namespace {
 
 // A row belongs to RT threads, each of which holds U units of eight neighbouring elements in registers: unit u of thread t starts at column
-// 8 (t + RT u).  RT 64: a workgroup of 256 has four rows, else one.  Workgroups go through the rows with the weights in registers.
+// 8 (t + RT u).  RT 64: a workgroup of 256 has four rows, else one.  Workgroups go through the rows with the weights in registers and the next row
+// on its way.  Whole vectors everywhere: a row's last unit, where it is short, lies at the row's end and has its first elements in common with the unit
+// before it, and units behind the row are that unit once more.  What a thread has twice (`twice` elements of a unit, the first ones) stays out of
+// the sums, and is stored twice with the same bits.  No load or store in the loops is under a condition: the wait for the next row would wait for
+// this row's stores too, which come behind it in the queue, where the compiler cannot count them.  Rows of fewer than eight elements go to the kernels for long ones, which look at each.
 template <int RT>
 struct RowGroup {
     static constexpr int THREADS = RT < 256 ? 256 : RT, ROWS = THREADS / RT, WAVES = RT / 64;
@@ -45,16 +49,28 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* slot) {
         }
     }
 }
-template <int U>
-__device__ __forceinline__ void load_factors(const float* p, float none, int64_t cols, int t, int rt, float (&v)[U][8]) {
+// Nothing is on its way into a loop from before it: what the loop waits for is then counted from its own loads and stores alone.
+__device__ __forceinline__ void loads_arrived() { __builtin_amdgcn_s_waitcnt(0xF70); }     // vmcnt(0)
+struct UnitPlace {
+    int64_t c;
+    int twice;                                // 8: a unit behind the row
+};
+template <int RT>
+__device__ __forceinline__ UnitPlace unit_place(int t, int u, int64_t cols) {
+    const int64_t c = 8 * (int64_t)(t + RT * u), last = cols - 8;
+    return c <= last ? UnitPlace{c, 0} : UnitPlace{last, c - last < 8 ? (int)(c - last) : 8};
+}
+__device__ __forceinline__ void load_factors(const float* p, float none, float (&v)[8]) {
+    if (p) {
+        load_row<true>(p, v);
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t c = 8 * (int64_t)(t + rt * u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] = none;
-        if (p && c < cols) load_part<float, true>(p + c, cols - c, v[u]);
+        for (int i = 0; i < 8; ++i) v[i] = none;
     }
 }
+
+// Two passes over what the registers hold, mean first, so that a mean far from zero costs the variance nothing.  Memory bounds it: 16384 x 4096 bf16
+// (268 MB) takes 43.6 us, 6.2 TB/s (part of the rows is still in the last-level cache).
 template <typename T, int RT, int U>
 __global__ void __launch_bounds__(RowGroup<RT>::THREADS)
 k_layernorm(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
@@ -65,40 +81,45 @@ k_layernorm(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __restrict_
     const int own = RT == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
     const float n = (float)cols;
     float w[U][8], b[U][8];
-    load_factors<U>(weight, 1.0f, cols, t, RT, w);
-    load_factors<U>(bias, 0.0f, cols, t, RT, b);
-    for (int64_t r = (int64_t)blockIdx.x * G::ROWS + own; r < rows; r += (int64_t)gridDim.x * G::ROWS) {
+    UnitPlace at[U];
+    RawUnit<T> next[U];
+    const int64_t hop = (int64_t)gridDim.x * G::ROWS;
+    int64_t r = (int64_t)blockIdx.x * G::ROWS + own;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        at[u] = unit_place<RT>(t, u, cols);
+        if (r < rows) load_whole(x + r * ldx + at[u].c, next[u]);
+        load_factors(weight ? weight + at[u].c : nullptr, 1.0f, w[u]);
+        load_factors(bias ? bias + at[u].c : nullptr, 0.0f, b[u]);
+    }
+    loads_arrived();
+    for (; r < rows; r += hop) {
         float v[U][8], sum[1] = {0.0f};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t c = 8 * (int64_t)(t + RT * u);
+            unpack(next[u], v[u]);
+            load_whole(x + (r + hop < rows ? r + hop : r) * ldx + at[u].c, next[u]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
-            if (c < cols) load_part<T, true>(x + r * ldx + c, cols - c, v[u]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[0] += v[u][i];
+            for (int i = 0; i < 8; ++i) sum[0] += i >= at[u].twice ? v[u][i] : 0.0f;
         }
         row_sums<RT>(sum, s_mean);
         const float mean = sum[0] / n;
         sum[0] = 0.0f;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t c = 8 * (int64_t)(t + RT * u);
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 v[u][i] -= mean;
-                if (c + i < cols) sum[0] = fmaf(v[u][i], v[u][i], sum[0]);
+                sum[0] = i >= at[u].twice ? fmaf(v[u][i], v[u][i], sum[0]) : sum[0];
             }
-        }
         row_sums<RT>(sum, s_var);
         const float rstd = 1.0f / sqrtf(sum[0] / n + eps);
         if (stats && t == 0) stats[r] = make_float2(mean, rstd);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t c = 8 * (int64_t)(t + RT * u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[u][i] = fmaf(v[u][i] * rstd, w[u][i], b[u][i]);
-            if (c < cols) store_part<T, true>(y + r * ldy + c, cols - c, v[u]);
+            store_row<true>(y + r * ldy + at[u].c, v[u]);
         }
     }
 }
@@ -114,7 +135,7 @@ k_layernorm_long(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __rest
         float sum[1] = {0.0f}, v[8];
         auto each = [&](auto f) __attribute__((always_inline)) {
             for (int64_t c = 8 * (int64_t)threadIdx.x; c < cols; c += 8192) {
-                load_part<T, true>(x + r * ldx + c, cols - c, v);
+                load_unit(x + r * ldx + c, cols - c, v);
                 f(c);
             }
         };
@@ -135,8 +156,8 @@ k_layernorm_long(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __rest
         if (stats && threadIdx.x == 0) stats[r] = make_float2(mean, rstd);
         each([&](int64_t c) {
             float w[8] = {1, 1, 1, 1, 1, 1, 1, 1}, b[8] = {};
-            if (weight) load_part<float, true>(weight + c, cols - c, w);
-            if (bias) load_part<float, true>(bias + c, cols - c, b);
+            if (weight) load_unit(weight + c, cols - c, w);
+            if (bias) load_unit(bias + c, cols - c, b);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - mean) * rstd, w[i], b[i]);
             store_part<T, true>(y + r * ldy + c, cols - c, v);
@@ -147,55 +168,77 @@ k_layernorm_long(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __rest
 // ---- gradients ----
 // xh = (x - mean) rstd, g = dy w:  dx = add + rstd (g - mean of g - xh * mean of g xh).  Both means come from one pass over what the registers
 // hold; the columns' sums of dy xh and dy stay in registers over all the rows of a workgroup, and leave as one row of `sums` [gridDim.x, 2 cols].
-template <typename T, int RT, int U>
+// Memory bounds it: 16384 x 4096 bf16 with `add` (537 MB) takes 93 us, 5.8 TB/s, and the sums' join 2.4 (with the rows' loads where they are used, not a
+// row ahead, 160).
+template <typename T, int RT, int U, bool ADD>
 __global__ void __launch_bounds__(RowGroup<RT>::THREADS)
 k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
                   const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows, int64_t cols, float* __restrict__ sums) {
     typedef RowGroup<RT> G;
+    constexpr bool AHEAD = RT * U <= 1024;               // (of 16384 columns a thread has no registers for the next row and the weights)
     __shared__ float s_sum[2][2 * G::WAVES], s_join[RT == 64 ? 3 * 512 : 1];
     const int t = RT == 64 ? (int)threadIdx.x & 63 : (int)threadIdx.x;
     const int own = RT == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
     const float n = (float)cols;
     float w[U][8], dw[U][8], db[U][8];
-    load_factors<U>(weight, 1.0f, cols, t, RT, w);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dw[u][i] = db[u][i] = 0.0f;
-    int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * G::ROWS + own; r < rows; r += (int64_t)gridDim.x * G::ROWS, turn ^= 1) {
-        float xh[U][8], g[U][8], sum[2] = {0.0f, 0.0f};
-        const float2 st = stats[r];
+    UnitPlace at[U];
+    RawUnit<T> nx[U], nd[U], na[U];
+    float2 nst = make_float2(0.0f, 0.0f);
+    const int64_t hop = (int64_t)gridDim.x * G::ROWS;
+    int64_t r = (int64_t)blockIdx.x * G::ROWS + own;
+    auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+        nst = stats[row];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t c = 8 * (int64_t)(t + RT * u);
+            load_whole(x + row * ldx + at[u].c, nx[u]);
+            load_whole(dy + row * ldd + at[u].c, nd[u]);
+            if (ADD) load_whole(add + row * lda + at[u].c, na[u]);
+        }
+    };
 #pragma unroll
-            for (int i = 0; i < 8; ++i) xh[u][i] = st.x, g[u][i] = 0.0f;                  // (xh becomes 0)
-            if (c < cols) {
-                load_part<T, true>(x + r * ldx + c, cols - c, xh[u]);
-                load_part<T, true>(dy + r * ldd + c, cols - c, g[u]);
-            }
+    for (int u = 0; u < U; ++u) at[u] = unit_place<RT>(t, u, cols);
+    if (AHEAD && r < rows) fetch(r);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (AHEAD) load_factors(weight ? weight + at[u].c : nullptr, 1.0f, w[u]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[u][i] = db[u][i] = 0.0f;
+    }
+    loads_arrived();
+    for (int turn = 0; r < rows; r += hop, turn ^= 1) {
+        float xh[U][8], g[U][8], sum[2] = {0.0f, 0.0f};
+        RawUnit<T> plus[U];
+        if (!AHEAD) fetch(r);
+        const float2 st = nst;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            unpack(nx[u], xh[u]);
+            unpack(nd[u], g[u]);
+            plus[u] = na[u];
+        }
+        if (AHEAD) fetch(r + hop < rows ? r + hop : r);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!AHEAD) load_factors(weight ? weight + at[u].c : nullptr, 1.0f, w[u]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 xh[u][i] = (xh[u][i] - st.x) * st.y;
                 dw[u][i] = fmaf(g[u][i], xh[u][i], dw[u][i]);
                 db[u][i] += g[u][i];
                 g[u][i] *= w[u][i];
-                sum[0] += g[u][i];
-                sum[1] = fmaf(g[u][i], xh[u][i], sum[1]);
+                sum[0] += i >= at[u].twice ? g[u][i] : 0.0f;
+                sum[1] = i >= at[u].twice ? fmaf(g[u][i], xh[u][i], sum[1]) : sum[1];
             }
         }
         row_sums<RT>(sum, s_sum[turn]);
         const float mg = sum[0] / n, mx = sum[1] / n;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t c = 8 * (int64_t)(t + RT * u);
-            if (c >= cols) continue;
             float a[8] = {};
-            if (add) load_part<T, true>(add + r * lda + c, cols - c, a);
+            if (ADD) unpack(plus[u], a);
 #pragma unroll
             for (int i = 0; i < 8; ++i) a[i] = fmaf(st.y, g[u][i] - mg - xh[u][i] * mx, a[i]);
-            store_part<T, true>(dx + r * ldo + c, cols - c, a);
+            store_row<true>(dx + r * ldo + at[u].c, a);
         }
     }
     if (!sums) return;
@@ -215,10 +258,8 @@ k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float
                 for (int i = 0; i < 8; ++i) s[0][i] += s_join[p * 512 + 64 * i + t];
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t c = 8 * (int64_t)(t + RT * u);
-            if (c < cols) store_part<float, true>(to + c, cols - c, s[u]);
-        }
+        for (int u = 0; u < U; ++u)
+            if (at[u].twice < 8) store_row<true>(to + at[u].c, s[u]);
     };
     leave(dw, out);
     leave(db, out + cols);
@@ -238,9 +279,9 @@ k_layernorm_grads_long(const T* dy, int64_t ldd, const T* x, int64_t ldx, const 
         auto each = [&](auto f) __attribute__((always_inline)) {
             for (int64_t c = 8 * (int64_t)threadIdx.x; c < cols; c += 8192) {
                 float w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-                load_part<T, true>(x + r * ldx + c, cols - c, xh);
-                load_part<T, true>(dy + r * ldd + c, cols - c, g);                   // (zeros behind the row)
-                if (weight) load_part<float, true>(weight + c, cols - c, w);
+                load_unit(x + r * ldx + c, cols - c, xh);
+                load_unit(dy + r * ldd + c, cols - c, g);                   // (zeros behind the row)
+                if (weight) load_unit(weight + c, cols - c, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     xh[i] = (xh[i] - st.x) * st.y;
@@ -260,7 +301,7 @@ k_layernorm_grads_long(const T* dy, int64_t ldd, const T* x, int64_t ldx, const 
         const float mg = sum[0] / n, mx = sum[1] / n;
         each([&](int64_t c) {
             float a[8] = {};
-            if (add) load_part<T, true>(add + r * lda + c, cols - c, a);
+            if (add) load_unit(add + r * lda + c, cols - c, a);
 #pragma unroll
             for (int i = 0; i < 8; ++i) a[i] = fmaf(st.y, g[i] - mg - xh[i] * mx, a[i]);
             store_part<T, true>(dx + r * ldo + c, cols - c, a);
@@ -281,8 +322,8 @@ k_layernorm_columns(const T* __restrict__ dy, int64_t ldd, const T* __restrict__
         for (int64_t r = first + wave; r < end; r += 4) {
             const float2 st = stats[r];
             float v[8], g[8];
-            load_part<T, true>(x + r * ldx + c, n, v);
-            load_part<T, true>(dy + r * ldd + c, n, g);
+            load_unit(x + r * ldx + c, n, v);
+            load_unit(dy + r * ldd + c, n, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 s[0][i] = fmaf(g[i], (v[i] - st.x) * st.y, s[0][i]);
@@ -307,9 +348,13 @@ k_layernorm_columns(const T* __restrict__ dy, int64_t ldd, const T* __restrict__
     }
 }
 
-#define NORM_REGS 16384                           // longest row whose gradient's kernel keeps it, and its columns' sums, in registers
-#define NORM_PARTS 512                            // rows of partial sums at most, the same on any chip so that the sums have the same order
+#define NORM_REGS 16384                           // longest row that a workgroup keeps, with its columns' sums, in registers
+// Workgroups of the gradients' kernel at most, each of which leaves a row of partial sums: one a CU, and the same on any chip so that the sums have the
+// same order.  More lose what their partial sums cost: 16384 x 4096 bf16 with `add`, us: 192 113, 256 97, 384 108, 512 108, 1024 119; 1111 x 2057 fp32:
+// 128 15.3, 256 13.5, 512 16.0.
+#define NORM_PARTS 256
 
+bool in_registers(int64_t cols) { return cols >= 8 && cols <= NORM_REGS; }
 int64_t norm_rows(int64_t cols) { return cols <= 512 ? 4 : 1; }          // rows of a workgroup at a time
 int64_t norm_parts(int64_t rows, int64_t cols) {
     const int64_t groups = ceil_div64(rows, norm_rows(cols));
@@ -320,7 +365,7 @@ int64_t column_chunk(int64_t rows, int64_t cols) {                       // rows
     return chunk < 32 ? 32 : chunk;
 }
 int64_t sum_rows(int64_t rows, int64_t cols) {
-    return cols <= NORM_REGS ? norm_parts(rows, cols) : ceil_div64(rows, column_chunk(rows, cols));
+    return in_registers(cols) ? norm_parts(rows, cols) : ceil_div64(rows, column_chunk(rows, cols));
 }
 // the threads of a row and the units of a thread: f(threads, units)
 template <typename F>
@@ -353,7 +398,7 @@ extern "C" int metis_layernorm(void* stream, const metis_mat* x, const float* we
             hipLaunchKernelGGL(kern, dim3((unsigned)(groups < most ? groups : most)), dim3(threads), 0, s, (const T*)x->ptr, x->ld, (T*)y->ptr,
                                y->ld, weight, bias, eps, (float2*)stats, rows, cols);
         };
-        if (cols > NORM_REGS) return go(k_layernorm_long<T>, 1024, rows, 512);
+        if (!in_registers(cols)) return go(k_layernorm_long<T>, 1024, rows, 512);
         by_length(cols, [&](auto rt, auto u) {
             constexpr int RT = decltype(rt)::value;
             go(k_layernorm<T, RT, decltype(u)::value>, RowGroup<RT>::THREADS, ceil_div64(rows, RowGroup<RT>::ROWS), RT == 1024 ? 512 : 2048);
@@ -395,7 +440,7 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
         typedef decltype(zero) T;
         const T *pd = (const T*)dy->ptr, *px = (const T*)x->ptr, *pa = add ? (const T*)add->ptr : nullptr;
         const int64_t la = add ? add->ld : 0;
-        if (cols > NORM_REGS) {
+        if (!in_registers(cols)) {
             if (columns) {
                 const int64_t chunk = column_chunk(rows, cols);
                 hipLaunchKernelGGL(k_layernorm_columns<T>, dim3((unsigned)ceil_div64(cols, 512), (unsigned)ceil_div64(rows, chunk)), dim3(256), 0, s,
@@ -407,7 +452,8 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
         } else {
             by_length(cols, [&](auto rt, auto u) {
                 constexpr int RT = decltype(rt)::value;
-                auto kern = k_layernorm_grads<T, RT, decltype(u)::value>;
+                constexpr int U = decltype(u)::value;
+                auto kern = add ? k_layernorm_grads<T, RT, U, true> : k_layernorm_grads<T, RT, U, false>;
                 hipLaunchKernelGGL(kern, dim3((unsigned)norm_parts(rows, cols)), dim3(RowGroup<RT>::THREADS), 0, s, pd, dy->ld, px, x->ld,
                                    (const float2*)stats, weight, pa, la, (T*)dx->ptr, dx->ld, rows, cols, sums);
             });

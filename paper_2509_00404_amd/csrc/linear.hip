@@ -321,64 +321,79 @@ int launch_few_shape(hipStream_t s, const MxOperand& x, const metis_mat* dense, 
 }
 
 // ---- gradient of the epilogue ----
-// dz = act'(pre) m dy, and the sum of its columns.  A workgroup has 512 columns, a lane eight of them, and its four waves take every fourth of
-// its rows: the columns' sums stay in registers.
-template <typename T>
+// dz = act'(pre) m dy, and the sum of its columns.  A lane has eight columns and goes down its rows with the next two on their way; the columns' sums stay in
+// registers.  WIDE: the four waves of a workgroup lie side by side, 2048 columns, else they take neighbouring rows of 512 columns.  Workgroups take
+// turns at the rows, so that what is read at any time lies together: with runs of rows of their own 16384 x 14336 bf16 takes 289 us (gelu) and 277
+// (relu), so 269 and 245.  Memory bounds it: 1.41 GB, 5.3 and 5.8 TB/s.
+template <typename T, int ACT, bool WIDE, bool PAST>
 __global__ void __launch_bounds__(256)
-k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64_t ldz, int act, MaskKey mask, int64_t rows, int64_t cols,
-               int64_t chunk, float* __restrict__ sums) {
-    __shared__ float s_sum[3 * 8 * 64];
+k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64_t ldz, MaskKey mask, int64_t rows, int64_t cols,
+               float* __restrict__ sums) {
+    __shared__ float s_sum[WIDE ? 1 : 3 * 8 * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t c = 512 * (int64_t)blockIdx.x + 8 * lane, n = cols - c;
-    const int64_t first = chunk * blockIdx.y, end = first + chunk < rows ? first + chunk : rows;
+    const int64_t c = (WIDE ? 2048 * (int64_t)blockIdx.x + 512 * wave : 512 * (int64_t)blockIdx.x) + 8 * lane, n = cols - c;
+    const int64_t hop = WIDE ? gridDim.y : 4 * (int64_t)gridDim.y;
     const uint32_t step = mask_step(mask);
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-    if (n > 0) {
-#pragma unroll 2
-        for (int64_t r = first + wave; r < end; r += 4) {
+    int64_t r = WIDE ? blockIdx.y : 4 * (int64_t)blockIdx.y + wave;
+    if (n > 0 && r < rows) {
+        RawUnit<T> nd[2], np[2];
+        auto fetch = [&](int64_t row, int k) __attribute__((always_inline)) {
+            load_raw<PAST>(dy + row * ldd + c, n, nd[k]);
+            if (ACT != METIS_ACT_NONE) load_raw<PAST>(pre + row * ldp + c, n, np[k]);
+        };
+        auto one = [&](int64_t row, int k) __attribute__((always_inline)) {
             float v[8], z[8];
-            load_part<T, true>(dy + r * ldd + c, n, v);
-            if (pre) load_part<T, true>(pre + r * ldp + c, n, z);
-            if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)r, v);
-            if (pre) {
-                auto all = [&](int a) __attribute__((always_inline)) {
+            unpack(nd[k], v);
+            if (ACT != METIS_ACT_NONE) unpack(np[k], z);
+            fetch(row + 2 * hop < rows ? row + 2 * hop : row, k);
+            if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)row, v);
+            if (ACT != METIS_ACT_NONE) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] *= act_slope<sizeof(T) == 2>(a, z[i]);
-                };
-                switch (act) {
-                    case METIS_ACT_RELU: all(METIS_ACT_RELU); break;
-                    case METIS_ACT_GELU: all(METIS_ACT_GELU); break;
-                    case METIS_ACT_GELU_TANH: all(METIS_ACT_GELU_TANH); break;
-                    case METIS_ACT_SILU: all(METIS_ACT_SILU); break;
-                    default: break;
-                }
+                for (int i = 0; i < 8; ++i) v[i] *= act_slope<sizeof(T) == 2>(ACT, z[i]);
             }
-            if (dz) store_part<T, true>(dz + r * ldz + c, n, v);
+            if (dz) store_unit<PAST>(dz + row * ldz + c, n, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        };
+        fetch(r, 0);
+        fetch(r + hop < rows ? r + hop : r, 1);
+        for (; r < rows; r += 2 * hop) {
+            one(r, 0);
+            if (r + hop < rows) one(r + hop, 1);
         }
     }
     if (!sums) return;
-    if (wave > 0) {
+    if constexpr (!WIDE) {
+        if (wave > 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s_sum[((wave - 1) * 8 + i) * 64 + lane] = sum[i];
+            for (int i = 0; i < 8; ++i) s_sum[((wave - 1) * 8 + i) * 64 + lane] = sum[i];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += s_sum[(p * 8 + i) * 64 + lane];
     }
-    __syncthreads();
-    if (wave > 0 || n <= 0) return;
-#pragma unroll
-    for (int p = 0; p < 3; ++p)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += s_sum[(p * 8 + i) * 64 + lane];
-    store_part<float, true>(sums + blockIdx.y * cols + c, n, sum);
+    if (n > 0) store_part<float, true>(sums + blockIdx.y * cols + c, n, sum);
 }
 
-// Rows of a workgroup: some 2048 workgroups in all, 32 rows each at least, the same on any chip so that the sums have the same order.
-int64_t grads_chunk(int64_t rows, int64_t cols) {
-    const int64_t strips = ceil_div64(cols, 512), chunks = ceil_div64(2048, strips);
-    const int64_t chunk = ceil_div64(rows, chunks);
-    return chunk < 32 ? 32 : chunk;
+// Past the caches from 128 MiB a matrix on, where the three do not fit the last-level cache: us, through / past, 16384 x 14336 283 / 269, 16384 x 4096 82 / 77,
+// 4096 x 4096 23.8 / 27.4.
+#define GRADS_PAST (128ll << 20)
+bool grads_wide(int64_t cols) { return cols >= 2048; }
+int64_t grads_strips(int64_t cols) { return ceil_div64(cols, grads_wide(cols) ? 2048 : 512); }
+// Workgroups that share the rows of a strip, each of which leaves a row of partial sums: 1024 in all where each has eight rows or more, else 512 with two rows at
+// least; the same on any chip so that the sums have the same order.  us, 512 / 1024 / 2048, gelu, bf16: 16384 x 14336 300 / 269 / 292, 16384 x 4096 87 / 77 /
+// 86, 4096 x 4096 25.0 / 23.8 / 29.4, 1000 x 4096 11.6 / 14.7.  Two / four / eight rows at least: 100 x 4096 7.8 / 8.4 / 10.8.
+int64_t grads_parts(int64_t rows, int64_t cols) {
+    const int64_t strips = grads_strips(cols), many = strips < 1024 ? 1024 / strips : 1, few = strips < 512 ? 512 / strips : 1;
+    if (rows >= 8 * many) return many;
+    const int64_t want = ceil_div64(rows, 2);
+    return want < few ? want : few;
 }
 
 bool same_layout(const metis_mat* a, const metis_mat* b) { return a->rows == b->rows && a->cols == b->cols && a->ld >= a->cols; }
@@ -430,7 +445,7 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
 
 extern "C" size_t metis_linear_grads_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || cols < 1 || cols > (1 << 28) || rows > 0xFFFFFFFFll) return 0;
-    const int64_t chunks = ceil_div64(rows, grads_chunk(rows, cols));
+    const int64_t chunks = grads_parts(rows, cols);
     return chunks > 1 ? align_up((size_t)chunks * cols * 4, 256) : 0;
 }
 
@@ -448,20 +463,32 @@ extern "C" int metis_linear_grads(void* stream, const metis_mat* dY, const metis
     if (rows == 0) return dbias ? launch_clear(s, dbias, cols) : METIS_OK;
     if ((pre && (!mat_ok(pre) || pre->dtype != dY->dtype)) || (dZ && (!mat_ok(dZ) || dZ->dtype != dY->dtype))) return METIS_INVALID_ARG;
     if ((pre && !same_layout(pre, dY)) || (dZ && !same_layout(dZ, dY))) return METIS_BAD_SHAPE;
-    const int64_t chunk = grads_chunk(rows, cols), chunks = ceil_div64(rows, chunk), strips = ceil_div64(cols, 512);
+    const int64_t chunks = grads_parts(rows, cols), strips = grads_strips(cols);
     if (!grid_fits(strips, 256) || chunks > 65535) return METIS_UNSUPPORTED;
     const bool parts = dbias && chunks > 1;
     if (parts && (!workspace || workspace_bytes < metis_linear_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;
     if (parts && (uintptr_t)workspace % 256) return METIS_INVALID_ARG;
     float* sums = parts ? (float*)workspace : dbias;
-    auto launch = [&](auto zero) {
+    auto launch = [&](auto zero, auto a) {
         typedef decltype(zero) T;
-        hipLaunchKernelGGL(k_linear_grads<T>, dim3((unsigned)strips, (unsigned)chunks), dim3(256), 0, s, (const T*)dY->ptr, dY->ld,
-                           pre ? (const T*)pre->ptr : nullptr, pre ? pre->ld : 0, dZ ? (T*)dZ->ptr : nullptr, dZ ? dZ->ld : 0, act,
-                           mask_key(mask), rows, cols, chunk, sums);
+        constexpr int ACT = decltype(a)::value;
+        const bool past = rows * cols * mat_size(dY) >= GRADS_PAST;
+        auto kern = grads_wide(cols) ? past ? k_linear_grads<T, ACT, true, true> : k_linear_grads<T, ACT, true, false> : k_linear_grads<T, ACT, false, false>;
+        hipLaunchKernelGGL(kern, dim3((unsigned)strips, (unsigned)chunks), dim3(256), 0, s, (const T*)dY->ptr, dY->ld,
+                           pre ? (const T*)pre->ptr : nullptr, pre ? pre->ld : 0, dZ ? (T*)dZ->ptr : nullptr, dZ ? dZ->ld : 0, mask_key(mask),
+                           rows, cols, sums);
     };
-    if (dY->dtype == METIS_BF16) launch(bf16_t());
-    else launch(float());
+    auto by_act = [&](auto zero) {
+        switch (act) {
+            case METIS_ACT_RELU: launch(zero, std::integral_constant<int, METIS_ACT_RELU>{}); break;
+            case METIS_ACT_GELU: launch(zero, std::integral_constant<int, METIS_ACT_GELU>{}); break;
+            case METIS_ACT_GELU_TANH: launch(zero, std::integral_constant<int, METIS_ACT_GELU_TANH>{}); break;
+            case METIS_ACT_SILU: launch(zero, std::integral_constant<int, METIS_ACT_SILU>{}); break;
+            default: launch(zero, std::integral_constant<int, METIS_ACT_NONE>{}); break;
+        }
+    };
+    if (dY->dtype == METIS_BF16) by_act(bf16_t());
+    else by_act(float());
     METIS_LAUNCH_CHECK();
     return parts ? launch_join(s, sums, chunks, cols, dbias, cols, nullptr) : METIS_OK;
 }
