@@ -167,9 +167,10 @@ inline bool act_ok(int act) { return act >= METIS_ACT_NONE && act <= METIS_ACT_S
 
 // ---- the epilogue ----
 struct MxPlain {};                                // a product's outputs as they are
-struct MxParts {                                  // stages of a part of the contraction, and from one part's outputs (fp32) to the next one's
+struct MxParts {                                  // fp32 sums of a part of the contraction, `units` of it, one part's behind the other's
+    float* sums;
+    int64_t ld, stride;
     int units;
-    int64_t stride;
 };
 template <typename T>
 struct MxFinish {

@@ -164,7 +164,9 @@ k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> 
     }
 }
 
-// ---- few tiles: the contraction in parts ----
+// ---- few tiles ----
+#include "mx_deep.h"
+
 #define PARTS_MAX 16
 // The parts' sums (fp32, rows of ld, a multiple of 8) added up in their order, through the epilogue.  A lane per eight outputs.
 template <typename OUT>
@@ -200,18 +202,18 @@ struct LinearParts {
     int count, units;                             // count 1: not cut
     int64_t ld, stride;                           // of the sums
 };
-// A stage of a lone workgroup a CU takes 1.4 us where its weights come from memory (its loads are one stage ahead), the joining launch 3.5, and
-// an output's sum of a part is written and read at some 400 of them a ns.  us, whole / cut in 2 / 4 / 8, without the quantizer: 128 x 4096 x 14336 85.5 /
-// 48.7 / 30.5 / 23.1; 256 rows 78.8 / 46.5 / 31.2 / 37.3; 512 72.8 / 46.6 / 50.2 / 63.1; 128 x 14336 x 4096 29.3 / 24.4 / 30.5 / 41.9, 256 rows 28.3 / 38.7;
-// 128 x 4096 x 4096 18.4 / 15.0 / 14.8 / 18.8, 256 rows 17.9 / 17.6 / 20.2.
+// Cut where the units that a tile is spared (1.1 us each where the weights come from memory) outweigh the sums, written and read at some 450 outputs a ns,
+// and the joining launch.  us without the quantizer, weights from memory, whole / cut in 2 / 4 / 8: 128 rows of 4096 x 14336 66.8 / 38.9 / 25.3 / 20.5, 256
+// 65.8 / 39.6 / 27.7 / 35.2, 512 64.9 / 41.6 / 50.1; of 14336 x 4096 24.1 / 21.5 / 27.9; of 4096 x 4096 21.8 / 17.1 / 15.8 / 18.5, 256 21.5 / 19.4 / 20.3, 512
+// 21.5 / 22.7; of 1024 x 4096 17.4 / 12.4 / 10.7 / 10.3.
 LinearParts linear_parts(int64_t rows, int64_t N, int64_t K) {
     const int64_t tiles = ceil_div64(rows, 128) * ceil_div64(N, 128), units = ceil_div64(K, MX_KI), ld = (N + 7) / 8 * 8;
     LinearParts p = {1, (int)units, ld, (rows * ld + 63) / 64 * 64};
     if (rows <= FEW_ROWS || tiles > 128) return p;
-    double least = 1.4 * units;
-    for (int64_t n = 2; n <= PARTS_MAX && n <= units / 2 && n * tiles <= 256; ++n) {
+    double least = 1.1 * units;
+    for (int64_t n = 2; n <= PARTS_MAX && n <= units / 2 && n * tiles <= 256; ++n) {       // (256: a CU each, and the same on any chip)
         const int64_t per = ceil_div64(units, n);
-        const double t = 1.4 * per + 3.5 + n * rows * ld / 400e3;
+        const double t = 1.1 * per + 0.5 + n * rows * ld / 450e3;
         if (t >= least) continue;
         least = t;
         p.units = (int)per;
@@ -219,30 +221,37 @@ LinearParts linear_parts(int64_t rows, int64_t N, int64_t K) {
     }
     return p;
 }
+template <typename END>
+int launch_deep(hipStream_t s, const MxOperand& x, const MxOperand& w, int64_t K, int parts, const END& end) {
+    const int64_t tm = ceil_div64(x.rows, 128), tn = ceil_div64(w.rows, 128);
+    const MxOrder order = mx_order(tm, tn, K, 128);
+    const int nblk = (int)(K / 32);
+    auto launch = [&](auto kern, int bytes, LdsLimitCache& lds_set) -> int {
+        if (!ensure_dyn_lds((const void*)kern, bytes, lds_set)) return METIS_HIP_ERROR;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn), (unsigned)parts), dim3(512), bytes, s, x, w, nblk, order, end);
+        METIS_LAUNCH_CHECK();
+        return METIS_OK;
+    };
+    static LdsLimitCache lds_set[3];
+    if (nblk % 4 || (uintptr_t)x.scales % 4 || (uintptr_t)w.scales % 4) return launch(k_mxfp4_deep<true, true, END>, mxd_lds(true), lds_set[0]);
+    if (nblk % 8) return launch(k_mxfp4_deep<false, true, END>, mxd_lds(false), lds_set[1]);
+    return launch(k_mxfp4_deep<false, false, END>, mxd_lds(false), lds_set[2]);
+}
 template <typename T>
 int launch_parts(hipStream_t s, const MxOperand& x, const MxOperand& w, int64_t K, const LinearParts& p, float* sums, const MxFinish<T>& f) {
-    constexpr size_t LDS = 2 * 256 * (size_t)(MX_CROW + MX_SROW);
-    const int64_t tm = ceil_div64(x.rows, 128), tn = ceil_div64(w.rows, 128), units = p.ld / 8;
+    const int64_t units = p.ld / 8;
     const int us = units_status(x.rows, units);
     if (us != METIS_OK) return us;
-    const MxOrder order = mx_order(tm, tn, K, 128);
-    auto launch = [&](auto kern, LdsLimitCache& lds_set) {
-        if (!ensure_dyn_lds((const void*)kern, LDS, lds_set)) return false;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn), (unsigned)p.count), dim3(512), LDS, s, x, w, K, sums, p.ld, true, order,
-                           MxParts{p.units, p.stride});
-        return true;
-    };
-    static LdsLimitCache lds_set[2];
-    const bool ok = K % MX_KI == 0 ? launch(k_mxfp4_gemm_nt<float, MX_WHOLE, 128, MxParts>, lds_set[0])
-                                   : launch(k_mxfp4_gemm_nt<float, MX_TAIL, 128, MxParts>, lds_set[1]);
-    if (!ok) return METIS_HIP_ERROR;
-    METIS_LAUNCH_CHECK();
+    const int ds = launch_deep(s, x, w, K, p.count, MxParts{sums, p.ld, p.stride, p.units});
+    if (ds != METIS_OK) return ds;
     const int64_t total = x.rows * units;
     hipLaunchKernelGGL(k_linear_join<T>, dim3((unsigned)ceil_div64(total, 256)), dim3(256), 0, s, sums, p.ld, p.stride, p.count, (uint64_t)total,
                        fast_div((uint32_t)units), w.rows, f);
     METIS_LAUNCH_CHECK();
     return METIS_OK;
 }
+// Up to 448 tiles of 128 x 128 (beyond, tiles of 256 x 256 are as quick or quicker: 768 rows of 14336 x 4096, 672 tiles, 49.8 us for 49.7).
+bool deep_tiles(int64_t rows, int64_t N) { return ceil_div64(rows, 128) * ceil_div64(N, 128) <= 448; }
 
 struct LinearPlace {
     size_t scales, sums, bytes;                   // places of the rows' scales behind their codes and of the parts' sums, and the end
@@ -438,7 +447,8 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
         const MxFinish<T> f = finish_of<T>(e, Y);
         if (few) return launch_few_shape<T>(s, x, fused ? X : nullptr, w, K, f);
         if (cut) return launch_parts<T>(s, x, w, K, place.parts, (float*)(ws + place.sums), f);
-        return launch_mx_gemm<T>(s, x, w, K, f.y, f.ldy, f);
+        if (deep_tiles(rows, N)) return launch_deep(s, x, w, K, 1, f);
+        return launch_mx_tile<T, 256>(s, x, w, K, f.y, f.ldy, f);
     };
     return Y->dtype == METIS_BF16 ? launch(bf16_t()) : launch(float());
 }

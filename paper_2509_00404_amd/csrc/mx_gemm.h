@@ -52,11 +52,11 @@ struct MxOperand {
 // load in flight; quantizers included: 8192 x 4096 x 4064 915 -> 118 us, where 4096 takes 117; 1000 x 1008 x 1248 187 -> 20.6.)
 typedef uint32_t mx_uvec2_any __attribute__((ext_vector_type(2), aligned(1)));
 enum { MX_WHOLE, MX_TAIL, MX_SHORT };
-// END: MxPlain, the product as it is; MxParts, the product of a part of the contraction, blockIdx.y; else what an epilogue makes of it (epilogue.h).
+// END: MxPlain, the product as it is; else what an epilogue makes of it (epilogue.h).
 template <typename OUT, int MODE, int BT, typename END = MxPlain>
 __global__ void __launch_bounds__(512, BT == 256 ? 2 : 4)
 k_mxfp4_gemm_nt(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C, int64_t ldc, bool vec, MxOrder order, END end) {
-    constexpr bool PARTS = std::is_same<END, MxParts>::value, PLAIN = PARTS || std::is_same<END, MxPlain>::value;
+    constexpr bool PLAIN = std::is_same<END, MxPlain>::value;
     constexpr bool LINES = !PLAIN || sizeof(OUT) == 2 || BT == 128;    // outputs by way of LDS, accumulator tiles transposed
     constexpr int TM = BT / 64, TN = BT / 128, BM = BT, BN = BT, NV = BT / 64;   // NV: 16-byte code vectors per thread, operand and stage
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -78,12 +78,7 @@ k_mxfp4_gemm_nt(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C, int64_
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 
-    int niter = (int)((K + MX_KI - 1) / MX_KI), first = 0;
-    if constexpr (PARTS) {
-        first = end.units * (int)blockIdx.y;
-        niter = niter - first < end.units ? niter - first : end.units;
-        C += end.stride * blockIdx.y;
-    }
+    const int niter = (int)((K + MX_KI - 1) / MX_KI);
     // this thread's share of a stage: code vectors v of each operand (row tid/8 + 64 v, 16-byte segment
     // tid % 8: a row's 128 bytes are read by 8 consecutive lanes) and the 8 scale bytes of one row;
     // rows past the operand's end re-read its last row.  Byte offsets fit 32 bits (checked by the host).
@@ -109,7 +104,7 @@ k_mxfp4_gemm_nt(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C, int64_
     const bool sc_a = srow < BT;
     uvec4_t ra[NV], rb[NV];
     uvec2_t rs;
-    auto clampst = [&](int st) { return first + (st < niter ? st : niter - 1); };
+    auto clampst = [&](int st) { return st < niter ? st : niter - 1; };
     auto seg_exists = [&](int st) __attribute__((always_inline)) { return 8u * st + (tid & 7) < sstride; };
     // where the 8 scale bytes are fetched (K > 256: an operand has more than 8)
     const uint32_t slast = (uint32_t)(sc_a ? A.rows : B.rows) * sstride - 8u;
@@ -218,8 +213,8 @@ k_mxfp4_gemm_nt(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C, int64_
         }
     };
 
-    load_stage(first);
-    store_stage(lds, first);
+    load_stage(0);
+    store_stage(lds, 0);
     __syncthreads();
     load_stage(clampst(1));
     read_codes(lds, 0, 0);

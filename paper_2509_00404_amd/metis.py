@@ -135,17 +135,15 @@ _SIGNATURES = {
     "metis_dequantize_mx8": (C.c_int, [C.c_void_p, C.POINTER(Mx8), C.POINTER(Mat)]),
     "metis_swiglu": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Mx8)]),
     "metis_swiglu_grads": (C.c_int, [C.c_void_p, C.POINTER(Mx8), C.POINTER(Mat), C.POINTER(Mat), C.POINTER(Mat)]),
-    "metis_dropout": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mask), C.POINTER(Mat), C.POINTER(Mat)]),
+    # (structs as addresses: packed bytes, or byref of the classes above)
+    "metis_dropout": (C.c_int, [C.c_void_p] * 5),
     "metis_mxfp4_linear_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
-    "metis_mxfp4_linear": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(MxFp4), C.POINTER(MxFp4), C.POINTER(Epilogue), C.POINTER(Mat),
-                                     C.c_void_p, C.c_size_t]),
+    "metis_mxfp4_linear": (C.c_int, [C.c_void_p] * 7 + [C.c_size_t]),
     "metis_linear_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
-    "metis_linear_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.c_int, C.POINTER(Mask), C.POINTER(Mat), C.c_void_p,
-                                     C.c_void_p, C.c_size_t]),
-    "metis_layernorm": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.c_void_p, C.c_void_p, C.c_float, C.POINTER(Mat), C.c_void_p]),
+    "metis_linear_grads": (C.c_int, [C.c_void_p] * 3 + [C.c_int] + [C.c_void_p] * 4 + [C.c_size_t]),
+    "metis_layernorm": (C.c_int, [C.c_void_p] * 4 + [C.c_float] + [C.c_void_p] * 2),
     "metis_layernorm_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
-    "metis_layernorm_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Mat), C.c_void_p, C.c_void_p, C.POINTER(Mat), C.POINTER(Mat),
-                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t]),
+    "metis_layernorm_grads": (C.c_int, [C.c_void_p] * 10 + [C.c_size_t]),
     "metis_factor_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int]),
     "metis_fp4_factor_grads": (C.c_int, [C.c_void_p, C.POINTER(Mat), C.POINTER(Split), C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_size_t]),
@@ -654,6 +652,18 @@ def swiglu_grads(saved, dact, dgate_up, act=None):
     return dgate_up
 
 
+# These calls take their structs packed: built as ctypes structures and passed by reference they cost the host 0.2 us each, of the 7 that a small
+# call takes.
+_MAT, _MASK, _EPILOGUE = struct.Struct("@Pqqqi0P"), struct.Struct("@dQP"), struct.Struct("@PiPPP")
+assert _MAT.size == C.sizeof(Mat) and _MASK.size == C.sizeof(Mask) and _EPILOGUE.size == C.sizeof(Epilogue)
+
+
+def _packed(t):
+    (rows, cols), (ld, step) = t.shape, t.stride()           # two axes
+    assert t.is_cuda and step == 1
+    return _MAT.pack(t.data_ptr(), rows, cols, ld, _DTYPES[t.dtype])
+
+
 class DropoutMask:
     """The mask of a dropout (see metis_dropout_mask): probability p, the layer's seed, and an int64 tensor on the device that counts the steps
     (None: 0).  The mask depends on these and an element's place alone, so the backward pass is given the same object."""
@@ -665,22 +675,25 @@ class DropoutMask:
     def c(self):
         return Mask(self.p, self.seed & 0xFFFFFFFFFFFFFFFF, self.step.data_ptr() if self.step is not None else None)
 
+    def packed(self):
+        return _MASK.pack(self.p, self.seed & 0xFFFFFFFFFFFFFFFF, self.step.data_ptr() if self.step is not None else 0)
+
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
-def _ref(x):
-    return C.byref(x) if x is not None else None
-
-
-def _scratch(nbytes, like):
-    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+def _space(workspace, nbytes, like):
+    """Address and size of a call's workspace; allocated where the caller brings none."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, None, 0
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
 def dropout(x, y, mask, residual=None):
     """y = residual + m x, m the factors of `mask` (a DropoutMask)."""
-    a, o, k, r = _mat(x), _mat(y), mask.c(), _mat(residual) if residual is not None else None
-    _check(lib().metis_dropout(_stream(), C.byref(a), C.byref(k), _ref(r), C.byref(o)))
+    _check(lib().metis_dropout(_stream(), _packed(x), mask.packed(), _packed(residual) if residual is not None else None, _packed(y)))
     return y
 
 
@@ -690,16 +703,14 @@ def mxfp4_linear_workspace_bytes(rows, N, K):
 
 def mxfp4_linear(X, W, Y, bias=None, act="none", pre=None, mask=None, residual=None, workspace=None):
     """Y [T, N] = residual + m act(Q(X) W^T + bias); X an MxTensor or a dense tensor, pre: output for what act is applied to."""
-    w, y = W.c(), _mat(Y)
+    rows, N, K = Y.shape[0], W.rows, W.cols
     dense = isinstance(X, torch.Tensor)
-    x = _mat(X) if dense else X.c()
+    x, w = _packed(X) if dense else X.c(), W.c()
     p, k, r = _mat(pre) if pre is not None else None, mask.c() if mask is not None else None, _mat(residual) if residual is not None else None
-    e = Epilogue(_ptr(bias, torch.float32, (w.rows,)), ACTIVATIONS[act], C.pointer(p) if p is not None else None,
-                 C.pointer(k) if k is not None else None, C.pointer(r) if r is not None else None)
-    if workspace is None:
-        workspace = _scratch(mxfp4_linear_workspace_bytes(x.rows, w.rows, w.cols), Y)
-    _check(lib().metis_mxfp4_linear(_stream(), C.byref(x) if dense else None, None if dense else C.byref(x), C.byref(w), C.byref(e), C.byref(y),
-                                    workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0))
+    e = _EPILOGUE.pack(_ptr(bias, torch.float32, (N,)) or 0, ACTIVATIONS[act], C.addressof(p) if p is not None else 0,
+                       C.addressof(k) if k is not None else 0, C.addressof(r) if r is not None else 0)
+    workspace, at, nbytes = _space(workspace, mxfp4_linear_workspace_bytes(rows, N, K) if workspace is None else 0, Y)
+    _check(lib().metis_mxfp4_linear(_stream(), x if dense else None, None if dense else C.byref(x), C.byref(w), e, _packed(Y), at, nbytes))
     return Y
 
 
@@ -709,19 +720,19 @@ def linear_grads_workspace_bytes(rows, cols):
 
 def linear_grads(dY, dZ=None, pre=None, act="none", mask=None, dbias=None, workspace=None):
     """dZ = act'(pre) m dY, and dbias [cols] fp32 = its column sums; either may be None."""
-    d, z, p, k = _mat(dY), _mat(dZ) if dZ is not None else None, _mat(pre) if pre is not None else None, mask.c() if mask is not None else None
-    if workspace is None and dbias is not None:
-        workspace = _scratch(linear_grads_workspace_bytes(d.rows, d.cols), dY)
-    _check(lib().metis_linear_grads(_stream(), C.byref(d), _ref(p), ACTIVATIONS[act], _ref(k), _ref(z), _ptr(dbias, torch.float32, (d.cols,)),
-                                    workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0))
+    rows, cols = dY.shape
+    workspace, at, nbytes = _space(workspace, linear_grads_workspace_bytes(rows, cols) if workspace is None and dbias is not None else 0, dY)
+    _check(lib().metis_linear_grads(_stream(), _packed(dY), _packed(pre) if pre is not None else None, ACTIVATIONS[act],
+                                    mask.packed() if mask is not None else None, _packed(dZ) if dZ is not None else None,
+                                    _ptr(dbias, torch.float32, (cols,)), at, nbytes))
     return dZ
 
 
 def layernorm(x, y, weight=None, bias=None, eps=1e-5, stats=None):
     """y = (x - mean) rstd weight + bias by rows; stats [rows, 2] fp32: mean and rstd, for the backward pass."""
-    a, o = _mat(x), _mat(y)
-    _check(lib().metis_layernorm(_stream(), C.byref(a), _ptr(weight, torch.float32, (a.cols,)), _ptr(bias, torch.float32, (a.cols,)), eps,
-                                 C.byref(o), _ptr(stats, torch.float32, (a.rows, 2))))
+    rows, cols = x.shape
+    _check(lib().metis_layernorm(_stream(), _packed(x), _ptr(weight, torch.float32, (cols,)), _ptr(bias, torch.float32, (cols,)), eps, _packed(y),
+                                 _ptr(stats, torch.float32, (rows, 2))))
     return y
 
 
@@ -731,13 +742,12 @@ def layernorm_grads_workspace_bytes(rows, cols):
 
 def layernorm_grads(dy, x, stats, dx, weight=None, dweight=None, dbias=None, add=None, workspace=None):
     """dx (with `add`, the gradient that reaches x past the norm) and, where given, dweight and dbias [cols] fp32."""
-    d, a, o, r = _mat(dy), _mat(x), _mat(dx), _mat(add) if add is not None else None
-    col = (a.cols,)
-    if workspace is None and (dweight is not None or dbias is not None):
-        workspace = _scratch(layernorm_grads_workspace_bytes(a.rows, a.cols), x)
-    _check(lib().metis_layernorm_grads(_stream(), C.byref(d), C.byref(a), _ptr(stats, torch.float32, (a.rows, 2)), _ptr(weight, torch.float32, col),
-                                       _ref(r), C.byref(o), _ptr(dweight, torch.float32, col), _ptr(dbias, torch.float32, col),
-                                       workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0))
+    rows, cols = x.shape
+    columns = dweight is not None or dbias is not None
+    workspace, at, nbytes = _space(workspace, layernorm_grads_workspace_bytes(rows, cols) if workspace is None and columns else 0, x)
+    _check(lib().metis_layernorm_grads(_stream(), _packed(dy), _packed(x), _ptr(stats, torch.float32, (rows, 2)),
+                                       _ptr(weight, torch.float32, (cols,)), _packed(add) if add is not None else None, _packed(dx),
+                                       _ptr(dweight, torch.float32, (cols,)), _ptr(dbias, torch.float32, (cols,)), at, nbytes))
     return dx
 
 
