@@ -1,6 +1,7 @@
 // What a product's outputs go through on their way to memory -- bias, activation, dropout, residual -- eight neighbouring elements of a row at a
 // time, and the pieces of it that other kernels share: the activations with their slopes, and the dropout mask.
 #pragma once
+#include <type_traits>
 #include "mx_tile.h"
 #include "elementwise.h"
 
@@ -148,21 +149,6 @@ __device__ __forceinline__ float act_slope(int act, float z) {
         default: return 1.0f;
     }
 }
-// `act` is uniform: one branch for the eight
-template <bool FAST>
-__device__ __forceinline__ void act_values(int act, float (&v)[8]) {
-    auto all = [&](int a) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = act_value<FAST>(a, v[i]);
-    };
-    switch (act) {
-        case METIS_ACT_RELU: all(METIS_ACT_RELU); break;
-        case METIS_ACT_GELU: all(METIS_ACT_GELU); break;
-        case METIS_ACT_GELU_TANH: all(METIS_ACT_GELU_TANH); break;
-        case METIS_ACT_SILU: all(METIS_ACT_SILU); break;
-        default: break;
-    }
-}
 inline bool act_ok(int act) { return act >= METIS_ACT_NONE && act <= METIS_ACT_SILU; }
 
 // ---- the epilogue ----
@@ -172,7 +158,9 @@ struct MxParts {                                  // fp32 sums of a part of the 
     int64_t ld, stride;
     int units;
 };
-template <typename T>
+// ACT: the activation, or ACT_ANY, `act`
+#define ACT_ANY (-1)
+template <typename T, int ACT = ACT_ANY>
 struct MxFinish {
     typedef T type;
     T* y;                                         // (residual may be y: no restrict)
@@ -184,44 +172,80 @@ struct MxFinish {
     int64_t ldr;
     MaskKey mask;
     int act;
+    bool narrow;                                  // rows near each other are within 2^31 bytes
 };
-// n <= 8 elements (row r, columns c .. c + n - 1, c a multiple of 8) whose bias is in b; step: mask_step(f.mask)
-template <typename T>
-__device__ __forceinline__ void finish_unit(const MxFinish<T>& f, uint32_t step, int64_t r, int64_t c, int64_t n, const float (&b)[8], float (&v)[8]) {
-    float res[8];
-    if (f.residual) load_part<T, true>(f.residual + r * f.ldr + c, n, res);
+// the activation and the mask of S units of eight elements, columns c .. c + 7, row(s)
+template <int S, typename T, int ACT, typename F>
+__device__ __forceinline__ void finish_values(const MxFinish<T, ACT>& f, uint32_t step, int64_t c, const F& row, float (&v)[S][8]) {
+    auto all = [&](auto a) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += b[i];
-    if (f.pre) store_part<T, true>(f.pre + r * f.ldp + c, n, v);
-    act_values<sizeof(T) == 2>(f.act, v);
-    if (f.mask.dropped) mask_apply(f.mask, step, (uint32_t)(c >> 3), (uint32_t)r, v);
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[s][i] = act_value<sizeof(T) == 2>(decltype(a)::value, v[s][i]);
+    };
+    switch (ACT != ACT_ANY ? ACT : f.act) {           // uniform
+        case METIS_ACT_RELU: all(std::integral_constant<int, METIS_ACT_RELU>{}); break;
+        case METIS_ACT_GELU: all(std::integral_constant<int, METIS_ACT_GELU>{}); break;
+        case METIS_ACT_GELU_TANH: all(std::integral_constant<int, METIS_ACT_GELU_TANH>{}); break;
+        case METIS_ACT_SILU: all(std::integral_constant<int, METIS_ACT_SILU>{}); break;
+        default: break;
+    }
+    if (f.mask.dropped) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) mask_apply(f.mask, step, (uint32_t)(c >> 3), row(s), v[s]);
+    }
+}
+// n <= 8 elements (row r, columns c .. c + n - 1, c a multiple of 8) whose bias is in b; step: mask_step(f.mask)
+template <typename T, int ACT>
+__device__ __forceinline__ void finish_unit(const MxFinish<T, ACT>& f, uint32_t step, int64_t r, int64_t c, int64_t n, const float (&b)[8], float (&v)[8]) {
+    float res[8], one[1][8];
+    if (f.residual) load_unit(f.residual + r * f.ldr + c, n, res);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) one[0][i] = v[i] + b[i];
+    if (f.pre) store_part<T, true>(f.pre + r * f.ldp + c, n, one[0]);
+    finish_values<1>(f, step, c, [&](int) __attribute__((always_inline)) { return (uint32_t)r; }, one);
     if (f.residual) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += res[i];
+        for (int i = 0; i < 8; ++i) one[0][i] += res[i];
     }
-    store_part<T, true>(f.y + r * f.ldy + c, n, v);
+    store_part<T, true>(f.y + r * f.ldy + c, n, one[0]);
 }
-template <typename T>
-__device__ __forceinline__ void finish_bias(const MxFinish<T>& f, int64_t c, int64_t N, float (&b)[8]) {
+template <typename T, int ACT>
+__device__ __forceinline__ void finish_bias(const MxFinish<T, ACT>& f, int64_t c, int64_t N, float (&b)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) b[i] = 0.0f;
-    if (f.bias && c < N) load_part<float, true>(f.bias + c, N - c, b);
+    if (f.bias && c < N) load_unit(f.bias + c, N - c, b);
 }
 
 // A wave's TM x TN accumulator tiles, transposed (a lane holds runs of four columns of one row), through the epilogue.  32 rows of its columns at
-// a time are staged at sm as fp32 (mx_wave_rows<float, TN> bytes), and a lane takes eight neighbouring columns of a row: one block of the
-// mask's numbers, and 16 bytes of every bf16 operand.
-template <int TM, int TN, typename T>
-__device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T>& f, int64_t m0, int64_t n0, int64_t M,
+// a time are staged at sm as fp32 (mx_wave_rows<float, TN> bytes), and a lane takes eight neighbouring columns of some of them: one block of the
+// mask's numbers, and 16 bytes of every bf16 operand.  Tiles inside the matrix have the residual's next 32 rows on their way meanwhile.
+// an element near row r0, which is uniform, by a 32-bit offset
+template <typename T>
+__device__ __forceinline__ T* narrow_at(T* p, int64_t ld, int64_t r0, uint32_t low, uint32_t c) {
+    return reinterpret_cast<T*>((uintptr_t)(p + r0 * ld) + (low * (uint32_t)ld + c) * (uint32_t)sizeof(T));      // r0 uniform
+}
+// What is computed from the epilogue's arguments is computed where it is used: the empty asm hides that they are the same for every tile of a
+// persistent workgroup (kept over its products, the strides' multiples alone took the scalar registers, and vector registers after them).
+template <typename T, int ACT>
+__device__ __forceinline__ MxFinish<T, ACT> finish_afresh(MxFinish<T, ACT> f) {
+    asm volatile("" : "+s"(f.y), "+s"(f.ldy), "+s"(f.bias), "+s"(f.pre), "+s"(f.ldp), "+s"(f.residual), "+s"(f.ldr));
+    asm volatile("" : "+s"(f.mask.seed), "+s"(f.mask.step), "+s"(f.mask.dropped), "+s"(f.mask.keep), "+s"(f.act));
+    return f;
+}
+template <int TM, int TN, typename T, int ACT>
+__device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T, ACT>& end, int64_t m0, int64_t n0, int64_t M,
                                                int64_t N, int lane) {
-    constexpr int LROW = 32 * TN * 4 + 16, UNITS = 4 * TN, ROWS = 64 / UNITS;
+    constexpr int LROW = 32 * TN * 4 + 16, UNITS = 4 * TN, ROWS = 64 / UNITS, S = 32 / ROWS;
+    const MxFinish<T, ACT> f = finish_afresh(end);
     const int li = lane & 31, half = lane >> 5, unit = lane % UNITS;
+    const uint32_t low = (uint32_t)(lane / UNITS);
     const int64_t c = n0 + 8 * unit;
     const uint32_t step = mask_step(f.mask);
+    const bool whole = f.narrow && m0 + 32 * TM <= M && n0 + 32 * TN <= N;
     float b[8];
     finish_bias(f, c, N, b);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
+    auto stage = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -229,13 +253,54 @@ __device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], u
                 mx_put4(reinterpret_cast<float*>(sm + li * LROW) + 32 * j + 2 * v + 4 * half, acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2],
                         acc[i][j][v + 3]);
         gs_wave_order();
+    };
+    auto staged = [&](int s) __attribute__((always_inline)) { return reinterpret_cast<const float*>(sm + (ROWS * s + low) * LROW + 32 * unit); };
+    if (whole) {
+        RawUnit<T> next[S];
+        auto fetch = [&](int i) __attribute__((always_inline)) {
+            if (!f.residual) return;
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                load_whole(narrow_at(const_cast<T*>(f.residual), f.ldr, m0 + 32 * i + ROWS * s, low, (uint32_t)c), next[s]);
+        };
+        fetch(0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            stage(i);
+            RawUnit<T> res[S];
+#pragma unroll
+            for (int s = 0; s < S; ++s) res[s] = next[s];
+            if (i + 1 < TM) fetch(i + 1);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int64_t r0 = m0 + 32 * i + ROWS * s;
+                float v[1][8];
+                load_row(staged(s), v[0]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[0][e] += b[e];
+                if (f.pre) store_row<true>(narrow_at(f.pre, f.ldp, r0, low, (uint32_t)c), v[0]);
+                finish_values<1>(f, step, c, [&](int) __attribute__((always_inline)) { return (uint32_t)r0 + low; }, v);
+                if (f.residual) {
+                    float x[8];
+                    unpack(res[s], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[0][e] += x[e];
+                }
+                store_row<true>(narrow_at(f.y, f.ldy, r0, low, (uint32_t)c), v[0]);
+            }
+            gs_wave_order();
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        stage(i);
 #pragma unroll 1
-        for (int t = 0; t < 32 / ROWS; ++t) {
-            const int row = ROWS * t + lane / UNITS;
-            const int64_t r = m0 + 32 * i + row;
+        for (int s = 0; s < S; ++s) {
+            const int64_t r = m0 + 32 * i + ROWS * s + low;
             if (r < M && c < N) {
                 float v[8];
-                load_row(reinterpret_cast<const float*>(sm + row * LROW + 32 * unit), v);
+                load_row(staged(s), v);
                 finish_unit(f, step, r, c, N - c, b, v);
             }
         }

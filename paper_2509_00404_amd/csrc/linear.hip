@@ -1,6 +1,7 @@
 // A linear layer on MXFP4 operands whose epilogue adds a bias, applies an activation, drops elements and adds a residual; and the gradient of
 // that epilogue.
 #include "mx_gemm.h"
+#include "linear.h"
 #include "experts.h"
 #include "column_sums.h"
 
@@ -266,19 +267,6 @@ LinearPlace linear_place(int64_t rows, int64_t N, int64_t K) {
     return p;
 }
 
-template <typename T>
-MxFinish<T> finish_of(const metis_epilogue* e, const metis_mat* Y) {
-    return {(T*)Y->ptr,
-            Y->ld,
-            e ? e->bias : nullptr,
-            e && e->pre ? (T*)e->pre->ptr : nullptr,
-            e && e->pre ? e->pre->ld : 0,
-            e && e->residual ? (const T*)e->residual->ptr : nullptr,
-            e && e->residual ? e->residual->ld : 0,
-            mask_key(e ? e->mask : nullptr),
-            e ? e->act : METIS_ACT_NONE};
-}
-
 // How few rows are shared out: 16 or 32 outputs a workgroup, and as many waves as let a CU hold its share of the workgroups at once (16 waves a CU, or 8
 // where they need more registers; four at least).  us, 16 / 32 outputs: one row 14336 x 4096 11.6 / 10.3, 4096 x 14336 10.5 / 16.0; 64 rows 35.5 / 18.8,
 // 23.3 / 27.6.  24 rows of 14336 x 4096 with four waves 13.2, with eight (half of the workgroups wait) 15.9.
@@ -440,6 +428,8 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
         if (qs != METIS_OK) return qs;
     }
     const bool cut = place.parts.count > 1 && workspace && workspace_bytes >= place.bytes && (uintptr_t)workspace % 256 == 0;
+    const int cus = device_cu_count();
+    if (cus < 1) return METIS_HIP_ERROR;
     const MxOperand x = {q.codes, q.scales, rows}, w = {W->codes, W->scales, N};
     hipStream_t s = (hipStream_t)stream;
     auto launch = [&](auto zero) {
@@ -448,6 +438,7 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
         if (few) return launch_few_shape<T>(s, x, fused ? X : nullptr, w, K, f);
         if (cut) return launch_parts<T>(s, x, w, K, place.parts, (float*)(ws + place.sums), f);
         if (deep_tiles(rows, N)) return launch_deep(s, x, w, K, 1, f);
+        if (mx_streams(ceil_div64(rows, 256) * ceil_div64(N, 256), K, cus)) return linear_stream(s, &q, W, e, Y);
         return launch_mx_tile<T, 256>(s, x, w, K, f.y, f.ldy, f);
     };
     return Y->dtype == METIS_BF16 ? launch(bf16_t()) : launch(float());

@@ -274,6 +274,26 @@ MxOrder mx_order(int64_t tiles_m, int64_t tiles_n, int64_t K, int bt) {
     return o;
 }
 
+// The streaming kernel: whole units, two at least (its transfers are two ahead of the products), and several tiles a CU or a long
+// contraction.  A lone tile a CU gains nothing from a stream that crosses tiles: us, the kernel above / streaming, 4096 x 4096 x
+// 512 13.0 / 13.2, x 1024 15.4 / 15.7, x 4096 (with quantizers) 56.6 / 55.9; 4352 x 4352 x 512 17.7 / 17.0, 8192 x 8192 x 512 39.6 / 35.5.
+bool mx_streams(int64_t tiles, int64_t K, int cus) { return K % MX_KI == 0 && K >= 2 * MX_KI && (tiles > cus || K >= 8 * MX_KI); }
+template <typename OUT, typename END>
+int launch_mx_stream(hipStream_t s, const MxOperand& a, const MxOperand& b, int64_t K, OUT* C, int64_t ldc, const END& end) {
+    const int64_t tm = ceil_div64(a.rows, 256), tn = ceil_div64(b.rows, 256);
+    if (tm * tn > 0x7FFFFFFF) return METIS_UNSUPPORTED;
+    const int cus = device_cu_count();
+    if (cus < 1) return METIS_HIP_ERROR;
+    auto kern = k_mxfp4_gemm_nt_stream<OUT, END>;
+    static LdsLimitCache lds_set;
+    if (!ensure_dyn_lds((const void*)kern, MXS_LDS, lds_set)) return METIS_HIP_ERROR;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn < cus ? tm * tn : cus)), dim3(512), MXS_LDS, s, a, b, K, C, ldc,
+                       (uintptr_t)C % 16 == 0 && (ldc * sizeof(OUT)) % 16 == 0, mx_order(tm, tn, K, 256), (int)(tm * tn), end);
+    METIS_LAUNCH_CHECK();
+    return METIS_OK;
+}
+
+// (with an epilogue, the caller looks whether the streaming kernel takes the product: csrc/linear_stream.hip)
 template <typename OUT, int BT, typename END>
 int launch_mx_tile(hipStream_t s, const MxOperand& a, const MxOperand& b, int64_t K, OUT* C, int64_t ldc, const END& end) {
     constexpr size_t LDS = 2 * (size_t)(2 * BT) * (MX_CROW + MX_SROW);
@@ -286,20 +306,10 @@ int launch_mx_tile(hipStream_t s, const MxOperand& a, const MxOperand& b, int64_
         hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn)), dim3(512), LDS, s, a, b, K, C, ldc, vec, order, end);
         return true;
     };
-    // The streaming kernel: whole units, two at least (its transfers are two ahead of the products), and several tiles a CU or a long
-    // contraction.  A lone tile a CU gains nothing from a stream that crosses tiles: us, the kernel above / streaming, 4096 x 4096 x
-    // 512 13.0 / 13.2, x 1024 15.4 / 15.7, x 4096 (with quantizers) 56.6 / 55.9; 4352 x 4352 x 512 17.7 / 17.0, 8192 x 8192 x 512 39.6 / 35.5.
     const int cus = device_cu_count();
     if (cus < 1) return METIS_HIP_ERROR;
-    if (BT == 256 && K % MX_KI == 0 && K >= 2 * MX_KI && (tm * tn > cus || K >= 8 * MX_KI)) {
-        auto kern = k_mxfp4_gemm_nt_stream<OUT, END>;
-        static LdsLimitCache stream_set;
-        if (!ensure_dyn_lds((const void*)kern, MXS_LDS, stream_set)) return METIS_HIP_ERROR;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn < cus ? tm * tn : cus)), dim3(512), MXS_LDS, s, a, b, K, C, ldc, vec, order,
-                           (int)(tm * tn), end);
-        METIS_LAUNCH_CHECK();
-        return METIS_OK;
-    }
+    if constexpr (std::is_same<END, MxPlain>::value)
+        if (BT == 256 && mx_streams(tm * tn, K, cus)) return launch_mx_stream<OUT>(s, a, b, K, C, ldc, end);
     static LdsLimitCache lds_set[3];
     const bool ok = K % MX_KI == 0 ? launch(k_mxfp4_gemm_nt<OUT, MX_WHOLE, BT, END>, lds_set[0])
                     : K > MX_KI    ? launch(k_mxfp4_gemm_nt<OUT, MX_TAIL, BT, END>, lds_set[1])
@@ -313,8 +323,9 @@ int launch_mx_tile(hipStream_t s, const MxOperand& a, const MxOperand& b, int64_
 // shorter.  With the quantizers, against 256 x 256 tiles, K = 4096: 27 of them 37.1 -> 22.6 us, 128 41.4 -> 26.6, 256 41.0 -> 27.0, 384
 // 43.1 -> 40.1.  448, multiplication alone: K = 4096 32.3 -> 30.4, 14336 96.1 -> 95.9.  With the quantizers, 512 would take 44.6 for 45.1
 // at K = 4096 but 139.1 for 137.6 at K = 14336, 640 57.5 for 47.2.
-template <typename OUT, typename END = MxPlain>
-int launch_mx_gemm(hipStream_t s, const MxOperand& a, const MxOperand& b, int64_t K, OUT* C, int64_t ldc, const END& end = {}) {
+template <typename OUT>
+int launch_mx_gemm(hipStream_t s, const MxOperand& a, const MxOperand& b, int64_t K, OUT* C, int64_t ldc) {
+    const MxPlain end;
     const int cus = device_cu_count();
     if (cus < 1) return METIS_HIP_ERROR;
     if (ceil_div64(a.rows, 128) * ceil_div64(b.rows, 128) <= 7 * (int64_t)cus / 4) return launch_mx_tile<OUT, 128>(s, a, b, K, C, ldc, end);

@@ -107,15 +107,18 @@ k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C,
         const uint32_t at = 2 * MXS_CODES + (x < 4 ? 1024u * wa : MXS_SCALES + 512u * wb) + 256u * (x & 3);
         raw[x] = *reinterpret_cast<const uvec2_t*>(lds + bu + at + 8u * li);
     };
+    auto start = [&]() GS_INLINE {                       // the scales of a unit's first steps
+#pragma unroll
+        for (int x = 0; x < 6; ++x) sx[x] = raw[x].x >> (8 * half);
+        mxs_settle_scales(sx);
+    };
     gs_meet<MXS_DMA>();
 #pragma unroll
     for (int x = 0; x < 6; ++x) {
         read_frag(0, 0, 0, x);
         read_scale(0, x);
     }
-#pragma unroll
-    for (int x = 0; x < 6; ++x) sx[x] = raw[x].x >> (8 * half);
-    mxs_settle_scales(sx);
+    start();
 
     uint32_t b0 = 0;                                     // buffer of the unit in work
     auto unit = [&](auto first_, auto last_) GS_INLINE {
@@ -133,7 +136,7 @@ k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C,
                         gs_meet<0>();
                         if constexpr (!last) advance();
                     }
-                    if constexpr (m >= 1 && m < 7) {
+                    if constexpr (m >= 1 && m < 7 && (PLAIN || !last)) {
                         read_frag(b1, 0, 0, m - 1);
                         read_scale(b1, m - 1);
                     }
@@ -148,9 +151,7 @@ k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C,
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
-#pragma unroll
-        for (int x = 0; x < 6; ++x) sx[x] = raw[x].x >> (8 * half);
-        mxs_settle_scales(sx);
+        if constexpr (PLAIN || !last) start();
         b0 = b1;
     };
     for (;;) {
@@ -167,6 +168,7 @@ k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C,
             mx_store_wave<OUT, LINES, 4, 2>(acc, lds + bl + wave * mx_wave_rows<OUT, 2>(), C, ldc, m0 + 128 * wa, n0 + 64 * wb, A.rows, B.rows,
                                             vec, mx_whole<LINES>(m0 + 256 <= A.rows && n0 + 256 <= B.rows, vec), gs_fresh_lane());
         else
+            // (the next tile's first fragments are read behind it: the epilogue has use for their registers, gelu with `pre` 699 us for 652)
             mx_finish_wave<4, 2>(acc, lds + bl + wave * mx_wave_rows<float, 2>(), end, m0 + 128 * wa, n0 + 64 * wb, A.rows, B.rows, gs_fresh_lane());
         pos += (int)gridDim.x;
         if (pos >= total) break;
@@ -174,6 +176,14 @@ k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C,
         gs_meet<63>();
         advance();
         gs_for<MXS_DMA>([&](auto k) GS_INLINE { issue(bl, k); });
+        if constexpr (!PLAIN) {
+#pragma unroll
+            for (int x = 0; x < 6; ++x) {
+                read_frag(b0, 0, 0, x);
+                read_scale(b0, x);
+            }
+            start();
+        }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // no transfer may outlive the workgroup's LDS
 }
