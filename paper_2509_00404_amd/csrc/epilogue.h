@@ -233,19 +233,34 @@ __device__ __forceinline__ MxFinish<T, ACT> finish_afresh(MxFinish<T, ACT> f) {
     asm volatile("" : "+s"(f.mask.seed), "+s"(f.mask.step), "+s"(f.mask.dropped), "+s"(f.mask.keep), "+s"(f.act));
     return f;
 }
-template <int TM, int TN, typename T, int ACT>
-__device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T, ACT>& end, int64_t m0, int64_t n0, int64_t M,
+template <bool WHOLE, int TM, int TN, typename T, int ACT>
+__device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T, ACT>& f, int64_t m0, int64_t n0, int64_t M,
                                                int64_t N, int lane) {
     constexpr int LROW = 32 * TN * 4 + 16, UNITS = 4 * TN, ROWS = 64 / UNITS, S = 32 / ROWS;
-    const MxFinish<T, ACT> f = finish_afresh(end);
     const int li = lane & 31, half = lane >> 5, unit = lane % UNITS;
     const uint32_t low = (uint32_t)(lane / UNITS);
-    const int64_t c = n0 + 8 * unit;
+    const int64_t c = n0 + 8 * unit, n = N - c;
     const uint32_t step = mask_step(f.mask);
-    const bool whole = f.narrow && m0 + 32 * TM <= M && n0 + 32 * TN <= N;
     float b[8];
     finish_bias(f, c, N, b);
-    auto stage = [&](int i) __attribute__((always_inline)) {
+    RawUnit<T> next[S];
+    auto here = [&](int64_t r0) __attribute__((always_inline)) { return WHOLE || (r0 + low < M && n > 0); };
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+        if (!f.residual) return;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int64_t r0 = m0 + 32 * i + ROWS * s;
+            if constexpr (WHOLE) load_whole(narrow_at(f.residual, f.ldr, r0, low, (uint32_t)c), next[s]);
+            else if (here(r0)) load_raw(f.residual + (r0 + low) * f.ldr + c, n, next[s]);
+        }
+    };
+    auto store = [&](T* p, int64_t ld, int64_t r0, const float (&v)[8]) __attribute__((always_inline)) {
+        if constexpr (WHOLE) store_row<true>(narrow_at(p, ld, r0, low, (uint32_t)c), v);
+        else store_part<T, true>(p + (r0 + low) * ld + c, n, v);
+    };
+    fetch(0);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -253,59 +268,37 @@ __device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], u
                 mx_put4(reinterpret_cast<float*>(sm + li * LROW) + 32 * j + 2 * v + 4 * half, acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2],
                         acc[i][j][v + 3]);
         gs_wave_order();
-    };
-    auto staged = [&](int s) __attribute__((always_inline)) { return reinterpret_cast<const float*>(sm + (ROWS * s + low) * LROW + 32 * unit); };
-    if (whole) {
-        RawUnit<T> next[S];
-        auto fetch = [&](int i) __attribute__((always_inline)) {
-            if (!f.residual) return;
+        RawUnit<T> res[S];
 #pragma unroll
-            for (int s = 0; s < S; ++s)
-                load_whole(narrow_at(const_cast<T*>(f.residual), f.ldr, m0 + 32 * i + ROWS * s, low, (uint32_t)c), next[s]);
-        };
-        fetch(0);
+        for (int s = 0; s < S; ++s) res[s] = next[s];
+        if (i + 1 < TM) fetch(i + 1);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            stage(i);
-            RawUnit<T> res[S];
-#pragma unroll
-            for (int s = 0; s < S; ++s) res[s] = next[s];
-            if (i + 1 < TM) fetch(i + 1);
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const int64_t r0 = m0 + 32 * i + ROWS * s;
-                float v[1][8];
-                load_row(staged(s), v[0]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[0][e] += b[e];
-                if (f.pre) store_row<true>(narrow_at(f.pre, f.ldp, r0, low, (uint32_t)c), v[0]);
-                finish_values<1>(f, step, c, [&](int) __attribute__((always_inline)) { return (uint32_t)r0 + low; }, v);
-                if (f.residual) {
-                    float x[8];
-                    unpack(res[s], x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[0][e] += x[e];
-                }
-                store_row<true>(narrow_at(f.y, f.ldy, r0, low, (uint32_t)c), v[0]);
-            }
-            gs_wave_order();
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        stage(i);
-#pragma unroll 1
         for (int s = 0; s < S; ++s) {
-            const int64_t r = m0 + 32 * i + ROWS * s + low;
-            if (r < M && c < N) {
-                float v[8];
-                load_row(staged(s), v);
-                finish_unit(f, step, r, c, N - c, b, v);
+            const int64_t r0 = m0 + 32 * i + ROWS * s;
+            if (!here(r0)) continue;
+            float v[1][8];
+            load_row(reinterpret_cast<const float*>(sm + (ROWS * s + low) * LROW + 32 * unit), v[0]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[0][e] += b[e];
+            if (f.pre) store(f.pre, f.ldp, r0, v[0]);
+            finish_values<1>(f, step, c, [&](int) __attribute__((always_inline)) { return (uint32_t)r0 + low; }, v);
+            if (f.residual) {
+                float x[8];
+                unpack(res[s], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[0][e] += x[e];
             }
+            store(f.y, f.ldy, r0, v[0]);
         }
         gs_wave_order();
     }
+}
+template <int TM, int TN, typename T, int ACT>
+__device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T, ACT>& end, int64_t m0, int64_t n0, int64_t M,
+                                               int64_t N, int lane) {
+    const MxFinish<T, ACT> f = finish_afresh(end);
+    if (f.narrow && m0 + 32 * TM <= M && n0 + 32 * TN <= N) mx_finish_rows<true>(acc, sm, f, m0, n0, M, N, lane);
+    else mx_finish_rows<false>(acc, sm, f, m0, n0, M, N, lane);
 }
 
 }  // namespace
