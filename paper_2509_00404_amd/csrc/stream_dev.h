@@ -25,13 +25,6 @@ __device__ __forceinline__ void gs_dma4(uint32_t lds, uint32_t voff, const uint8
     asm volatile("s_add_u32 m0, %1, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0"
                  : "=&s"(copy) : "s"(lds), "v"(voff), "s"(base), "n"(AT) : "memory", "m0", "scc");
 }
-// the lane's byte, as a word, to lds + AT + 4 lane
-template <int AT>
-__device__ __forceinline__ void gs_dma1(uint32_t lds, uint32_t voff, const uint8_t* base) {
-    const uint8_t* copy;
-    asm volatile("s_add_u32 m0, %1, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_ubyte %2, %0"
-                 : "=&s"(copy) : "s"(lds), "v"(voff), "s"(base), "n"(AT) : "memory", "m0", "scc");
-}
 #pragma clang diagnostic pop
 // all but the N youngest of the wave's transfers have arrived and its LDS reads are done; then the workgroup meets
 template <int N>

@@ -226,3 +226,31 @@ def test_no_rows(metis):
     db = torch.ones(16, device="cuda")
     metis.linear_grads(e, e, dbias=db)
     assert (db == 0).all()
+
+
+@pytest.mark.parametrize("T,N,K", [(100, 200, 1056), (150, 300, 2080), (200, 140, 544), (130, 129, 288), (70, 64, 352), (3, 40, 1056), (40, 33, 96)])
+def test_scales_of_neighbours_stay_out(metis, T, N, K):
+    """Rows of scale bytes that end inside a word, in buffers that start anywhere and are surrounded by bytes that stand for no number; and a row of the
+    operand that is no number keeps that to itself."""
+    g = torch.Generator().manual_seed(T)
+    x, w = torch.randn((T, K), generator=g).cuda(), torch.randn((N, K), generator=g).cuda()
+    X, W = metis.quantize_mx(x, metis.MxTensor(T, K)), metis.quantize_mx(w, metis.MxTensor(N, K))
+    ref = metis.mxfp4_gemm_nt(X, W, torch.empty((T, N), device="cuda"))
+    for off in (1, 2, 3):
+        wide = []
+        for q in (X, W):
+            b = torch.full((q.scales.numel() + 64,), 255, dtype=torch.uint8, device="cuda")
+            b[8 + off:8 + off + q.scales.numel()] = q.scales.flatten()
+            wide.append(metis.MxTensor(q.rows, q.cols, buffers=(q.codes, b[8 + off:8 + off + q.scales.numel()])))
+        if K % 256 == 0:
+            continue
+        y = metis.mxfp4_linear(wide[0], wide[1], torch.empty((T, N), device="cuda"))
+        assert (y - ref).abs().max() <= 1e-5 * ref.abs().max()
+        wide[1].scales[1 * (K // 32) + 1] = 255
+        wide[0].scales[2 * (K // 32)] = 255
+        y = metis.mxfp4_linear(wide[0], wide[1], torch.empty((T, N), device="cuda"))
+        bad = torch.isnan(y)
+        want = torch.zeros_like(bad)
+        want[:, 1] = True
+        want[2, :] = True
+        assert torch.equal(bad, want)
