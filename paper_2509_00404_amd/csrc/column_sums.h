@@ -31,6 +31,29 @@ k_clear(float* __restrict__ p, int64_t n) {
     if (i < n) p[i] = 0.0f;
 }
 
+// Column sums of a workgroup of WAVES waves whose lanes have eight columns each, lane % 8 of 64, and some of the rows: added over the lanes of a wave,
+// then over the waves, in the same order every time; out[64 * strip ...].  lds: 64 WAVES floats that nobody else uses meanwhile.
+template <int WAVES>
+__device__ __forceinline__ void group_columns(float (&sum)[8], float* lds, float* __restrict__ out, int64_t strip, int64_t cols) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 8; d < 64; d <<= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += __shfl_xor(sum[i], d);
+    if (lane < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds[64 * wave + 8 * lane + i] = sum[i];
+    }
+    __syncthreads();
+    const int64_t c = 64 * strip + lane;
+    if (wave == 0 && c < cols) {
+        float s = lds[lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) s += lds[64 * w + lane];
+        out[c] = s;
+    }
+}
+
 int launch_join(hipStream_t s, const float* P, int64_t parts, int64_t n, float* out, int64_t split, float* out2) {
     hipLaunchKernelGGL(k_join_sums, dim3((unsigned)ceil_div64(n, 64)), dim3(1024), 0, s, P, parts, n, out, split, out2);
     METIS_LAUNCH_CHECK();

@@ -171,9 +171,9 @@ k_layernorm_long(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __rest
 // Memory bounds it: 16384 x 4096 bf16 with `add` (537 MB) takes 93 us, 5.8 TB/s, and the sums' join 2.4 (with the rows' loads where they are used, not a
 // row ahead, 160).
 template <typename T, int RT, int U, bool ADD>
-__global__ void __launch_bounds__(RowGroup<RT>::THREADS)
-k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
-                  const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows, int64_t cols, float* __restrict__ sums) {
+__device__ __forceinline__ void norm_grads_rows(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats,
+                                                const float* __restrict__ weight, const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows,
+                                                int64_t cols, float* __restrict__ sums, uint32_t block, uint32_t blocks) {
     typedef RowGroup<RT> G;
     constexpr bool AHEAD = RT * U <= 1024;               // (of 16384 columns a thread has no registers for the next row and the weights)
     __shared__ float s_sum[2][2 * G::WAVES], s_join[RT == 64 ? 3 * 512 : 1];
@@ -184,8 +184,8 @@ k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float
     UnitPlace at[U];
     RawUnit<T> nx[U], nd[U], na[U];
     float2 nst = make_float2(0.0f, 0.0f);
-    const int64_t hop = (int64_t)gridDim.x * G::ROWS;
-    int64_t r = (int64_t)blockIdx.x * G::ROWS + own;
+    const int64_t hop = (int64_t)blocks * G::ROWS;
+    int64_t r = (int64_t)block * G::ROWS + own;
     auto fetch = [&](int64_t row) __attribute__((always_inline)) {
         nst = stats[row];
 #pragma unroll
@@ -242,7 +242,7 @@ k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float
         }
     }
     if (!sums) return;
-    float* out = sums + (int64_t)blockIdx.x * 2 * cols;
+    float* out = sums + (int64_t)block * 2 * cols;
     auto leave = [&](float (&s)[U][8], float* to) __attribute__((always_inline)) {
         if constexpr (RT == 64) {                                                     // the four waves' sums in their order
             __syncthreads();
@@ -263,6 +263,54 @@ k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float
     };
     leave(dw, out);
     leave(db, out + cols);
+}
+
+template <typename T, int RT, int U, bool ADD>
+__global__ void __launch_bounds__(RowGroup<RT>::THREADS)
+k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
+                  const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows, int64_t cols, float* __restrict__ sums) {
+    norm_grads_rows<T, RT, U, ADD>(dy, ldd, x, ldx, stats, weight, add, lda, dx, ldo, rows, cols, sums, blockIdx.x, gridDim.x);
+}
+
+// Few rows, one launch: the first `strips` workgroups have 64 columns each and go down all the rows, eight lanes a row, for the columns' sums; the others
+// have rows.  (Both read x and dy: where dx takes the place of one, the rows follow in a launch of their own.)
+template <typename T, int RT, int U, bool ADD>
+__global__ void __launch_bounds__(RowGroup<RT>::THREADS)
+k_layernorm_grads_few(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
+                      const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows, int64_t cols, float* dweight, float* dbias, uint32_t strips) {
+    constexpr int WAVES = RowGroup<RT>::THREADS / 64, STEP = RowGroup<RT>::THREADS / 8;
+    if (blockIdx.x >= strips) {
+        norm_grads_rows<T, RT, U, ADD>(dy, ldd, x, ldx, stats, weight, add, lda, dx, ldo, rows, cols, nullptr, blockIdx.x - strips, gridDim.x - strips);
+        return;
+    }
+    __shared__ float s_columns[2 * 64 * WAVES];
+    const int64_t c = 64 * (int64_t)blockIdx.x + 8 * (threadIdx.x & 7), n = cols - c;
+    float dw[8] = {}, db[8] = {};
+    int64_t r = threadIdx.x >> 3;
+    if (n > 0 && r < rows) {
+        RawUnit<T> nx, nd;
+        float2 nst;
+        auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+            nst = stats[row];
+            load_raw(x + row * ldx + c, n, nx);
+            load_raw(dy + row * ldd + c, n, nd);
+        };
+        fetch(r);
+        for (; r < rows; r += STEP) {
+            float v[8], g[8];
+            const float2 st = nst;
+            unpack(nx, v);
+            unpack(nd, g);
+            fetch(r + STEP < rows ? r + STEP : r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dw[i] = fmaf(g[i], (v[i] - st.x) * st.y, dw[i]);
+                db[i] += g[i];
+            }
+        }
+    }
+    if (dweight) group_columns<WAVES>(dw, s_columns, dweight, blockIdx.x, cols);
+    if (dbias) group_columns<WAVES>(db, s_columns + 64 * WAVES, dbias, blockIdx.x, cols);
 }
 
 // Long rows: two passes over a row for its gradient, and the columns' sums by a kernel that goes down the columns.
@@ -367,6 +415,9 @@ int64_t column_chunk(int64_t rows, int64_t cols) {                       // rows
 int64_t sum_rows(int64_t rows, int64_t cols) {
     return in_registers(cols) ? norm_parts(rows, cols) : ceil_div64(rows, column_chunk(rows, cols));
 }
+// Few rows: one launch.  us, fp32, two launches / one: 16 x 4096 7.0 / 4.6, 128 x 4096 9.2 / 5.5, 256 x 4096 12.5 / 7.6, 256 x 256 7.1 / 6.5, 512 x 4096
+// 13.8 / 13.9, 512 x 256 6.7 / 9.1.
+bool norm_few(int64_t rows, int64_t cols) { return in_registers(cols) && rows <= 256; }
 // the threads of a row and the units of a thread: f(threads, units)
 template <typename F>
 void by_length(int64_t cols, F f) {
@@ -433,9 +484,10 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
     if (rows < 1 || cols < 1 || !norm_mat(x, x) || !norm_mat(dy, x) || !norm_mat(dx, x) || (add && !norm_mat(add, x))) return METIS_BAD_SHAPE;
     const int st = norm_limits(rows, cols);
     if (st != METIS_OK) return st;
+    const bool few = columns && norm_few(rows, cols);
     if (columns && (!workspace || workspace_bytes < metis_layernorm_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;
     if (columns && (uintptr_t)workspace % 256) return METIS_INVALID_ARG;
-    float* sums = columns ? (float*)workspace : nullptr;
+    float* sums = columns && !few ? (float*)workspace : nullptr;
     auto launch = [&](auto zero) {
         typedef decltype(zero) T;
         const T *pd = (const T*)dy->ptr, *px = (const T*)x->ptr, *pa = add ? (const T*)add->ptr : nullptr;
@@ -453,6 +505,14 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
             by_length(cols, [&](auto rt, auto u) {
                 constexpr int RT = decltype(rt)::value;
                 constexpr int U = decltype(u)::value;
+                if (few) {
+                    const unsigned strips = (unsigned)ceil_div64(cols, 64), groups = (unsigned)ceil_div64(rows, RowGroup<RT>::ROWS);
+                    const bool over = dx->ptr == x->ptr || dx->ptr == dy->ptr;
+                    auto kern = add ? k_layernorm_grads_few<T, RT, U, true> : k_layernorm_grads_few<T, RT, U, false>;
+                    hipLaunchKernelGGL(kern, dim3(over ? strips : strips + groups), dim3(RowGroup<RT>::THREADS), 0, s, pd, dy->ld, px, x->ld,
+                                       (const float2*)stats, weight, pa, la, (T*)dx->ptr, dx->ld, rows, cols, dweight, dbias, strips);
+                    if (!over) return;
+                }
                 auto kern = add ? k_layernorm_grads<T, RT, U, true> : k_layernorm_grads<T, RT, U, false>;
                 hipLaunchKernelGGL(kern, dim3((unsigned)norm_parts(rows, cols)), dim3(RowGroup<RT>::THREADS), 0, s, pd, dy->ld, px, x->ld,
                                    (const float2*)stats, weight, pa, la, (T*)dx->ptr, dx->ld, rows, cols, sums);
@@ -461,6 +521,6 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
         return hipGetLastError() == hipSuccess ? METIS_OK : METIS_HIP_ERROR;
     };
     const int ls = x->dtype == METIS_BF16 ? launch(bf16_t()) : launch(float());
-    if (ls != METIS_OK || !columns) return ls;
+    if (ls != METIS_OK || !columns || few) return ls;
     return launch_join(s, sums, sum_rows(rows, cols), 2 * cols, dweight, cols, dbias);
 }

@@ -381,12 +381,52 @@ k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64
 // Past the caches from 128 MiB a matrix on, where the three do not fit the last-level cache: us, through / past, 16384 x 14336 283 / 269, 16384 x 4096 82 / 77,
 // 4096 x 4096 23.8 / 27.4.
 #define GRADS_PAST (128ll << 20)
+// Few rows, one launch: a workgroup has 64 columns and all the rows, 32 at a time, eight lanes a row.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256)
+k_linear_grads_few(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64_t ldz, MaskKey mask, int64_t rows, int64_t cols, float* dbias) {
+    __shared__ float s_sum[4 * 64];
+    const int64_t c = 64 * (int64_t)blockIdx.x + 8 * (threadIdx.x & 7), n = cols - c;
+    const uint32_t step = mask_step(mask);
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    int64_t r = threadIdx.x >> 3;
+    if (n > 0 && r < rows) {
+        RawUnit<T> nd, np;
+        auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+            load_raw(dy + row * ldd + c, n, nd);
+            if (ACT != METIS_ACT_NONE) load_raw(pre + row * ldp + c, n, np);
+        };
+        fetch(r);
+        for (; r < rows; r += 32) {
+            float v[8], z[8];
+            unpack(nd, v);
+            if (ACT != METIS_ACT_NONE) unpack(np, z);
+            fetch(r + 32 < rows ? r + 32 : r);
+            if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)r, v);
+            if (ACT != METIS_ACT_NONE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= act_slope<sizeof(T) == 2>(ACT, z[i]);
+            }
+            if (dz) store_part<T, true>(dz + r * ldz + c, n, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        }
+    }
+    if (dbias) group_columns<4>(sum, s_sum, dbias, blockIdx.x, cols);
+}
+
 bool grads_wide(int64_t cols) { return cols >= 2048; }
+// us, bf16, gelu, rows in parts and a joining launch / k_linear_grads_few: 4 x 4096 6.7 / 4.4, 32 x 4096 6.8 / 4.5, 128 x 14336 10.1 / 6.8, 128 x 1000
+// 7.4 / 6.2, 256 x 14336 12.1 / 9.9, 256 x 4096 8.0 / 9.1, 256 x 256 6.6 / 8.9.
+bool grads_few(int64_t rows) { return rows <= 128; }
 int64_t grads_strips(int64_t cols) { return ceil_div64(cols, grads_wide(cols) ? 2048 : 512); }
 // Workgroups that share the rows of a strip, each of which leaves a row of partial sums: 1024 in all where each has eight rows or more, else 512 with two rows at
 // least; the same on any chip so that the sums have the same order.  us, 512 / 1024 / 2048, gelu, bf16: 16384 x 14336 300 / 269 / 292, 16384 x 4096 87 / 77 /
-// 86, 4096 x 4096 25.0 / 23.8 / 29.4, 1000 x 4096 11.6 / 14.7.  Two / four / eight rows at least: 100 x 4096 7.8 / 8.4 / 10.8.
+// 86, 4096 x 4096 25.0 / 23.8 / 29.4, 1000 x 4096 11.6 / 14.7.  Two / four / eight rows at least: 100 rows 7.8 / 8.4 / 10.8.
 int64_t grads_parts(int64_t rows, int64_t cols) {
+    if (grads_few(rows)) return 1;
     const int64_t strips = grads_strips(cols), many = strips < 1024 ? 1024 / strips : 1, few = strips < 512 ? 512 / strips : 1;
     if (rows >= 8 * many) return many;
     const int64_t want = ceil_div64(rows, 2);
@@ -464,7 +504,8 @@ extern "C" int metis_linear_grads(void* stream, const metis_mat* dY, const metis
     if (rows == 0) return dbias ? launch_clear(s, dbias, cols) : METIS_OK;
     if ((pre && (!mat_ok(pre) || pre->dtype != dY->dtype)) || (dZ && (!mat_ok(dZ) || dZ->dtype != dY->dtype))) return METIS_INVALID_ARG;
     if ((pre && !same_layout(pre, dY)) || (dZ && !same_layout(dZ, dY))) return METIS_BAD_SHAPE;
-    const int64_t chunks = grads_parts(rows, cols), strips = grads_strips(cols);
+    const bool few = grads_few(rows);
+    const int64_t chunks = grads_parts(rows, cols), strips = few ? ceil_div64(cols, 64) : grads_strips(cols);
     if (!grid_fits(strips, 256) || chunks > 65535) return METIS_UNSUPPORTED;
     const bool parts = dbias && chunks > 1;
     if (parts && (!workspace || workspace_bytes < metis_linear_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;
@@ -474,6 +515,12 @@ extern "C" int metis_linear_grads(void* stream, const metis_mat* dY, const metis
         typedef decltype(zero) T;
         constexpr int ACT = decltype(a)::value;
         const bool past = rows * cols * mat_size(dY) >= GRADS_PAST;
+        if (few) {
+            hipLaunchKernelGGL((k_linear_grads_few<T, ACT>), dim3((unsigned)strips), dim3(256), 0, s, (const T*)dY->ptr, dY->ld,
+                               pre ? (const T*)pre->ptr : nullptr, pre ? pre->ld : 0, dZ ? (T*)dZ->ptr : nullptr, dZ ? dZ->ld : 0, mask_key(mask),
+                               rows, cols, dbias);
+            return;
+        }
         auto kern = grads_wide(cols) ? past ? k_linear_grads<T, ACT, true, true> : k_linear_grads<T, ACT, true, false> : k_linear_grads<T, ACT, false, false>;
         hipLaunchKernelGGL(kern, dim3((unsigned)strips, (unsigned)chunks), dim3(256), 0, s, (const T*)dY->ptr, dY->ld,
                            pre ? (const T*)pre->ptr : nullptr, pre ? pre->ld : 0, dZ ? (T*)dZ->ptr : nullptr, dZ ? dZ->ld : 0, mask_key(mask),

@@ -113,6 +113,27 @@ def test_layernorm_grads(metis, T, D, dtype):
             assert (wo[:, :pad] == 7).all() and (wo[:, D + pad:] == 7).all()
 
 
+@pytest.mark.parametrize("T,D", [(255, 65), (256, 64), (256, 4090), (257, 63), (129, 9000), (256, 7), (31, 16390)])
+def test_layernorm_grads_near_the_rules(metis, T, D):
+    """The same sums and the same rows wherever dx goes: the columns' sums read dy and x before dx takes the place of either."""
+    x, dy, add, w, _ = _inputs(T, D, torch.float32, T * D)
+    stats = torch.from_numpy(oep.layernorm(_f64(x), None, None, 1e-5)[1]).float()
+    xd, d, a, wgt = (t.cuda() for t in (x, dy, add, w))
+    first = None
+    for place in (None, "dy", "x", "add", "add and x"):
+        xs, ds, as_ = xd.clone(), d.clone(), a.clone()
+        if place == "add and x":
+            as_ = xs
+        dx = {None: torch.empty_like(xd), "dy": ds, "x": xs, "add": as_, "add and x": xs}[place]
+        dw, db = torch.empty_like(wgt), torch.empty_like(wgt)
+        metis.layernorm_grads(ds, xs, stats.cuda(), dx, wgt, dw, db, as_)
+        first = first or (dx, dw, db)
+        assert torch.equal(dw, first[1]) and torch.equal(db, first[2]) and (place == "add and x" or torch.equal(dx, first[0]))
+    xh, dy64 = (_f64(x) - _f64(stats)[:, :1]) * _f64(stats)[:, 1:], _f64(dy)
+    assert np.all(np.abs(_f64(first[1]) - (dy64 * xh).sum(0)) <= (T + 164) * u * np.abs(dy64 * xh).sum(0) + 1e-37)
+    assert np.all(np.abs(_f64(first[2]) - dy64.sum(0)) <= (T + 160) * u * np.abs(dy64).sum(0) + 1e-37)
+
+
 def test_gradients_are_the_forward_pass_differences(metis):
     """fp32; a step h: results rounded to 2^-23 of magnitudes up to 5, their 30 products with dy summed, over 2 h; and h^2 / 6 of third derivatives of
     rows of unit scale."""

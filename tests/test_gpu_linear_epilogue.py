@@ -204,6 +204,22 @@ def test_gradient_of_the_epilogue(metis, T, N, dtype):
             assert torch.equal(alone, dz)
 
 
+@pytest.mark.parametrize("T,N", [(127, 65), (128, 64), (128, 2049), (129, 63), (129, 2049)])
+def test_gradient_near_the_rule(metis, T, N):
+    """The same bits wherever dz goes, and dbias the sums of the dz it wrote (fp32; T + 160 roundings)."""
+    g = torch.Generator().manual_seed(T * N)
+    dy, pre = torch.randn((T, N), generator=g).cuda(), torch.randn((T, N), generator=g).cuda()
+    first = None
+    for place in (None, "dy", "pre"):
+        d, z, db = dy.clone(), pre.clone(), torch.empty(N, device="cuda")
+        dz = {None: torch.empty_like(d), "dy": d, "pre": z}[place]
+        metis.linear_grads(d, dz, pre=z, act="gelu", mask=metis.DropoutMask(0.25, 5), dbias=db)
+        first = first or (dz, db)
+        assert torch.equal(dz, first[0]) and torch.equal(db, first[1])
+    s = _f64(first[0])
+    assert np.all(np.abs(_f64(first[1]) - s.sum(0)) <= (T + 160) * 2.0 ** -24 * np.abs(s).sum(0) + 1e-37)
+
+
 def test_gradient_is_the_forward_pass_differences(metis):
     """dz against differences of the forward pass itself: fp32, a step of 2^-7 (second-order error 2^-14 / 6 of a third derivative below 2, results
     of magnitude up to 8 rounded to 2^-21, over 2^-6)."""
