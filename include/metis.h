@@ -602,7 +602,7 @@ int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_mxfp4* Xq, 
 
 /*
  * Gradient of that epilogue: dZ = act'(pre) m dY, of what the activation is applied to, and dbias (device fp32 [cols]) = the sum of dZ's rows,
- * of its values before they are rounded, in an order that depends on the shape alone.  (The residual's gradient is dY itself.)  relu' (0) = 0.
+ * of its values before they are rounded, in an order that depends on shape and type alone.  (The residual's gradient is dY itself.)  relu' (0) = 0.
  *   pre        as the forward pass left it; not looked at for METIS_ACT_NONE
  *   mask       the forward pass's, or null
  *   dZ, dbias  either may be null; dZ may be dY or pre itself
@@ -626,7 +626,7 @@ int metis_layernorm(void* stream, const metis_mat* x, const float* weight, const
 /*
  * Its gradients, with xh = (x - mean) rstd from `stats` and g = dy weight:
  *   dx = add + rstd (g - mean of g - xh * mean of g xh)    add: null, or the gradient that reaches x past the norm
- *   dweight, dbias (device fp32 [cols], each may be null) = sums over the rows of dy xh and of dy, in an order that depends on the shape alone
+ *   dweight, dbias (device fp32 [cols], each may be null) = sums over the rows of dy xh and of dy, in an order that depends on shape and type alone
  * dy, x, add, dx: one type (bf16 or fp32), any strides and alignments of elements; dx may be dy, x or add itself.
  * workspace: metis_layernorm_grads_workspace_bytes bytes where dweight or dbias is wanted, 256-byte aligned.  Without rows both become 0.
  * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (as above).

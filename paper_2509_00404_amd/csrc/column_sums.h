@@ -31,27 +31,33 @@ k_clear(float* __restrict__ p, int64_t n) {
     if (i < n) p[i] = 0.0f;
 }
 
-// Column sums of a workgroup of WAVES waves whose lanes have eight columns each, lane % 8 of 64, and some of the rows: added over the lanes of a wave,
-// then over the waves, in the same order every time; out[64 * strip ...].  lds: 64 WAVES floats that nobody else uses meanwhile.
-template <int WAVES>
+// Column sums of a workgroup of WAVES waves whose lanes have eight columns each, lane % W of W units, and some of the rows: added over the lanes of a
+// wave, then over the waves, in the same order every time; out[8 W * strip ...].  lds: 8 W WAVES floats that nobody else uses meanwhile.
+template <int WAVES, int W>
 __device__ __forceinline__ void group_columns(float (&sum)[8], float* lds, float* __restrict__ out, int64_t strip, int64_t cols) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int d = 8; d < 64; d <<= 1)
+    for (int d = W; d < 64; d <<= 1)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += __shfl_xor(sum[i], d);
-    if (lane < 8) {
+    if (lane < W) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) lds[64 * wave + 8 * lane + i] = sum[i];
+        for (int i = 0; i < 8; ++i) lds[8 * W * wave + 8 * lane + i] = sum[i];
     }
     __syncthreads();
-    const int64_t c = 64 * strip + lane;
-    if (wave == 0 && c < cols) {
+    const int64_t c = 8 * W * strip + lane;
+    if (wave == 0 && lane < 8 * W && c < cols) {
         float s = lds[lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) s += lds[64 * w + lane];
+        for (int w = 1; w < WAVES; ++w) s += lds[8 * W * w + lane];
         out[c] = s;
     }
+}
+
+// Strips of a row's lines in turn on one XCD (workgroups go round the eight): strip of workgroup `block` of `strips`.
+__device__ __forceinline__ uint32_t xcd_strip(uint32_t block, uint32_t strips) {
+    const uint32_t x = block % 8, each = strips / 8, more = strips % 8;
+    return x * each + (x < more ? x : more) + block / 8;
 }
 
 int launch_join(hipStream_t s, const float* P, int64_t parts, int64_t n, float* out, int64_t split, float* out2) {

@@ -162,6 +162,25 @@ __device__ __forceinline__ void unpack(const RawUnit<float>& r, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = r.w[i >> 2][i & 3];
 }
+// The unit at column c of a row, without a condition of the lane's: where the row ends inside it, the whole vector at the row's end, whose first `back`
+// elements are the unit's before it.  (A path of its own for that lane would make its whole wave wait for memory there.)  Rows of fewer than eight
+// elements have one unit, back 0.  unpack(r, back, v): the unit's own elements, zeros behind them.
+__device__ __forceinline__ int unit_back(int64_t c, int64_t cols) { return cols < 8 || c + 8 <= cols ? 0 : (int)(c + 8 - cols); }
+template <bool PAST = false, typename T>
+__device__ __forceinline__ void load_back(const T* row, int64_t c, int back, int64_t cols, RawUnit<T>& r) {
+    if (cols >= 8) load_whole<PAST>(row + (c - back), r);
+    else load_raw<PAST>(row + c, cols, r);
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const RawUnit<T>& r, int back, float (&v)[8]) {
+    unpack(r, v);
+    if (back) {
+#pragma unroll
+        for (int s = 4; s > 0; s >>= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = back & s ? (i + s < 8 ? v[i + s] : 0.0f) : v[i];
+    }
+}
 template <typename T>
 __device__ __forceinline__ void load_unit(const T* p, int64_t n, float (&v)[8]) {
     RawUnit<T> r;

@@ -272,35 +272,37 @@ k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float
     norm_grads_rows<T, RT, U, ADD>(dy, ldd, x, ldx, stats, weight, add, lda, dx, ldo, rows, cols, sums, blockIdx.x, gridDim.x);
 }
 
-// Few rows, one launch: the first `strips` workgroups have 64 columns each and go down all the rows, eight lanes a row, for the columns' sums; the others
-// have rows.  (Both read x and dy: where dx takes the place of one, the rows follow in a launch of their own.)
+// Few rows, one launch: the first `strips` workgroups have 8 W columns each, a 128-byte line of fp32 or so, and go down all the rows, 128 at a time, for
+// the columns' sums; the others have rows.  (Both read x and dy: where dx takes the place of one, the rows follow in a launch of their own.)
 template <typename T, int RT, int U, bool ADD>
 __global__ void __launch_bounds__(RowGroup<RT>::THREADS)
 k_layernorm_grads_few(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
                       const T* add, int64_t lda, T* dx, int64_t ldo, int64_t rows, int64_t cols, float* dweight, float* dbias, uint32_t strips) {
-    constexpr int WAVES = RowGroup<RT>::THREADS / 64, STEP = RowGroup<RT>::THREADS / 8;
+    constexpr int WAVES = RowGroup<RT>::THREADS / 64, STEP = 128, W = RowGroup<RT>::THREADS / STEP;
     if (blockIdx.x >= strips) {
         norm_grads_rows<T, RT, U, ADD>(dy, ldd, x, ldx, stats, weight, add, lda, dx, ldo, rows, cols, nullptr, blockIdx.x - strips, gridDim.x - strips);
         return;
     }
-    __shared__ float s_columns[2 * 64 * WAVES];
-    const int64_t c = 64 * (int64_t)blockIdx.x + 8 * (threadIdx.x & 7), n = cols - c;
+    const uint32_t strip = xcd_strip(blockIdx.x, strips);
+    __shared__ float s_columns[2 * 8 * W * WAVES];
+    const int64_t c = 8 * W * (int64_t)strip + 8 * (threadIdx.x % W);
+    const int back = unit_back(c, cols);
     float dw[8] = {}, db[8] = {};
-    int64_t r = threadIdx.x >> 3;
-    if (n > 0 && r < rows) {
+    int64_t r = threadIdx.x / W;
+    if (c < cols && r < rows) {
         RawUnit<T> nx, nd;
         float2 nst;
         auto fetch = [&](int64_t row) __attribute__((always_inline)) {
             nst = stats[row];
-            load_raw(x + row * ldx + c, n, nx);
-            load_raw(dy + row * ldd + c, n, nd);
+            load_whole(x + row * ldx + (c - back), nx);
+            load_whole(dy + row * ldd + (c - back), nd);
         };
         fetch(r);
         for (; r < rows; r += STEP) {
             float v[8], g[8];
             const float2 st = nst;
-            unpack(nx, v);
-            unpack(nd, g);
+            unpack(nx, back, v);
+            unpack(nd, back, g);
             fetch(r + STEP < rows ? r + STEP : r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -309,8 +311,8 @@ k_layernorm_grads_few(const T* dy, int64_t ldd, const T* x, int64_t ldx, const f
             }
         }
     }
-    if (dweight) group_columns<WAVES>(dw, s_columns, dweight, blockIdx.x, cols);
-    if (dbias) group_columns<WAVES>(db, s_columns + 64 * WAVES, dbias, blockIdx.x, cols);
+    if (dweight) group_columns<WAVES, W>(dw, s_columns, dweight, strip, cols);
+    if (dbias) group_columns<WAVES, W>(db, s_columns + 8 * W * WAVES, dbias, strip, cols);
 }
 
 // Long rows: two passes over a row for its gradient, and the columns' sums by a kernel that goes down the columns.
@@ -415,9 +417,12 @@ int64_t column_chunk(int64_t rows, int64_t cols) {                       // rows
 int64_t sum_rows(int64_t rows, int64_t cols) {
     return in_registers(cols) ? norm_parts(rows, cols) : ceil_div64(rows, column_chunk(rows, cols));
 }
-// Few rows: one launch.  us, fp32, two launches / one: 16 x 4096 7.0 / 4.6, 128 x 4096 9.2 / 5.5, 256 x 4096 12.5 / 7.6, 256 x 256 7.1 / 6.5, 512 x 4096
-// 13.8 / 13.9, 512 x 256 6.7 / 9.1.
-bool norm_few(int64_t rows, int64_t cols) { return in_registers(cols) && rows <= 256; }
+// Few rows: one launch.  us, two launches / one, fp32: 128 x 4096 9.3 / 5.2, 512 x 4096 13.9 / 9.0, 700 x 4096 14.6 / 12.3, 1000 x 4096 16.2 / 17.5,
+// 512 x 14336 29.8 / 28.2, 1000 x 256 8.8 / 6.6, 1111 x 2057 13.7 / 12.4, 1500 x 1000 10.9 / 12.0, 2000 x 256 7.4 / 9.0; bf16: 4 x 4096 6.7 / 4.7,
+// 512 x 14336 23.4 / 17.5, 1000 x 6000 17.6 / 13.9.
+bool norm_few(int64_t rows, int64_t cols, int64_t size) {
+    return in_registers(cols) && (rows <= 512 || (rows <= 1280 && rows * cols * size <= 12 << 20));
+}
 // the threads of a row and the units of a thread: f(threads, units)
 template <typename F>
 void by_length(int64_t cols, F f) {
@@ -484,7 +489,7 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
     if (rows < 1 || cols < 1 || !norm_mat(x, x) || !norm_mat(dy, x) || !norm_mat(dx, x) || (add && !norm_mat(add, x))) return METIS_BAD_SHAPE;
     const int st = norm_limits(rows, cols);
     if (st != METIS_OK) return st;
-    const bool few = columns && norm_few(rows, cols);
+    const bool few = columns && norm_few(rows, cols, mat_size(x));
     if (columns && (!workspace || workspace_bytes < metis_layernorm_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;
     if (columns && (uintptr_t)workspace % 256) return METIS_INVALID_ARG;
     float* sums = columns && !few ? (float*)workspace : nullptr;
@@ -506,7 +511,7 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
                 constexpr int RT = decltype(rt)::value;
                 constexpr int U = decltype(u)::value;
                 if (few) {
-                    const unsigned strips = (unsigned)ceil_div64(cols, 64), groups = (unsigned)ceil_div64(rows, RowGroup<RT>::ROWS);
+                    const unsigned strips = (unsigned)ceil_div64(cols, RowGroup<RT>::THREADS / 16), groups = (unsigned)ceil_div64(rows, RowGroup<RT>::ROWS);
                     const bool over = dx->ptr == x->ptr || dx->ptr == dy->ptr;
                     auto kern = add ? k_layernorm_grads_few<T, RT, U, true> : k_layernorm_grads_few<T, RT, U, false>;
                     hipLaunchKernelGGL(kern, dim3(over ? strips : strips + groups), dim3(RowGroup<RT>::THREADS), 0, s, pd, dy->ld, px, x->ld,

@@ -329,6 +329,7 @@ k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64
     __shared__ float s_sum[WIDE ? 1 : 3 * 8 * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t c = (WIDE ? 2048 * (int64_t)blockIdx.x + 512 * wave : 512 * (int64_t)blockIdx.x) + 8 * lane, n = cols - c;
+    const int back = unit_back(c, cols);
     const int64_t hop = WIDE ? gridDim.y : 4 * (int64_t)gridDim.y;
     const uint32_t step = mask_step(mask);
     float sum[8];
@@ -338,13 +339,13 @@ k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64
     if (n > 0 && r < rows) {
         RawUnit<T> nd[2], np[2];
         auto fetch = [&](int64_t row, int k) __attribute__((always_inline)) {
-            load_raw<PAST>(dy + row * ldd + c, n, nd[k]);
-            if (ACT != METIS_ACT_NONE) load_raw<PAST>(pre + row * ldp + c, n, np[k]);
+            load_back<PAST>(dy + row * ldd, c, back, cols, nd[k]);
+            if (ACT != METIS_ACT_NONE) load_back<PAST>(pre + row * ldp, c, back, cols, np[k]);
         };
         auto one = [&](int64_t row, int k) __attribute__((always_inline)) {
             float v[8], z[8];
-            unpack(nd[k], v);
-            if (ACT != METIS_ACT_NONE) unpack(np[k], z);
+            unpack(nd[k], back, v);
+            if (ACT != METIS_ACT_NONE) unpack(np[k], back, z);
             fetch(row + 2 * hop < rows ? row + 2 * hop : row, k);
             if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)row, v);
             if (ACT != METIS_ACT_NONE) {
@@ -381,29 +382,32 @@ k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64
 // Past the caches from 128 MiB a matrix on, where the three do not fit the last-level cache: us, through / past, 16384 x 14336 283 / 269, 16384 x 4096 82 / 77,
 // 4096 x 4096 23.8 / 27.4.
 #define GRADS_PAST (128ll << 20)
-// Few rows, one launch: a workgroup has 64 columns and all the rows, 32 at a time, eight lanes a row.
+// Few rows, one launch: a workgroup has 16 columns and all the rows, 128 at a time, two lanes a row.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 k_linear_grads_few(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64_t ldz, MaskKey mask, int64_t rows, int64_t cols, float* dbias) {
-    __shared__ float s_sum[4 * 64];
-    const int64_t c = 64 * (int64_t)blockIdx.x + 8 * (threadIdx.x & 7), n = cols - c;
+    constexpr int W = 2, STEP = 256 / W;
+    const uint32_t strip = xcd_strip(blockIdx.x, gridDim.x);
+    __shared__ float s_sum[4 * 8 * W];
+    const int64_t c = 8 * W * (int64_t)strip + 8 * (threadIdx.x % W), n = cols - c;
+    const int back = unit_back(c, cols);
     const uint32_t step = mask_step(mask);
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-    int64_t r = threadIdx.x >> 3;
+    int64_t r = threadIdx.x / W;
     if (n > 0 && r < rows) {
         RawUnit<T> nd, np;
         auto fetch = [&](int64_t row) __attribute__((always_inline)) {
-            load_raw(dy + row * ldd + c, n, nd);
-            if (ACT != METIS_ACT_NONE) load_raw(pre + row * ldp + c, n, np);
+            load_back(dy + row * ldd, c, back, cols, nd);
+            if (ACT != METIS_ACT_NONE) load_back(pre + row * ldp, c, back, cols, np);
         };
         fetch(r);
-        for (; r < rows; r += 32) {
+        for (; r < rows; r += STEP) {
             float v[8], z[8];
-            unpack(nd, v);
-            if (ACT != METIS_ACT_NONE) unpack(np, z);
-            fetch(r + 32 < rows ? r + 32 : r);
+            unpack(nd, back, v);
+            if (ACT != METIS_ACT_NONE) unpack(np, back, z);
+            fetch(r + STEP < rows ? r + STEP : r);
             if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)r, v);
             if (ACT != METIS_ACT_NONE) {
 #pragma unroll
@@ -414,19 +418,19 @@ k_linear_grads_few(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, i
             for (int i = 0; i < 8; ++i) sum[i] += v[i];
         }
     }
-    if (dbias) group_columns<4>(sum, s_sum, dbias, blockIdx.x, cols);
+    if (dbias) group_columns<4, W>(sum, s_sum, dbias, strip, cols);
 }
 
 bool grads_wide(int64_t cols) { return cols >= 2048; }
-// us, bf16, gelu, rows in parts and a joining launch / k_linear_grads_few: 4 x 4096 6.7 / 4.4, 32 x 4096 6.8 / 4.5, 128 x 14336 10.1 / 6.8, 128 x 1000
-// 7.4 / 6.2, 256 x 14336 12.1 / 9.9, 256 x 4096 8.0 / 9.1, 256 x 256 6.6 / 8.9.
-bool grads_few(int64_t rows) { return rows <= 128; }
+// us, bf16, gelu, rows in parts and a joining launch / k_linear_grads_few: 4 x 14336 6.9 / 4.5, 128 x 4096 8.1 / 5.0, 512 x 14336 16.6 / 14.7, 512 x 256
+// 7.0 / 6.5, 700 x 4096 11.4 / 8.9, 1000 x 4096 12.0 / 10.5, 1000 x 256 9.6 / 9.4, 1111 x 1000 8.1 / 10.2, 1500 x 256 8.6 / 12.2.
+bool grads_few(int64_t rows, int64_t cols) { return rows <= 768 && cols <= 65536; }
 int64_t grads_strips(int64_t cols) { return ceil_div64(cols, grads_wide(cols) ? 2048 : 512); }
 // Workgroups that share the rows of a strip, each of which leaves a row of partial sums: 1024 in all where each has eight rows or more, else 512 with two rows at
 // least; the same on any chip so that the sums have the same order.  us, 512 / 1024 / 2048, gelu, bf16: 16384 x 14336 300 / 269 / 292, 16384 x 4096 87 / 77 /
-// 86, 4096 x 4096 25.0 / 23.8 / 29.4, 1000 x 4096 11.6 / 14.7.  Two / four / eight rows at least: 100 rows 7.8 / 8.4 / 10.8.
+// 86, 4096 x 4096 25.0 / 23.8 / 29.4, 1000 x 4096 11.6 / 14.7.
 int64_t grads_parts(int64_t rows, int64_t cols) {
-    if (grads_few(rows)) return 1;
+    if (grads_few(rows, cols)) return 1;
     const int64_t strips = grads_strips(cols), many = strips < 1024 ? 1024 / strips : 1, few = strips < 512 ? 512 / strips : 1;
     if (rows >= 8 * many) return many;
     const int64_t want = ceil_div64(rows, 2);
@@ -504,8 +508,8 @@ extern "C" int metis_linear_grads(void* stream, const metis_mat* dY, const metis
     if (rows == 0) return dbias ? launch_clear(s, dbias, cols) : METIS_OK;
     if ((pre && (!mat_ok(pre) || pre->dtype != dY->dtype)) || (dZ && (!mat_ok(dZ) || dZ->dtype != dY->dtype))) return METIS_INVALID_ARG;
     if ((pre && !same_layout(pre, dY)) || (dZ && !same_layout(dZ, dY))) return METIS_BAD_SHAPE;
-    const bool few = grads_few(rows);
-    const int64_t chunks = grads_parts(rows, cols), strips = few ? ceil_div64(cols, 64) : grads_strips(cols);
+    const bool few = grads_few(rows, cols);
+    const int64_t chunks = grads_parts(rows, cols), strips = few ? ceil_div64(cols, 16) : grads_strips(cols);
     if (!grid_fits(strips, 256) || chunks > 65535) return METIS_UNSUPPORTED;
     const bool parts = dbias && chunks > 1;
     if (parts && (!workspace || workspace_bytes < metis_linear_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;

@@ -113,7 +113,7 @@ def test_layernorm_grads(metis, T, D, dtype):
             assert (wo[:, :pad] == 7).all() and (wo[:, D + pad:] == 7).all()
 
 
-@pytest.mark.parametrize("T,D", [(255, 65), (256, 64), (256, 4090), (257, 63), (129, 9000), (256, 7), (31, 16390)])
+@pytest.mark.parametrize("T,D", [(255, 65), (256, 64), (256, 4090), (512, 10), (512, 9000), (513, 9000), (1280, 63), (1281, 63), (129, 9), (256, 7), (31, 16390)])
 def test_layernorm_grads_near_the_rules(metis, T, D):
     """The same sums and the same rows wherever dx goes: the columns' sums read dy and x before dx takes the place of either."""
     x, dy, add, w, _ = _inputs(T, D, torch.float32, T * D)

@@ -204,7 +204,7 @@ def test_gradient_of_the_epilogue(metis, T, N, dtype):
             assert torch.equal(alone, dz)
 
 
-@pytest.mark.parametrize("T,N", [(127, 65), (128, 64), (128, 2049), (129, 63), (129, 2049)])
+@pytest.mark.parametrize("T,N", [(127, 65), (128, 64), (128, 2049), (129, 17), (768, 63), (769, 63), (769, 2049), (2, 65536), (2, 65537), (130, 9), (5, 7)])
 def test_gradient_near_the_rule(metis, T, N):
     """The same bits wherever dz goes, and dbias the sums of the dz it wrote (fp32; T + 160 roundings)."""
     g = torch.Generator().manual_seed(T * N)
