@@ -195,20 +195,55 @@ __device__ __forceinline__ void finish_values(const MxFinish<T, ACT>& f, uint32_
         for (int s = 0; s < S; ++s) mask_apply(f.mask, step, (uint32_t)(c >> 3), row(s), v[s]);
     }
 }
-// n <= 8 elements (row r, columns c .. c + n - 1, c a multiple of 8) whose bias is in b; step: mask_step(f.mask)
+// What the epilogue reads for a unit of eight elements (row r, columns from c on, a multiple of 8), fetched ahead of its use.
+template <typename T>
+struct UnitInputs {
+    RawUnit<float> bias;
+    RawUnit<T> residual;
+    int back;
+};
 template <typename T, int ACT>
-__device__ __forceinline__ void finish_unit(const MxFinish<T, ACT>& f, uint32_t step, int64_t r, int64_t c, int64_t n, const float (&b)[8], float (&v)[8]) {
-    float res[8], one[1][8];
-    if (f.residual) load_unit(f.residual + r * f.ldr + c, n, res);
+__device__ __forceinline__ void finish_inputs(const MxFinish<T, ACT>& f, int64_t r, int64_t c, int64_t N, UnitInputs<T>& in) {
+    in.back = unit_back(c, N);
+    in.bias = RawUnit<float>{};
+    if (f.bias) load_back(f.bias, c, in.back, N, in.bias);
+    if (f.residual) load_back(f.residual + r * f.ldr, c, in.back, N, in.residual);
+}
+// One element of each, where there are no registers for all: finish_inputs then finds their lines in the cache.  finish_near_by: after the product.
+template <typename T>
+struct UnitNear {
+    float bias;
+    T residual;
+};
+template <typename T, int ACT>
+__device__ __forceinline__ UnitNear<T> finish_near(const MxFinish<T, ACT>& f, int64_t r, int64_t c, int64_t N) {
+    const int64_t at = c < N ? c : N - 1;
+    UnitNear<T> near = {};
+    if (f.bias) near.bias = f.bias[at];
+    if (f.residual) near.residual = f.residual[r * f.ldr + at];
+    return near;
+}
+template <typename T>
+__device__ __forceinline__ void finish_near_by(const UnitNear<T>& near) {
+    asm volatile("" :: "v"(near.bias), "v"(near.residual));
+}
+// step: mask_step(f.mask)
+template <typename T, int ACT>
+__device__ __forceinline__ void finish_unit(const MxFinish<T, ACT>& f, uint32_t step, int64_t r, int64_t c, int64_t N, const UnitInputs<T>& in,
+                                            const float (&v)[8]) {
+    float b[8], one[1][8];
+    unpack(in.bias, in.back, b);
 #pragma unroll
     for (int i = 0; i < 8; ++i) one[0][i] = v[i] + b[i];
-    if (f.pre) store_part<T, true>(f.pre + r * f.ldp + c, n, one[0]);
+    if (f.pre) store_part<T, true>(f.pre + r * f.ldp + c, N - c, one[0]);
     finish_values<1>(f, step, c, [&](int) __attribute__((always_inline)) { return (uint32_t)r; }, one);
     if (f.residual) {
+        float res[8];
+        unpack(in.residual, in.back, res);
 #pragma unroll
         for (int i = 0; i < 8; ++i) one[0][i] += res[i];
     }
-    store_part<T, true>(f.y + r * f.ldy + c, n, one[0]);
+    store_part<T, true>(f.y + r * f.ldy + c, N - c, one[0]);
 }
 template <typename T, int ACT>
 __device__ __forceinline__ void finish_bias(const MxFinish<T, ACT>& f, int64_t c, int64_t N, float (&b)[8]) {

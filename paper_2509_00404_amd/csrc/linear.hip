@@ -68,6 +68,8 @@ k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> 
     int r = wave;                                        // (waves <= runs)
 #pragma unroll
     for (int o = 0; o < OF; ++o) run_load<false>(wc[o], wsc[o], r, nblk, g, w[0][o], ws[0][o]);
+    // what the epilogue reads for the thread's unit of eight outputs (the first, where few waves have more) is brought near behind the first weights
+    const auto near = finish_near(f, (int)threadIdx.x / (2 * OF) < rows ? (int)threadIdx.x / (2 * OF) : 0, n0 + 8 * (threadIdx.x % (2 * OF)), N);
     const uint8_t *tc[TG], *tsc[TG];                     // this lane's rows
     if constexpr (FUSE) {
         uint8_t* s_scales = s_mem + rows * few_codes_row(nblk);
@@ -146,12 +148,14 @@ k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> 
             *reinterpret_cast<lf_f4*>(s_part + ((wave * TG + t) * 16 + li) * PROW + 16 * o + 4 * g) = acc[o][t];
     __syncthreads();
     const uint32_t step = mask_step(f.mask);
+    finish_near_by(near);
     for (int u = threadIdx.x; u < rows * 2 * OF; u += blockDim.x) {
         const int row = u / (2 * OF), unit = u % (2 * OF);
         const int64_t c = n0 + 8 * unit;
         if (c >= N) continue;
-        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}, b[8];
-        finish_bias(f, c, N, b);
+        UnitInputs<OUT> in;
+        finish_inputs(f, row, c, N, in);
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         for (int p = 0; p < waves; ++p) {
             const lf_f4* q = reinterpret_cast<const lf_f4*>(s_part + (p * TG * 16 + row) * PROW + 8 * unit);
             const lf_f4 lo = q[0], hi = q[1];
@@ -161,7 +165,7 @@ k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> 
                 v[4 + i] += hi[i];
             }
         }
-        finish_unit(f, step, row, c, N - c, b, v);
+        finish_unit(f, step, row, c, N, in, v);
     }
 }
 
@@ -177,8 +181,9 @@ k_linear_join(const float* __restrict__ sums, int64_t ld, int64_t stride, int pa
     if (u >= total) return;
     const int64_t r = (int64_t)div_by(units, u), c = 8 * (int64_t)(u - (uint64_t)r * units.d);
     const float* p = sums + r * ld + c;
-    float v[8], b[8];
-    finish_bias(f, c, N, b);
+    float v[8];
+    UnitInputs<OUT> in;
+    finish_inputs(f, r, c, N, in);
     load_row(p, v);
     int i = 1;
     for (; i + 3 < parts; i += 4) {
@@ -196,7 +201,7 @@ k_linear_join(const float* __restrict__ sums, int64_t ld, int64_t stride, int pa
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += x[e];
     }
-    finish_unit(f, mask_step(f.mask), r, c, N - c, b, v);
+    finish_unit(f, mask_step(f.mask), r, c, N, in, v);
 }
 
 struct LinearParts {
