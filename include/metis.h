@@ -628,7 +628,8 @@ int metis_layernorm(void* stream, const metis_mat* x, const float* weight, const
  *   dx = add + rstd (g - mean of g - xh * mean of g xh)    add: null, or the gradient that reaches x past the norm
  *   dweight, dbias (device fp32 [cols], each may be null) = sums over the rows of dy xh and of dy, in an order that depends on shape and type alone
  * dy, x, add, dx: one type (bf16 or fp32), any strides and alignments of elements; dx may be dy, x or add itself.
- * workspace: metis_layernorm_grads_workspace_bytes bytes where dweight or dbias is wanted, 256-byte aligned.  Without rows both become 0.
+ * workspace: metis_layernorm_grads_workspace_bytes bytes where dweight or dbias is wanted, 256-byte aligned (may be null where that is 0).  Without rows
+ * both become 0.
  * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_WORKSPACE_TOO_SMALL, METIS_UNSUPPORTED (as above).
  */
 size_t metis_layernorm_grads_workspace_bytes(int64_t rows, int64_t cols);

@@ -468,6 +468,7 @@ extern "C" int metis_layernorm(void* stream, const metis_mat* x, const float* we
 
 extern "C" size_t metis_layernorm_grads_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || cols < 1 || norm_limits(rows, cols) != METIS_OK) return 0;
+    if (norm_few(rows, cols, 4)) return 0;                // (of either type)
     return align_up((size_t)sum_rows(rows, cols) * 2 * cols * 4, 256);
 }
 
@@ -490,8 +491,8 @@ extern "C" int metis_layernorm_grads(void* stream, const metis_mat* dy, const me
     const int st = norm_limits(rows, cols);
     if (st != METIS_OK) return st;
     const bool few = columns && norm_few(rows, cols, mat_size(x));
-    if (columns && (!workspace || workspace_bytes < metis_layernorm_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;
-    if (columns && (uintptr_t)workspace % 256) return METIS_INVALID_ARG;
+    if (columns && !few && (!workspace || workspace_bytes < metis_layernorm_grads_workspace_bytes(rows, cols))) return METIS_WORKSPACE_TOO_SMALL;
+    if (columns && !few && (uintptr_t)workspace % 256) return METIS_INVALID_ARG;
     float* sums = columns && !few ? (float*)workspace : nullptr;
     auto launch = [&](auto zero) {
         typedef decltype(zero) T;

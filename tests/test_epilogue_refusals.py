@@ -135,7 +135,8 @@ def test_layernorm(metis):
     assert grads(dy=(5, 40, 40, 0)) == SHAPE and grads(dx=(4, 41, 41, 0)) == SHAPE and grads(add=(4, 40, 39, 0)) == SHAPE and grads(x=(4, 40, 39, 0)) == SHAPE
     wide = (4, huge, huge, 0)
     assert grads(wide, wide, wide) == UNSUPPORTED and L.metis_layernorm_grads_workspace_bytes(4, huge) == 0
-    for shape in ((4, 40, 40, 0), (700, 40, 40, 0), (4, 40000, 40000, 0)):
+    assert L.metis_layernorm_grads_workspace_bytes(4, 40) == 0 and L.metis_layernorm_grads_workspace_bytes(512, 16384) == 0
+    for shape in ((1281, 40, 40, 0), (700, 16384, 16384, 0), (4, 40000, 40000, 0), (4, 7, 7, 0)):
         need = L.metis_layernorm_grads_workspace_bytes(*shape[:2])
         assert need > 0 and grads(shape, shape, shape, size=need - 1) == WORKSPACE and grads(shape, shape, shape, ws=None) == WORKSPACE
         assert grads(shape, shape, shape, ws=FAKE + 4) == INVALID
