@@ -581,8 +581,9 @@ int metis_dropout(void* stream, const metis_mat* x, const metis_dropout_mask* ma
  *   e          null: no epilogue.  bias: device fp32 [N], or null.  act: see below.  pre: null, or an output of Y's shape and type: Q(X) W^T + bias,
  *              rounded (the activation is applied to what is not rounded yet).  mask: null, or a dropout.  residual: null, or a matrix of Y's
  *              shape and type, which may be Y itself; Y, pre and residual must not overlap otherwise.
- *   workspace  with X: metis_mxfp4_linear_workspace_bytes bytes, 256-byte aligned; also without it, where that many bytes let few rows
- *              run faster (a call without is right too).  Calls that may run at the same time have workspaces of their own.
+ *   workspace  with X: metis_mxfp4_linear_workspace_bytes bytes, 256-byte aligned (may be null where that is 0); with Xq, that many let a product of
+ *              more than 64 rows and few outputs run faster (a call without is right too).  Calls that may run at the same time have workspaces of
+ *              their own.
  *   act        relu max(z, 0); gelu z Phi(z), Phi the normal distribution; gelu_tanh z sigmoid(2 sqrt(2 / pi) (z + 0.044715 z^3)); silu
  *              z sigmoid(z).  For bf16 outputs their exponentials are the hardware's: results are within 4e-5, relatively.
  * Any strides of Y, pre, residual, and alignments of their elements.  No rows is no work.

@@ -65,9 +65,12 @@ k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> 
     }
     uvec4_t w[2][OF][4];
     uint32_t ws[2][OF][4];
-    int r = wave;                                        // (waves <= runs)
+    int r = wave;
+    const int have = waves < runs ? waves : runs;        // waves with runs (FUSE: the others help to quantize)
+    if (!FUSE || r < runs) {
 #pragma unroll
-    for (int o = 0; o < OF; ++o) run_load<false>(wc[o], wsc[o], r, nblk, g, w[0][o], ws[0][o]);
+        for (int o = 0; o < OF; ++o) run_load<false>(wc[o], wsc[o], r, nblk, g, w[0][o], ws[0][o]);
+    }
     // what the epilogue reads for the thread's unit of eight outputs (the first, where few waves have more) is brought near behind the first weights
     const auto near = finish_near(f, (int)threadIdx.x / (2 * OF) < rows ? (int)threadIdx.x / (2 * OF) : 0, n0 + 8 * (threadIdx.x % (2 * OF)), N);
     const uint8_t *tc[TG], *tsc[TG];                     // this lane's rows
@@ -141,11 +144,13 @@ k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> 
     }
     if constexpr (FUSE) __syncthreads();                 // the sums take the rows' place
     float* s_part = reinterpret_cast<float*>(s_mem);
+    if (wave < have) {
 #pragma unroll
-    for (int o = 0; o < OF; ++o)
+        for (int o = 0; o < OF; ++o)
 #pragma unroll
-        for (int t = 0; t < TG; ++t)
-            *reinterpret_cast<lf_f4*>(s_part + ((wave * TG + t) * 16 + li) * PROW + 16 * o + 4 * g) = acc[o][t];
+            for (int t = 0; t < TG; ++t)
+                *reinterpret_cast<lf_f4*>(s_part + ((wave * TG + t) * 16 + li) * PROW + 16 * o + 4 * g) = acc[o][t];
+    }
     __syncthreads();
     const uint32_t step = mask_step(f.mask);
     finish_near_by(near);
@@ -156,7 +161,7 @@ k_linear_few(MxOperand X, DenseRows dense, MxOperand W, int nblk, MxFinish<OUT> 
         UnitInputs<OUT> in;
         finish_inputs(f, row, c, N, in);
         float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        for (int p = 0; p < waves; ++p) {
+        for (int p = 0; p < have; ++p) {
             const lf_f4* q = reinterpret_cast<const lf_f4*>(s_part + (p * TG * 16 + row) * PROW + 8 * unit);
             const lf_f4 lo = q[0], hi = q[1];
 #pragma unroll
@@ -276,22 +281,23 @@ LinearPlace linear_place(int64_t rows, int64_t N, int64_t K) {
 // where they need more registers; four at least).  us, 16 / 32 outputs: one row 14336 x 4096 11.6 / 10.3, 4096 x 14336 10.5 / 16.0; 64 rows 35.5 / 18.8,
 // 23.3 / 27.6.  24 rows of 14336 x 4096 with four waves 13.2, with eight (half of the workgroups wait) 15.9.
 struct FewShape {
-    int tg, of, waves;
+    int tg, of, waves, fused;                     // waves where the rows are quantized already, and where they are not
 };
 FewShape few_shape(int64_t rows, int64_t N, int64_t K) {
     const int tg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, of = N >= 8192 ? 2 : 1;
     const int64_t wgs = ceil_div64(N, 16 * of);
     // waves that a CU holds at once, over the workgroups that it has to hold
-    const int64_t room = 256 * (tg == 1 ? 16 : tg == 2 && of == 1 ? 16 : 8) / wgs;
+    const int64_t room = (tg == 1 ? 16 : tg == 2 && of == 1 ? 16 : 8) / ceil_div64(wgs, 256);
     const int64_t runs = few_runs((int)(K / 32));
     int64_t most = room < few_waves(tg, of) ? room : few_waves(tg, of);
     most = most < 4 ? 4 : most;
     const int64_t per = (runs + most - 1) / most;
-    return {tg, of, (int)((runs + per - 1) / per)};
+    return {tg, of, (int)((runs + per - 1) / per), (int)(rows * runs < most ? rows * runs : most)};
 }
-// Quantized on the spot up to 16384 elements in all.  us, with the quantizer's launch / on the spot, 14336 x 4096: one row 13.0 / 10.9, four 14.9 / 15.1,
-// eight 15.7 / 19.6; 4096 x 14336: one row 13.3 / 11.3, four 13.7 / 15.6.
-bool few_fused(int64_t rows, int64_t K) { return rows <= 16 && rows * K <= 16384; }
+// Quantized on the spot up to four eights of elements a thread.  us, with the quantizer's launch / on the spot: 14336 x 4096 (8 waves) one row 12.1 /
+// 10.6, four 12.6 / 12.2, six 12.8 / 13.5; 4096 x 4096 (16 waves) one 7.5 / 6.0, eight 8.3 / 7.9, twelve 8.6 / 9.2; 4096 x 14336 two 12.4 / 11.9, three 12.7 /
+// 13.1; 1024 x 1024 sixteen 5.6 / 4.6.
+bool few_fused(int64_t rows, int64_t N, int64_t K) { return rows <= 16 && rows * few_runs((int)(K / 32)) <= 4 * few_shape(rows, N, K).fused; }
 template <typename OUT, int TG, int OF, typename IN>
 int launch_few(hipStream_t s, const MxOperand& x, const metis_mat* dense, const MxOperand& w, int64_t K, const MxFinish<OUT>& f, int waves) {
     constexpr bool FUSE = !std::is_void<IN>::value;
@@ -313,7 +319,8 @@ int launch_few_shape(hipStream_t s, const MxOperand& x, const metis_mat* dense, 
     auto by_type = [&](auto tg, auto of) {
         constexpr int TG = decltype(tg)::value, OF = decltype(of)::value;
         if (!dense) return launch_few<OUT, TG, OF, void>(s, x, dense, w, K, f, p.waves);
-        if constexpr (TG == 1) return dense->dtype == METIS_BF16 ? launch_few<OUT, TG, OF, bf16_t>(s, x, dense, w, K, f, p.waves) : launch_few<OUT, TG, OF, float>(s, x, dense, w, K, f, p.waves);
+        if constexpr (TG == 1) return dense->dtype == METIS_BF16 ? launch_few<OUT, TG, OF, bf16_t>(s, x, dense, w, K, f, p.fused)
+                                                                             : launch_few<OUT, TG, OF, float>(s, x, dense, w, K, f, p.fused);
         else return (int)METIS_INVALID_ARG;
     };
     auto by_of = [&](auto tg) {
@@ -448,7 +455,7 @@ bool same_layout(const metis_mat* a, const metis_mat* b) { return a->rows == b->
 
 extern "C" size_t metis_mxfp4_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K) {
     if (rows < 1 || N < 1 || K < 32 || K % 32 || rows > 0xFFFFFFFFll / (K / 2) || N > 0xFFFFFFFFll / (K / 2)) return 0;
-    return linear_place(rows, N, K).bytes;
+    return few_fused(rows, N, K) ? 0 : linear_place(rows, N, K).bytes;
 }
 
 extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_mxfp4* Xq, const metis_mxfp4* W, const metis_epilogue* e,
@@ -468,12 +475,14 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
     metis_mxfp4 q = X ? metis_mxfp4{ws, ws + place.scales, rows, K} : *Xq;
     const int st = mx_operands_status(X ? W : &q, W);
     if (st != METIS_OK) return st;
-    const bool few = rows <= FEW_ROWS, fused = few && X && few_fused(rows, K);
+    const bool few = rows <= FEW_ROWS, fused = few && X && few_fused(rows, N, K);
     if (X) {
         if (rows * (K / 2) > 0xFFFFFFFFll) return METIS_UNSUPPORTED;
+    }
+    if (X && !fused) {
         if (!workspace || workspace_bytes < place.bytes) return METIS_WORKSPACE_TOO_SMALL;
         if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;
-        const int qs = fused ? METIS_OK : metis_quantize_mx(stream, X, &q);
+        const int qs = metis_quantize_mx(stream, X, &q);
         if (qs != METIS_OK) return qs;
     }
     const bool cut = place.parts.count > 1 && workspace && workspace_bytes >= place.bytes && (uintptr_t)workspace % 256 == 0;

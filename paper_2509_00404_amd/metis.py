@@ -709,7 +709,7 @@ def mxfp4_linear(X, W, Y, bias=None, act="none", pre=None, mask=None, residual=N
     p, k, r = _mat(pre) if pre is not None else None, mask.c() if mask is not None else None, _mat(residual) if residual is not None else None
     e = _EPILOGUE.pack(_ptr(bias, torch.float32, (N,)) or 0, ACTIVATIONS[act], C.addressof(p) if p is not None else 0,
                        C.addressof(k) if k is not None else 0, C.addressof(r) if r is not None else 0)
-    workspace, at, nbytes = _space(workspace, mxfp4_linear_workspace_bytes(rows, N, K) if workspace is None else 0, Y)
+    workspace, at, nbytes = _space(workspace, mxfp4_linear_workspace_bytes(rows, N, K) if workspace is None and (dense or rows > 64) else 0, Y)
     _check(lib().metis_mxfp4_linear(_stream(), x if dense else None, None if dense else C.byref(x), C.byref(w), e, _packed(Y), at, nbytes))
     return Y
 

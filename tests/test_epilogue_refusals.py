@@ -73,8 +73,9 @@ def test_linear(metis):
     assert call(xp=FAKE + 8) == SHAPE and call(wp=FAKE + 8) == SHAPE and call(x=None, xq=(4, 64), codes=FAKE + 8) == SHAPE
     assert call(y=(5, 40, 40, 0)) == SHAPE and call(y=(4, 41, 41, 0)) == SHAPE and call(y=(4, 40, 39, 0)) == SHAPE
     assert call(pre=(4, 41, 41, 0)) == SHAPE and call(pre=(4, 40, 39, 0)) == SHAPE and call(res=(5, 40, 40, 0)) == SHAPE
-    need = L.metis_mxfp4_linear_workspace_bytes(4, 40, 64)
-    assert need >= 4 * 32 + 4 * 2 and call(size=need - 1) == WORKSPACE and call(ws=None) == WORKSPACE and call(ws=FAKE + 16) == INVALID
+    need, many = L.metis_mxfp4_linear_workspace_bytes(20, 40, 64), dict(x=(20, 64, 64, 0), y=(20, 40, 40, 0))
+    assert need >= 20 * 32 + 20 * 2 and call(size=need - 1, **many) == WORKSPACE and call(ws=None, **many) == WORKSPACE
+    assert call(ws=FAKE + 16, **many) == INVALID and L.metis_mxfp4_linear_workspace_bytes(4, 40, 64) == 0
     assert L.metis_mxfp4_linear_workspace_bytes(4, 40, 48) == 0 and L.metis_mxfp4_linear_workspace_bytes(0, 40, 64) == 0
     big = 1 << 28
     assert call(x=(4, 64, 64, 0), w=(big, 64), y=(4, big, big, 0)) == UNSUPPORTED

@@ -111,6 +111,16 @@ def test_linear_of_many_tiles(metis, T, N, K, dtype):
     layer.check(p=0.3, inplace=True, dense=True)
 
 
+@pytest.mark.parametrize("T,N,K", [(16, 40, 32), (13, 33, 96), (16, 300, 512), (16, 1024, 1024), (12, 257, 2080), (13, 257, 2080), (4, 8200, 2080), (8, 8200, 96), (2, 70, 14336),
+                                   (5, 1, 544)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_quantized_on_the_spot(metis, T, N, K, dtype):
+    """Around the rule for it: more waves than runs of the contraction, runs that end inside, one output."""
+    layer = _Layer(metis, T, N, K, dtype, T + K)
+    layer.check(act="gelu", p=0.2, residual=True, pre=True, dense=True, pad=1)
+    layer.check(dense=True, bias=False)
+
+
 def test_plain_product_is_the_gemm_without_an_epilogue(metis):
     """An epilogue of nothing rounds what metis_mxfp4_gemm_nt rounds."""
     for T, N, K in [(300, 520, 512), (4352, 4112, 512), (4096, 4096, 96)]:
