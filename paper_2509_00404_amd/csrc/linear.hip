@@ -214,9 +214,9 @@ struct LinearParts {
     int64_t ld, stride;                           // of the sums
 };
 // Cut where the units that a tile is spared (1.1 us each where the weights come from memory) outweigh the sums, written and read at some 450 outputs a ns,
-// and the joining launch.  us without the quantizer, weights from memory, whole / cut in 2 / 4 / 8: 128 rows of 4096 x 14336 66.8 / 38.9 / 25.3 / 20.5, 256
-// 65.8 / 39.6 / 27.7 / 35.2, 512 64.9 / 41.6 / 50.1; of 14336 x 4096 24.1 / 21.5 / 27.9; of 4096 x 4096 21.8 / 17.1 / 15.8 / 18.5, 256 21.5 / 19.4 / 20.3, 512
-// 21.5 / 22.7; of 1024 x 4096 17.4 / 12.4 / 10.7 / 10.3.
+// and the joining launch.  us without the quantizer, weights from memory, whole / cut in 2 / 4 / 8: 128 rows of 4096 x 14336 65.2 / 38.7 / 24.9 / 20.1, 256
+// 64.2 / 39.2 / 27.3, 512 63.2 / 41.3; 128 of 14336 x 4096 22.3 / 20.7; of 4096 x 4096 21.0 / 16.8 / 15.3 / 18.5, 256 20.6 / 18.9 / 19.9, 512 20.5 / 23.2; of
+// 1024 x 4096 15.7 / 12.3 / 10.6 / 10.3.
 LinearParts linear_parts(int64_t rows, int64_t N, int64_t K) {
     const int64_t tiles = ceil_div64(rows, 128) * ceil_div64(N, 128), units = ceil_div64(K, MX_KI), ld = (N + 7) / 8 * 8;
     LinearParts p = {1, (int)units, ld, (rows * ld + 63) / 64 * 64};
@@ -333,15 +333,15 @@ int launch_few_shape(hipStream_t s, const MxOperand& x, const metis_mat* dense, 
 // dz = act'(pre) m dy, and the sum of its columns.  A lane has eight columns and goes down its rows with the next two on their way; the columns' sums stay in
 // registers.  WIDE: the four waves of a workgroup lie side by side, 2048 columns, else they take neighbouring rows of 512 columns.  Workgroups take
 // turns at the rows, so that what is read at any time lies together: with runs of rows of their own 16384 x 14336 bf16 takes 289 us (gelu) and 277
-// (relu), so 269 and 245.  Memory bounds it: 1.41 GB, 5.3 and 5.8 TB/s.
-template <typename T, int ACT, bool WIDE, bool PAST>
+// (relu), so 269 and 245; BACK: the last unit of a row is short (see load_back; for rows of whole units as well, 265 for 256).  Memory bounds it: 1.41 GB, 5.3 and 5.8 TB/s.
+template <typename T, int ACT, bool WIDE, bool PAST, bool BACK>
 __global__ void __launch_bounds__(256)
 k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64_t ldz, MaskKey mask, int64_t rows, int64_t cols,
                float* __restrict__ sums) {
     __shared__ float s_sum[WIDE ? 1 : 3 * 8 * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t c = (WIDE ? 2048 * (int64_t)blockIdx.x + 512 * wave : 512 * (int64_t)blockIdx.x) + 8 * lane, n = cols - c;
-    const int back = unit_back(c, cols);
+    const int back = BACK ? unit_back(c, cols) : 0;
     const int64_t hop = WIDE ? gridDim.y : 4 * (int64_t)gridDim.y;
     const uint32_t step = mask_step(mask);
     float sum[8];
@@ -351,8 +351,13 @@ k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64
     if (n > 0 && r < rows) {
         RawUnit<T> nd[2], np[2];
         auto fetch = [&](int64_t row, int k) __attribute__((always_inline)) {
-            load_back<PAST>(dy + row * ldd, c, back, cols, nd[k]);
-            if (ACT != METIS_ACT_NONE) load_back<PAST>(pre + row * ldp, c, back, cols, np[k]);
+            if constexpr (BACK) {
+                load_back<PAST>(dy + row * ldd, c, back, cols, nd[k]);
+                if (ACT != METIS_ACT_NONE) load_back<PAST>(pre + row * ldp, c, back, cols, np[k]);
+            } else {
+                load_whole<PAST>(dy + row * ldd + c, nd[k]);
+                if (ACT != METIS_ACT_NONE) load_whole<PAST>(pre + row * ldp + c, np[k]);
+            }
         };
         auto one = [&](int64_t row, int k) __attribute__((always_inline)) {
             float v[8], z[8];
@@ -364,7 +369,7 @@ k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] *= act_slope<sizeof(T) == 2>(ACT, z[i]);
             }
-            if (dz) store_unit<PAST>(dz + row * ldz + c, n, v);
+            if (dz) store_unit<PAST>(dz + row * ldz + c, BACK ? n : 8, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += v[i];
         };
@@ -539,7 +544,9 @@ extern "C" int metis_linear_grads(void* stream, const metis_mat* dY, const metis
                                rows, cols, dbias);
             return;
         }
-        auto kern = grads_wide(cols) ? past ? k_linear_grads<T, ACT, true, true> : k_linear_grads<T, ACT, true, false> : k_linear_grads<T, ACT, false, false>;
+        auto kern = k_linear_grads<T, ACT, false, false, true>;
+        if (grads_wide(cols) && cols % 8) kern = past ? k_linear_grads<T, ACT, true, true, true> : k_linear_grads<T, ACT, true, false, true>;
+        else if (grads_wide(cols)) kern = past ? k_linear_grads<T, ACT, true, true, false> : k_linear_grads<T, ACT, true, false, false>;
         hipLaunchKernelGGL(kern, dim3((unsigned)strips, (unsigned)chunks), dim3(256), 0, s, (const T*)dY->ptr, dY->ld,
                            pre ? (const T*)pre->ptr : nullptr, pre ? pre->ld : 0, dZ ? (T*)dZ->ptr : nullptr, dZ ? dZ->ld : 0, mask_key(mask),
                            rows, cols, sums);
