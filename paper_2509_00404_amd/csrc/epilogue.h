@@ -254,18 +254,24 @@ __device__ __forceinline__ void finish_bias(const MxFinish<T, ACT>& f, int64_t c
 
 // A wave's TM x TN accumulator tiles, transposed (a lane holds runs of four columns of one row), through the epilogue.  32 rows of its columns at
 // a time are staged at sm as fp32 (mx_wave_rows<float, TN> bytes), and a lane takes eight neighbouring columns of some of them: one block of the
-// mask's numbers, and 16 bytes of every bf16 operand.  Tiles inside the matrix have the residual's next 32 rows on their way meanwhile.
+// mask's numbers, and 16 bytes of every bf16 operand.  The residual's next 32 rows are on their way meanwhile.
 // an element near row r0, which is uniform, by a 32-bit offset
 template <typename T>
 __device__ __forceinline__ T* narrow_at(T* p, int64_t ld, int64_t r0, uint32_t low, uint32_t c) {
-    return reinterpret_cast<T*>((uintptr_t)(p + r0 * ld) + (low * (uint32_t)ld + c) * (uint32_t)sizeof(T));      // r0 uniform
+    return in_global(reinterpret_cast<T*>((uintptr_t)(p + r0 * ld) + (low * (uint32_t)ld + c) * (uint32_t)sizeof(T)));
 }
 // What is computed from the epilogue's arguments is computed where it is used: the empty asm hides that they are the same for every tile of a
-// persistent workgroup (kept over its products, the strides' multiples alone took the scalar registers, and vector registers after them).
+// persistent workgroup (kept over its products, the strides' multiples alone took the scalar registers, and vector registers after them).  The pointers are
+// global memory's again behind it: flat instructions took 8192 x 8192 x 1024 in fp32 with a residual 149 us, these 132.
 template <typename T, int ACT>
 __device__ __forceinline__ MxFinish<T, ACT> finish_afresh(MxFinish<T, ACT> f) {
     asm volatile("" : "+s"(f.y), "+s"(f.ldy), "+s"(f.bias), "+s"(f.pre), "+s"(f.ldp), "+s"(f.residual), "+s"(f.ldr));
     asm volatile("" : "+s"(f.mask.seed), "+s"(f.mask.step), "+s"(f.mask.dropped), "+s"(f.mask.keep), "+s"(f.act));
+    f.y = in_global(f.y);
+    f.bias = in_global(f.bias);
+    f.pre = in_global(f.pre);
+    f.residual = in_global(f.residual);
+    f.mask.step = in_global(f.mask.step);
     return f;
 }
 template <bool WHOLE, int TM, int TN, typename T, int ACT>
@@ -293,9 +299,13 @@ __device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], u
         if constexpr (WHOLE) store_row<true>(narrow_at(p, ld, r0, low, (uint32_t)c), v);
         else store_part<T, true>(p + (r0 + low) * ld + c, n, v);
     };
-    fetch(0);
+    // The streamed kernel's fp32 instances (an activation of their own) have no registers for the next 32 rows beside these: 8192 x 8192 x 4096 with a
+    // residual 261 us with them ahead, 231 without.
+    constexpr bool AHEAD = sizeof(T) < 4 || TN < 2 || ACT == ACT_ANY;
+    if (AHEAD) fetch(0);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
+        if (!AHEAD) fetch(i);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -306,7 +316,7 @@ __device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], u
         RawUnit<T> res[S];
 #pragma unroll
         for (int s = 0; s < S; ++s) res[s] = next[s];
-        if (i + 1 < TM) fetch(i + 1);
+        if (AHEAD && i + 1 < TM) fetch(i + 1);
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const int64_t r0 = m0 + 32 * i + ROWS * s;
