@@ -134,6 +134,18 @@ def test_layernorm_grads_near_the_rules(metis, T, D):
     assert np.all(np.abs(_f64(first[2]) - dy64.sum(0)) <= (T + 160) * u * np.abs(dy64).sum(0) + 1e-37)
 
 
+@pytest.mark.parametrize("T,D", [(5, 2057), (1300, 77), (3, 9), (2, 5), (40, 9003)])
+def test_missing_values_stay_in_their_columns(metis, T, D):
+    for at in {max(D - 9, 0), D // 8 * 8 - 1 if D > 8 else 0, D - 1}:
+        x, dy, stats = torch.zeros((T, D), device="cuda"), torch.ones((T, D), device="cuda"), torch.tensor([[-1.0, 1.0]], device="cuda").repeat(T, 1)
+        x[1, at] = float("nan")
+        dw, db, dx = torch.empty(D, device="cuda"), torch.empty(D, device="cuda"), torch.empty_like(x)
+        metis.layernorm_grads(dy, x, stats, dx, None, dw, db)
+        assert torch.isnan(dw).sum() == 1 and torch.isnan(dw[at]) and (dw[torch.arange(D, device="cuda") != at] == T).all() and (db == T).all()
+        rows = torch.isnan(dx).any(1)
+        assert rows.sum() == 1 and rows[1]
+
+
 def test_gradients_are_the_forward_pass_differences(metis):
     """fp32; a step h: results rounded to 2^-23 of magnitudes up to 5, their 30 products with dy summed, over 2 h; and h^2 / 6 of third derivatives of
     rows of unit scale."""

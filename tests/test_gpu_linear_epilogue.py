@@ -230,6 +230,20 @@ def test_gradient_near_the_rule(metis, T, N):
     assert np.all(np.abs(_f64(first[1]) - s.sum(0)) <= (T + 160) * 2.0 ** -24 * np.abs(s).sum(0) + 1e-37)
 
 
+@pytest.mark.parametrize("T,N", [(5, 2057), (800, 2057), (900, 77), (3, 9), (2, 5)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_missing_values_stay_in_their_columns(metis, T, N, dtype):
+    """A row's short last unit is read together with elements of the one before it."""
+    for at in {max(N - 9, 0), N // 8 * 8 - 1 if N > 8 else 0, N - 1}:
+        dy, pre = torch.ones((T, N), dtype=dtype, device="cuda"), torch.zeros((T, N), dtype=dtype, device="cuda")
+        dy[1, at] = float("nan")
+        db = torch.empty(N, device="cuda")
+        dz = metis.linear_grads(dy, torch.empty_like(dy), pre=pre, act="silu", dbias=db)
+        bad = torch.isnan(dz)
+        assert bad.sum() == 1 and bad[1, at] and torch.isnan(db).sum() == 1 and torch.isnan(db[at])
+        assert (dz[~bad] == 0.5).all() and (db[torch.arange(N, device="cuda") != at] == 0.5 * T).all()       # silu'(0) = 1/2, exact sums
+
+
 def test_gradient_is_the_forward_pass_differences(metis):
     """dz against differences of the forward pass itself: fp32, a step of 2^-7 (second-order error 2^-14 / 6 of a third derivative below 2, results
     of magnitude up to 8 rounded to 2^-21, over 2^-6)."""
