@@ -173,6 +173,7 @@ struct MxFinish {
     MaskKey mask;
     int act;
     bool narrow;                                  // rows near each other are within 2^31 bytes
+    bool lines;                                   // rows of y and pre start at whole lines
 };
 // the activation and the mask of S units of eight elements, columns c .. c + 7, row(s)
 template <int S, typename T, int ACT, typename F>
@@ -274,7 +275,7 @@ __device__ __forceinline__ MxFinish<T, ACT> finish_afresh(MxFinish<T, ACT> f) {
     f.mask.step = in_global(f.mask.step);
     return f;
 }
-template <bool WHOLE, int TM, int TN, typename T, int ACT>
+template <bool WHOLE, bool PAST, int TM, int TN, typename T, int ACT>
 __device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T, ACT>& f, int64_t m0, int64_t n0, int64_t M,
                                                int64_t N, int lane) {
     constexpr int LROW = 32 * TN * 4 + 16, UNITS = 4 * TN, ROWS = 64 / UNITS, S = 32 / ROWS;
@@ -296,7 +297,7 @@ __device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], u
         }
     };
     auto store = [&](T* p, int64_t ld, int64_t r0, const float (&v)[8]) __attribute__((always_inline)) {
-        if constexpr (WHOLE) store_row<true>(narrow_at(p, ld, r0, low, (uint32_t)c), v);
+        if constexpr (WHOLE) store_unit<PAST>(narrow_at(p, ld, r0, low, (uint32_t)c), 8, v);
         else store_part<T, true>(p + (r0 + low) * ld + c, n, v);
     };
     // The streamed kernel's fp32 instances (an activation of their own) have no registers for the next 32 rows beside these: 8192 x 8192 x 4096 with a
@@ -338,12 +339,17 @@ __device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], u
         gs_wave_order();
     }
 }
+// The streamed kernel's bf16 outputs, where a row's 64 columns are a whole line, leave past the caches, which keep the operands: 16384 x 14336 x 4096 with gelu
+// and pre 644 us, so 605; 16384 x 4096 x 14336 with a residual 518, so 501.  Parts of lines cost more than they spare: 3000 x 6001 x 1024 39, past the caches 46;
+// fp32 (half a line a store) 8192 x 8192 x 4096 178, 222.  (Not a choice at each store: the branches took half of it back.)
 template <int TM, int TN, typename T, int ACT>
 __device__ __forceinline__ void mx_finish_wave(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T, ACT>& end, int64_t m0, int64_t n0, int64_t M,
                                                int64_t N, int lane) {
     const MxFinish<T, ACT> f = finish_afresh(end);
-    if (f.narrow && m0 + 32 * TM <= M && n0 + 32 * TN <= N) mx_finish_rows<true>(acc, sm, f, m0, n0, M, N, lane);
-    else mx_finish_rows<false>(acc, sm, f, m0, n0, M, N, lane);
+    constexpr bool LINES = sizeof(T) == 2 && ACT != ACT_ANY;
+    if (!f.narrow || m0 + 32 * TM > M || n0 + 32 * TN > N) mx_finish_rows<false, false>(acc, sm, f, m0, n0, M, N, lane);
+    else if (LINES && f.lines) mx_finish_rows<true, LINES>(acc, sm, f, m0, n0, M, N, lane);
+    else mx_finish_rows<true, false>(acc, sm, f, m0, n0, M, N, lane);
 }
 
 }  // namespace

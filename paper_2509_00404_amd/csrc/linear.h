@@ -5,6 +5,7 @@
 namespace {
 
 inline bool near_rows(const metis_mat* m) { return !m || m->ld <= (1 << 24); }          // 16 of them, and their columns, within 2^31 bytes
+inline bool whole_lines(const metis_mat* m) { return !m || ((uintptr_t)m->ptr % 128 == 0 && m->ld * mat_size(m) % 128 == 0); }
 template <typename T, int ACT = ACT_ANY>
 MxFinish<T, ACT> finish_of(const metis_epilogue* e, const metis_mat* Y) {
     return {(T*)Y->ptr,
@@ -16,7 +17,8 @@ MxFinish<T, ACT> finish_of(const metis_epilogue* e, const metis_mat* Y) {
             e && e->residual ? e->residual->ld : 0,
             mask_key(e ? e->mask : nullptr),
             e ? e->act : METIS_ACT_NONE,
-            near_rows(Y) && near_rows(e ? e->pre : nullptr) && near_rows(e ? e->residual : nullptr)};
+            near_rows(Y) && near_rows(e ? e->pre : nullptr) && near_rows(e ? e->residual : nullptr),
+            whole_lines(Y) && whole_lines(e ? e->pre : nullptr)};
 }
 
 }  // namespace
