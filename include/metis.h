@@ -616,10 +616,10 @@ int metis_linear_grads(void* stream, const metis_mat* dY, const metis_mat* pre, 
                        void* workspace, size_t workspace_bytes);
 
 /*
- * Layer norm of the rows of x [rows, cols]: y = (x - mean) rstd weight + bias, mean and variance of the row in fp32 (the variance from the
- * differences), rstd = 1 / sqrt(variance + eps).  weight, bias: device fp32 [cols], each may be null (ones, zeros).  stats: null, or device fp32
- * [rows, 2], 8-byte aligned: mean and rstd, for the backward pass.  x, y: one type (bf16 or fp32), any strides and alignments of elements; y may be x itself.
- * eps >= 0 (with 0, a row of equal elements is NaN).  No rows is no work.
+ * Layer norm of the rows of x [rows, cols]: y = (x - mean) rstd weight + bias, the mean from a sum in 64 bits and to twice fp32's places, the variance from the
+ * differences to it, rstd = 1 / sqrt(variance + eps).  weight, bias: device fp32 [cols], each may be null (ones, zeros).  stats: null, or device fp32
+ * [rows, 2], 8-byte aligned: mean and rstd, rounded, for the backward pass.  x, y: one type (bf16 or fp32), any strides and alignments of elements; y may be x
+ * itself.  eps >= 0: a row of equal elements is its bias, exactly, and NaN with eps = 0.  No rows is no work.
  * Errors: METIS_INVALID_ARG, METIS_BAD_SHAPE, METIS_UNSUPPORTED (more than 2^28 columns or 2^32 - 1 rows).
  */
 int metis_layernorm(void* stream, const metis_mat* x, const float* weight, const float* bias, float eps, metis_mat* y, float* stats);

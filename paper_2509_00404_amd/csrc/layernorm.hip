@@ -27,9 +27,35 @@ __device__ __forceinline__ float wave_sum(float v) {
     for (int i = 0; i < 4; ++i) s += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 16 * i + 15));
     return s;
 }
-// Sums of N values over a row's threads.  slot: LDS of N * WAVES floats, not written again before the workgroup has met once more.
-template <int RT, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float* slot) {
+// the sum of each 16 lanes, the same in all of them
+__device__ __forceinline__ double sixteen_sum(double v) {
+    auto half = [&](uint32_t h, auto ctrl) __attribute__((always_inline)) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)h, decltype(ctrl)::value, 0xF, 0xF, true);
+    };
+    auto add = [&](auto ctrl) __attribute__((always_inline)) {
+        const uint64_t w = __builtin_bit_cast(uint64_t, v);
+        v += __builtin_bit_cast(double, (uint64_t)half((uint32_t)(w >> 32), ctrl) << 32 | half((uint32_t)w, ctrl));
+    };
+    add(std::integral_constant<int, 0xB1>{});
+    add(std::integral_constant<int, 0x4E>{});
+    add(std::integral_constant<int, 0x141>{});
+    add(std::integral_constant<int, 0x140>{});
+    return v;
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, sixteen_sum(v));
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)w, 16 * i + 15);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(w >> 32), 16 * i + 15);
+        s += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    }
+    return s;
+}
+// Sums of N values over a row's threads.  slot: LDS of N * WAVES values, not written again before the workgroup has met once more.
+template <int RT, int N, typename V>
+__device__ __forceinline__ void row_sums(V (&v)[N], V* slot) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
     if constexpr (RT > 64) {
@@ -42,12 +68,59 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* slot) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float s = 0.0f;
+            if constexpr (W == 16 && sizeof(V) == 8) {                // (sixteen reads and additions one behind the other take longer)
+                v[i] = sixteen_sum(slot[i * W + (threadIdx.x & 15)]);
+                continue;
+            }
+            V s = 0;
 #pragma unroll
             for (int w = 0; w < W; ++w) s += slot[i * W + w];
             v[i] = s;
         }
     }
+}
+// A row's mean, from a sum in 64 bits, as two fp32 numbers: elements near each other keep all of their differences to it, however far from zero they are.  A row of
+// equal elements has that element as its mean, and no lower part: the sum is exact, and the quotient is once it is corrected.  variance: from the sum of
+// (v - hi)^2, of whose mean lo^2 is at most half.
+struct RowLength {
+    double n, inverse;
+    __device__ __forceinline__ RowLength(int64_t cols) : n((double)cols), inverse(1.0 / n) {}
+};
+struct RowMean {
+    float hi, lo;
+    __device__ __forceinline__ RowMean(double sum, const RowLength& row) {
+        const double near = sum * row.inverse, mean = fma(fma(-near, row.n, sum), row.inverse, near);
+        hi = (float)(mean == mean ? mean : near);                     // (infinite sums)
+        lo = (float)(mean - (double)hi);
+    }
+    __device__ __forceinline__ float variance(double squares, const RowLength& row) const { return fmaf(-lo, lo, (float)(squares * row.inverse)); }
+};
+// The sum of a unit's elements.  bf16: in fp32, which loses nothing unless they are more than 2^13 times apart (8 bits each), and is then off by
+// 2^-24 of the largest; an eighth of it, which is in fp32's range where they are.
+template <typename T>
+__device__ __forceinline__ double unit_sum(const float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        float s = v[0] * 0.125f;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s = fmaf(v[i], 0.125f, s);
+        return 8.0 * s;
+    } else {
+        double s = v[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s += v[i];
+        return s;
+    }
+}
+__device__ __forceinline__ float unit_squares(const float (&v)[8]) {
+    float s = v[0] * v[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s = fmaf(v[i], v[i], s);
+    return s;
+}
+// v, zeros in place of the first `twice`
+__device__ __forceinline__ void unit_own(const float (&v)[8], int twice, float (&own)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) own[i] = i >= twice ? v[i] : 0.0f;
 }
 // Nothing is on its way into a loop from before it: what the loop waits for is then counted from its own loads and stores alone.
 __device__ __forceinline__ void loads_arrived() { __builtin_amdgcn_s_waitcnt(0xF70); }     // vmcnt(0)
@@ -69,17 +142,19 @@ __device__ __forceinline__ void load_factors(const float* p, float none, float (
     }
 }
 
-// Two passes over what the registers hold, mean first, so that a mean far from zero costs the variance nothing.  Memory bounds it: 16384 x 4096 bf16
-// (268 MB) takes 43.6 us, 6.2 TB/s (part of the rows is still in the last-level cache).
+// Two passes over what the registers hold, mean first (RowMean), so that a mean far from zero costs neither the variance nor the results anything.
+// Memory bounds it: 16384 x 4096 bf16 (268 MB) takes 43.6 us, 6.2 TB/s (part of the rows is still in the last-level cache).
 template <typename T, int RT, int U>
 __global__ void __launch_bounds__(RowGroup<RT>::THREADS)
 k_layernorm(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
             float2* __restrict__ stats, int64_t rows, int64_t cols) {
     typedef RowGroup<RT> G;
-    __shared__ float s_mean[G::WAVES], s_var[G::WAVES];
+    __shared__ double s_mean[G::WAVES];
+    __shared__ float s_var[G::WAVES];
     const int t = RT == 64 ? (int)threadIdx.x & 63 : (int)threadIdx.x;
     const int own = RT == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
-    const float n = (float)cols;
+    const RowLength length(cols);
+    const bool units = cols % 8 == 0;                            // (nothing is held twice but whole units: no element is looked at)
     float w[U][8], b[U][8];
     UnitPlace at[U];
     RawUnit<T> next[U];
@@ -95,71 +170,74 @@ k_layernorm(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __restrict_
     loads_arrived();
     for (; r < rows; r += hop) {
         float v[U][8], sum[1] = {0.0f};
+        double whole[1] = {0.0};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             unpack(next[u], v[u]);
             load_whole(x + (r + hop < rows ? r + hop : r) * ldx + at[u].c, next[u]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[0] += i >= at[u].twice ? v[u][i] : 0.0f;
+            float own[8];
+            if (!units) unit_own(v[u], at[u].twice, own);
+            const double s = units ? unit_sum<T>(v[u]) : unit_sum<T>(own);
+            whole[0] += at[u].twice < 8 ? s : 0.0;
         }
-        row_sums<RT>(sum, s_mean);
-        const float mean = sum[0] / n;
-        sum[0] = 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[u][i] -= mean;
-                sum[0] = i >= at[u].twice ? fmaf(v[u][i], v[u][i], sum[0]) : sum[0];
-            }
-        row_sums<RT>(sum, s_var);
-        const float rstd = 1.0f / sqrtf(sum[0] / n + eps);
-        if (stats && t == 0) stats[r] = make_float2(mean, rstd);
+        row_sums<RT>(whole, s_mean);
+        const RowMean mean(whole[0], length);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = fmaf(v[u][i] * rstd, w[u][i], b[u][i]);
+            for (int i = 0; i < 8; ++i) v[u][i] -= mean.hi;
+            float own[8];
+            if (!units) unit_own(v[u], at[u].twice, own);
+            const float s = units ? unit_squares(v[u]) : unit_squares(own);
+            sum[0] += at[u].twice < 8 ? s : 0.0f;
+        }
+        row_sums<RT>(sum, s_var);
+        const float rstd = 1.0f / sqrtf(mean.variance(sum[0], length) + eps), low = -mean.lo * rstd;
+        if (stats && t == 0) stats[r] = make_float2(mean.hi, rstd);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = fmaf(fmaf(v[u][i], rstd, low), w[u][i], b[u][i]);
             store_row<true>(y + r * ldy + at[u].c, v[u]);
         }
     }
 }
 
-// Rows longer than what registers hold: three passes over the row, which stays in the caches.
+// Rows longer than what registers hold: three passes over the row, which stays in the caches.  Sums in 64 bits: a thread has up to 2^18 of their terms.
 template <typename T>
 __global__ void __launch_bounds__(1024)
 k_layernorm_long(const T* x, int64_t ldx, T* y, int64_t ldy, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
                  float2* __restrict__ stats, int64_t rows, int64_t cols) {
-    __shared__ float s_mean[16], s_var[16];
-    const float n = (float)cols;
+    __shared__ double s_mean[16], s_var[16];
+    const RowLength length(cols);
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        float sum[1] = {0.0f}, v[8];
+        double sum[1] = {0.0};
+        float v[8];
         auto each = [&](auto f) __attribute__((always_inline)) {
             for (int64_t c = 8 * (int64_t)threadIdx.x; c < cols; c += 8192) {
                 load_unit(x + r * ldx + c, cols - c, v);
                 f(c);
             }
         };
-        each([&](int64_t) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[0] += v[i];
-        });
+        each([&](int64_t) { sum[0] += unit_sum<T>(v); });
         row_sums<1024>(sum, s_mean);
-        const float mean = sum[0] / n;
-        sum[0] = 0.0f;
+        const RowMean mean(sum[0], length);
+        sum[0] = 0.0;
         each([&](int64_t c) {
+            float d[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c + i < cols) sum[0] = fmaf(v[i] - mean, v[i] - mean, sum[0]);
+            for (int i = 0; i < 8; ++i) d[i] = c + i < cols ? v[i] - mean.hi : 0.0f;
+            sum[0] += unit_squares(d);
         });
         row_sums<1024>(sum, s_var);
-        const float rstd = 1.0f / sqrtf(sum[0] / n + eps);
-        if (stats && threadIdx.x == 0) stats[r] = make_float2(mean, rstd);
+        const float rstd = 1.0f / sqrtf(mean.variance(sum[0], length) + eps), low = -mean.lo * rstd;
+        if (stats && threadIdx.x == 0) stats[r] = make_float2(mean.hi, rstd);
         each([&](int64_t c) {
             float w[8] = {1, 1, 1, 1, 1, 1, 1, 1}, b[8] = {};
             if (weight) load_unit(weight + c, cols - c, w);
             if (bias) load_unit(bias + c, cols - c, b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - mean) * rstd, w[i], b[i]);
+            for (int i = 0; i < 8; ++i) v[i] = fmaf(fmaf(v[i] - mean.hi, rstd, low), w[i], b[i]);
             store_part<T, true>(y + r * ldy + c, cols - c, v);
         });
     }
