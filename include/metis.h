@@ -603,7 +603,8 @@ int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_mxfp4* Xq, 
 
 /*
  * Gradient of that epilogue: dZ = act'(pre) m dY, of what the activation is applied to, and dbias (device fp32 [cols]) = the sum of dZ's rows,
- * of its values before they are rounded, in an order that depends on shape and type alone.  (The residual's gradient is dY itself.)  relu' (0) = 0.
+ * of its values before they are rounded, in an order that depends on shape and type alone.  (The residual's gradient is dY itself.)  relu' (0) = 0.  A dropped element's is 0 whatever dY and
+ * `pre` hold in its place.
  *   pre        as the forward pass left it; not looked at for METIS_ACT_NONE
  *   mask       the forward pass's, or null
  *   dZ, dbias  either may be null; dZ may be dY or pre itself

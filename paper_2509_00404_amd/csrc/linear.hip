@@ -364,11 +364,12 @@ k_linear_grads(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, int64
             unpack(nd[k], back, v);
             if (ACT != METIS_ACT_NONE) unpack(np[k], back, z);
             fetch(row + 2 * hop < rows ? row + 2 * hop : row, k);
-            if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)row, v);
             if (ACT != METIS_ACT_NONE) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] *= act_slope<sizeof(T) == 2>(ACT, z[i]);
             }
+            // (the mask last: a dropped element is 0 whatever its slope is)
+            if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)row, v);
             if (dz) store_unit<PAST>(dz + row * ldz + c, BACK ? n : 8, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += v[i];
@@ -425,11 +426,12 @@ k_linear_grads_few(const T* dy, int64_t ldd, const T* pre, int64_t ldp, T* dz, i
             unpack(nd, back, v);
             if (ACT != METIS_ACT_NONE) unpack(np, back, z);
             fetch(r + STEP < rows ? r + STEP : r);
-            if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)r, v);
             if (ACT != METIS_ACT_NONE) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] *= act_slope<sizeof(T) == 2>(ACT, z[i]);
             }
+            // (the mask last: a dropped element is 0 whatever its slope is)
+            if (mask.dropped) mask_apply(mask, step, (uint32_t)(c >> 3), (uint32_t)r, v);
             if (dz) store_part<T, true>(dz + r * ldz + c, n, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += v[i];
