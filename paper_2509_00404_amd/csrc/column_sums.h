@@ -5,13 +5,13 @@
 
 namespace {
 
-// out[c] = sum over p of P[p, c] (parts rows of n).  Columns from `split` on go to `out2`.  A workgroup has 64 columns, its sixteen waves every
-// sixteenth part.
+// out[c] = sum over p of P[p, c] (parts rows of n), c from `first` on.  Columns from `split` on go to `out2`.  A workgroup has 64 columns, its sixteen waves
+// every sixteenth part.
 __global__ void __launch_bounds__(1024)
-k_join_sums(const float* __restrict__ P, int64_t parts, int64_t n, float* __restrict__ out, int64_t split, float* __restrict__ out2) {
+k_join_sums(const float* __restrict__ P, int64_t parts, int64_t n, float* __restrict__ out, int64_t split, float* __restrict__ out2, int64_t first) {
     __shared__ float s_sum[16 * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = 64 * (int64_t)blockIdx.x + lane;
+    const int64_t c = first + 64 * (int64_t)blockIdx.x + lane;
     float sum = 0.0f;
     if (c < n) {
 #pragma unroll 8
@@ -61,8 +61,13 @@ __device__ __forceinline__ uint32_t xcd_strip(uint32_t block, uint32_t strips) {
 }
 
 int launch_join(hipStream_t s, const float* P, int64_t parts, int64_t n, float* out, int64_t split, float* out2) {
-    hipLaunchKernelGGL(k_join_sums, dim3((unsigned)ceil_div64(n, 64)), dim3(1024), 0, s, P, parts, n, out, split, out2);
-    METIS_LAUNCH_CHECK();
+    // (1024 threads for 64 columns: from 2^28 columns on, or 2^27 with two sums each, a launch of them all would have 2^32)
+    const int64_t most = 1ll << 27;
+    for (int64_t first = 0; first < n; first += most) {
+        const int64_t columns = n - first < most ? n - first : most;
+        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)ceil_div64(columns, 64)), dim3(1024), 0, s, P, parts, n, out, split, out2, first);
+        METIS_LAUNCH_CHECK();
+    }
     return METIS_OK;
 }
 int launch_clear(hipStream_t s, float* p, int64_t n) {

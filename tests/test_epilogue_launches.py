@@ -1,0 +1,114 @@
+"""What the calls around the products ask of the HIP runtime, without a GPU (the library runs behind the stand-in of test_launches; addresses are never
+read): launches that fail are reported by the call that made them, and the largest sizes stay below 2^32 threads along an axis of a grid, which is what HIP
+takes."""
+import ctypes as C
+import os
+import shutil
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+FAKE, OTHER = 1 << 30, 1 << 60
+COUNT = "    if (++launches == failing) error = 1;\n"
+NOTE = """
+    unsigned long long gs[3] = {g.x, g.y, g.z}, bs[3] = {b.x, b.y, b.z};
+    for (int i = 0; i < 3; ++i) if (gs[i] * bs[i] > widest) widest = gs[i] * bs[i];
+"""
+
+
+class _Calls:
+    def __init__(self, metis):
+        self.m, self.L, self.keep = metis, metis.lib(), []
+
+    def ref(self, x):
+        self.keep.append(x)
+        return C.byref(x)
+
+    def mat(self, rows, cols, dtype=0, at=FAKE):
+        return self.ref(self.m.Mat(at, rows, cols, cols, dtype))
+
+    def linear(self, T, N, K, dense=True, workspace=FAKE, out=0):
+        x, q = (self.mat(T, K), None) if dense else (None, self.ref(self.m.MxFp4(FAKE, FAKE, T, K)))
+        return self.L.metis_mxfp4_linear(None, x, q, self.ref(self.m.MxFp4(FAKE, FAKE, N, K)), None, self.mat(T, N, out, OTHER), workspace, 1 << 60 if workspace else 0)
+
+    def layernorm(self, T, N):
+        return self.L.metis_layernorm(None, self.mat(T, N), None, None, 1e-5, self.mat(T, N), FAKE)
+
+    def layernorm_grads(self, T, N, at=OTHER):
+        return self.L.metis_layernorm_grads(None, self.mat(T, N), self.mat(T, N), FAKE, None, None, self.mat(T, N, 0, at), FAKE, FAKE, FAKE, 1 << 60)
+
+    def linear_grads(self, T, N):
+        return self.L.metis_linear_grads(None, self.mat(T, N), self.mat(T, N), 2, None, self.mat(T, N), FAKE, FAKE, 1 << 60)
+
+    def dropout(self, T, N):
+        return self.L.metis_dropout(None, self.mat(T, N), self.ref(self.m.Mask(0.1, 1, None)), None, self.mat(T, N))
+
+
+def _failed(stub, c):
+    for name, call, launches in [
+        ("one token", lambda: c.linear(1, 14336, 4096), 1), ("few rows", lambda: c.linear(24, 4096, 14336), 2),
+        ("few rows, quantized", lambda: c.linear(24, 4096, 14336, False), 1), ("few tiles", lambda: c.linear(1111, 2057, 2080), 2),
+        ("parts", lambda: c.linear(128, 4096, 14336), 3), ("parts, quantized, no workspace", lambda: c.linear(128, 4096, 14336, False, None), 1),
+        ("many tiles", lambda: c.linear(4096, 4096, 1024, False), 1), ("streamed", lambda: c.linear(16384, 4096, 14336, False, None, 1), 1),
+        ("layer norm", lambda: c.layernorm(16384, 4096), 1), ("layer norm, long rows", lambda: c.layernorm(4, 40000), 1),
+        ("its gradients", lambda: c.layernorm_grads(16384, 4096), 2), ("its gradients, few rows", lambda: c.layernorm_grads(64, 4096), 1),
+        ("its gradients, few rows in their place", lambda: c.layernorm_grads(64, 4096, FAKE), 2),
+        ("its gradients, long rows", lambda: c.layernorm_grads(64, 40000), 3), ("the epilogue's gradient", lambda: c.linear_grads(16384, 14336), 2),
+        ("the epilogue's gradient, few rows", lambda: c.linear_grads(64, 14336), 1), ("dropout", lambda: c.dropout(333, 1027), 1),
+    ]:
+        stub.fail_at(0)
+        assert call() == 0, name
+        assert stub.launch_count() == launches, (name, stub.launch_count())
+        for i in range(1, launches + 1):
+            stub.fail_at(i)
+            status = call()
+            assert status == -4, f"{name}: launch {i} of {launches} failed, status {status}"
+
+
+def _largest(stub, c):
+    widest = C.c_ulonglong.in_dll(stub, "widest")
+    wide, tall = 1 << 28, (1 << 32) - 1
+    for name, call in [
+        ("layer norm, columns", lambda: c.layernorm(4, wide)), ("layer norm, rows", lambda: c.layernorm(tall, 8)),
+        ("its gradients, 2^27 columns", lambda: c.layernorm_grads(4, wide // 2)), ("its gradients, columns", lambda: c.layernorm_grads(4, wide)),
+        ("its gradients, many rows of them", lambda: c.layernorm_grads(5000, wide)), ("its gradients, rows", lambda: c.layernorm_grads(tall, 8)),
+        ("its gradients, rows of one", lambda: c.layernorm_grads(tall, 1)),
+        ("the epilogue's gradient, columns", lambda: c.linear_grads(4, wide)), ("the epilogue's gradient, rows", lambda: c.linear_grads(tall, 8)),
+        ("dropout, columns", lambda: c.dropout(15, wide)), ("dropout, rows", lambda: c.dropout(tall // 256 * 256, 8)),
+        ("no rows", lambda: c.layernorm_grads(0, wide)), ("product, outputs", lambda: c.linear(1, wide - 1, 32)), ("product, few rows", lambda: c.linear(64, wide - 1, 32)),
+        ("product, long contraction", lambda: c.linear(64, 1, 1 << 26)),
+    ]:
+        widest.value = 0
+        stub.fail_at(0)
+        status = call()
+        assert status == 0 and stub.launch_count() > 0, (name, status)
+        assert widest.value < 2 ** 32, (name, widest.value)
+
+
+@pytest.mark.parametrize("check", ["failed", "largest"])
+def test_behind_a_stand_in_for_the_runtime(tmp_path, check):
+    from paper_2509_00404_amd import metis
+    from test_launches import RUNTIME
+    if not os.path.exists(metis.LIB_PATH) or not shutil.which("gcc"):
+        pytest.skip("library not built, or no C compiler")
+    assert RUNTIME.count(COUNT) == 1
+    text = "unsigned long long widest;\n" + RUNTIME.replace(COUNT, NOTE + COUNT)
+    src, runtime = tmp_path / "runtime.c", tmp_path / "runtime.so"
+    src.write_text(text)
+    subprocess.run(["gcc", "-shared", "-fPIC", "-o", str(runtime), str(src)], check=True)
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), check, str(runtime)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+def _child(check, runtime):
+    stub = C.CDLL(runtime, mode=C.RTLD_GLOBAL)
+    sys.path.insert(0, ROOT)
+    from paper_2509_00404_amd import metis
+    {"failed": _failed, "largest": _largest}[check](stub, _Calls(metis))
+
+
+if __name__ == "__main__":
+    _child(*sys.argv[1:])
