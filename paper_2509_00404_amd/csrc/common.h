@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <mutex>
 #include "../../include/metis.h"
 
 #define METIS_WAVE 64
@@ -49,15 +50,19 @@ __device__ __forceinline__ bf16_t f32_to_bf16_rne(float f) {
 }
 
 // Raising a kernel's dynamic LDS limit is a driver call of tens of microseconds: remember, per device, the largest
-// value already set for that kernel (one zero-initialised cache per call site).  Races only repeat the call.
-struct LdsLimitCache { int bytes[16]; };
+// value already set for that kernel (one zero-initialised cache per kernel, at its one call site).  Look, set and note
+// are one step: between two threads' calls a smaller limit would otherwise be set behind a larger one that is noted.
+struct LdsLimitCache { int bytes[64]; };
+inline std::mutex g_lds_limits;
 static inline bool ensure_dyn_lds(const void* fn, size_t bytes, LdsLimitCache& c) {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return false;
-    const bool slot = dev >= 0 && dev < 16;
+    const bool slot = dev >= 0 && dev < 64;
+    if (slot && __atomic_load_n(&c.bytes[dev], __ATOMIC_ACQUIRE) >= (int)bytes) return true;
+    std::lock_guard<std::mutex> lock(g_lds_limits);
     if (slot && c.bytes[dev] >= (int)bytes) return true;
     if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return false;
-    if (slot) c.bytes[dev] = (int)bytes;
+    if (slot) __atomic_store_n(&c.bytes[dev], (int)bytes, __ATOMIC_RELEASE);
     return true;
 }
 

@@ -1,11 +1,12 @@
 """What the calls around the products ask of the HIP runtime, without a GPU (the library runs behind the stand-in of test_launches; addresses are never
-read): launches that fail are reported by the call that made them, and the largest sizes stay below 2^32 threads along an axis of a grid, which is what HIP
-takes."""
+read): launches that fail are reported by the call that made them, the largest sizes stay below 2^32 threads along an axis of a grid, which is what HIP
+takes, and a kernel's limit of dynamic LDS is never left below what a call needs, whichever threads call at once."""
 import ctypes as C
 import os
 import shutil
 import subprocess
 import sys
+import threading
 
 import pytest
 
@@ -17,6 +18,34 @@ NOTE = """
     unsigned long long gs[3] = {g.x, g.y, g.z}, bs[3] = {b.x, b.y, b.z};
     for (int i = 0; i < 3; ++i) if (gs[i] * bs[i] > widest) widest = gs[i] * bs[i];
 """
+# A limit above 64 KB is set by a call that lets others overtake it: it returns once another has set one, or after a second without.
+SET = "int hipFuncSetAttribute(const void* f, int a, int v) { return 0; }\n"
+LIMITS = """
+#include <unistd.h>
+static const void* fns[64];
+static int limits[64], fn_count;
+static volatile int turns, waiting, exceeded;
+static int slot(const void* f) {
+    for (int i = 0; i < fn_count; ++i) if (fns[i] == f) return i;
+    fns[fn_count] = f;
+    limits[fn_count] = 65536;
+    return fn_count++;
+}
+int is_waiting(void) { return waiting; }
+int exceeded_count(void) { return exceeded; }
+int hipFuncSetAttribute(const void* f, int a, int v) {
+    limits[slot(f)] = v;
+    const int mine = ++turns;
+    if (v > 65536) {
+        waiting = 1;
+        for (int i = 0; i < 100 && turns == mine; ++i) usleep(10000);
+        usleep(20000);
+        waiting = 0;
+    }
+    return 0;
+}
+"""
+CHECK = "    if (l > (size_t)limits[slot(f)]) { ++exceeded; error = 1; }\n"
 
 
 class _Calls:
@@ -88,14 +117,31 @@ def _largest(stub, c):
         assert widest.value < 2 ** 32, (name, widest.value)
 
 
-@pytest.mark.parametrize("check", ["failed", "largest"])
+def _threads(stub, c):
+    """64 rows quantized already: of one kernel instance, K = 4096 takes 8 waves and 73 728 bytes of LDS, 3584 seven and 64 512."""
+    status = []
+    large, small = (lambda: status.append(c.linear(64, 8192, 4096, False))), (lambda: status.append(c.linear(64, 8192, 3584, False)))
+    threads = [threading.Thread(target=large), threading.Thread(target=small)]
+    threads[0].start()
+    while threads[0].is_alive() and not stub.is_waiting():
+        pass
+    assert stub.is_waiting()                             # the larger limit is set, and not noted yet
+    threads[1].start()
+    for t in threads:
+        t.join()
+    large()
+    assert status == [0, 0, 0] and stub.exceeded_count() == 0, (status, stub.exceeded_count())
+
+
+@pytest.mark.parametrize("check", ["failed", "largest", "threads"])
 def test_behind_a_stand_in_for_the_runtime(tmp_path, check):
     from paper_2509_00404_amd import metis
     from test_launches import RUNTIME
     if not os.path.exists(metis.LIB_PATH) or not shutil.which("gcc"):
         pytest.skip("library not built, or no C compiler")
-    assert RUNTIME.count(COUNT) == 1
-    text = "unsigned long long widest;\n" + RUNTIME.replace(COUNT, NOTE + COUNT)
+    assert RUNTIME.count(COUNT) == 1 and RUNTIME.count(SET) == 1
+    text = RUNTIME.replace(COUNT, NOTE + COUNT)
+    text = "#include <stddef.h>\nunsigned long long widest;\n" + LIMITS + text.replace(SET, "").replace(COUNT, COUNT + CHECK)
     src, runtime = tmp_path / "runtime.c", tmp_path / "runtime.so"
     src.write_text(text)
     subprocess.run(["gcc", "-shared", "-fPIC", "-o", str(runtime), str(src)], check=True)
@@ -107,7 +153,7 @@ def _child(check, runtime):
     stub = C.CDLL(runtime, mode=C.RTLD_GLOBAL)
     sys.path.insert(0, ROOT)
     from paper_2509_00404_amd import metis
-    {"failed": _failed, "largest": _largest}[check](stub, _Calls(metis))
+    {"failed": _failed, "largest": _largest, "threads": _threads}[check](stub, _Calls(metis))
 
 
 if __name__ == "__main__":
