@@ -97,18 +97,24 @@ __device__ __forceinline__ void store_part(T* p, int64_t n, const float (&v)[8])
 template <typename T> struct RawUnit;
 template <> struct RawUnit<bf16_t> { ew_u4 w; };
 template <> struct RawUnit<float> { ew_f4 w[2]; };
-// PAST: past the caches, for what is read or written once and is larger than they are
-template <bool PAST, typename V>
-__device__ __forceinline__ V load_vector(const V* p) {
-    if constexpr (PAST) return __builtin_nontemporal_load(p);
-    else return *p;
+// PAST: past the caches, for what is read or written once and is larger than they are.  (Each load names its vector's type: a template's parameter deduced
+// from it would lose the alignment that it lacks.)
+template <bool PAST = false>
+__device__ __forceinline__ void load_whole(const bf16_t* p, RawUnit<bf16_t>& r) {
+    const ew_u4_any* at = reinterpret_cast<const ew_u4_any*>(p);
+    if constexpr (PAST) r.w = __builtin_nontemporal_load(at);
+    else r.w = *at;
 }
 template <bool PAST = false>
-__device__ __forceinline__ void load_whole(const bf16_t* p, RawUnit<bf16_t>& r) { r.w = load_vector<PAST>(reinterpret_cast<const ew_u4_any*>(p)); }
-template <bool PAST = false>
 __device__ __forceinline__ void load_whole(const float* p, RawUnit<float>& r) {
-    r.w[0] = load_vector<PAST>(reinterpret_cast<const ew_f4_any*>(p));
-    r.w[1] = load_vector<PAST>(reinterpret_cast<const ew_f4_any*>(p) + 1);
+    const ew_f4_any* at = reinterpret_cast<const ew_f4_any*>(p);
+    if constexpr (PAST) {
+        r.w[0] = __builtin_nontemporal_load(at);
+        r.w[1] = __builtin_nontemporal_load(at + 1);
+    } else {
+        r.w[0] = at[0];
+        r.w[1] = at[1];
+    }
 }
 template <bool PAST = false>
 __device__ __forceinline__ void load_raw(const bf16_t* p, int64_t n, RawUnit<bf16_t>& r) {
