@@ -581,6 +581,8 @@ int metis_dropout(void* stream, const metis_mat* x, const metis_dropout_mask* ma
  *   e          null: no epilogue.  bias: device fp32 [N], or null.  act: see below.  pre: null, or an output of Y's shape and type: Q(X) W^T + bias,
  *              rounded (the activation is applied to what is not rounded yet).  mask: null, or a dropout.  residual: null, or a matrix of Y's
  *              shape and type, which may be Y itself; Y, pre and residual must not overlap otherwise.
+ *              Neither Y nor pre may overlap W, Xq or the bias.  Either may overlap X where the workspace's size is not 0: X is then quantized before the first
+ *              output; where it is 0, such calls are refused (METIS_INVALID_ARG).
  *   workspace  with X: metis_mxfp4_linear_workspace_bytes bytes, 256-byte aligned (may be null where that is 0); with Xq, that many let a product of
  *              more than 64 rows and few outputs run faster (a call without is right too).  Calls that may run at the same time have workspaces of
  *              their own.

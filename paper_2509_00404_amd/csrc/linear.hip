@@ -456,6 +456,17 @@ int64_t grads_parts(int64_t rows, int64_t cols) {
     return want < few ? want : few;
 }
 
+// whether two matrices of few rows have memory in common
+bool share_memory(const metis_mat* a, const metis_mat* b) {
+    auto row = [](const metis_mat* m, int64_t i) { return (uintptr_t)m->ptr + (uintptr_t)(i * m->ld * mat_size(m)); };
+    auto meet = [](uintptr_t p, int64_t n, uintptr_t q, int64_t k) { return p < q + (uintptr_t)k && q < p + (uintptr_t)n; };
+    const int64_t na = a->cols * mat_size(a), nb = b->cols * mat_size(b);
+    if (!meet(row(a, 0), (int64_t)(row(a, a->rows - 1) - row(a, 0)) + na, row(b, 0), (int64_t)(row(b, b->rows - 1) - row(b, 0)) + nb)) return false;
+    for (int64_t i = 0; i < a->rows; ++i)
+        for (int64_t j = 0; j < b->rows; ++j)
+            if (meet(row(a, i), na, row(b, j), nb)) return true;
+    return false;
+}
 bool same_layout(const metis_mat* a, const metis_mat* b) { return a->rows == b->rows && a->cols == b->cols && a->ld >= a->cols; }
 
 }  // namespace
@@ -486,6 +497,8 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
     if (X) {
         if (rows * (K / 2) > 0xFFFFFFFFll) return METIS_UNSUPPORTED;
     }
+    // (workgroups that are done store outputs while others still quantize X)
+    if (fused && (share_memory(X, Y) || (e && e->pre && share_memory(X, e->pre)))) return METIS_INVALID_ARG;
     if (X && !fused) {
         if (!workspace || workspace_bytes < place.bytes) return METIS_WORKSPACE_TOO_SMALL;
         if ((uintptr_t)workspace % 256) return METIS_INVALID_ARG;

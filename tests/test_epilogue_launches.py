@@ -1,6 +1,6 @@
 """What the calls around the products ask of the HIP runtime, without a GPU (the library runs behind the stand-in of test_launches; addresses are never
 read): launches that fail are reported by the call that made them, the largest sizes stay below 2^32 threads along an axis of a grid, which is what HIP
-takes, and a kernel's limit of dynamic LDS is never left below what a call needs, whichever threads call at once."""
+takes, outputs over rows that are still read are refused, and a kernel's limit of dynamic LDS is never left below what a call needs, whichever threads call at once."""
 import ctypes as C
 import os
 import shutil
@@ -117,6 +117,30 @@ def _largest(stub, c):
         assert widest.value < 2 ** 32, (name, widest.value)
 
 
+def _in_place(stub, c):
+    """Outputs over X: refused, with nothing launched, where X is quantized on the spot; any memory between its rows is free."""
+    m, L, INVALID = c.m, c.L, -1
+
+    def call(T=4, N=64, K=64, x=(FAKE, 64), y=(OTHER, 64), pre=None, dtype=0, out=0):
+        e = c.ref(m.Epilogue(None, 0, C.pointer(m.Mat(pre[0], T, N, pre[1], out)) if pre else None, None, None))
+        stub.fail_at(0)
+        status = L.metis_mxfp4_linear(None, c.ref(m.Mat(x[0], T, K, x[1], dtype)), None, c.ref(m.MxFp4(OTHER, OTHER, N, K)), e,
+                                      c.ref(m.Mat(y[0], T, N, y[1], out)), FAKE, 1 << 40)
+        assert (status == 0) == (stub.launch_count() > 0)
+        return status
+
+    assert L.metis_mxfp4_linear_workspace_bytes(4, 64, 64) == 0 and L.metis_mxfp4_linear_workspace_bytes(16, 64, 64) == 0
+    assert call() == 0 and call(y=(FAKE, 64)) == INVALID and call(pre=(FAKE, 64)) == INVALID and call(pre=(OTHER, 64)) == 0
+    assert call(y=(FAKE + 3 * 128 + 126, 64)) == INVALID and call(y=(FAKE + 4 * 128, 64)) == 0          # the last element; right behind it
+    assert call(y=(FAKE - 4 * 128 + 2, 64)) == INVALID and call(y=(FAKE - 4 * 128, 64)) == 0
+    wide = (FAKE, 128)
+    assert call(x=wide, y=(FAKE + 128, 128)) == 0 and call(x=wide, y=(FAKE + 126, 128)) == INVALID      # columns beside X's in one buffer
+    assert call(x=wide, y=(FAKE + 128, 128), pre=(FAKE + 2, 128)) == INVALID
+    assert call(T=3, x=(FAKE, 128), y=(FAKE + 128, 192)) == INVALID and call(T=2, x=(FAKE, 128), y=(FAKE + 128, 192)) == 0
+    assert call(T=1, y=(FAKE + 64, 64), dtype=1, out=1) == INVALID and call(T=16, y=(FAKE, 64)) == INVALID and call(T=16, x=wide, y=(FAKE + 128, 128)) == 0
+    assert L.metis_mxfp4_linear_workspace_bytes(17, 64, 64) > 0 and call(T=17, y=(FAKE, 64)) == 0 and call(T=17, pre=(FAKE, 64)) == 0
+
+
 def _threads(stub, c):
     """64 rows quantized already: of one kernel instance, K = 4096 takes 8 waves and 73 728 bytes of LDS, 3584 seven and 64 512."""
     status = []
@@ -133,7 +157,7 @@ def _threads(stub, c):
     assert status == [0, 0, 0] and stub.exceeded_count() == 0, (status, stub.exceeded_count())
 
 
-@pytest.mark.parametrize("check", ["failed", "largest", "threads"])
+@pytest.mark.parametrize("check", ["failed", "largest", "in_place", "threads"])
 def test_behind_a_stand_in_for_the_runtime(tmp_path, check):
     from paper_2509_00404_amd import metis
     from test_launches import RUNTIME
@@ -153,7 +177,7 @@ def _child(check, runtime):
     stub = C.CDLL(runtime, mode=C.RTLD_GLOBAL)
     sys.path.insert(0, ROOT)
     from paper_2509_00404_amd import metis
-    {"failed": _failed, "largest": _largest, "threads": _threads}[check](stub, _Calls(metis))
+    {"failed": _failed, "largest": _largest, "in_place": _in_place, "threads": _threads}[check](stub, _Calls(metis))
 
 
 if __name__ == "__main__":
