@@ -165,6 +165,7 @@ k_mxfp4_deep(MxOperand A, MxOperand B, int nblk, MxOrder order, END end) {
         else unit(it, std::false_type{});
     }
     gs_meet<0>();                                        // every wave has its fragments: the ring takes the rows on their way out
+    static_assert(8 * mx_wave_rows<float, 1>() <= mxd_lds(LOOSE), "the staged rows fit the ring");
     if constexpr (PARTS)
         mx_store_wave<float, true, 2, 1>(acc, lds + wave * mx_wave_rows<float, 1>(), end.sums + end.stride * blockIdx.y, end.ld, m0 + 64 * wa,
                                          n0 + 32 * wb, A.rows, B.rows, true, m0 + 128 <= A.rows && n0 + 128 <= B.rows, lane);

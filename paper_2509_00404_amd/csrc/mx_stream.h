@@ -162,6 +162,7 @@ k_mxfp4_gemm_nt_stream(MxOperand A, MxOperand B, int64_t K, OUT* __restrict__ C,
 #pragma unroll
         for (int i = 0; i < 4; ++i) mxs_settle(acc[i]);
         const uint32_t bl = MXS_UNIT - b0;               // the last unit's buffer
+        static_assert(!LINES || 8 * mx_wave_rows<std::conditional_t<PLAIN, OUT, float>, 2>() <= MXS_UNIT, "the staged rows fit one buffer (fp32's fill it)");
         int m0, n0;
         tile_of(pos, m0, n0);
         if constexpr (PLAIN)
