@@ -583,9 +583,9 @@ int metis_dropout(void* stream, const metis_mat* x, const metis_dropout_mask* ma
  *              shape and type, which may be Y itself; Y, pre and residual must not overlap otherwise.
  *              Neither Y nor pre may overlap W, Xq or the bias.  Either may overlap X where the workspace's size is not 0: X is then quantized before the first
  *              output; where it is 0, such calls are refused (METIS_INVALID_ARG).
- *   workspace  with X: metis_mxfp4_linear_workspace_bytes bytes, 256-byte aligned (may be null where that is 0); with Xq, that many let a product of
- *              more than 64 rows and few outputs run faster (a call without is right too).  Calls that may run at the same time have workspaces of
- *              their own.
+ *   workspace  with X: metis_mxfp4_linear_workspace_bytes bytes, 256-byte aligned (may be null where that is 0); with Xq, optional:
+ *              metis_mxfp4_linear_quantized_workspace_bytes bytes (0 for most sizes) let a product of more than 64 rows and few outputs run faster, and a call
+ *              without is right too.  Calls that may run at the same time have workspaces of their own.
  *   act        relu max(z, 0); gelu z Phi(z), Phi the normal distribution; gelu_tanh z sigmoid(2 sqrt(2 / pi) (z + 0.044715 z^3)); silu
  *              z sigmoid(z).  For bf16 outputs their exponentials are the hardware's: results are within 4e-5, relatively.
  * Any strides of Y, pre, residual, and alignments of their elements.  No rows is no work.
@@ -600,6 +600,7 @@ typedef struct {
     const metis_mat*          residual;
 } metis_epilogue;
 size_t metis_mxfp4_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K);
+size_t metis_mxfp4_linear_quantized_workspace_bytes(int64_t rows, int64_t N, int64_t K);
 int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_mxfp4* Xq, const metis_mxfp4* W, const metis_epilogue* epilogue, metis_mat* Y,
                        void* workspace, size_t workspace_bytes);
 

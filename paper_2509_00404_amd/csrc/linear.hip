@@ -268,11 +268,12 @@ struct LinearPlace {
     size_t scales, sums, bytes;                   // places of the rows' scales behind their codes and of the parts' sums, and the end
     LinearParts parts;
 };
-LinearPlace linear_place(int64_t rows, int64_t N, int64_t K) {
+// dense: the rows' codes and scales have a place too
+LinearPlace linear_place(int64_t rows, int64_t N, int64_t K, bool dense) {
     LinearPlace p;
     p.parts = linear_parts(rows, N, K);
-    p.scales = align_up((size_t)rows * (K / 2), 256);
-    p.sums = p.scales + align_up((size_t)rows * (K / 32), 256);
+    p.scales = dense ? align_up((size_t)rows * (K / 2), 256) : 0;
+    p.sums = p.scales + (dense ? align_up((size_t)rows * (K / 32), 256) : 0);
     p.bytes = p.sums + (p.parts.count > 1 ? (size_t)p.parts.count * p.parts.stride * 4 : 0);
     return p;
 }
@@ -471,9 +472,14 @@ bool same_layout(const metis_mat* a, const metis_mat* b) { return a->rows == b->
 
 }  // namespace
 
+static bool linear_sizes_ok(int64_t rows, int64_t N, int64_t K) {
+    return rows >= 1 && N >= 1 && K >= 32 && K % 32 == 0 && rows <= 0xFFFFFFFFll / (K / 2) && N <= 0xFFFFFFFFll / (K / 2);
+}
 extern "C" size_t metis_mxfp4_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K) {
-    if (rows < 1 || N < 1 || K < 32 || K % 32 || rows > 0xFFFFFFFFll / (K / 2) || N > 0xFFFFFFFFll / (K / 2)) return 0;
-    return few_fused(rows, N, K) ? 0 : linear_place(rows, N, K).bytes;
+    return !linear_sizes_ok(rows, N, K) || few_fused(rows, N, K) ? 0 : linear_place(rows, N, K, true).bytes;
+}
+extern "C" size_t metis_mxfp4_linear_quantized_workspace_bytes(int64_t rows, int64_t N, int64_t K) {
+    return linear_sizes_ok(rows, N, K) ? linear_place(rows, N, K, false).bytes : 0;
 }
 
 extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_mxfp4* Xq, const metis_mxfp4* W, const metis_epilogue* e,
@@ -489,7 +495,7 @@ extern "C" int metis_mxfp4_linear(void* stream, const metis_mat* X, const metis_
     if (e && ((e->pre && !same_layout(e->pre, Y)) || (e->residual && !same_layout(e->residual, Y)))) return METIS_BAD_SHAPE;
     if (X && (X->ld < K || !mat_aligned16(X))) return METIS_BAD_SHAPE;
     uint8_t* ws = (uint8_t*)workspace;
-    const LinearPlace place = linear_place(rows, N, K);
+    const LinearPlace place = linear_place(rows, N, K, X != nullptr);
     metis_mxfp4 q = X ? metis_mxfp4{ws, ws + place.scales, rows, K} : *Xq;
     const int st = mx_operands_status(X ? W : &q, W);
     if (st != METIS_OK) return st;

@@ -138,6 +138,7 @@ _SIGNATURES = {
     # (structs as addresses: packed bytes, or byref of the classes above)
     "metis_dropout": (C.c_int, [C.c_void_p] * 5),
     "metis_mxfp4_linear_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "metis_mxfp4_linear_quantized_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
     "metis_mxfp4_linear": (C.c_int, [C.c_void_p] * 7 + [C.c_size_t]),
     "metis_linear_grads_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
     "metis_linear_grads": (C.c_int, [C.c_void_p] * 3 + [C.c_int] + [C.c_void_p] * 4 + [C.c_size_t]),
@@ -697,8 +698,10 @@ def dropout(x, y, mask, residual=None):
     return y
 
 
-def mxfp4_linear_workspace_bytes(rows, N, K):
-    return int(lib().metis_mxfp4_linear_workspace_bytes(rows, N, K))
+def mxfp4_linear_workspace_bytes(rows, N, K, quantized=False):
+    """Of a product of dense rows, or of an MxTensor's (quantized)."""
+    L = lib()
+    return int((L.metis_mxfp4_linear_quantized_workspace_bytes if quantized else L.metis_mxfp4_linear_workspace_bytes)(rows, N, K))
 
 
 def mxfp4_linear(X, W, Y, bias=None, act="none", pre=None, mask=None, residual=None, workspace=None):
@@ -709,7 +712,7 @@ def mxfp4_linear(X, W, Y, bias=None, act="none", pre=None, mask=None, residual=N
     p, k, r = _mat(pre) if pre is not None else None, mask.c() if mask is not None else None, _mat(residual) if residual is not None else None
     e = _EPILOGUE.pack(_ptr(bias, torch.float32, (N,)) or 0, ACTIVATIONS[act], C.addressof(p) if p is not None else 0,
                        C.addressof(k) if k is not None else 0, C.addressof(r) if r is not None else 0)
-    workspace, at, nbytes = _space(workspace, mxfp4_linear_workspace_bytes(rows, N, K) if workspace is None and (dense or rows > 64) else 0, Y)
+    workspace, at, nbytes = _space(workspace, mxfp4_linear_workspace_bytes(rows, N, K, not dense) if workspace is None and (dense or rows > 64) else 0, Y)
     _check(lib().metis_mxfp4_linear(_stream(), x if dense else None, None if dense else C.byref(x), C.byref(w), e, _packed(Y), at, nbytes))
     return Y
 

@@ -97,6 +97,20 @@ def _failed(stub, c):
             assert status == -4, f"{name}: launch {i} of {launches} failed, status {status}"
 
 
+def _workspaces(stub, c):
+    """Rows quantized already: cut into parts, which are joined, from the very byte on that the query asks for."""
+    L, quantized = c.L, c.L.metis_mxfp4_linear_quantized_workspace_bytes
+    for T, N, K, cut in [(128, 4096, 14336, True), (128, 1024, 4096, True), (129, 777, 2080, True), (1111, 2057, 2080, False), (16384, 4096, 14336, False),
+                         (64, 4096, 14336, False), (1, 14336, 4096, False), (300, 520, 512, False)]:
+        need = quantized(T, N, K)
+        assert (need > 0) == cut, (T, N, K)
+        for at, size, launches in ((FAKE, need, 1 + cut), (FAKE, need - cut, 1), (None, 0, 1), (FAKE + 64, need, 1)):
+            stub.fail_at(0)
+            assert L.metis_mxfp4_linear(None, None, c.ref(c.m.MxFp4(FAKE, FAKE, T, K)), c.ref(c.m.MxFp4(FAKE, FAKE, N, K)), None, c.mat(T, N, 0, OTHER), at, size) == 0
+            assert stub.launch_count() == launches, (T, N, K, size)
+    assert quantized(0, 40, 64) == 0 and quantized(128, 1024, 4080) == 0 and quantized(1 << 28, 40, 64) == 0
+
+
 def _largest(stub, c):
     widest = C.c_ulonglong.in_dll(stub, "widest")
     wide, tall = 1 << 28, (1 << 32) - 1
@@ -157,7 +171,7 @@ def _threads(stub, c):
     assert status == [0, 0, 0] and stub.exceeded_count() == 0, (status, stub.exceeded_count())
 
 
-@pytest.mark.parametrize("check", ["failed", "largest", "in_place", "threads"])
+@pytest.mark.parametrize("check", ["failed", "workspaces", "largest", "in_place", "threads"])
 def test_behind_a_stand_in_for_the_runtime(tmp_path, check):
     from paper_2509_00404_amd import metis
     from test_launches import RUNTIME
@@ -177,7 +191,7 @@ def _child(check, runtime):
     stub = C.CDLL(runtime, mode=C.RTLD_GLOBAL)
     sys.path.insert(0, ROOT)
     from paper_2509_00404_amd import metis
-    {"failed": _failed, "largest": _largest, "in_place": _in_place, "threads": _threads}[check](stub, _Calls(metis))
+    {"failed": _failed, "workspaces": _workspaces, "largest": _largest, "in_place": _in_place, "threads": _threads}[check](stub, _Calls(metis))
 
 
 if __name__ == "__main__":
