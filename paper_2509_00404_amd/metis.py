@@ -689,7 +689,9 @@ def _space(workspace, nbytes, like):
         if nbytes == 0:
             return None, None, 0
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    return workspace, workspace.data_ptr(), workspace.numel()
+    else:
+        assert workspace.is_cuda and workspace.is_contiguous()
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def dropout(x, y, mask, residual=None):
