@@ -66,8 +66,8 @@ __device__ __forceinline__ float logistic(float x) {
 }
 // Upper tail of the normal distribution at a = |z|: exp(-a^2 / 2) R(a), R(a) = erfcx(a / sqrt 2) / 2.  R is smooth and falls from 1/2 as 1 / a; as a
 // polynomial in t = 1 / (1 + c a), fitted for the least relative error for a <= 14 (beyond, the exponential is below fp32's range), it is within 1.4e-5
-// of its value with degree 5, for results of 8 bits, and within 5e-7 with degree 8 (FINE), for gradients whose sums are fp32.  The result keeps its
-// relative accuracy however small it is.
+// of its value with degree 5, for results of 8 bits, and within 6e-7 with degree 8 (FINE), for gradients whose sums are fp32; the exponential's rounded argument
+// adds up to 2e-5 of what little is left at a = 14, 2e-6 at 5.
 template <bool FINE>
 __device__ __forceinline__ float normal_tail(float a, float& bell) {
     bell = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
@@ -253,9 +253,6 @@ __device__ __forceinline__ void finish_bias(const MxFinish<T, ACT>& f, int64_t c
     if (f.bias && c < N) load_unit(f.bias + c, N - c, b);
 }
 
-// A wave's TM x TN accumulator tiles, transposed (a lane holds runs of four columns of one row), through the epilogue.  32 rows of its columns at
-// a time are staged at sm as fp32 (mx_wave_rows<float, TN> bytes), and a lane takes eight neighbouring columns of some of them: one block of the
-// mask's numbers, and 16 bytes of every bf16 operand.  The residual's next 32 rows are on their way meanwhile.
 // an element near row r0, which is uniform, by a 32-bit offset
 template <typename T>
 __device__ __forceinline__ T* narrow_at(T* p, int64_t ld, int64_t r0, uint32_t low, uint32_t c) {
@@ -275,6 +272,9 @@ __device__ __forceinline__ MxFinish<T, ACT> finish_afresh(MxFinish<T, ACT> f) {
     f.mask.step = in_global(f.mask.step);
     return f;
 }
+// A wave's TM x TN accumulator tiles, transposed (a lane holds runs of four columns of one row), through the epilogue.  32 rows of its columns at
+// a time are staged at sm as fp32 (mx_wave_rows<float, TN> bytes), and a lane takes eight neighbouring columns of some of them: one block of the
+// mask's numbers, and 16 bytes of every bf16 operand.  The residual's next 32 rows are on their way meanwhile.
 template <bool WHOLE, bool PAST, int TM, int TN, typename T, int ACT>
 __device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], uint8_t* sm, const MxFinish<T, ACT>& f, int64_t m0, int64_t n0, int64_t M,
                                                int64_t N, int lane) {
@@ -301,7 +301,7 @@ __device__ __forceinline__ void mx_finish_rows(const float16_t (&acc)[TM][TN], u
         else store_part<T, true>(p + (r0 + low) * ld + c, n, v);
     };
     // The streamed kernel's fp32 instances (an activation of their own) have no registers for the next 32 rows beside these: 8192 x 8192 x 4096 with a
-    // residual 261 us with them ahead, 231 without.
+    // residual 261 us with them ahead, 231 without.  (They spill 80 to 106 registers, the bf16 ones 8 to 16, and no other instance more than 6.)
     constexpr bool AHEAD = sizeof(T) < 4 || TN < 2 || ACT == ACT_ANY;
     if (AHEAD) fetch(0);
 #pragma unroll

@@ -350,8 +350,8 @@ k_layernorm_grads(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float
     norm_grads_rows<T, RT, U, ADD>(dy, ldd, x, ldx, stats, weight, add, lda, dx, ldo, rows, cols, sums, blockIdx.x, gridDim.x);
 }
 
-// Few rows, one launch: the first `strips` workgroups have 8 W columns each, a 128-byte line of fp32 or so, and go down all the rows, 128 at a time, for
-// the columns' sums; the others have rows.  (Both read x and dy: where dx takes the place of one, the rows follow in a launch of their own.)
+// Few rows, one launch: the first `strips` workgroups have 8 W columns each, 16 or, of longer rows, 64, and go down all the rows, 128 at a time,
+// for the columns' sums; the others have rows.  (Both read x and dy: where dx takes the place of one, the rows follow in a launch of their own.)
 template <typename T, int RT, int U, bool ADD>
 __global__ void __launch_bounds__(RowGroup<RT>::THREADS)
 k_layernorm_grads_few(const T* dy, int64_t ldd, const T* x, int64_t ldx, const float2* __restrict__ stats, const float* __restrict__ weight,
