@@ -1,4 +1,4 @@
-"""Layer norm's gradients at the widest rows they take: the columns' sums of all columns."""
+"""Layer norm at the widest rows it takes, and its gradients: the columns' sums of all columns."""
 import pytest
 import torch
 
@@ -25,3 +25,22 @@ def test_sums_of_every_column(metis, T, N):
     assert (db == T + 1).all()
     assert torch.equal(dw, (T + 1) * (x[0].float() - 1))
     assert torch.isfinite(dx).all()
+
+
+@pytest.mark.parametrize("N", [(1 << 27) + 5, 1 << 28])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_one_row(metis, N, dtype):
+    """Equal elements are 0 exactly; of two values beside each other, d apart and in turn, the mean is between them and the results are +-1.  The sum is
+    exact (whole multiples of 2^-14 below 2^38: 52 bits), the mean 1 / N off the middle where N is odd, the variance within 2^-16 (sums of eight terms in fp32,
+    the rest in 64 bits), and the results round once more."""
+    x = torch.full((1, N), 1000.3, device="cuda").to(dtype)
+    stats = torch.empty((1, 2), device="cuda")
+    y = metis.layernorm(x, torch.empty_like(x), stats=stats)
+    assert (y == 0).all() and stats[0, 0] == x[0, 0].float()
+    d = 4.0 if dtype == torch.bfloat16 else 2.0 ** -13
+    x[0, 1::2] += d
+    y = metis.layernorm(x, torch.empty_like(x), eps=0.0, stats=stats)
+    off = 4.0 / N + 2.0 ** -16
+    last = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+    assert (y[0, 0::2].float() + 1).abs().max() <= off + last and (y[0, 1::2].float() - 1).abs().max() <= off + last
+    assert abs(stats[0, 1].item() * d / 2 - 1) <= off
